@@ -15,6 +15,12 @@
  *                        and step on the host, the per-step closed loop also
  *                        on the GPU (davet_policy_step_device)
  *   davet_run_schedule   the whole loop: views once, then T steps
+ *   davet_cache_*        the attention of a denoiser (or decoder) that keeps
+ *                        keys and values in a paged cache and computes only a
+ *                        chunk of new tokens: entry into the cache, attention,
+ *                        and with davet_evict_select eviction by weight
+ *   davet_token_logprobs log probabilities, entropy and top alternatives of
+ *                        rows of logits
  *
  * Conventions, for every entry point:
  *   - Pointers are DEVICE pointers unless the comment says host.  Arrays are
@@ -73,6 +79,8 @@ typedef enum davet_dtype { DAVET_F32 = 0, DAVET_BF16 = 1, DAVET_F16 = 2 } davet_
 #define DAVET_MAX_SEQS 64        /* sequences per packed batch            */
 #define DAVET_MAX_LEVELS 4       /* K                                     */
 #define DAVET_MAX_RESP 1024      /* response length L                     */
+#define DAVET_MAX_PAGE_SIZE 256  /* tokens of a cache page                */
+#define DAVET_MAX_TOP 64         /* alternatives of davet_token_logprobs  */
 
 /* Evidence realizers (Sec. 4.3: any construction with an ordered
  * evidence-cost hierarchy; pooling is the paper's default, pruning varies
@@ -516,6 +524,158 @@ int davet_run_schedule(const davet_model_cfg* cfg, const davet_weights* w,
                        float* conf_trace, int32_t* argmax_trace,
                        davet_mailbox* mailbox, void* workspace,
                        size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------- paged cache -- */
+
+/* Keys and values of one layer in pages.  Element e of the key of cache index
+ * j of sequence s, key head h, is
+ *   k[((page * n_kv_heads + h) * page_size + j % page_size) * head_dim + e],
+ *   page = page_table[s * max_pages + j / page_size]
+ * and v alike.  An entry of the page table outside [0, n_pages) is a hole: it
+ * holds no keys (nothing is read from it, nothing is written to it).  Sequences
+ * may share pages that they only read.  page_size: a power of two in [16, 256];
+ * head_dim 64 or 128; n_kv_heads up to 1024; every dtype.  k and v 16-byte
+ * aligned; page_table is a DEVICE array, read when the call runs.
+ *
+ * A chunk on a cache: HOST arrays cu_q [n_seqs + 1] and kv_len [n_seqs].  Rows
+ * cu_q[s] .. cu_q[s+1] of the chunk's tensors are the new tokens of sequence s,
+ * the LAST ones of its kv_len[s] cached tokens: row i of n sits at cache index
+ * kv_len[s] - n + i.  A sequence may have no new tokens, and no tokens at all.
+ * Lengths are taken when the call is made: a captured graph replays those of
+ * its capture.  Tensor rows have strides (ld, in elements) and start at 16-byte
+ * boundaries; query head h of [.., n_heads * head_dim] reads key head
+ * h / (n_heads / n_kv_heads).  Rows past cu_q[n_seqs] are left as they are.
+ * Errors of all: EINVAL (null, misaligned, bad scalar), ESHAPE (n_seqs, lengths,
+ * strides, page or head counts; kv_len beyond max_pages * page_size), EDTYPE,
+ * ENOMEM (workspace). */
+typedef struct davet_kv_cache {
+  void* k;
+  void* v;                    /* may be NULL for davet_cache_weights          */
+  const int32_t* page_table;  /* device [n_seqs, max_pages]                   */
+  int32_t max_pages;          /* entries of a page table row                  */
+  int32_t n_pages;            /* pages of k (and of v)                        */
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t dtype;              /* of k, v and of the chunk's tensors           */
+} davet_kv_cache;
+
+/* A chunk's projected rows into the cache, in one pass:
+ *   qkv [rows, (n_heads + 2 n_kv_heads) * head_dim], stride ld_qkv: query heads,
+ *   key heads, value heads (the row order of davet_layer_weights.wqkv).
+ *   norm 1: queries and keys of each head become x / sqrt(mean x^2 + eps) * gain
+ *   first (q_gain, k_gain: device float32 [head_dim], NULL for ones); 0: not.
+ *   Then the rotary embedding: elements (i, i + head_dim/2) turn by
+ *   p * theta^(-2i/head_dim), p = pos[row] (device int32 [rows]) or, with pos
+ *   NULL, the row's cache index.  Angles are exact for every int32 position.
+ * Queries go to q_out [rows, n_heads * head_dim], stride ld_q, which may be qkv
+ * itself (same address and stride: the query columns in place) and must not
+ * overlap it otherwise; keys to the cache; values are copied to it bit for bit.
+ * Norm and rotation run in float32 and round once.  The chunk's cache slots must
+ * be distinct (no page shared among the sequences that write it). */
+int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
+                       const int32_t* cu_q, const int32_t* kv_len,
+                       const void* qkv, int64_t ld_qkv, int32_t n_heads,
+                       const int32_t* pos, int32_t norm, const float* q_gain,
+                       const float* k_gain, float eps, float theta, void* q_out,
+                       int64_t ld_q, hipStream_t stream);
+
+/* Workspace (256-byte aligned) that davet_cache_attention and
+ * davet_cache_weights need for chunks of at most max_q tokens in all.  Calls
+ * that may overlap in time need one each; its contents mean nothing between
+ * calls. */
+int davet_cache_workspace_bytes(int32_t n_heads, int32_t head_dim,
+                                int32_t max_q, size_t* bytes /*host*/);
+
+/* Attention of a chunk over the cache (which holds the chunk's own keys and
+ * values already: davet_cache_append first):
+ *   out[row, h] = sum_j softmax_j(scale * q[row, h] . k_j) v_j
+ *   lse[row, h] = ln sum_j exp(scale * q[row, h] . k_j)
+ * over the visible keys: every key of the sequence (block 0: the bidirectional
+ * denoiser), or, with block B >= 1, all cached tokens before the chunk and the
+ * chunk's own up to the end of the query's block, blocks of B counted from the
+ * chunk's first token (B = 1: causal).  Holes hold no keys.  What is not visible
+ * never contributes, whatever it holds (NaN and infinities included).  A row
+ * that sees no key, or whose every score is -inf, gets zeros and lse -inf.
+ *   scale: positive, or 0 for 1 / sqrt(head_dim).
+ *   q, out [rows, n_heads * head_dim] with strides, not overlapping; lse float32
+ *   [rows, n_heads] or NULL.
+ * The 16-bit modes round probabilities to 16 bits before they meet the values
+ * (with few rows, to twice 16); scores, sums and outputs are float32 until the
+ * store.  Results do not depend on timing. */
+int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs,
+                          const int32_t* cu_q, const int32_t* kv_len,
+                          const void* q, int64_t ld_q, int32_t n_heads,
+                          float scale, int32_t block, void* out, int64_t ld_out,
+                          float* lse, void* workspace, size_t ws_bytes,
+                          hipStream_t stream);
+
+/* Attention weight that each cached key received from a chunk, over all its
+ * queries and heads:
+ *   weights[s, j] = prev[s, j] + sum_{row, h} exp(scale * q . k_j - lse[row, h])
+ * for j < kv_len[s], with q, scale and block as given to the
+ * davet_cache_attention call that wrote lse (rows with lse -inf give nothing).
+ * prev and weights: device float32 rows of stride ld_weights; prev may be NULL
+ * (zeros) or weights itself, to accumulate over layers and steps.  Entries
+ * past kv_len[s] are left as they are; keys in holes receive nothing. */
+int davet_cache_weights(const davet_kv_cache* cache, int32_t n_seqs,
+                        const int32_t* cu_q, const int32_t* kv_len,
+                        const void* q, int64_t ld_q, int32_t n_heads,
+                        float scale, int32_t block, const float* lse,
+                        const float* prev, float* weights, int64_t ld_weights,
+                        void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Which cache entries stay.  Of the n[s] entries of sequence s (HOST) keep[s]
+ * (HOST, 0 <= keep <= n) stay: its first `first` and last `last` entries for
+ * sure (first + last <= keep unless keep is 0), then those ranked first by
+ * (weight descending, index ascending), NaN with -inf, -0 with +0.
+ *   weights: device float32, rows of stride ld_weights.
+ *   kept: device int32, rows of stride ld_kept: the keep[s] indices, ascending
+ *   (entries past keep[s] are left as they are).
+ *   weights_out: their weights in that order, rows of stride ld_weights_out, or
+ *   NULL; it must not overlap weights.  Whole numbers only depend on the
+ * weights: the same weights give the same indices. */
+int davet_evict_select(int32_t n_seqs, const int32_t* n, const int32_t* keep,
+                       const float* weights, int64_t ld_weights, int32_t first,
+                       int32_t last, int32_t* kept, int64_t ld_kept,
+                       float* weights_out, int64_t ld_weights_out,
+                       hipStream_t stream);
+
+/* Moves the entries that stay: cache index kept[s, j] under cache->page_table
+ * becomes index j under dst_table (device [n_seqs, dst_max_pages], pages of the
+ * same k and v) for j < keep[s], keys and values, every head.  Call it for each
+ * layer, then free the old pages.  An index outside the source table, or in a
+ * hole, gives zeros; a hole of dst_table takes nothing.  Destination pages must
+ * be distinct and none of them a source page of the call (a page shared with
+ * other sequences may be a source: it is only read). */
+int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
+                       const int32_t* keep, const int32_t* kept,
+                       int64_t ld_kept, const int32_t* dst_table,
+                       int32_t dst_max_pages, hipStream_t stream);
+
+/* Log probabilities, entropy and top alternatives of rows of logits (for
+ * instance davet_denoise_step's logits_out), temperature 1, natural logarithm:
+ *   logp[r] = logits[r, targets[r]] - logsumexp(logits[r, :])
+ *   entropy[r] = -sum_w p_w ln p_w
+ *   top_ids, top_logp [rows, top]: the `top` (0 .. 64) largest logits' ids and
+ *   log probabilities, by (logit descending, id ascending).
+ * logits [rows, vocab] of dtype, row stride ld, aligned to their element.
+ * exclude: a token left out of everything (probability 0; -1: none), as
+ * davet_denoise_step leaves out [MASK].  A target outside [0, vocab) or excluded
+ * has logp -inf.  Only logits above -inf are listed; where there are fewer than
+ * `top`, ids are -1 and log probabilities -inf.  A row without any: logp -inf,
+ * entropy 0.  A NaN or +inf logit makes the row's probabilities NaN; ids are
+ * ranked all the same, NaN never listed.  logp (with targets), entropy may be
+ * NULL.  workspace: davet_logprobs_workspace_bytes, 256-byte aligned (NULL / 0
+ * where that is 0).
+ * Errors: EINVAL, ESHAPE (rows, vocab, ld, top), EDTYPE, ENOMEM. */
+int davet_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top,
+                                   size_t* bytes /*host*/);
+int davet_token_logprobs(int32_t rows, int32_t vocab, const void* logits,
+                         int32_t dtype, int64_t ld, int32_t exclude,
+                         const int32_t* targets, float* logp, float* entropy,
+                         int32_t top, float* top_logp, int32_t* top_ids,
+                         void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------ profiling -- */
 

@@ -20,6 +20,8 @@ Contents (each function cites the passage of the paper it follows):
              ranked commitment (Eq. 2; Sec. 5.1 decoding settings)
   stats   -- mean confidence and prediction churn for the risk (Sec. 4.2)
   loop    -- the full schedule loop (Sec. 3.1 and Fig. 2's procedure)
+  cache   -- a paged key/value cache: entry, attention, eviction; token log
+             probabilities
 
 Precision: the denoiser runs in float64 on bf16-rounded (or fp32) inputs;
 the policy runs in IEEE double with the operation order printed in the
@@ -27,4 +29,4 @@ equations.  Readings of silent or ambiguous passages are listed in the
 design notes of the repository and restated where each is used.
 """
 
-from . import views, realizers, policy, model, decode, stats, loop  # noqa: F401
+from . import views, realizers, policy, model, decode, stats, loop, cache  # noqa: F401

@@ -68,6 +68,18 @@ class Policy(C.Structure):
                 ("demand", C.c_double), ("early", C.c_int32), ("K", C.c_int32)]
 
 
+class KvCacheT(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p),
+                ("page_table", C.c_void_p), ("max_pages", C.c_int32),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+MAX_PAGE_SIZE = 256
+MAX_TOP = 64
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError("libdavet.so is not built (%s); run "
                       "`python paper_2608_01821_amd/build.py`" % LIB_PATH)
@@ -75,6 +87,7 @@ _L = C.CDLL(LIB_PATH)
 
 _vp = C.c_void_p
 _i32 = C.c_int32
+_i64 = C.c_int64
 _P_i32 = C.POINTER(C.c_int32)
 _P_f64 = C.POINTER(C.c_double)
 _P_i64 = C.POINTER(C.c_int64)
@@ -130,6 +143,27 @@ _SIGS = {
     "davet_mailbox_create": (C.c_int, [_P_vp]),
     "davet_mailbox_destroy": (C.c_int, [_vp]),
     "davet_set_wait_limit": (C.c_int, [C.c_double]),
+    "davet_cache_append": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _P_i32,
+                                     _vp, _i64, _i32, _vp, _i32, _vp, _vp,
+                                     C.c_float, C.c_float, _vp, _i64, _vp]),
+    "davet_cache_workspace_bytes": (C.c_int, [_i32, _i32, _i32,
+                                              C.POINTER(C.c_size_t)]),
+    "davet_cache_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                        _P_i32, _vp, _i64, _i32, C.c_float,
+                                        _i32, _vp, _i64, _vp, _vp, C.c_size_t,
+                                        _vp]),
+    "davet_cache_weights": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _P_i32,
+                                      _vp, _i64, _i32, C.c_float, _i32, _vp,
+                                      _vp, _vp, _i64, _vp, C.c_size_t, _vp]),
+    "davet_evict_select": (C.c_int, [_i32, _P_i32, _P_i32, _vp, _i64, _i32,
+                                     _i32, _vp, _i64, _vp, _i64, _vp]),
+    "davet_cache_gather": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _vp,
+                                     _i64, _vp, _i32, _vp]),
+    "davet_logprobs_workspace_bytes": (C.c_int, [_i32, _i32, _i32,
+                                                 C.POINTER(C.c_size_t)]),
+    "davet_token_logprobs": (C.c_int, [_i32, _i32, _vp, _i32, _i64, _i32, _vp,
+                                       _vp, _vp, _i32, _vp, _vp, _vp,
+                                       C.c_size_t, _vp]),
     "davet_prof_enable": (C.c_int, [_i32]),
     "davet_prof_reset": (C.c_int, []),
     "davet_prof_only": (C.c_int, [_i32]),
@@ -474,6 +508,218 @@ def davet_run_schedule(cfg, weights: Weights, geoms, visual, view_bufs,
         lv, bu, _ptr(conf_trace), _ptr(argmax_trace), mb, _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream(stream)))
     return list(lv), list(bu)
+
+
+# ---- paged cache and token log probabilities.  These take row-strided tensors
+# (last dimension dense) and check that each holds what the call reads or
+# writes; without `stream` they run on the current stream of their tensors'
+# device, whichever device is current.
+
+def _rows(t, width, n_rows, name):
+    """(address, row stride in elements) of a 2-D tensor whose rows are dense
+    and hold `width` elements."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("davet: %s must be 2-D with dense rows" % name)
+    if t.shape[0] < n_rows or t.shape[1] < width:
+        raise ValueError("davet: %s must hold [%d, %d]" % (name, n_rows, width))
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if ld < width:
+        raise ValueError("davet: %s: rows overlap" % name)
+    return t.data_ptr(), ld
+
+
+def _dense(t, n, name):
+    if t is None:
+        return None
+    if t.numel() < n:
+        raise ValueError("davet: %s must hold %d elements" % (name, n))
+    return _ptr(t)
+
+
+def _typed(t, size, name):
+    if t is not None and t.element_size() != size:
+        raise ValueError("davet: %s must have %d-byte elements" % (name, size))
+
+
+def _nbytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _ints(vals):
+    return vals if isinstance(vals, C.Array) else (C.c_int32 * len(vals))(*vals)
+
+
+def _launch(stream, call, *tensors):
+    """call(stream handle) with the device of the tensors current."""
+    import torch
+    dev = tensors[0].device
+    for t in tensors:
+        if t is not None and (t.device != dev or not t.is_cuda):
+            raise ValueError("davet: tensor arguments must be on one GPU")
+    if dev.index == torch.cuda.current_device():
+        return _check(call(_stream(stream)))
+    with torch.cuda.device(dev):
+        return _check(call(_stream(stream)))
+
+
+class KvCache:
+    """A davet_kv_cache: ``k`` and ``v`` [n_pages, n_kv_heads, page_size,
+    head_dim] (``v`` may be None for davet_cache_weights) and ``page_table``
+    int32 [n_seqs, max_pages], dense device tensors, which it keeps alive."""
+
+    def __init__(self, k, v, page_table, dtype):
+        if k.dim() != 4 or (v is not None and v.shape != k.shape):
+            raise ValueError("davet: k and v must be [n_pages, n_kv_heads, "
+                             "page_size, head_dim] alike")
+        if page_table.dim() != 2:
+            raise ValueError("davet: page_table must be [n_seqs, max_pages]")
+        size = 4 if dtype == DAVET_F32 else 2
+        _typed(k, size, "k")
+        _typed(v, size, "v")
+        _typed(page_table, 4, "page_table")
+        self.k, self.v, self.page_table = k, v, page_table
+        self.tensors = (k, v, page_table)
+        self.n_seqs, self.head_dim, self.size = len(page_table), k.shape[3], size
+        self.n_kv_heads, self.page_size = k.shape[1], k.shape[2]
+        self.struct = KvCacheT(_addr(k), _addr(v), _addr(page_table),
+                               page_table.shape[1], k.shape[0], k.shape[2],
+                               k.shape[1], k.shape[3], int(dtype))
+        self._ref = C.byref(self.struct)
+
+    def _chunk(self, cu_q, kv_len):
+        n = len(kv_len)
+        if len(cu_q) != n + 1 or n > self.n_seqs:
+            raise ValueError("davet: cu_q needs an entry more than kv_len, and "
+                             "page_table a row for each of those")
+        return n, _ints(cu_q), _ints(kv_len), max(0, cu_q[n])
+
+
+def davet_cache_append(cache: KvCache, cu_q, kv_len, qkv, n_heads, q_out,
+                       pos=None, norm=False, q_gain=None, k_gain=None, eps=1e-6,
+                       theta=10000.0, stream=None):
+    n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    D = cache.head_dim
+    _typed(qkv, cache.size, "qkv")
+    _typed(q_out, cache.size, "q_out")
+    for t, name in ((pos, "pos"), (q_gain, "q_gain"), (k_gain, "k_gain")):
+        _typed(t, 4, name)
+    x, ldx = _rows(qkv, (n_heads + 2 * cache.n_kv_heads) * D, rows, "qkv")
+    q, ldq = _rows(q_out, n_heads * D, rows, "q_out")
+    p, gq, gk = (_dense(t, m, name) for t, m, name in (
+        (pos, rows, "pos"), (q_gain, D, "q_gain"), (k_gain, D, "k_gain")))
+    _launch(stream, lambda s: _L.davet_cache_append(
+        cache._ref, n, cu, kv, x, ldx, n_heads, p, 1 if norm else 0, gq, gk, eps,
+        theta, q, ldq, s), *cache.tensors, qkv, q_out, pos, q_gain, k_gain)
+
+
+def davet_cache_workspace_bytes(n_heads, head_dim, max_q):
+    out = C.c_size_t(0)
+    _check(_L.davet_cache_workspace_bytes(int(n_heads), int(head_dim),
+                                          int(max_q), C.byref(out)))
+    return out.value
+
+
+def davet_cache_attention(cache: KvCache, cu_q, kv_len, q, n_heads, out,
+                          lse=None, scale=0.0, block=0, workspace=None,
+                          stream=None):
+    n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    D = cache.head_dim
+    _typed(q, cache.size, "q")
+    _typed(out, cache.size, "out")
+    _typed(lse, 4, "lse")
+    x, ldx = _rows(q, n_heads * D, rows, "q")
+    o, ldo = _rows(out, n_heads * D, rows, "out")
+    e, ws, nb = _dense(lse, rows * n_heads, "lse"), _ptr(workspace), \
+        _nbytes(workspace)
+    _launch(stream, lambda s: _L.davet_cache_attention(
+        cache._ref, n, cu, kv, x, ldx, n_heads, scale, block, o, ldo, e, ws, nb,
+        s), *cache.tensors, q, out, lse, workspace)
+
+
+def davet_cache_weights(cache: KvCache, cu_q, kv_len, q, n_heads, lse, weights,
+                        prev=None, scale=0.0, block=0, workspace=None,
+                        stream=None):
+    n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    _typed(q, cache.size, "q")
+    for t, name in ((lse, "lse"), (prev, "prev"), (weights, "weights")):
+        _typed(t, 4, name)
+    most = max(kv)
+    x, ldx = _rows(q, n_heads * cache.head_dim, rows, "q")
+    w, ldw = _rows(weights, most, n, "weights")
+    p = None
+    if prev is not None:
+        p, ldp = _rows(prev, most, n, "prev")
+        if ldp != ldw and n > 1:
+            raise ValueError("davet: prev and weights need one row stride")
+    e, ws, nb = _dense(lse, rows * n_heads, "lse"), _ptr(workspace), \
+        _nbytes(workspace)
+    _launch(stream, lambda s: _L.davet_cache_weights(
+        cache._ref, n, cu, kv, x, ldx, n_heads, scale, block, e, p, w, ldw, ws,
+        nb, s), *cache.tensors, q, lse, weights, prev, workspace)
+
+
+def davet_evict_select(n, keep, weights, kept, first=0, last=0,
+                       weights_out=None, stream=None):
+    """``n`` and ``keep``: host lists, one entry a sequence."""
+    if len(n) != len(keep):
+        raise ValueError("davet: n and keep need one entry a sequence")
+    for t, name in ((weights, "weights"), (kept, "kept"),
+                    (weights_out, "weights_out")):
+        _typed(t, 4, name)
+    w, ldw = _rows(weights, max(n), len(n), "weights")
+    k, ldk = _rows(kept, max(keep), len(n), "kept")
+    o, ldo = (None, 0) if weights_out is None else \
+        _rows(weights_out, max(keep), len(n), "weights_out")
+    _launch(stream, lambda s: _L.davet_evict_select(
+        len(n), _ints(n), _ints(keep), w, ldw, first, last, k, ldk, o, ldo, s),
+        weights, kept, weights_out)
+
+
+def davet_cache_gather(cache: KvCache, kept, keep, dst_table, stream=None):
+    """``keep``: host list; ``dst_table``: dense int32 [n_seqs, pages]."""
+    n = len(keep)
+    _typed(kept, 4, "kept")
+    _typed(dst_table, 4, "dst_table")
+    if n > cache.n_seqs or dst_table.dim() != 2 or len(dst_table) < n:
+        raise ValueError("davet: the page tables need a row a sequence")
+    k, ldk = _rows(kept, max(keep), n, "kept")
+    dst = _ptr(dst_table)
+    _launch(stream, lambda s: _L.davet_cache_gather(
+        cache._ref, n, _ints(keep), k, ldk, dst, dst_table.shape[1], s),
+        *cache.tensors, kept, dst_table)
+
+
+def davet_logprobs_workspace_bytes(rows, vocab, top):
+    out = C.c_size_t(0)
+    _check(_L.davet_logprobs_workspace_bytes(int(rows), int(vocab), int(top),
+                                             C.byref(out)))
+    return out.value
+
+
+def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
+                         top_logp=None, top_ids=None, exclude=-1,
+                         workspace=None, stream=None):
+    """``logits`` [rows, vocab]; ``top_logp`` and ``top_ids`` [rows, top], dense
+    (both or neither)."""
+    rows, vocab = logits.shape
+    _typed(logits, 4 if dtype == DAVET_F32 else 2, "logits")
+    for t, name in ((targets, "targets"), (logp, "logp"), (entropy, "entropy"),
+                    (top_logp, "top_logp"), (top_ids, "top_ids")):
+        _typed(t, 4, name)
+    top = 0
+    if top_ids is not None or top_logp is not None:
+        if top_ids is None or top_logp is None or top_ids.shape != top_logp.shape \
+                or top_ids.dim() != 2 or len(top_ids) < rows:
+            raise ValueError("davet: top_logp and top_ids must be [rows, top]")
+        top = top_ids.shape[1]
+    x, ld = _rows(logits, vocab, rows, "logits")
+    g, lp, en = (_dense(t, rows, name) for t, name in (
+        (targets, "targets"), (logp, "logp"), (entropy, "entropy")))
+    tl, ti = (_ptr(top_logp), _ptr(top_ids)) if top else (None, None)
+    ws, nb = _ptr(workspace), _nbytes(workspace)
+    _launch(stream, lambda s: _L.davet_token_logprobs(
+        rows, vocab, x, int(dtype), ld, exclude, g, lp, en, top, tl, ti, ws, nb,
+        s), logits, targets, logp, entropy, top_logp, top_ids, workspace)
 
 
 def prof_enable(max_launches):

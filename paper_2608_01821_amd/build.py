@@ -35,6 +35,8 @@ POLICY_FLAGS = [
 
 HIP_SOURCES = ["views.hip", "realizers.hip", "unmask.hip", "rowops.hip", "gemm16.hip",
                "gemm_f32.hip", "attention.hip", "step.hip", "policy_dev.hip",
+               "cache_append.hip", "cache_attention.hip", "cache_evict.hip",
+               "logprobs.hip",
                "runtime.cpp",
                "schedule.cpp"]
 POLICY_SOURCES = ["policy.cpp", "parser.cpp"]

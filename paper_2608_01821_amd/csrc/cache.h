@@ -1,0 +1,62 @@
+// Shared by the kernels over a paged key/value cache: its description as the
+// kernels see it, the packed chunk of new tokens, and the host's checks.
+#pragma once
+
+#include "common.h"
+
+namespace davet {
+
+// The cache as kernels see it.  Keys (and values) of page p, head h, slot o
+// start at element (((p * n_kv + h) << lg) + o) * head_dim, 64-bit arithmetic.
+struct CacheView {
+  void* k;
+  void* v;
+  const int32_t* table;     // [n_seqs, max_pages]
+  int32_t max_pages, n_pages, lg, n_kv;
+};
+
+// The chunk: sequence s owns rows row0[s] .. row0[s+1], the last tokens of its
+// kv[s] cached ones.
+struct ChunkPack {
+  int32_t n_seqs;
+  int32_t row0[DAVET_MAX_SEQS + 1];
+  int32_t kv[DAVET_MAX_SEQS];
+};
+
+constexpr int kCacheGroup = 16;   // smallest page: 16 aligned keys share one
+
+// Keys visible to query i of a chunk of n among kv cached tokens: all of them
+// (block 0), or those up to the end of the query's block.
+__host__ __device__ inline int visible_end(int i, int n, int kv, int block) {
+  if (block == 0) return kv;
+  const int64_t e = ((int64_t)i / block + 1) * block;
+  return kv - n + (int)(e < n ? e : n);
+}
+
+// The last entry of an ascending offset list (first[0] = 0, n + 1 entries)
+// that is not above `at`: the sequence that owns a row, or a workgroup.
+__device__ __forceinline__ int owner(const int32_t* first, int n, int at) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= at) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Checks of a cache and, below, of a chunk on it; both fill what kernels take.
+int check_cache(const davet_kv_cache* c, bool need_v, const char* who,
+                CacheView* out);
+int check_chunk(const davet_kv_cache* c, int32_t n_seqs, const int32_t* cu_q,
+                const int32_t* kv_len, const char* who, ChunkPack* out);
+int check_rows(const void* p, int64_t ld, int64_t width, int dtype,
+               const char* who, const char* what);
+// n_heads a multiple of the cache's heads, at most 1024
+int check_heads(const davet_kv_cache* c, int32_t n_heads, const char* who);
+// whether [a, a + an) and [b, b + bn) bytes overlap
+inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return an && bn && x < y + bn && y < x + an;
+}
+
+}  // namespace davet

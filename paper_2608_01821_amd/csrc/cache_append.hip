@@ -1,0 +1,290 @@
+// The cache's host checks, and the entry of a chunk into it: per-head RMSNorm
+// and rotary embedding of queries and keys, and the copy of the values, in one
+// pass over the projected rows.
+//
+// For head row x (D elements, h = D / 2) of a token at position p:
+//   y = x * rsqrt(mean(x^2) + eps) * gain          (norm optional)
+//   out[i]     = y[i] cos a_i - y[i + h] sin a_i
+//   out[i + h] = y[i + h] cos a_i + y[i] sin a_i,   a_i = p theta^(-2 i / D)
+//
+// A thread owns elements 8j .. 8j+7 of both halves of one head, so that the
+// pairs that turn together, and one of the two 16-byte (fp32: 32-byte) pieces
+// of each half, are in its registers: D / 16 threads a head, the sum of squares
+// is a butterfly over them.  A workgroup takes whole rows: the D / 2 angles of
+// a row are computed once, into LDS, and serve all its heads.  The angle is
+// reduced in float64 turns (p * theta^(-2i/D) / 2 pi minus its nearest whole
+// number), which keeps far positions exact; what is left, at most half a turn,
+// goes through the fp32 sine and cosine.  A rotary table would be read instead,
+// but bounds the positions and is one more buffer to own.
+
+#include <math.h>
+
+#include "cache.h"
+
+namespace davet {
+
+int check_cache(const davet_kv_cache* c, bool need_v, const char* who,
+                CacheView* out) {
+  const std::string w = std::string(who) + ": ";
+  DAVET_CHECK_ARG(c, DAVET_EINVAL, w + "cache is null");
+  DAVET_CHECK_ARG(c->dtype == DAVET_F32 || is16(c->dtype), DAVET_EDTYPE,
+                  w + "cache.dtype must be DAVET_F32, DAVET_BF16 or DAVET_F16");
+  DAVET_CHECK_ARG(c->k && c->page_table && (c->v || !need_v), DAVET_EINVAL,
+                  w + "null cache pointer");
+  DAVET_CHECK_ARG((((uintptr_t)c->k | (uintptr_t)c->v) & 15) == 0 &&
+                      ((uintptr_t)c->page_table & 3) == 0,
+                  DAVET_EINVAL,
+                  w + "cache.k and cache.v must be 16-byte aligned");
+  DAVET_CHECK_ARG(c->head_dim == 64 || c->head_dim == 128, DAVET_ESHAPE,
+                  w + "cache.head_dim must be 64 or 128");
+  DAVET_CHECK_ARG(c->page_size >= kCacheGroup &&
+                      c->page_size <= DAVET_MAX_PAGE_SIZE &&
+                      (c->page_size & (c->page_size - 1)) == 0,
+                  DAVET_ESHAPE,
+                  w + "cache.page_size must be a power of two in [16, 256]");
+  DAVET_CHECK_ARG(c->n_kv_heads >= 1 && c->n_kv_heads <= 1024 &&
+                      c->n_pages >= 1 && c->max_pages >= 1,
+                  DAVET_ESHAPE,
+                  w + "cache: n_kv_heads in [1, 1024], n_pages and max_pages >= 1");
+  if (out)
+    *out = CacheView{c->k,         c->v,          c->page_table,
+                     c->max_pages, c->n_pages,    __builtin_ctz(c->page_size),
+                     c->n_kv_heads};
+  return DAVET_OK;
+}
+
+int check_chunk(const davet_kv_cache* c, int32_t n_seqs, const int32_t* cu_q,
+                const int32_t* kv_len, const char* who, ChunkPack* out) {
+  const std::string w = std::string(who) + ": ";
+  DAVET_CHECK_ARG(n_seqs >= 1 && n_seqs <= DAVET_MAX_SEQS, DAVET_ESHAPE,
+                  w + "n_seqs out of range [1, 64]");
+  DAVET_CHECK_ARG(cu_q && kv_len, DAVET_EINVAL, w + "null pointer");
+  DAVET_CHECK_ARG(cu_q[0] == 0, DAVET_ESHAPE, w + "cu_q[0] must be 0");
+  out->n_seqs = n_seqs;
+  out->row0[0] = 0;
+  for (int s = 0; s < n_seqs; ++s) {
+    DAVET_CHECK_ARG(cu_q[s + 1] >= cu_q[s], DAVET_ESHAPE,
+                    w + "cu_q must be non-decreasing");
+    DAVET_CHECK_ARG(kv_len[s] >= cu_q[s + 1] - cu_q[s], DAVET_ESHAPE,
+                    w + "kv_len counts the chunk: it must not be below its length");
+    DAVET_CHECK_ARG(kv_len[s] <= (int64_t)c->max_pages * c->page_size &&
+                        kv_len[s] <= (1 << 30),
+                    DAVET_ESHAPE,
+                    w + "kv_len beyond max_pages * page_size (or 2^30)");
+    out->row0[s + 1] = cu_q[s + 1];
+    out->kv[s] = kv_len[s];
+  }
+  DAVET_CHECK_ARG(cu_q[n_seqs] <= (1 << 24), DAVET_ESHAPE,
+                  w + "more than 2^24 new tokens");
+  return DAVET_OK;
+}
+
+int check_rows(const void* p, int64_t ld, int64_t width, int dtype,
+               const char* who, const char* what) {
+  const std::string w = std::string(who) + ": " + what;
+  DAVET_CHECK_ARG(p, DAVET_EINVAL, w + " is null");
+  DAVET_CHECK_ARG(((uintptr_t)p & 15) == 0 &&
+                      (ld * (int64_t)dtype_size(dtype)) % 16 == 0,
+                  DAVET_EINVAL, w + ": rows must start at 16-byte boundaries");
+  DAVET_CHECK_ARG(ld >= width && ld < (1ll << 31), DAVET_ESHAPE,
+                  w + ": row stride below the row's width");
+  return DAVET_OK;
+}
+
+int check_heads(const davet_kv_cache* c, int32_t n_heads, const char* who) {
+  DAVET_CHECK_ARG(n_heads >= 1 && n_heads <= 1024 &&
+                      n_heads % c->n_kv_heads == 0,
+                  DAVET_ESHAPE,
+                  std::string(who) +
+                      ": n_heads must be a multiple of n_kv_heads, at most 1024");
+  return DAVET_OK;
+}
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Freqs { double turns[64]; };   // theta^(-2 i / D) / (2 pi)
+
+// 8 elements between memory and fp32 registers
+template <typename F>
+__device__ __forceinline__ void load8(const typename F::st* p, float (&v)[8]) {
+  if constexpr (F::dtype == DAVET_F32) {
+    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0];
+    const f32x4 b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+  } else {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = F::load((uint16_t)(w[i] & 0xffffu));
+      v[2 * i + 1] = F::load((uint16_t)(w[i] >> 16));
+    }
+  }
+}
+template <typename F>
+__device__ __forceinline__ void store8(typename F::st* p, const float (&v)[8]) {
+  if constexpr (F::dtype == DAVET_F32) {
+    reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = F::store2(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<u32x4*>(p) = w;
+  }
+}
+// 8 elements moved as they are (values keep every bit)
+template <typename F>
+__device__ __forceinline__ void copy8(const typename F::st* s,
+                                      typename F::st* d) {
+  constexpr int N = sizeof(typename F::st) * 8 / 16;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    reinterpret_cast<u32x4*>(d)[i] = reinterpret_cast<const u32x4*>(s)[i];
+}
+
+template <typename F, int D>
+__global__ void __launch_bounds__(kThreads)
+cache_append_kernel(CacheView cv, ChunkPack cp, Freqs fr,
+                    const typename F::st* qkv, int64_t ld_qkv,
+                    int n_heads, const int32_t* __restrict__ pos, int norm,
+                    const float* __restrict__ q_gain,
+                    const float* __restrict__ k_gain, float eps,
+                    typename F::st* q_out, int64_t ld_q, int rows_per_wg) {
+  using st = typename F::st;
+  constexpr int H = D / 2, TH = D / 16;       // threads a head
+  constexpr int kMaxRows = 4;
+  __shared__ float cs[kMaxRows][2][H];
+  const int total = cp.row0[cp.n_seqs];
+  const int r0 = blockIdx.x * rows_per_wg;
+  const int nr = min(rows_per_wg, total - r0);
+  for (int t = threadIdx.x; t < nr * H; t += kThreads) {
+    const int r = r0 + t / H, i = t % H;
+    const int s = owner(cp.row0, cp.n_seqs, r);
+    const int p = pos ? pos[r] : cp.kv[s] - cp.row0[s + 1] + r;
+    const double turns = (double)p * fr.turns[i];
+    const float part = (float)(turns - rint(turns));
+    cs[t / H][0][i] = cospif(2.f * part);
+    cs[t / H][1][i] = sinpif(2.f * part);
+  }
+  __syncthreads();
+  const int heads = n_heads + 2 * cv.n_kv;
+  const int j = threadIdx.x % TH;
+  for (int u = threadIdx.x / TH; u < nr * heads; u += kThreads / TH) {
+    const int lr = u / heads, h = u % heads, r = r0 + lr;
+    const st* x = qkv + (int64_t)r * ld_qkv + (int64_t)h * D + 8 * j;
+    st* out;
+    if (h < n_heads) {
+      out = q_out + (int64_t)r * ld_q + (int64_t)h * D + 8 * j;
+    } else {
+      const int s = owner(cp.row0, cp.n_seqs, r);
+      const int at = cp.kv[s] - cp.row0[s + 1] + r;
+      const int page = cv.table[(int64_t)s * cv.max_pages + (at >> cv.lg)];
+      const int kh = h - n_heads < cv.n_kv ? h - n_heads
+                                           : h - n_heads - cv.n_kv;
+      st* base = static_cast<st*>(h - n_heads < cv.n_kv ? cv.k : cv.v);
+      // a hole in the page table takes nothing
+      out = (unsigned)page < (unsigned)cv.n_pages
+                ? base + ((((int64_t)page * cv.n_kv + kh) << cv.lg) +
+                          (at & ((1 << cv.lg) - 1))) * D + 8 * j
+                : nullptr;
+      if (h >= n_heads + cv.n_kv) {           // values: the same for all TH
+        if (out) {
+          copy8<F>(x, out);
+          copy8<F>(x + H, out + H);
+        }
+        continue;
+      }
+    }
+    float a[8], b[8];
+    load8<F>(x, a);
+    load8<F>(x + H, b);
+    if (norm) {
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + b[i] * b[i];
+#pragma unroll
+      for (int o = 1; o < TH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+      const float inv = 1.0f / sqrtf(ss * (1.0f / D) + eps);
+      const float* g = h < n_heads ? q_gain : k_gain;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        a[i] *= inv * (g ? g[8 * j + i] : 1.f);
+        b[i] *= inv * (g ? g[H + 8 * j + i] : 1.f);
+      }
+    }
+    float c[8], d[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float co = cs[lr][0][8 * j + i], si = cs[lr][1][8 * j + i];
+      c[i] = a[i] * co - b[i] * si;
+      d[i] = b[i] * co + a[i] * si;
+    }
+    if (out) {
+      store8<F>(out, c);
+      store8<F>(out + H, d);
+    }
+  }
+}
+
+}  // namespace
+}  // namespace davet
+
+extern "C" int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
+                                  const int32_t* cu_q, const int32_t* kv_len,
+                                  const void* qkv, int64_t ld_qkv,
+                                  int32_t n_heads, const int32_t* pos,
+                                  int32_t norm, const float* q_gain,
+                                  const float* k_gain, float eps, float theta,
+                                  void* q_out, int64_t ld_q,
+                                  hipStream_t stream) {
+  using namespace davet;
+  static const char who[] = "davet_cache_append";
+  CacheView cv;
+  ChunkPack cp;
+  int rc = check_cache(cache, true, who, &cv);
+  if (!rc) rc = check_heads(cache, n_heads, who);
+  if (!rc) rc = check_chunk(cache, n_seqs, cu_q, kv_len, who, &cp);
+  const int D = cache ? cache->head_dim : 0;
+  const int64_t width = (int64_t)(n_heads + 2 * (cache ? cache->n_kv_heads : 0)) * D;
+  const int total = rc ? 0 : cp.row0[n_seqs];
+  if (!rc && total > 0)
+    rc = check_rows(qkv, ld_qkv, width, cache->dtype, who, "qkv");
+  if (!rc && total > 0)
+    rc = check_rows(q_out, ld_q, (int64_t)n_heads * D, cache->dtype, who, "q_out");
+  if (rc) return rc;
+  DAVET_CHECK_ARG(norm == 0 || norm == 1, DAVET_EINVAL,
+                  "davet_cache_append: norm must be 0 or 1");
+  DAVET_CHECK_ARG(theta > 0.f && std::isfinite(theta) &&
+                      (!norm || (eps >= 0.f && std::isfinite(eps))),
+                  DAVET_EINVAL,
+                  "davet_cache_append: theta > 0 and eps >= 0 required, finite");
+  if (total == 0) return DAVET_OK;
+  const size_t es = dtype_size(cache->dtype);
+  DAVET_CHECK_ARG((q_out == qkv && ld_q == ld_qkv) ||
+                      !overlap(q_out, ((total - 1) * ld_q + n_heads * D) * es, qkv,
+                               ((total - 1) * ld_qkv + width) * es),
+                  DAVET_EINVAL,
+                  "davet_cache_append: q_out overlaps qkv (in place needs the "
+                  "same address and row stride)");
+  Freqs fr{};
+  for (int i = 0; i < D / 2; ++i)
+    fr.turns[i] = pow((double)theta, -2.0 * i / D) / (2.0 * M_PI);
+  const int rpw = total >= 2048 ? 2 : 1;
+  const int grid = (total + rpw - 1) / rpw;
+  ProfScope ps(KC_MISC, stream);
+#define APPEND(F, DIM)                                                         \
+  hipLaunchKernelGGL((cache_append_kernel<F, DIM>), dim3(grid), dim3(kThreads),\
+                     0, stream, cv, cp, fr, (const F::st*)qkv, ld_qkv, n_heads,\
+                     pos, norm, q_gain, k_gain, eps, (F::st*)q_out, ld_q, rpw)
+#define APPEND_D(F) do { if (D == 128) APPEND(F, 128); else APPEND(F, 64); } while (0)
+  if (cache->dtype == DAVET_F16) APPEND_D(F16S);
+  else if (cache->dtype == DAVET_BF16) APPEND_D(BF16S);
+  else APPEND_D(F32S);
+#undef APPEND_D
+#undef APPEND
+  DAVET_HIP(hipGetLastError());
+  return DAVET_OK;
+}

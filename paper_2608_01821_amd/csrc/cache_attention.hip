@@ -1,0 +1,1100 @@
+// Attention of a chunk of new tokens over a paged key/value cache, and the
+// attention weight each cached key received.
+//
+//   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),
+//   lse_i = ln sum_j exp(scale q_i.k_j)
+//
+// over the keys j visible to query i.  The g = n_heads / n_kv_heads query heads
+// that share a key head are rows of one tile: row r of (sequence, key head) is
+// query r / g, head r % g of the group, so a decode step's few queries fill the
+// matrix tile and every key is fetched once for all of them.
+//
+// A wavefront owns 32 rows and computes S^T = K Q^T with 32 x 32 matrix ops: a
+// lane holds the scores of ONE row, the softmax statistics are per lane, and the
+// probabilities are already laid out as the B operand of O^T += V^T P^T.  fp32
+// runs the same code on v_mfma_f32_32x32x2: eight of them consume the eight
+// elements that one 16-bit op takes, in the same lane layout.
+//
+// Keys move global -> LDS by DMA.  A page holds at least 16 aligned keys, so the
+// 4 (8, 2) rows that one load instruction moves share a page and its address is
+// scalar; the page ids of 64 pages at a time sit in one register per lane.
+//
+// Two forms, by the rows of a (sequence, key head):
+//   wide    128 rows a workgroup: four wavefronts of 32 rows share 64-key tiles
+//   narrow  32 rows a workgroup: each of four wavefronts streams its own 32-key
+//           tiles through its own two buffers, with no barrier, and the four are
+//           joined in LDS at the end
+// Either way the keys of a tile may be cut into pieces, one workgroup each, that
+// leave (max, sum, O) in fp32 in the workspace; a second kernel joins them in
+// piece order, so no result depends on timing.
+
+#include <math.h>
+
+#include <algorithm>
+
+#include "cache.h"
+
+namespace davet {
+namespace {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s* lds_v4s_ptr;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxPieces = 64;
+constexpr int kMaxPartRows = 1 << 17;     // rows x pieces in the workspace
+constexpr int kWeightKeys = 128;          // keys a workgroup of the weights
+constexpr int kWeightParts = 2048;        // workgroups that leave partial sums
+
+// Fragments of 8 elements along the contracted axis and the op that takes them.
+template <typename S> struct Frag;
+template <> struct Frag<F16S> {
+  using v8 = f16x8;
+  // Probabilities are stored as 2^kBias times themselves: fp16 has few bits
+  // below 2^-14, and a running maximum 2^8 behind still stays below 65504.
+  static constexpr int kBias = 6;
+};
+template <> struct Frag<BF16S> { using v8 = bf16x8; static constexpr int kBias = 0; };
+template <> struct Frag<F32S> { using v8 = f32x8; static constexpr int kBias = 0; };
+
+template <typename F>
+__device__ __forceinline__ f32x16 mm(typename Frag<F>::v8 a,
+                                     typename Frag<F>::v8 b, f32x16 c) {
+  if constexpr (F::dtype == DAVET_F32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  } else {
+    return F::mfma32(a, b, c);
+  }
+}
+
+__device__ __forceinline__ void dma16(const void* g, void* lds) {
+  __builtin_amdgcn_global_load_lds(g, (lds_ptr)lds, 16, 0, 0);
+}
+__device__ __forceinline__ void sync_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// x combined with the value of lane l ^ 32
+__device__ __forceinline__ float pair_max32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x),
+                                                  __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x),
+                                                  __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// LDS layout of a tile row of D elements: 16-byte chunks, chunk c of row r in
+// slot c ^ f(r).  K: the 16 rows that a fragment read takes at one chunk cover
+// all 64 banks.  V, 16-bit: the 64-byte pieces of four consecutive keys that a
+// transposing read takes do; fp32: those of the two half-waves' keys.
+template <typename F, int D>
+struct Tile {
+  using st = typename F::st;
+  static constexpr int RB = D * (int)sizeof(st);   // bytes a row
+  static constexpr int C = RB / 16;                // chunks a row
+  static constexpr int RPI = 1024 / RB;            // rows a load instruction
+  __device__ static __forceinline__ int k_slot(int r, int c) {
+    return C == 8 ? c ^ ((r >> 1) & 7) : c ^ (r & 15);
+  }
+  __device__ static __forceinline__ int v_slot(int r, int c) {
+    if constexpr (F::dtype == DAVET_F32) return c ^ (((r >> 2) & 1) << 3);
+    return C == 8 ? c ^ (((r >> 1) & 1) << 2) : c ^ ((r & 3) << 2);
+  }
+  // elements 16 ks + 8 hh .. +7 of K row r
+  __device__ static __forceinline__ typename Frag<F>::v8 k_frag(const char* b,
+                                                                int r, int ks,
+                                                                int hh) {
+    if constexpr (F::dtype == DAVET_F32) {
+      const int c = ks * 4 + hh * 2;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(b + r * RB + (k_slot(r, c) << 4));
+      const f32x4 y = *reinterpret_cast<const f32x4*>(b + r * RB + (k_slot(r, c + 1) << 4));
+      return f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    } else {
+      return *reinterpret_cast<const typename Frag<F>::v8*>(
+          b + r * RB + (k_slot(r, ks * 2 + hh) << 4));
+    }
+  }
+  __device__ static __forceinline__ const char* v_at(const char* b, int r, int d) {
+    const int byte = d * (int)sizeof(st);
+    return b + r * RB + (v_slot(r, byte >> 4) << 4) + (byte & 15);
+  }
+  // V^T: dim 32 dt + lane % 32 of keys 16 ps + 8 (e / 4) + 4 hh + e % 4, e < 8
+  __device__ static __forceinline__ typename Frag<F>::v8 v_frag(const char* b,
+                                                                int ps, int dt,
+                                                                int lane) {
+    const int hh = lane >> 5;
+    if constexpr (F::dtype == DAVET_F32) {
+      f32x8 f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        f[e] = *reinterpret_cast<const float*>(
+            v_at(b, ps * 16 + (e >> 2) * 8 + hh * 4 + (e & 3),
+                 dt * 32 + (lane & 31)));
+      return f;
+    } else {
+      // transposing reads: in each group of 16 lanes, lane j addresses key
+      // 4 hh + j / 4 and four dims from 4 (j % 4); lane i then holds element
+      // i % 4 of the piece of lane 4 r + i / 4, for r = 0 .. 3
+      const int j = lane & 15;
+      const int r = ps * 16 + hh * 4 + (j >> 2);
+      const int d = dt * 32 + 16 * ((lane >> 4) & 1) + 4 * (j & 3);
+      const v4s t0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)v_at(b, r, d));
+      const v4s t1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)v_at(b, r + 8, d));
+      const u32x2 v0 = __builtin_bit_cast(u32x2, t0);
+      const u32x2 v1 = __builtin_bit_cast(u32x2, t1);
+      return __builtin_bit_cast(typename Frag<F>::v8, u32x4{v0[0], v0[1], v1[0], v1[1]});
+    }
+  }
+};
+
+// 8 consecutive elements of global memory as a fragment
+template <typename F>
+__device__ __forceinline__ typename Frag<F>::v8 load_frag(const typename F::st* p) {
+  if constexpr (F::dtype == DAVET_F32) {
+    const f32x4 x = reinterpret_cast<const f32x4*>(p)[0];
+    const f32x4 y = reinterpret_cast<const f32x4*>(p)[1];
+    return f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  } else {
+    return *reinterpret_cast<const typename Frag<F>::v8*>(p);
+  }
+}
+
+// 64 consecutive entries of a sequence's page table row, one a lane; moves on
+// as the keys do (page numbers must not fall behind `base`).
+struct PageIds {
+  const int32_t* row;
+  int max_pages, base, ids;
+  __device__ __forceinline__ void init(const int32_t* r, int mp) {
+    row = r;
+    max_pages = mp;
+    base = -64;
+    ids = -1;
+  }
+  __device__ __forceinline__ int at(int page) {
+    if (page - base >= 64) {
+      base = page;
+      const int e = page + (int)(threadIdx.x & 63);
+      ids = e < max_pages ? row[e] : -1;
+    }
+    return __builtin_amdgcn_readlane(ids, page - base);
+  }
+};
+
+// Launch plan, by value: workgroups of sequence order[i] start at blk[i] (of
+// one eighth of the grid when the key heads divide by 8).
+struct AttnPlan {
+  int32_t blk[DAVET_MAX_SEQS + 1];
+  uint8_t order[DAVET_MAX_SEQS];
+  int32_t piece;        // keys a piece
+  int32_t pieces;       // most pieces of a sequence; 1: no partials
+  int32_t xcd;          // key heads dealt out to the 8 XCDs
+};
+
+// One sequence's workgroups: [key head][piece][row tile], row tile fastest.
+// With `xcd`, workgroup b runs on XCD b % 8 and takes key heads = b mod 8 only,
+// so the tiles and pieces of a key head share one L2 and every XCD has the same
+// work.
+struct Place { int s, hk, piece, tile; };
+__device__ __forceinline__ Place place(const AttnPlan& ap, const ChunkPack& cp,
+                                       int n_kv, int g, int rows) {
+  const int b = ap.xcd ? (int)blockIdx.x >> 3 : (int)blockIdx.x;
+  const int i = owner(ap.blk, cp.n_seqs, b);
+  Place p;
+  p.s = ap.order[i];
+  const int n = cp.row0[p.s + 1] - cp.row0[p.s];
+  const int nt = (n * g + rows - 1) / rows;
+  const int np = (cp.kv[p.s] + ap.piece - 1) / ap.piece;
+  int rem = b - ap.blk[i];
+  const int h = rem / (nt * np);
+  rem -= h * nt * np;
+  p.hk = ap.xcd ? ((int)blockIdx.x & 7) + 8 * h : h;
+  p.piece = rem / nt;
+  p.tile = rem - p.piece * nt;
+  return p;
+}
+
+struct Scale {
+  float c, c_lo;        // scale * log2(e) as a sum of two floats
+  float scale;
+};
+
+// (x - m) scale log2(e) for fp32 operands, where the rounding of the constant
+// would show; far differences stop at a weight of 0 (-inf times its rest might
+// be +inf).
+__device__ __forceinline__ float exact_arg(float d, const Scale& s) {
+  d = d < -1e4f / s.c ? -1e4f / s.c : d;
+  return fmaf(d, s.c, d * s.c_lo);
+}
+
+// G wavefronts share a tile (4: wide, 1: narrow); BUFS buffers a tile stream.
+template <typename F, int D, int G, int BUFS, int MINB>
+__global__ void __launch_bounds__(256, MINB)
+cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
+                  const typename F::st* __restrict__ q, int64_t ld_q,
+                  typename F::st* __restrict__ out, int64_t ld_o,
+                  float* __restrict__ lse, int n_heads, int block, Scale sc_,
+                  float* __restrict__ part, int part_rows) {
+  using st = typename F::st;
+  using T = Tile<F, D>;
+  using v8 = typename Frag<F>::v8;
+  constexpr int KT = G == 4 ? 64 : 32;            // keys a tile
+  constexpr int MT = KT / 32;
+  constexpr int KG = 4 / G;                       // tile streams
+  constexpr int TILE = KT * T::RB;                // bytes of K (or V)
+  constexpr int GROUP = BUFS * 2 * TILE;
+  constexpr int MERGE = G == 1 ? 4 * (32 * D + 64) * 4 : 0;
+  constexpr int LDS = KG * GROUP > MERGE ? KG * GROUP : MERGE;
+  constexpr int OWN = KT / G;                     // tile rows a wave moves
+  constexpr int NI = OWN / T::RPI;                // its loads, of K and of V
+  constexpr float BIAS = Frag<F>::kBias;
+  __shared__ __attribute__((aligned(1024))) char smem[LDS];
+
+  const int g = n_heads / cv.n_kv;
+  const Place pl = place(ap, cp, cv.n_kv, g, 32 * G);
+  const int s = pl.s, hk = pl.hk;
+  const int row0 = cp.row0[s], n = cp.row0[s + 1] - row0, kv = cp.kv[s];
+  const int rows = n * g;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wrow = pl.tile * 32 * G + (G == 4 ? wave * 32 : 0);
+  const int r = min(wrow + l32, rows - 1);
+  const int qi = r / g, qh = hk * g + r % g;
+  const bool live = wrow < rows;                  // of the wave
+  // keys of this piece, up to the last one that any row of the tile sees
+  const int tile_last = min(pl.tile * 32 * G + 32 * G, rows) - 1;
+  const int end = min((pl.piece + 1) * ap.piece,
+                      visible_end(tile_last / g, n, kv, block));
+  const int begin = pl.piece * ap.piece;
+  const int lim = visible_end(qi, n, kv, block);
+  // keys before this are visible to every row of the wave
+  const int lim_all = min(visible_end(min(wrow, rows - 1) / g, n, kv, block), kv);
+
+  v8 qf[D / 16];
+  {
+    const st* qp = q + (int64_t)(row0 + qi) * ld_q + (int64_t)qh * D + hh * 8;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = load_frag<F>(qp + ks * 16);
+  }
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  const int grp = G == 4 ? 0 : wave;
+  char* gbuf = smem + grp * GROUP;
+  PageIds pages;
+  pages.init(cv.table + (int64_t)s * cv.max_pages, cv.max_pages);
+  const int lg = cv.lg, psz = 1 << lg;
+
+  // Moves this wave's rows of the tile at key k0 into buffer b; returns the
+  // 16-key groups of the whole tile that lie in holes.  Keys past the last
+  // cached one repeat it; rows of holes are zeroed (their scores are masked,
+  // but a NaN left in LDS would meet a weight of 0).
+  auto issue = [&](int k0, int b) -> int {
+    char* kd = gbuf + b * 2 * TILE;
+    char* vd = kd + TILE;
+    // one 16-key group: its rows of K and of V
+    auto move = [&](int gi, int key, int page, bool hole) {
+      const int64_t base =
+          ((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * D;
+      const int last = kv - 1 - key;              // last valid row of the group
+#pragma unroll
+      for (int j = 0; j < 16 / T::RPI; ++j) {
+        const int lr = j * T::RPI + lane / T::C, tr = gi * 16 + lr;
+        char* kl = kd + (gi * 16 + j * T::RPI) * T::RB;
+        char* vl = vd + (gi * 16 + j * T::RPI) * T::RB;
+        if (hole) {
+          *reinterpret_cast<u32x4*>(kl + lane * 16) = u32x4{0, 0, 0, 0};
+          *reinterpret_cast<u32x4*>(vl + lane * 16) = u32x4{0, 0, 0, 0};
+        } else {
+          const int64_t row = base + (int64_t)min(lr, last) * D;
+          const int c = lane % T::C;
+          dma16(reinterpret_cast<const char*>(static_cast<const st*>(cv.k) + row) +
+                    T::k_slot(tr, c) * 16, kl);
+          dma16(reinterpret_cast<const char*>(static_cast<const st*>(cv.v) + row) +
+                    T::v_slot(tr, c) * 16, vl);
+        }
+      }
+    };
+    int holes = 0, my_key = 0, my_page = 0;
+#pragma unroll
+    for (int gi = 0; gi < KT / 16; ++gi) {
+      const int key = min(k0 + gi * 16, (kv - 1) & ~15);
+      const int page = pages.at(key >> lg);
+      const bool hole = (unsigned)page >= (unsigned)cv.n_pages;
+      holes |= hole << gi;
+      if constexpr (G == 4) {
+        if (gi == wave) { my_key = key; my_page = page; }
+      } else {
+        move(gi, key, page, hole);
+      }
+    }
+    if constexpr (G == 4) move(wave, my_key, my_page, (holes >> wave) & 1);
+    return holes;
+  };
+
+  auto compute = [&](int k0, const char* Kb, int holes) {
+    const char* Vb = Kb + TILE;
+    f32x16 sc[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[mt][e] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+        sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
+    }
+    // keys past a row's limit, or in a hole, score -inf
+    const bool masked = k0 + KT > lim_all || holes;
+    if (masked) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int at = mt * 32 + (e >> 2) * 8 + hh * 4 + (e & 3);
+          if (k0 + at >= lim || ((holes >> (at >> 4)) & 1)) sc[mt][e] = -INFINITY;
+        }
+    }
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, sc[mt][e]);
+    tmax = pair_max32(tmax);
+    // the maximum moves only when it is 2^8 behind: O is rescaled rarely
+    const float m_new =
+        m_run == -INFINITY || (tmax - m_run) * sc_.c > 8.0f ? tmax : m_run;
+    // while nothing is visible every weight is 0, not exp(-inf + inf)
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * sc_.c);
+    const float neg_m = BIAS - ref * sc_.c;
+    float psum = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = sc[mt][e];
+        const float p = __builtin_amdgcn_exp2f(
+            F::dtype == DAVET_F32 ? exact_arg(x - ref, sc_) : fmaf(x, sc_.c, neg_m));
+        sc[mt][e] = p;
+        psum += p;
+      }
+    psum = pair_sum32(psum);
+    l_run = l_run * alpha + psum;
+    m_run = m_new;
+    if (__any(alpha != 1.0f)) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+    }
+    if (masked) {
+      // A masked weight of 0 times an infinite (or NaN) value is NaN: where
+      // the tile holds such a value, keys are added one by one, and those of
+      // weight 0 are left out.
+      bool bad = false;
+#pragma unroll 1
+      for (int i = lane; i < TILE / 16; i += 64) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(Vb + i * 16);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if constexpr (F::dtype == DAVET_F32)
+            bad |= (w[u] & 0x7f800000u) == 0x7f800000u;
+          else
+            bad |= F::nonfinite((uint16_t)(w[u] & 0xffffu)) ||
+                   F::nonfinite((uint16_t)(w[u] >> 16));
+        }
+      }
+      if (__any(bad)) {
+#pragma unroll 1
+        for (int at = 0; at < KT; ++at) {
+          float p = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (mt == at >> 5 && e == ((at >> 3) & 3) * 4 + (at & 3))
+                p = sc[mt][e];
+          p = __shfl(p, l32 + 32 * ((at >> 2) & 1), 64);
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const st x = *reinterpret_cast<const st*>(
+                  T::v_at(Vb, at, dt * 32 + (e >> 2) * 8 + hh * 4 + (e & 3)));
+              if (p != 0.f) o[dt][e] = fmaf(p, F::load(x), o[dt][e]);
+            }
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int ps = 0; ps < KT / 16; ++ps) {
+      float pv[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pv[e] = sc[ps >> 1][(ps & 1) * 8 + e];
+      v8 hi, lo;
+      if constexpr (F::dtype == DAVET_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) hi[e] = pv[e];
+      } else {
+        u32x4 w, w2;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] = F::store2(pv[2 * e], pv[2 * e + 1]);
+          if constexpr (G == 1)
+            w2[e] = F::store2(pv[2 * e] - F::load((uint16_t)(w[e] & 0xffffu)),
+                              pv[2 * e + 1] - F::load((uint16_t)(w[e] >> 16)));
+        }
+        hi = __builtin_bit_cast(v8, w);
+        if constexpr (G == 1) lo = __builtin_bit_cast(v8, w2);
+      }
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        const v8 vf = T::v_frag(Vb, ps, dt, lane);
+        o[dt] = mm<F>(vf, hi, o[dt]);
+        // Few rows wait for memory, not for the matrix cores: what rounding to
+        // 16 bits took off the probabilities is multiplied as well.
+        if constexpr (G == 1 && F::dtype != DAVET_F32) o[dt] = mm<F>(vf, lo, o[dt]);
+      }
+    }
+  };
+
+  if constexpr (G == 4) {
+    const int nt = max(0, (end - begin + KT - 1) / KT);
+    if constexpr (BUFS == 1) {
+      // one buffer, refilled once every wave is done with it; the other
+      // workgroups of the CU hide the load
+      int holes = nt > 0 ? issue(begin, 0) : 0;
+      for (int it = 0; it < nt; ++it) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        sync_lds();
+        if (live) compute(begin + it * KT, gbuf, holes);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        sync_lds();
+        if (it + 1 < nt) holes = issue(begin + (it + 1) * KT, 0);
+      }
+    } else {
+      int holes = nt > 0 ? issue(begin, 0) : 0;
+      for (int it = 0; it < nt; ++it) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        sync_lds();
+        const int cur = holes;
+        if (it + 1 < nt) holes = issue(begin + (it + 1) * KT, (it + 1) & 1);
+        if (live) compute(begin + it * KT, gbuf + (it & 1) * 2 * TILE, cur);
+      }
+    }
+  } else {
+    // tiles wave, wave + 4, ... of the piece
+    int k0 = begin + wave * KT;
+    int holes = k0 < end ? issue(k0, 0) : 0;
+    for (int it = 0; k0 < end; ++it, k0 += 4 * KT) {
+      const int cur = holes;
+      if constexpr (BUFS == 2) {
+        if (k0 + 4 * KT < end) {
+          holes = issue(k0 + 4 * KT, (it + 1) & 1);
+          // the loads of the next tile may stay out; holes issue fewer
+          if (holes)
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+          else
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * NI) : "memory");
+        } else {
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        }
+        compute(k0, gbuf + (it & 1) * 2 * TILE, cur);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      } else {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        compute(k0, gbuf, cur);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (k0 + 4 * KT < end) holes = issue(k0 + 4 * KT, 0);
+      }
+    }
+  }
+
+  const float bias_ln = BIAS * kLn2;
+  if constexpr (G == 1) {
+    // join the four streams: O as [wave][dim][32 rows], then max and sum
+    __syncthreads();
+    float* mo = reinterpret_cast<float*>(smem);
+    float* ml = mo + 4 * D * 32;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        mo[(wave * D + dt * 32 + (e >> 2) * 8 + hh * 4 + (e & 3)) * 32 + l32] =
+            o[dt][e];
+    if (hh == 0) {
+      ml[wave * 64 + l32] = m_run;
+      ml[wave * 64 + 32 + l32] = l_run;
+    }
+    __syncthreads();
+    // thread: row l32, dims (D / 8) (t / 32) ..
+    constexpr int DP = D / 8;
+    const int d0 = (threadIdx.x >> 5) * DP;
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + l32]);
+    float wt[4], l = 0.f;
+    bool use[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = ml[w * 64 + l32], lw = ml[w * 64 + 32 + l32];
+      use[w] = lw != 0.f;                 // (NaN scores: sum NaN, maximum -inf)
+      wt[w] = use[w] ? __builtin_amdgcn_exp2f((mw - m) * sc_.c) : 0.f;
+      if (use[w]) l += wt[w] * lw;
+    }
+    float acc[DP];
+#pragma unroll
+    for (int i = 0; i < DP; ++i) {
+      acc[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        if (use[w]) acc[i] += wt[w] * mo[(w * D + d0 + i) * 32 + l32];
+    }
+    if (wrow + l32 >= rows) return;
+    if (ap.pieces > 1) {
+      const int64_t at = (int64_t)pl.piece * part_rows +
+                         (int64_t)(row0 + qi) * n_heads + qh;
+      float* po = part + at * D + d0;
+#pragma unroll
+      for (int i = 0; i < DP; i += 4)
+        *reinterpret_cast<f32x4*>(po + i) =
+            f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+      if (d0 == 0) {
+        float* pm = part + (int64_t)ap.pieces * part_rows * D + at * 2;
+        pm[0] = m;
+        pm[1] = l;
+      }
+      return;
+    }
+    // a row that sees nothing (or only scores of -inf) is zeros, lse -inf
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    st* op = out + (int64_t)(row0 + qi) * ld_o + (int64_t)qh * D + d0;
+#pragma unroll
+    for (int i = 0; i < DP; i += 2) {
+      if constexpr (F::dtype == DAVET_F32) {
+        op[i] = acc[i] * inv;
+        op[i + 1] = acc[i + 1] * inv;
+      } else {
+        *reinterpret_cast<uint32_t*>(op + i) =
+            F::store2(acc[i] * inv, acc[i + 1] * inv);
+      }
+    }
+    if (lse && d0 == 0)
+      lse[(int64_t)(row0 + qi) * n_heads + qh] =
+          l == 0.f ? -INFINITY : m * sc_.scale + (logf(l) - bias_ln);
+  } else {
+    if (wrow + l32 >= rows) return;
+    const int64_t at = (int64_t)pl.piece * part_rows +
+                       (int64_t)(row0 + qi) * n_heads + qh;
+    if (ap.pieces > 1) {
+      float* po = part + at * D + hh * 4;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<f32x4*>(po + dt * 32 + u * 8) =
+              f32x4{o[dt][u * 4], o[dt][u * 4 + 1], o[dt][u * 4 + 2], o[dt][u * 4 + 3]};
+      if (hh == 0) {
+        float* pm = part + (int64_t)ap.pieces * part_rows * D + at * 2;
+        pm[0] = m_run;
+        pm[1] = l_run;
+      }
+      return;
+    }
+    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+    st* op = out + (int64_t)(row0 + qi) * ld_o + (int64_t)qh * D + hh * 4;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = o[dt][u * 4 + e] * inv;
+        if constexpr (F::dtype == DAVET_F32)
+          *reinterpret_cast<f32x4*>(op + dt * 32 + u * 8) = f32x4{x[0], x[1], x[2], x[3]};
+        else
+          *reinterpret_cast<u32x2*>(op + dt * 32 + u * 8) =
+              u32x2{F::store2(x[0], x[1]), F::store2(x[2], x[3])};
+      }
+    if (lse && hh == 0)
+      lse[(int64_t)(row0 + qi) * n_heads + qh] =
+          l_run == 0.f ? -INFINITY
+                       : m_run * sc_.scale + (logf(l_run) - bias_ln);
+  }
+}
+
+// Joins the pieces of every row: with m the largest piece maximum and
+// w_p = 2^((m_p - m) c), o = sum w_p O_p / sum w_p l_p, in piece order.  D / 4
+// threads a row, four dims each.
+template <typename F, int D>
+__global__ void __launch_bounds__(256)
+cache_merge_kernel(ChunkPack cp, const float* __restrict__ part, int part_rows,
+                   int piece, int pieces, typename F::st* __restrict__ out,
+                   int64_t ld_o, float* __restrict__ lse, int n_heads, Scale sc_) {
+  constexpr int TR = D / 4;
+  const int64_t row = (int64_t)blockIdx.x * (256 / TR) + threadIdx.x / TR;
+  if (row >= part_rows) return;
+  const int d0 = (threadIdx.x % TR) * 4;
+  const int tok = (int)(row / n_heads), h = (int)(row % n_heads);
+  const int s = owner(cp.row0, cp.n_seqs, tok);
+  const int np = (cp.kv[s] + piece - 1) / piece;
+  const float* pm = part + (int64_t)pieces * part_rows * D;
+  float m = -INFINITY;
+  for (int p = 0; p < np; ++p)
+    m = fmaxf(m, pm[((int64_t)p * part_rows + row) * 2]);
+  float l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < np; ++p) {
+    const int64_t at = (int64_t)p * part_rows + row;
+    const float mp = pm[at * 2], lp = pm[at * 2 + 1];
+    const f32x4 o = *reinterpret_cast<const f32x4*>(part + at * D + d0);
+    if (lp != 0.f) {
+      const float w = __builtin_amdgcn_exp2f((mp - m) * sc_.c);
+      l += w * lp;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] += w * o[i];
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  typename F::st* op = out + (int64_t)tok * ld_o + (int64_t)h * D + d0;
+  if constexpr (F::dtype == DAVET_F32)
+    *reinterpret_cast<f32x4*>(op) = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+  else
+    *reinterpret_cast<u32x2*>(op) = u32x2{F::store2(acc[0] * inv, acc[1] * inv),
+                                          F::store2(acc[2] * inv, acc[3] * inv)};
+  if (lse && d0 == 0)
+    lse[row] = l == 0.f
+                   ? -INFINITY
+                   : m * sc_.scale + (logf(l) - Frag<F>::kBias * kLn2);
+}
+
+// Weights: w_j = prev_j + sum over the rows r that see key j of
+// exp(scale q_r.k_j - lse_r).  S = Q K^T this time: a lane holds 16 rows' scores
+// of ONE key and adds them in registers.  A workgroup takes 128 keys (32 a wave,
+// held as fragments) and walks the rows of its key heads in tiles of 32 that the
+// four waves share through LDS.  Chunks of (key head, row range) leave partial
+// sums that a second kernel adds in order.
+struct WeightPlan {
+  int32_t blk[DAVET_MAX_SEQS + 1];    // first 128-key block of each sequence
+  int32_t heads;                      // key heads a chunk
+  int32_t qsplit;                     // row ranges a key head (heads = 1)
+  int32_t chunks;
+};
+
+template <typename F, int D>
+__global__ void __launch_bounds__(256, 2)
+cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
+                     const typename F::st* __restrict__ q, int64_t ld_q,
+                     const float* __restrict__ lse, int n_heads, int block,
+                     float scale, const float* __restrict__ prev,
+                     float* __restrict__ weights, int64_t ld_w,
+                     float* __restrict__ part) {
+  using st = typename F::st;
+  using T = Tile<F, D>;
+  using v8 = typename Frag<F>::v8;
+  constexpr int QB = 32 * T::RB;
+  constexpr int NI = 32 / T::RPI / 4;             // loads a wave
+  __shared__ __attribute__((aligned(1024))) char qs[2][QB];
+  __shared__ __attribute__((aligned(16))) float ls[2][32];
+  const int nblk = wp.blk[cp.n_seqs];
+  const int blk = blockIdx.x % nblk, chunk = blockIdx.x / nblk;
+  const int s = owner(wp.blk, cp.n_seqs, blk);
+  const int g = n_heads / cv.n_kv;
+  const int row0 = cp.row0[s], n = cp.row0[s + 1] - row0, kv = cp.kv[s];
+  const int rows = n * g, nqb = (rows + 31) / 32;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int key = (blk - wp.blk[s]) * kWeightKeys + wave * 32 + l32;
+  const int kc = min(key, kv - 1);
+  const int page = cv.table[(int64_t)s * cv.max_pages + (kc >> cv.lg)];
+  const bool hole = (unsigned)page >= (unsigned)cv.n_pages;
+  const int64_t kbase = hole ? 0 : (((int64_t)page * cv.n_kv) << cv.lg) + (kc & ((1 << cv.lg) - 1));
+  int h0, h1, b0 = 0, b1 = nqb;
+  if (wp.qsplit > 1) {
+    h0 = chunk / wp.qsplit;
+    h1 = h0 + 1;
+    const int per = (nqb + wp.qsplit - 1) / wp.qsplit;
+    b0 = min(nqb, (chunk % wp.qsplit) * per);
+    b1 = min(nqb, b0 + per);
+  } else {
+    h0 = chunk * wp.heads;
+    h1 = min(h0 + wp.heads, cv.n_kv);
+  }
+  const int nb = b1 - b0, steps = (h1 - h0) * nb;
+  float next_lse = INFINITY;      // of the step whose rows are under way
+  auto issue = [&](int step, int b) {
+    const int h = h0 + step / nb, qb = b0 + step % nb;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int lr = (wave * NI + i) * T::RPI + lane / T::C;
+      const int r = min(qb * 32 + lr, rows - 1);
+      const st* src = q + (int64_t)(row0 + r / g) * ld_q +
+                      (int64_t)(h * g + r % g) * D;
+      dma16(reinterpret_cast<const char*>(src) + T::k_slot(lr, lane % T::C) * 16,
+            qs[b] + (wave * NI + i) * 1024);
+    }
+    if (threadIdx.x < 32) {
+      // rows past the last, and rows that saw nothing, give 0: exp(x - inf)
+      const int r = qb * 32 + threadIdx.x;
+      next_lse = INFINITY;
+      if (r < rows)
+        next_lse = lse[(int64_t)(row0 + r / g) * n_heads + h * g + r % g];
+    }
+  };
+  v8 kf[D / 16];
+  float acc = 0.f;
+  if (steps > 0) issue(0, 0);
+  for (int step = 0; step < steps; ++step) {
+    const int h = h0 + step / nb, qb = b0 + step % nb;
+    if (qb == b0) {
+      const st* kp = static_cast<const st*>(cv.k) + (kbase + ((int64_t)h << cv.lg)) * D + hh * 8;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) kf[ks] = load_frag<F>(kp + ks * 16);
+    }
+    if (threadIdx.x < 32)
+      ls[step & 1][threadIdx.x] = next_lse == -INFINITY ? INFINITY : next_lse;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    sync_lds();
+    if (step + 1 < steps) issue(step + 1, (step + 1) & 1);
+    const char* Qb = qs[step & 1];
+    f32x16 sc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      sc = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[ks], sc);
+    const int first_lim = visible_end(min(qb * 32, rows - 1) / g, n, kv, block);
+    const bool masked = (blk - wp.blk[s] + 1) * kWeightKeys > first_lim;
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const f32x4 lv = *reinterpret_cast<const f32x4*>(&ls[step & 1][u * 8 + hh * 4]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float p = __builtin_amdgcn_exp2f(fmaf(sc[u * 4 + e], scale, -lv[e]) * kLog2e);
+        if (masked) {
+          const int r = qb * 32 + u * 8 + hh * 4 + e;
+          if (r >= rows || key >= visible_end(r / g, n, kv, block)) p = 0.f;
+        }
+        // (a row past the last repeats one: its lse is +inf, its weight 0)
+        sum += p;
+      }
+    }
+    acc += sum;
+  }
+  acc = pair_sum32(acc);
+  if (hole) acc = 0.f;
+  if (hh == 0) {
+    if (wp.chunks > 1) {
+      part[((int64_t)chunk * nblk + blk) * kWeightKeys + wave * 32 + l32] = acc;
+    } else if (key < kv) {
+      const int64_t at = (int64_t)s * ld_w + key;
+      weights[at] = (prev ? prev[at] : 0.f) + acc;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kWeightKeys)
+cache_weights_join_kernel(ChunkPack cp, WeightPlan wp,
+                          const float* __restrict__ part,
+                          const float* __restrict__ prev,
+                          float* __restrict__ weights, int64_t ld_w) {
+  const int nblk = wp.blk[cp.n_seqs], blk = blockIdx.x;
+  const int s = owner(wp.blk, cp.n_seqs, blk);
+  const int key = (blk - wp.blk[s]) * kWeightKeys + threadIdx.x;
+  if (key >= cp.kv[s]) return;
+  float acc = 0.f;
+#pragma unroll 8
+  for (int c = 0; c < wp.chunks; ++c)
+    acc += part[((int64_t)c * nblk + blk) * kWeightKeys + threadIdx.x];
+  const int64_t at = (int64_t)s * ld_w + key;
+  weights[at] = (prev ? prev[at] : 0.f) + acc;
+}
+
+Scale make_scale(float scale, int D) {
+  const double s = scale == 0.f ? 1.0 / sqrt((double)D) : (double)scale;
+  const double c = s * 1.4426950408889634074;
+  Scale r;
+  r.c = (float)c;
+  r.c_lo = (float)(c - (double)r.c);
+  r.scale = (float)s;
+  return r;
+}
+
+size_t attn_part_floats(int64_t rows, int pieces, int D) {
+  return (size_t)rows * pieces * (D + 2);
+}
+
+int max_pieces(int64_t rows) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxPieces, kMaxPartRows / rows));
+}
+
+// Cuts the keys into pieces so that the workgroups fill the chip once: `want`
+// of them run at a time.
+AttnPlan plan_attn(const ChunkPack& cp, int n_kv, int g, int rows, int want,
+                   int unit, int cap) {
+  AttnPlan ap{};
+  ap.xcd = n_kv % 8 == 0;
+  int64_t work = 0;
+  int longest = 1;
+  for (int s = 0; s < cp.n_seqs; ++s) {
+    const int64_t nt = ((int64_t)(cp.row0[s + 1] - cp.row0[s]) * g + rows - 1) / rows;
+    work += nt * n_kv * cp.kv[s];
+    if (nt) longest = std::max(longest, cp.kv[s]);
+    ap.order[s] = (uint8_t)s;
+  }
+  std::stable_sort(ap.order, ap.order + cp.n_seqs,
+                   [&](uint8_t a, uint8_t b) { return cp.kv[a] > cp.kv[b]; });
+  int64_t piece = std::max<int64_t>((work + want - 1) / want,
+                                    ((int64_t)longest + cap - 1) / cap);
+  piece = std::max<int64_t>(align_up(piece, unit), 4 * unit);
+  auto blocks = [&](int64_t p, int s) {
+    const int64_t nt = ((int64_t)(cp.row0[s + 1] - cp.row0[s]) * g + rows - 1) / rows;
+    return nt * n_kv * ((cp.kv[s] + p - 1) / p);
+  };
+  for (; piece < longest; piece = align_up(piece + piece / 16, unit)) {
+    int64_t t = 0;
+    for (int s = 0; s < cp.n_seqs; ++s) t += blocks(piece, s);
+    if (t <= want) break;
+  }
+  piece = std::min<int64_t>(piece, align_up(longest, unit));
+  ap.piece = (int)piece;
+  ap.pieces = (int)((longest + piece - 1) / piece);
+  int64_t at = 0;
+  for (int i = 0; i < cp.n_seqs; ++i) {
+    ap.blk[i] = (int)at;
+    at += blocks(piece, ap.order[i]) / (ap.xcd ? 8 : 1);
+  }
+  ap.blk[cp.n_seqs] = (int)at;
+  return ap;
+}
+
+template <typename F, int D>
+int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
+                  int64_t ld_q, void* out, int64_t ld_o, float* lse,
+                  int n_heads, int block, Scale sc, float* part,
+                  hipStream_t stream) {
+  using st = typename F::st;
+  const int g = n_heads / cv.n_kv;
+  const int64_t rows = (int64_t)cp.row0[cp.n_seqs] * n_heads;
+  int most = 0;
+  for (int s = 0; s < cp.n_seqs; ++s)
+    most = std::max(most, cp.row0[s + 1] - cp.row0[s]);
+  const bool wide = (int64_t)most * g > 64;
+  constexpr bool f32 = F::dtype == DAVET_F32;
+  constexpr int WB = F::dtype == DAVET_BF16 ? 2 : 1;    // wide: buffers
+  constexpr int WM = F::dtype == DAVET_F16 ? 3 : 2;     // workgroups a CU
+  constexpr int NB = f32 && D == 128 ? 1 : 2;           // narrow
+  constexpr int NM = !f32 && D == 64 ? 2 : 1;
+  const AttnPlan ap = plan_attn(cp, cv.n_kv, g, wide ? 128 : 32,
+                                256 * (wide ? WM : NM), wide ? 64 : 128,
+                                max_pieces(rows));
+  const int64_t grid = (int64_t)ap.blk[cp.n_seqs] * (ap.xcd ? 8 : 1);
+  DAVET_CHECK_ARG(grid < (1ll << 31), DAVET_ESHAPE,
+                  "davet_cache_attention: too many row tiles");
+  {
+    ProfScope ps(KC_MISC, stream);
+    if (wide)
+      hipLaunchKernelGGL((cache_attn_kernel<F, D, 4, WB, WM>), dim3((unsigned)grid),
+                         dim3(256), 0, stream, cv, cp, ap, (const st*)q, ld_q,
+                         (st*)out, ld_o, lse, n_heads, block, sc, part, (int)rows);
+    else
+      hipLaunchKernelGGL((cache_attn_kernel<F, D, 1, NB, NM>), dim3((unsigned)grid),
+                         dim3(256), 0, stream, cv, cp, ap, (const st*)q, ld_q,
+                         (st*)out, ld_o, lse, n_heads, block, sc, part, (int)rows);
+    DAVET_HIP(hipGetLastError());
+  }
+  if (ap.pieces > 1) {
+    ProfScope ps(KC_MISC, stream);
+    const int per = 256 / (D / 4);
+    hipLaunchKernelGGL((cache_merge_kernel<F, D>),
+                       dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0,
+                       stream, cp, part, (int)rows, ap.piece, ap.pieces, (st*)out,
+                       ld_o, lse, n_heads, sc);
+    DAVET_HIP(hipGetLastError());
+  }
+  return DAVET_OK;
+}
+
+template <typename F, int D>
+int run_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
+                int64_t ld_q, const float* lse, int n_heads, int block,
+                float scale, const float* prev, float* weights, int64_t ld_w,
+                float* part, hipStream_t stream) {
+  WeightPlan wp{};
+  int most = 0;
+  for (int s = 0; s < cp.n_seqs; ++s) {
+    const int n = cp.row0[s + 1] - cp.row0[s];
+    most = std::max(most, n);
+    wp.blk[s + 1] = wp.blk[s] + (cp.kv[s] + kWeightKeys - 1) / kWeightKeys;
+  }
+  const int nblk = wp.blk[cp.n_seqs];
+  if (nblk == 0) return DAVET_OK;
+  const int g = n_heads / cv.n_kv;
+  const int64_t nqb = ((int64_t)most * g + 31) / 32;
+  // 1024 workgroups fill the chip twice
+  const int want = std::max(1, kWeightParts / 2 / nblk);
+  wp.qsplit = 1;
+  if (want >= cv.n_kv) {
+    wp.heads = 1;
+    wp.qsplit = (int)std::max<int64_t>(1, std::min<int64_t>(want / cv.n_kv, nqb / 2));
+    wp.chunks = cv.n_kv * wp.qsplit;
+  } else {
+    wp.heads = (cv.n_kv + want - 1) / want;
+    wp.chunks = (cv.n_kv + wp.heads - 1) / wp.heads;
+  }
+  const int64_t grid = (int64_t)nblk * wp.chunks;
+  DAVET_CHECK_ARG(grid < (1ll << 31), DAVET_ESHAPE,
+                  "davet_cache_weights: too many key blocks");
+  {
+    ProfScope ps(KC_MISC, stream);
+    hipLaunchKernelGGL((cache_weights_kernel<F, D>), dim3((unsigned)grid), dim3(256),
+                       0, stream, cv, cp, wp, (const typename F::st*)q, ld_q, lse,
+                       n_heads, block, scale, prev, weights, ld_w, part);
+    DAVET_HIP(hipGetLastError());
+  }
+  if (wp.chunks > 1) {
+    ProfScope ps(KC_MISC, stream);
+    hipLaunchKernelGGL(cache_weights_join_kernel, dim3(nblk), dim3(kWeightKeys),
+                       0, stream, cp, wp, part, prev, weights, ld_w);
+    DAVET_HIP(hipGetLastError());
+  }
+  return DAVET_OK;
+}
+
+size_t workspace_bytes(int64_t total_q, int n_heads, int D) {
+  const int64_t rows = total_q * n_heads;
+  size_t b = 0;
+  if (rows > 0 && max_pieces(rows) > 1)
+    b = attn_part_floats(rows, max_pieces(rows), D) * sizeof(float);
+  const size_t w = (size_t)kWeightParts * kWeightKeys * sizeof(float);
+  return align_up(std::max(b, w), 256);
+}
+
+int check_workspace(const void* ws, size_t have, int64_t total_q, int n_heads,
+                    int D, const char* who) {
+  const size_t need = workspace_bytes(total_q, n_heads, D);
+  DAVET_CHECK_ARG(ws && ((uintptr_t)ws & 255) == 0 && have >= need, DAVET_ENOMEM,
+                  std::string(who) + ": workspace missing, misaligned or below " +
+                      std::to_string(need) + " bytes");
+  return DAVET_OK;
+}
+
+}  // namespace
+}  // namespace davet
+
+extern "C" int davet_cache_workspace_bytes(int32_t n_heads, int32_t head_dim,
+                                           int32_t max_q, size_t* bytes) {
+  using namespace davet;
+  DAVET_CHECK_ARG(bytes, DAVET_EINVAL, "davet_cache_workspace_bytes: bytes is null");
+  DAVET_CHECK_ARG(n_heads >= 1 && n_heads <= 1024 &&
+                      (head_dim == 64 || head_dim == 128) && max_q >= 1 &&
+                      max_q <= (1 << 24),
+                  DAVET_ESHAPE, "davet_cache_workspace_bytes: sizes out of range");
+  // the need of a chunk is not monotonic in its rows (fewer rows may be cut
+  // into more pieces): the bound is that of the worst chunk up to max_q
+  const int64_t rows = (int64_t)max_q * n_heads;
+  size_t b = workspace_bytes(max_q, n_heads, head_dim);
+  const int64_t most = std::min<int64_t>(rows * kMaxPieces, kMaxPartRows);
+  b = std::max(b, align_up((size_t)most * (head_dim + 2) * sizeof(float), 256));
+  *bytes = b;
+  return DAVET_OK;
+}
+
+extern "C" int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs,
+                                     const int32_t* cu_q, const int32_t* kv_len,
+                                     const void* q, int64_t ld_q, int32_t n_heads,
+                                     float scale, int32_t block, void* out,
+                                     int64_t ld_out, float* lse, void* workspace,
+                                     size_t ws_bytes, hipStream_t stream) {
+  using namespace davet;
+  static const char who[] = "davet_cache_attention";
+  CacheView cv;
+  ChunkPack cp;
+  int rc = check_cache(cache, true, who, &cv);
+  if (!rc) rc = check_heads(cache, n_heads, who);
+  if (!rc) rc = check_chunk(cache, n_seqs, cu_q, kv_len, who, &cp);
+  const int D = cache ? cache->head_dim : 0;
+  const int64_t total = rc ? 0 : cp.row0[n_seqs];
+  if (!rc && total > 0)
+    rc = check_rows(q, ld_q, (int64_t)n_heads * D, cache->dtype, who, "q");
+  if (!rc && total > 0)
+    rc = check_rows(out, ld_out, (int64_t)n_heads * D, cache->dtype, who, "out");
+  if (rc) return rc;
+  DAVET_CHECK_ARG(scale >= 0.f && std::isfinite(scale), DAVET_EINVAL,
+                  "davet_cache_attention: scale must be positive and finite, or 0");
+  DAVET_CHECK_ARG(block >= 0, DAVET_EINVAL,
+                  "davet_cache_attention: block must not be negative");
+  if (total == 0) return DAVET_OK;
+  DAVET_CHECK_ARG(total * n_heads <= (1ll << 30), DAVET_ESHAPE,
+                  "davet_cache_attention: too many query rows");
+  rc = check_workspace(workspace, ws_bytes, total, n_heads, D, who);
+  if (rc) return rc;
+  const size_t es = dtype_size(cache->dtype);
+  DAVET_CHECK_ARG(!overlap(out, ((total - 1) * ld_out + n_heads * D) * es, q,
+                           ((total - 1) * ld_q + n_heads * D) * es),
+                  DAVET_EINVAL, "davet_cache_attention: out overlaps q");
+  const Scale sc = make_scale(scale, D);
+  float* part = static_cast<float*>(workspace);
+#define ATT(F, DIM) run_attention<F, DIM>(cv, cp, q, ld_q, out, ld_out, lse,   \
+                                          n_heads, block, sc, part, stream)
+  if (cache->dtype == DAVET_F16) return D == 128 ? ATT(F16S, 128) : ATT(F16S, 64);
+  if (cache->dtype == DAVET_BF16) return D == 128 ? ATT(BF16S, 128) : ATT(BF16S, 64);
+  return D == 128 ? ATT(F32S, 128) : ATT(F32S, 64);
+#undef ATT
+}
+
+extern "C" int davet_cache_weights(const davet_kv_cache* cache, int32_t n_seqs,
+                                   const int32_t* cu_q, const int32_t* kv_len,
+                                   const void* q, int64_t ld_q, int32_t n_heads,
+                                   float scale, int32_t block, const float* lse,
+                                   const float* prev, float* weights,
+                                   int64_t ld_weights, void* workspace,
+                                   size_t ws_bytes, hipStream_t stream) {
+  using namespace davet;
+  static const char who[] = "davet_cache_weights";
+  CacheView cv;
+  ChunkPack cp;
+  int rc = check_cache(cache, false, who, &cv);
+  if (!rc) rc = check_heads(cache, n_heads, who);
+  if (!rc) rc = check_chunk(cache, n_seqs, cu_q, kv_len, who, &cp);
+  const int D = cache ? cache->head_dim : 0;
+  const int total = rc ? 0 : cp.row0[n_seqs];
+  if (!rc && total > 0)
+    rc = check_rows(q, ld_q, (int64_t)n_heads * D, cache->dtype, who, "q");
+  if (rc) return rc;
+  DAVET_CHECK_ARG((lse || total == 0) && weights, DAVET_EINVAL,
+                  "davet_cache_weights: null pointer");
+  DAVET_CHECK_ARG(scale >= 0.f && std::isfinite(scale) && block >= 0, DAVET_EINVAL,
+                  "davet_cache_weights: scale must be positive and finite, or 0, "
+                  "and block not negative");
+  for (int s = 0; s < n_seqs; ++s)
+    DAVET_CHECK_ARG(kv_len[s] <= ld_weights, DAVET_ESHAPE,
+                    "davet_cache_weights: kv_len beyond ld_weights");
+  DAVET_CHECK_ARG((int64_t)total * n_heads <= (1ll << 30), DAVET_ESHAPE,
+                  "davet_cache_weights: too many query rows");
+  rc = check_workspace(workspace, ws_bytes, total, n_heads, D, who);
+  if (rc) return rc;
+  const float sc = make_scale(scale, D).scale;
+  float* part = static_cast<float*>(workspace);
+#define WGT(F, DIM) run_weights<F, DIM>(cv, cp, q, ld_q, lse, n_heads, block, sc, \
+                                        prev, weights, ld_weights, part, stream)
+  if (cache->dtype == DAVET_F16) return D == 128 ? WGT(F16S, 128) : WGT(F16S, 64);
+  if (cache->dtype == DAVET_BF16) return D == 128 ? WGT(BF16S, 128) : WGT(BF16S, 64);
+  return D == 128 ? WGT(F32S, 128) : WGT(F32S, 64);
+#undef WGT
+}
