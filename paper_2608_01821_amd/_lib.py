@@ -515,51 +515,73 @@ def davet_run_schedule(cfg, weights: Weights, geoms, visual, view_bufs,
 # writes; without `stream` they run on the current stream of their tensors'
 # device, whichever device is current.
 
-def _rows(t, width, n_rows, name):
-    """(address, row stride in elements) of a 2-D tensor whose rows are dense
-    and hold `width` elements."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("davet: %s must be 2-D with dense rows" % name)
-    if t.shape[0] < n_rows or t.shape[1] < width:
+def _rows(t, width, n_rows, size, name):
+    """(address, row stride in elements) of a 2-D tensor of `size`-byte elements
+    whose rows are dense and hold `width` of them."""
+    if t.dim() != 2 or t.element_size() != size:
+        raise ValueError("davet: %s must be 2-D with %d-byte elements"
+                         % (name, size))
+    n, w = t.shape
+    if n < n_rows or w < width:
         raise ValueError("davet: %s must hold [%d, %d]" % (name, n_rows, width))
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if ld < width:
-        raise ValueError("davet: %s: rows overlap" % name)
+    ld, one = t.stride()
+    if one != 1 and w > 1:
+        raise ValueError("davet: the rows of %s must be dense" % name)
+    if n < 2:
+        ld = w
+    elif ld < width:
+        raise ValueError("davet: the rows of %s overlap" % name)
     return t.data_ptr(), ld
 
 
-def _dense(t, n, name):
+def _dense(t, n, name, size=4):
+    """Address of a dense tensor of at least `n` `size`-byte elements, or None."""
     if t is None:
         return None
-    if t.numel() < n:
-        raise ValueError("davet: %s must hold %d elements" % (name, n))
-    return _ptr(t)
+    if t.numel() < n or t.element_size() != size or not t.is_contiguous():
+        raise ValueError("davet: %s must be dense, with %d elements of %d bytes"
+                         % (name, n, size))
+    return t.data_ptr()
 
 
-def _typed(t, size, name):
-    if t is not None and t.element_size() != size:
-        raise ValueError("davet: %s must have %d-byte elements" % (name, size))
-
-
-def _nbytes(t):
-    return 0 if t is None else t.numel() * t.element_size()
+def _space(t):
+    """(address, bytes) of a workspace."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError("davet: the workspace must be dense")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _ints(vals):
     return vals if isinstance(vals, C.Array) else (C.c_int32 * len(vals))(*vals)
 
 
-def _launch(stream, call, *tensors):
-    """call(stream handle) with the device of the tensors current."""
-    import torch
-    dev = tensors[0].device
+def _gpu(first, *tensors):
+    """Index of the GPU that holds all tensors (None entries aside)."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("davet: tensor arguments must be on a GPU")
     for t in tensors:
-        if t is not None and (t.device != dev or not t.is_cuda):
+        if t is not None and t.get_device() != dev:
             raise ValueError("davet: tensor arguments must be on one GPU")
-    if dev.index == torch.cuda.current_device():
-        return _check(call(_stream(stream)))
-    with torch.cuda.device(dev):
-        return _check(call(_stream(stream)))
+    return dev
+
+
+def _launch(dev, stream, fn, *args):
+    """fn(*args, stream handle) with GPU `dev` current; without `stream`, on its
+    current one."""
+    import torch
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _launch(dev, stream, fn, *args)
+    if stream is None:
+        s = torch.cuda.current_stream().cuda_stream
+    else:
+        s = stream if isinstance(stream, int) else stream.cuda_stream
+    status = fn(*args, s)
+    if status:
+        _check(status)
 
 
 class KvCache:
@@ -568,21 +590,18 @@ class KvCache:
     int32 [n_seqs, max_pages], dense device tensors, which it keeps alive."""
 
     def __init__(self, k, v, page_table, dtype):
-        if k.dim() != 4 or (v is not None and v.shape != k.shape):
-            raise ValueError("davet: k and v must be [n_pages, n_kv_heads, "
-                             "page_size, head_dim] alike")
-        if page_table.dim() != 2:
-            raise ValueError("davet: page_table must be [n_seqs, max_pages]")
         size = 4 if dtype == DAVET_F32 else 2
-        _typed(k, size, "k")
-        _typed(v, size, "v")
-        _typed(page_table, 4, "page_table")
+        if k.dim() != 4 or (v is not None and v.shape != k.shape) or \
+                page_table.dim() != 2:
+            raise ValueError("davet: k and v must be [n_pages, n_kv_heads, "
+                             "page_size, head_dim] alike, page_table [n_seqs, "
+                             "max_pages]")
+        addr = (_dense(k, 0, "k", size), _dense(v, 0, "v", size),
+                _dense(page_table, 0, "page_table"))
         self.k, self.v, self.page_table = k, v, page_table
-        self.tensors = (k, v, page_table)
         self.n_seqs, self.head_dim, self.size = len(page_table), k.shape[3], size
         self.n_kv_heads, self.page_size = k.shape[1], k.shape[2]
-        self.struct = KvCacheT(_addr(k), _addr(v), _addr(page_table),
-                               page_table.shape[1], k.shape[0], k.shape[2],
+        self.struct = KvCacheT(*addr, page_table.shape[1], k.shape[0], k.shape[2],
                                k.shape[1], k.shape[3], int(dtype))
         self._ref = C.byref(self.struct)
 
@@ -593,23 +612,22 @@ class KvCache:
                              "page_table a row for each of those")
         return n, _ints(cu_q), _ints(kv_len), max(0, cu_q[n])
 
+    def _gpu(self, *tensors):
+        return _gpu(self.k, self.v, self.page_table, *tensors)
+
 
 def davet_cache_append(cache: KvCache, cu_q, kv_len, qkv, n_heads, q_out,
                        pos=None, norm=False, q_gain=None, k_gain=None, eps=1e-6,
                        theta=10000.0, stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
-    D = cache.head_dim
-    _typed(qkv, cache.size, "qkv")
-    _typed(q_out, cache.size, "q_out")
-    for t, name in ((pos, "pos"), (q_gain, "q_gain"), (k_gain, "k_gain")):
-        _typed(t, 4, name)
-    x, ldx = _rows(qkv, (n_heads + 2 * cache.n_kv_heads) * D, rows, "qkv")
-    q, ldq = _rows(q_out, n_heads * D, rows, "q_out")
-    p, gq, gk = (_dense(t, m, name) for t, m, name in (
-        (pos, rows, "pos"), (q_gain, D, "q_gain"), (k_gain, D, "k_gain")))
-    _launch(stream, lambda s: _L.davet_cache_append(
-        cache._ref, n, cu, kv, x, ldx, n_heads, p, 1 if norm else 0, gq, gk, eps,
-        theta, q, ldq, s), *cache.tensors, qkv, q_out, pos, q_gain, k_gain)
+    D, size = cache.head_dim, cache.size
+    x, ldx = _rows(qkv, (n_heads + 2 * cache.n_kv_heads) * D, rows, size, "qkv")
+    q, ldq = _rows(q_out, n_heads * D, rows, size, "q_out")
+    p = _dense(pos, rows, "pos")
+    gq, gk = _dense(q_gain, D, "q_gain"), _dense(k_gain, D, "k_gain")
+    _launch(cache._gpu(qkv, q_out, pos, q_gain, k_gain), stream,
+            _L.davet_cache_append, cache._ref, n, cu, kv, x, ldx, n_heads, p,
+            1 if norm else 0, gq, gk, eps, theta, q, ldq)
 
 
 def davet_cache_workspace_bytes(n_heads, head_dim, max_q):
@@ -623,70 +641,56 @@ def davet_cache_attention(cache: KvCache, cu_q, kv_len, q, n_heads, out,
                           lse=None, scale=0.0, block=0, workspace=None,
                           stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
-    D = cache.head_dim
-    _typed(q, cache.size, "q")
-    _typed(out, cache.size, "out")
-    _typed(lse, 4, "lse")
-    x, ldx = _rows(q, n_heads * D, rows, "q")
-    o, ldo = _rows(out, n_heads * D, rows, "out")
-    e, ws, nb = _dense(lse, rows * n_heads, "lse"), _ptr(workspace), \
-        _nbytes(workspace)
-    _launch(stream, lambda s: _L.davet_cache_attention(
-        cache._ref, n, cu, kv, x, ldx, n_heads, scale, block, o, ldo, e, ws, nb,
-        s), *cache.tensors, q, out, lse, workspace)
+    width = n_heads * cache.head_dim
+    x, ldx = _rows(q, width, rows, cache.size, "q")
+    o, ldo = _rows(out, width, rows, cache.size, "out")
+    e, (ws, nb) = _dense(lse, rows * n_heads, "lse"), _space(workspace)
+    _launch(cache._gpu(q, out, lse, workspace), stream, _L.davet_cache_attention,
+            cache._ref, n, cu, kv, x, ldx, n_heads, scale, block, o, ldo, e, ws, nb)
 
 
 def davet_cache_weights(cache: KvCache, cu_q, kv_len, q, n_heads, lse, weights,
                         prev=None, scale=0.0, block=0, workspace=None,
                         stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
-    _typed(q, cache.size, "q")
-    for t, name in ((lse, "lse"), (prev, "prev"), (weights, "weights")):
-        _typed(t, 4, name)
     most = max(kv)
-    x, ldx = _rows(q, n_heads * cache.head_dim, rows, "q")
-    w, ldw = _rows(weights, most, n, "weights")
+    x, ldx = _rows(q, n_heads * cache.head_dim, rows, cache.size, "q")
+    w, ldw = _rows(weights, most, n, 4, "weights")
     p = None
     if prev is not None:
-        p, ldp = _rows(prev, most, n, "prev")
+        p, ldp = _rows(prev, most, n, 4, "prev")
         if ldp != ldw and n > 1:
             raise ValueError("davet: prev and weights need one row stride")
-    e, ws, nb = _dense(lse, rows * n_heads, "lse"), _ptr(workspace), \
-        _nbytes(workspace)
-    _launch(stream, lambda s: _L.davet_cache_weights(
-        cache._ref, n, cu, kv, x, ldx, n_heads, scale, block, e, p, w, ldw, ws,
-        nb, s), *cache.tensors, q, lse, weights, prev, workspace)
+    e, (ws, nb) = _dense(lse, rows * n_heads, "lse"), _space(workspace)
+    _launch(cache._gpu(q, lse, weights, prev, workspace), stream,
+            _L.davet_cache_weights, cache._ref, n, cu, kv, x, ldx, n_heads, scale,
+            block, e, p, w, ldw, ws, nb)
 
 
 def davet_evict_select(n, keep, weights, kept, first=0, last=0,
                        weights_out=None, stream=None):
     """``n`` and ``keep``: host lists, one entry a sequence."""
-    if len(n) != len(keep):
+    seqs = len(n)
+    if seqs != len(keep) or seqs == 0:
         raise ValueError("davet: n and keep need one entry a sequence")
-    for t, name in ((weights, "weights"), (kept, "kept"),
-                    (weights_out, "weights_out")):
-        _typed(t, 4, name)
-    w, ldw = _rows(weights, max(n), len(n), "weights")
-    k, ldk = _rows(kept, max(keep), len(n), "kept")
+    most = max(keep)
+    w, ldw = _rows(weights, max(n), seqs, 4, "weights")
+    k, ldk = _rows(kept, most, seqs, 4, "kept")
     o, ldo = (None, 0) if weights_out is None else \
-        _rows(weights_out, max(keep), len(n), "weights_out")
-    _launch(stream, lambda s: _L.davet_evict_select(
-        len(n), _ints(n), _ints(keep), w, ldw, first, last, k, ldk, o, ldo, s),
-        weights, kept, weights_out)
+        _rows(weights_out, most, seqs, 4, "weights_out")
+    _launch(_gpu(weights, kept, weights_out), stream, _L.davet_evict_select, seqs,
+            _ints(n), _ints(keep), w, ldw, first, last, k, ldk, o, ldo)
 
 
 def davet_cache_gather(cache: KvCache, kept, keep, dst_table, stream=None):
     """``keep``: host list; ``dst_table``: dense int32 [n_seqs, pages]."""
     n = len(keep)
-    _typed(kept, 4, "kept")
-    _typed(dst_table, 4, "dst_table")
-    if n > cache.n_seqs or dst_table.dim() != 2 or len(dst_table) < n:
+    if n == 0 or n > cache.n_seqs or dst_table.dim() != 2 or len(dst_table) < n:
         raise ValueError("davet: the page tables need a row a sequence")
-    k, ldk = _rows(kept, max(keep), n, "kept")
-    dst = _ptr(dst_table)
-    _launch(stream, lambda s: _L.davet_cache_gather(
-        cache._ref, n, _ints(keep), k, ldk, dst, dst_table.shape[1], s),
-        *cache.tensors, kept, dst_table)
+    k, ldk = _rows(kept, max(keep), n, 4, "kept")
+    dst = _dense(dst_table, 0, "dst_table")
+    _launch(cache._gpu(kept, dst_table), stream, _L.davet_cache_gather, cache._ref,
+            n, _ints(keep), k, ldk, dst, dst_table.shape[1])
 
 
 def davet_logprobs_workspace_bytes(rows, vocab, top):
@@ -702,24 +706,21 @@ def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
     """``logits`` [rows, vocab]; ``top_logp`` and ``top_ids`` [rows, top], dense
     (both or neither)."""
     rows, vocab = logits.shape
-    _typed(logits, 4 if dtype == DAVET_F32 else 2, "logits")
-    for t, name in ((targets, "targets"), (logp, "logp"), (entropy, "entropy"),
-                    (top_logp, "top_logp"), (top_ids, "top_ids")):
-        _typed(t, 4, name)
-    top = 0
+    x, ld = _rows(logits, vocab, rows, 4 if dtype == DAVET_F32 else 2, "logits")
+    g, lp, en = _dense(targets, rows, "targets"), _dense(logp, rows, "logp"), \
+        _dense(entropy, rows, "entropy")
+    top, tl, ti = 0, None, None
     if top_ids is not None or top_logp is not None:
-        if top_ids is None or top_logp is None or top_ids.shape != top_logp.shape \
-                or top_ids.dim() != 2 or len(top_ids) < rows:
+        if top_ids is None or top_logp is None or top_ids.dim() != 2 or \
+                top_ids.shape != top_logp.shape:
             raise ValueError("davet: top_logp and top_ids must be [rows, top]")
         top = top_ids.shape[1]
-    x, ld = _rows(logits, vocab, rows, "logits")
-    g, lp, en = (_dense(t, rows, name) for t, name in (
-        (targets, "targets"), (logp, "logp"), (entropy, "entropy")))
-    tl, ti = (_ptr(top_logp), _ptr(top_ids)) if top else (None, None)
-    ws, nb = _ptr(workspace), _nbytes(workspace)
-    _launch(stream, lambda s: _L.davet_token_logprobs(
-        rows, vocab, x, int(dtype), ld, exclude, g, lp, en, top, tl, ti, ws, nb,
-        s), logits, targets, logp, entropy, top_logp, top_ids, workspace)
+        tl = _dense(top_logp, rows * top, "top_logp")
+        ti = _dense(top_ids, rows * top, "top_ids")
+    ws, nb = _space(workspace)
+    _launch(_gpu(logits, targets, logp, entropy, top_logp, top_ids, workspace),
+            stream, _L.davet_token_logprobs, rows, vocab, x, int(dtype), ld,
+            exclude, g, lp, en, top, tl, ti, ws, nb)
 
 
 def prof_enable(max_launches):

@@ -257,6 +257,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   constexpr int NI = OWN / T::RPI;                // its loads, of K and of V
   constexpr float BIAS = Frag<F>::kBias;
   __shared__ __attribute__((aligned(1024))) char smem[LDS];
+  __shared__ int s_bad;         // some value of a masked tile is not finite
 
   const int g = n_heads / cv.n_kv;
   const Place pl = place(ap, cp, cv.n_kv, g, 32 * G);
@@ -266,21 +267,22 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wrow = pl.tile * 32 * G + (G == 4 ? wave * 32 : 0);
-  const int r = min(wrow + l32, rows - 1);
-  const int qi = r / g, qh = hk * g + r % g;
   const bool live = wrow < rows;                  // of the wave
   // keys of this piece, up to the last one that any row of the tile sees
   const int tile_last = min(pl.tile * 32 * G + 32 * G, rows) - 1;
   const int end = min((pl.piece + 1) * ap.piece,
                       visible_end(tile_last / g, n, kv, block));
   const int begin = pl.piece * ap.piece;
-  const int lim = visible_end(qi, n, kv, block);
+  const int lim = visible_end(min(wrow + l32, rows - 1) / g, n, kv, block);
   // keys before this are visible to every row of the wave
-  const int lim_all = min(visible_end(min(wrow, rows - 1) / g, n, kv, block), kv);
+  const int lim_all = visible_end(min(wrow, rows - 1) / g, n, kv, block);
+  const int lim_tile = visible_end(pl.tile * 32 * G / g, n, kv, block);
 
   v8 qf[D / 16];
   {
-    const st* qp = q + (int64_t)(row0 + qi) * ld_q + (int64_t)qh * D + hh * 8;
+    const int r = min(wrow + l32, rows - 1);
+    const st* qp = q + (int64_t)(row0 + r / g) * ld_q +
+                   (int64_t)(hk * g + r % g) * D + hh * 8;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = load_frag<F>(qp + ks * 16);
   }
@@ -291,6 +293,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
 
+  if (threadIdx.x == 0) s_bad = 0;
+  __syncthreads();
   const int grp = G == 4 ? 0 : wave;
   char* gbuf = smem + grp * GROUP;
   PageIds pages;
@@ -380,16 +384,39 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * sc_.c);
     const float neg_m = BIAS - ref * sc_.c;
     float psum = 0.f;
+    // probabilities as operands of 16 keys each; lo: what rounding to 16 bits
+    // took off them (few rows wait for memory, not for the matrix cores)
+    v8 hi[KT / 16], lo[KT / 16];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int ps = 0; ps < KT / 16; ++ps) {
+      u32x4 w, w2;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = sc[mt][e];
-        const float p = __builtin_amdgcn_exp2f(
-            F::dtype == DAVET_F32 ? exact_arg(x - ref, sc_) : fmaf(x, sc_.c, neg_m));
-        sc[mt][e] = p;
-        psum += p;
+      for (int e = 0; e < 8; e += 2) {
+        float p[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const float x = sc[ps >> 1][(ps & 1) * 8 + e + u];
+          p[u] = __builtin_amdgcn_exp2f(F::dtype == DAVET_F32
+                                            ? exact_arg(x - ref, sc_)
+                                            : fmaf(x, sc_.c, neg_m));
+          psum += p[u];
+        }
+        if constexpr (F::dtype == DAVET_F32) {
+          hi[ps][e] = p[0];
+          hi[ps][e + 1] = p[1];
+        } else {
+          const uint32_t h = F::store2(p[0], p[1]);
+          w[e / 2] = h;
+          if constexpr (G == 1)
+            w2[e / 2] = F::store2(p[0] - F::load((uint16_t)(h & 0xffffu)),
+                                  p[1] - F::load((uint16_t)(h >> 16)));
+        }
       }
+      if constexpr (F::dtype != DAVET_F32) {
+        hi[ps] = __builtin_bit_cast(v8, w);
+        if constexpr (G == 1) lo[ps] = __builtin_bit_cast(v8, w2);
+      }
+    }
     psum = pair_sum32(psum);
     l_run = l_run * alpha + psum;
     m_run = m_new;
@@ -399,76 +426,48 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
     }
-    if (masked) {
-      // A masked weight of 0 times an infinite (or NaN) value is NaN: where
-      // the tile holds such a value, keys are added one by one, and those of
-      // weight 0 are left out.
-      bool bad = false;
-#pragma unroll 1
-      for (int i = lane; i < TILE / 16; i += 64) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(Vb + i * 16);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if constexpr (F::dtype == DAVET_F32)
-            bad |= (w[u] & 0x7f800000u) == 0x7f800000u;
-          else
-            bad |= F::nonfinite((uint16_t)(w[u] & 0xffffu)) ||
-                   F::nonfinite((uint16_t)(w[u] >> 16));
-        }
-      }
-      if (__any(bad)) {
-#pragma unroll 1
-        for (int at = 0; at < KT; ++at) {
-          float p = 0.f;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (mt == at >> 5 && e == ((at >> 3) & 3) * 4 + (at & 3))
-                p = sc[mt][e];
-          p = __shfl(p, l32 + 32 * ((at >> 2) & 1), 64);
-#pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const st x = *reinterpret_cast<const st*>(
-                  T::v_at(Vb, at, dt * 32 + (e >> 2) * 8 + hh * 4 + (e & 3)));
-              if (p != 0.f) o[dt][e] = fmaf(p, F::load(x), o[dt][e]);
-            }
-        }
-        return;
-      }
-    }
-#pragma unroll
-    for (int ps = 0; ps < KT / 16; ++ps) {
-      float pv[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pv[e] = sc[ps >> 1][(ps & 1) * 8 + e];
-      v8 hi, lo;
-      if constexpr (F::dtype == DAVET_F32) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) hi[e] = pv[e];
-      } else {
-        u32x4 w, w2;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          w[e] = F::store2(pv[2 * e], pv[2 * e + 1]);
-          if constexpr (G == 1)
-            w2[e] = F::store2(pv[2 * e] - F::load((uint16_t)(w[e] & 0xffffu)),
-                              pv[2 * e + 1] - F::load((uint16_t)(w[e] >> 16)));
-        }
-        hi = __builtin_bit_cast(v8, w);
-        if constexpr (G == 1) lo = __builtin_bit_cast(v8, w2);
-      }
+    for (int ps = 0; ps < KT / 16; ++ps)
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
         const v8 vf = T::v_frag(Vb, ps, dt, lane);
-        o[dt] = mm<F>(vf, hi, o[dt]);
-        // Few rows wait for memory, not for the matrix cores: what rounding to
-        // 16 bits took off the probabilities is multiplied as well.
-        if constexpr (G == 1 && F::dtype != DAVET_F32) o[dt] = mm<F>(vf, lo, o[dt]);
+        o[dt] = mm<F>(vf, hi[ps], o[dt]);
+        if constexpr (G == 1 && F::dtype != DAVET_F32)
+          o[dt] = mm<F>(vf, lo[ps], o[dt]);
       }
+  };
+
+  // A masked weight of 0 times an infinite (or NaN) value would be NaN.  Where
+  // a tile has masked places its values are looked over first (each wave its
+  // rows) and those that are not finite become 0; the rows that do see them
+  // get them added at the end.
+  auto tile_masked = [&](int k0, int holes) {
+    return k0 + KT > lim_tile || holes != 0;
+  };
+  auto clean = [&](char* Vb) {
+    char* at = Vb + (G == 4 ? wave * (TILE / 4) : 0);
+    bool found = false;
+#pragma unroll 1
+    for (int i = lane; i < TILE / G / 16; i += 64) {
+      u32x4 w = *reinterpret_cast<const u32x4*>(at + i * 16);
+      bool bad = false;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if constexpr (F::dtype == DAVET_F32) {
+          const bool b = (w[u] & 0x7f800000u) == 0x7f800000u;
+          bad |= b;
+          w[u] = b ? 0u : w[u];
+        } else {
+          const bool b0 = F::nonfinite((uint16_t)(w[u] & 0xffffu));
+          const bool b1 = F::nonfinite((uint16_t)(w[u] >> 16));
+          bad |= b0 || b1;
+          w[u] = (b0 ? 0u : w[u] & 0xffffu) | (b1 ? 0u : w[u] & 0xffff0000u);
+        }
+      }
+      if (bad) *reinterpret_cast<u32x4*>(at + i * 16) = w;
+      found |= bad;
     }
+    if (__any(found) && lane == 0) s_bad = 1;
   };
 
   if constexpr (G == 4) {
@@ -480,6 +479,11 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       for (int it = 0; it < nt; ++it) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         sync_lds();
+        if (tile_masked(begin + it * KT, holes)) {
+          clean(gbuf + TILE);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          sync_lds();
+        }
         if (live) compute(begin + it * KT, gbuf, holes);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         sync_lds();
@@ -492,6 +496,11 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         sync_lds();
         const int cur = holes;
         if (it + 1 < nt) holes = issue(begin + (it + 1) * KT, (it + 1) & 1);
+        if (tile_masked(begin + it * KT, cur)) {
+          clean(gbuf + (it & 1) * 2 * TILE + TILE);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          sync_lds();
+        }
         if (live) compute(begin + it * KT, gbuf + (it & 1) * 2 * TILE, cur);
       }
     }
@@ -512,10 +521,18 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         } else {
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         }
+        if (tile_masked(k0, cur)) {
+          clean(gbuf + (it & 1) * 2 * TILE + TILE);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
         compute(k0, gbuf + (it & 1) * 2 * TILE, cur);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       } else {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (tile_masked(k0, cur)) {
+          clean(gbuf + TILE);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
         compute(k0, gbuf, cur);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (k0 + 4 * KT < end) holes = issue(k0 + 4 * KT, 0);
@@ -523,6 +540,15 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     }
   }
 
+  // The lane's coordinates again, from the lane number, so that none of them
+  // is held in a register across the key loop.
+  int lane_e;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\t"
+               "v_mbcnt_hi_u32_b32 %0, -1, %0"
+               : "=v"(lane_e));
+  const int l32e = lane_e & 31, hhe = lane_e >> 5;
+  const int re = min(wrow + l32e, rows - 1);
+  const int qi = re / g, qh = hk * g + re % g;
   const float bias_ln = BIAS * kLn2;
   if constexpr (G == 1) {
     // join the four streams: O as [wave][dim][32 rows], then max and sum
@@ -533,24 +559,24 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        mo[(wave * D + dt * 32 + (e >> 2) * 8 + hh * 4 + (e & 3)) * 32 + l32] =
+        mo[(wave * D + dt * 32 + (e >> 2) * 8 + hhe * 4 + (e & 3)) * 32 + l32e] =
             o[dt][e];
-    if (hh == 0) {
-      ml[wave * 64 + l32] = m_run;
-      ml[wave * 64 + 32 + l32] = l_run;
+    if (hhe == 0) {
+      ml[wave * 64 + l32e] = m_run;
+      ml[wave * 64 + 32 + l32e] = l_run;
     }
     __syncthreads();
-    // thread: row l32, dims (D / 8) (t / 32) ..
+    // thread: row l32e, dims (D / 8) (t / 32) ..
     constexpr int DP = D / 8;
-    const int d0 = (threadIdx.x >> 5) * DP;
+    const int d0 = (wave * 2 + hhe) * DP;
     float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + l32]);
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + l32e]);
     float wt[4], l = 0.f;
     bool use[4];
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float mw = ml[w * 64 + l32], lw = ml[w * 64 + 32 + l32];
+      const float mw = ml[w * 64 + l32e], lw = ml[w * 64 + 32 + l32e];
       use[w] = lw != 0.f;                 // (NaN scores: sum NaN, maximum -inf)
       wt[w] = use[w] ? __builtin_amdgcn_exp2f((mw - m) * sc_.c) : 0.f;
       if (use[w]) l += wt[w] * lw;
@@ -561,78 +587,113 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       acc[i] = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w)
-        if (use[w]) acc[i] += wt[w] * mo[(w * D + d0 + i) * 32 + l32];
+        if (use[w]) acc[i] += wt[w] * mo[(w * D + d0 + i) * 32 + l32e];
     }
-    if (wrow + l32 >= rows) return;
+    if (wrow + l32e < rows) {
+      if (ap.pieces > 1) {
+        const int64_t at = (int64_t)pl.piece * part_rows +
+                           (int64_t)(row0 + qi) * n_heads + qh;
+        float* po = part + at * D + d0;
+#pragma unroll
+        for (int i = 0; i < DP; i += 4)
+          *reinterpret_cast<f32x4*>(po + i) =
+              f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+        if (d0 == 0) {
+          float* pm = part + (int64_t)ap.pieces * part_rows * D + at * 2;
+          pm[0] = m;
+          pm[1] = l;
+        }
+      } else {
+        // a row that sees nothing (or only scores of -inf): zeros, lse -inf
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        st* op = out + (int64_t)(row0 + qi) * ld_o + (int64_t)qh * D + d0;
+#pragma unroll
+        for (int i = 0; i < DP; i += 2) {
+          if constexpr (F::dtype == DAVET_F32) {
+            op[i] = acc[i] * inv;
+            op[i + 1] = acc[i + 1] * inv;
+          } else {
+            *reinterpret_cast<uint32_t*>(op + i) =
+                F::store2(acc[i] * inv, acc[i + 1] * inv);
+          }
+        }
+        if (lse && d0 == 0)
+          lse[(int64_t)(row0 + qi) * n_heads + qh] =
+              l == 0.f ? -INFINITY : m * sc_.scale + (logf(l) - bias_ln);
+      }
+    }
+  } else if (wrow + l32e < rows) {
     if (ap.pieces > 1) {
       const int64_t at = (int64_t)pl.piece * part_rows +
                          (int64_t)(row0 + qi) * n_heads + qh;
-      float* po = part + at * D + d0;
-#pragma unroll
-      for (int i = 0; i < DP; i += 4)
-        *reinterpret_cast<f32x4*>(po + i) =
-            f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
-      if (d0 == 0) {
-        float* pm = part + (int64_t)ap.pieces * part_rows * D + at * 2;
-        pm[0] = m;
-        pm[1] = l;
-      }
-      return;
-    }
-    // a row that sees nothing (or only scores of -inf) is zeros, lse -inf
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    st* op = out + (int64_t)(row0 + qi) * ld_o + (int64_t)qh * D + d0;
-#pragma unroll
-    for (int i = 0; i < DP; i += 2) {
-      if constexpr (F::dtype == DAVET_F32) {
-        op[i] = acc[i] * inv;
-        op[i + 1] = acc[i + 1] * inv;
-      } else {
-        *reinterpret_cast<uint32_t*>(op + i) =
-            F::store2(acc[i] * inv, acc[i + 1] * inv);
-      }
-    }
-    if (lse && d0 == 0)
-      lse[(int64_t)(row0 + qi) * n_heads + qh] =
-          l == 0.f ? -INFINITY : m * sc_.scale + (logf(l) - bias_ln);
-  } else {
-    if (wrow + l32 >= rows) return;
-    const int64_t at = (int64_t)pl.piece * part_rows +
-                       (int64_t)(row0 + qi) * n_heads + qh;
-    if (ap.pieces > 1) {
-      float* po = part + at * D + hh * 4;
+      float* po = part + at * D + hhe * 4;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
           *reinterpret_cast<f32x4*>(po + dt * 32 + u * 8) =
               f32x4{o[dt][u * 4], o[dt][u * 4 + 1], o[dt][u * 4 + 2], o[dt][u * 4 + 3]};
-      if (hh == 0) {
+      if (hhe == 0) {
         float* pm = part + (int64_t)ap.pieces * part_rows * D + at * 2;
         pm[0] = m_run;
         pm[1] = l_run;
       }
-      return;
+    } else {
+      const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
+      st* op = out + (int64_t)(row0 + qi) * ld_o + (int64_t)qh * D + hhe * 4;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = o[dt][u * 4 + e] * inv;
+          if constexpr (F::dtype == DAVET_F32)
+            *reinterpret_cast<f32x4*>(op + dt * 32 + u * 8) =
+                f32x4{x[0], x[1], x[2], x[3]};
+          else
+            *reinterpret_cast<u32x2*>(op + dt * 32 + u * 8) =
+                u32x2{F::store2(x[0], x[1]), F::store2(x[2], x[3])};
+        }
+      if (lse && hhe == 0)
+        lse[(int64_t)(row0 + qi) * n_heads + qh] =
+            l_run == 0.f ? -INFINITY
+                         : m_run * sc_.scale + (logf(l_run) - bias_ln);
     }
-    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
-    st* op = out + (int64_t)(row0 + qi) * ld_o + (int64_t)qh * D + hh * 4;
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = o[dt][u * 4 + e] * inv;
-        if constexpr (F::dtype == DAVET_F32)
-          *reinterpret_cast<f32x4*>(op + dt * 32 + u * 8) = f32x4{x[0], x[1], x[2], x[3]};
-        else
-          *reinterpret_cast<u32x2*>(op + dt * 32 + u * 8) =
-              u32x2{F::store2(x[0], x[1]), F::store2(x[2], x[3])};
+  }
+
+  // Values that `clean` took out, for the rows that see them: a positive weight
+  // times an infinity (or NaN) is that, whatever the weight.  One thread a dim;
+  // speed does not matter here.
+  __syncthreads();
+  if (s_bad && wave * 64 + lane_e < D) {
+    const int d = wave * 64 + lane_e;
+    for (int k0 = begin; k0 < end; k0 += KT) {
+      int holes = 0;
+      for (int gi = 0; gi < KT / 16; ++gi) {
+        const int key = min(k0 + gi * 16, (kv - 1) & ~15);
+        const int page = cv.table[(int64_t)s * cv.max_pages + (key >> lg)];
+        holes |= ((unsigned)page >= (unsigned)cv.n_pages) << gi;
       }
-    if (lse && hh == 0)
-      lse[(int64_t)(row0 + qi) * n_heads + qh] =
-          l_run == 0.f ? -INFINITY
-                       : m_run * sc_.scale + (logf(l_run) - bias_ln);
+      if (!tile_masked(k0, holes)) continue;
+      for (int key = k0; key < min(k0 + KT, end); ++key) {
+        const int page = cv.table[(int64_t)s * cv.max_pages + (key >> lg)];
+        if ((unsigned)page >= (unsigned)cv.n_pages) continue;
+        const float x = F::load(static_cast<const st*>(
+            cv.v)[((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * D + d]);
+        if (fabsf(x) < INFINITY) continue;
+        for (int rr = pl.tile * 32 * G; rr <= tile_last; ++rr) {
+          if (key >= visible_end(rr / g, n, kv, block)) continue;
+          const int tok = row0 + rr / g, hd = hk * g + rr % g;
+          if (ap.pieces > 1) {
+            part[((int64_t)pl.piece * part_rows + (int64_t)tok * n_heads + hd) * D + d] += x;
+          } else {
+            st* at = out + (int64_t)tok * ld_o + (int64_t)hd * D + d;
+            *at = F::store(F::load(*at) + x);
+          }
+        }
+      }
+    }
   }
 }
 
