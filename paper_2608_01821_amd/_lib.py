@@ -553,8 +553,14 @@ def _space(t):
     return t.data_ptr(), t.numel() * t.element_size()
 
 
+_I32 = [C.c_int32 * n for n in range(MAX_SEQS + 2)]
+
+
 def _ints(vals):
-    return vals if isinstance(vals, C.Array) else (C.c_int32 * len(vals))(*vals)
+    if isinstance(vals, C.Array):
+        return vals
+    n = len(vals)
+    return _I32[n](*vals) if n < len(_I32) else (C.c_int32 * n)(*vals)
 
 
 def _gpu(first, *tensors):
@@ -568,18 +574,24 @@ def _gpu(first, *tensors):
     return dev
 
 
+_torch = None
+
+
 def _launch(dev, stream, fn, *args):
     """fn(*args, stream handle) with GPU `dev` current; without `stream`, on its
     current one."""
-    import torch
-    if dev != torch.cuda.current_device():
-        with torch.cuda.device(dev):
+    global _torch
+    if _torch is None:
+        import torch as _torch
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
             return _launch(dev, stream, fn, *args)
     if stream is None:
-        s = torch.cuda.current_stream().cuda_stream
-    else:
-        s = stream if isinstance(stream, int) else stream.cuda_stream
-    status = fn(*args, s)
+        # the handle alone: torch.cuda.current_stream() builds an object, 2 us
+        stream = _torch._C._cuda_getCurrentRawStream(dev)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    status = fn(*args, stream)
     if status:
         _check(status)
 

@@ -106,44 +106,38 @@ constexpr int kThreads = 256;
 
 struct Freqs { double turns[64]; };   // theta^(-2 i / D) / (2 pi)
 
-// 8 elements between memory and fp32 registers
+// 8 elements as memory holds them
 template <typename F>
-__device__ __forceinline__ void load8(const typename F::st* p, float (&v)[8]) {
-  if constexpr (F::dtype == DAVET_F32) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0];
-    const f32x4 b = reinterpret_cast<const f32x4*>(p)[1];
+struct Piece {
+  static constexpr int N = sizeof(typename F::st) / 2;    // 16-byte words
+  u32x4 w[N];
+  __device__ __forceinline__ void load(const typename F::st* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-  } else {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ __forceinline__ void store(typename F::st* p) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = F::load((uint16_t)(w[i] & 0xffffu));
-      v[2 * i + 1] = F::load((uint16_t)(w[i] >> 16));
+    for (int i = 0; i < N; ++i) reinterpret_cast<u32x4*>(p)[i] = w[i];
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (F::dtype == DAVET_F32)
+        v[i] = __uint_as_float(w[i >> 2][i & 3]);
+      else
+        v[i] = F::load((uint16_t)(w[0][i >> 1] >> (16 * (i & 1))));
     }
   }
-}
-template <typename F>
-__device__ __forceinline__ void store8(typename F::st* p, const float (&v)[8]) {
-  if constexpr (F::dtype == DAVET_F32) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
-  } else {
-    u32x4 w;
+  __device__ __forceinline__ void put(const float (&v)[8]) {
+    if constexpr (F::dtype == DAVET_F32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = F::store2(v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<u32x4*>(p) = w;
+      for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = __float_as_uint(v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[0][i] = F::store2(v[2 * i], v[2 * i + 1]);
+    }
   }
-}
-// 8 elements moved as they are (values keep every bit)
-template <typename F>
-__device__ __forceinline__ void copy8(const typename F::st* s,
-                                      typename F::st* d) {
-  constexpr int N = sizeof(typename F::st) * 8 / 16;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    reinterpret_cast<u32x4*>(d)[i] = reinterpret_cast<const u32x4*>(s)[i];
-}
+};
 
 template <typename F, int D>
 __global__ void __launch_bounds__(kThreads)
@@ -155,11 +149,32 @@ cache_append_kernel(CacheView cv, ChunkPack cp, Freqs fr,
                     typename F::st* q_out, int64_t ld_q, int rows_per_wg) {
   using st = typename F::st;
   constexpr int H = D / 2, TH = D / 16;       // threads a head
+  constexpr int UN = 2;
   constexpr int kMaxRows = 4;
   __shared__ float cs[kMaxRows][2][H];
   const int total = cp.row0[cp.n_seqs];
   const int r0 = blockIdx.x * rows_per_wg;
   const int nr = min(rows_per_wg, total - r0);
+  const int heads = n_heads + 2 * cv.n_kv;
+  const int j = threadIdx.x % TH;
+  // Head rows threadIdx.x / TH, + 256 / TH, ... of the workgroup's rows, UN at a
+  // time; the first ones are on their way while the angles are computed.
+  Piece<F> a[UN], b[UN];
+  const int step = kThreads / TH;
+  auto load = [&](int u0) {
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int u = u0 + i * step;
+      if (u < nr * heads) {
+        const st* x = qkv + (int64_t)(r0 + u / heads) * ld_qkv +
+                      (int64_t)(u % heads) * D + 8 * j;
+        a[i].load(x);
+        b[i].load(x + H);
+      }
+    }
+  };
+  const int first = threadIdx.x / TH;
+  load(first);
   for (int t = threadIdx.x; t < nr * H; t += kThreads) {
     const int r = r0 + t / H, i = t % H;
     const int s = owner(cp.row0, cp.n_seqs, r);
@@ -170,61 +185,66 @@ cache_append_kernel(CacheView cv, ChunkPack cp, Freqs fr,
     cs[t / H][1][i] = sinpif(2.f * part);
   }
   __syncthreads();
-  const int heads = n_heads + 2 * cv.n_kv;
-  const int j = threadIdx.x % TH;
-  for (int u = threadIdx.x / TH; u < nr * heads; u += kThreads / TH) {
-    const int lr = u / heads, h = u % heads, r = r0 + lr;
-    const st* x = qkv + (int64_t)r * ld_qkv + (int64_t)h * D + 8 * j;
-    st* out;
-    if (h < n_heads) {
-      out = q_out + (int64_t)r * ld_q + (int64_t)h * D + 8 * j;
-    } else {
-      const int s = owner(cp.row0, cp.n_seqs, r);
-      const int at = cp.kv[s] - cp.row0[s + 1] + r;
-      const int page = cv.table[(int64_t)s * cv.max_pages + (at >> cv.lg)];
-      const int kh = h - n_heads < cv.n_kv ? h - n_heads
-                                           : h - n_heads - cv.n_kv;
-      st* base = static_cast<st*>(h - n_heads < cv.n_kv ? cv.k : cv.v);
-      // a hole in the page table takes nothing
-      out = (unsigned)page < (unsigned)cv.n_pages
-                ? base + ((((int64_t)page * cv.n_kv + kh) << cv.lg) +
-                          (at & ((1 << cv.lg) - 1))) * D + 8 * j
-                : nullptr;
-      if (h >= n_heads + cv.n_kv) {           // values: the same for all TH
-        if (out) {
-          copy8<F>(x, out);
-          copy8<F>(x + H, out + H);
+  for (int u0 = first; u0 < nr * heads; u0 += UN * step) {
+    if (u0 != first) load(u0);
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int u = u0 + i * step;
+      if (u >= nr * heads) break;
+      const int lr = u / heads, h = u % heads, r = r0 + lr;
+      st* out;
+      if (h < n_heads) {
+        out = q_out + (int64_t)r * ld_q + (int64_t)h * D + 8 * j;
+      } else {
+        const int s = owner(cp.row0, cp.n_seqs, r);
+        const int at = cp.kv[s] - cp.row0[s + 1] + r;
+        const int page = cv.table[(int64_t)s * cv.max_pages + (at >> cv.lg)];
+        const bool key = h - n_heads < cv.n_kv;
+        const int kh = key ? h - n_heads : h - n_heads - cv.n_kv;
+        st* base = static_cast<st*>(key ? cv.k : cv.v);
+        // a hole in the page table takes nothing
+        out = (unsigned)page < (unsigned)cv.n_pages
+                  ? base + ((((int64_t)page * cv.n_kv + kh) << cv.lg) +
+                            (at & ((1 << cv.lg) - 1))) * D + 8 * j
+                  : nullptr;
+        if (!key) {                     // values, as they are
+          if (out) {
+            a[i].store(out);
+            b[i].store(out + H);
+          }
+          continue;
         }
-        continue;
       }
-    }
-    float a[8], b[8];
-    load8<F>(x, a);
-    load8<F>(x + H, b);
-    if (norm) {
-      float ss = 0.f;
+      float x[8], y[8];
+      a[i].get(x);
+      b[i].get(y);
+      if (norm) {
+        float ss = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + b[i] * b[i];
+        for (int e = 0; e < 8; ++e) ss += x[e] * x[e] + y[e] * y[e];
 #pragma unroll
-      for (int o = 1; o < TH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-      const float inv = 1.0f / sqrtf(ss * (1.0f / D) + eps);
-      const float* g = h < n_heads ? q_gain : k_gain;
+        for (int o = 1; o < TH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+        const float inv = 1.0f / sqrtf(ss * (1.0f / D) + eps);
+        const float* g = h < n_heads ? q_gain : k_gain;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        a[i] *= inv * (g ? g[8 * j + i] : 1.f);
-        b[i] *= inv * (g ? g[H + 8 * j + i] : 1.f);
+        for (int e = 0; e < 8; ++e) {
+          x[e] *= inv * (g ? g[8 * j + e] : 1.f);
+          y[e] *= inv * (g ? g[H + 8 * j + e] : 1.f);
+        }
       }
-    }
-    float c[8], d[8];
+      float c[8], d[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float co = cs[lr][0][8 * j + i], si = cs[lr][1][8 * j + i];
-      c[i] = a[i] * co - b[i] * si;
-      d[i] = b[i] * co + a[i] * si;
-    }
-    if (out) {
-      store8<F>(out, c);
-      store8<F>(out + H, d);
+      for (int e = 0; e < 8; ++e) {
+        const float co = cs[lr][0][8 * j + e], si = cs[lr][1][8 * j + e];
+        c[e] = x[e] * co - y[e] * si;
+        d[e] = y[e] * co + x[e] * si;
+      }
+      if (out) {
+        a[i].put(c);
+        b[i].put(d);
+        a[i].store(out);
+        b[i].store(out + H);
+      }
     }
   }
 }
@@ -269,9 +289,16 @@ extern "C" int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
                   DAVET_EINVAL,
                   "davet_cache_append: q_out overlaps qkv (in place needs the "
                   "same address and row stride)");
-  Freqs fr{};
-  for (int i = 0; i < D / 2; ++i)
-    fr.turns[i] = pow((double)theta, -2.0 * i / D) / (2.0 * M_PI);
+  // 64 powers are 2 us of host time: the last table is kept, by its arguments
+  static thread_local Freqs fr;
+  static thread_local float fr_theta = 0.f;
+  static thread_local int fr_dim = 0;
+  if (fr_theta != theta || fr_dim != D) {
+    for (int i = 0; i < D / 2; ++i)
+      fr.turns[i] = pow((double)theta, -2.0 * i / D) / (2.0 * M_PI);
+    fr_theta = theta;
+    fr_dim = D;
+  }
   const int rpw = total >= 2048 ? 2 : 1;
   const int grid = (total + rpw - 1) / rpw;
   ProfScope ps(KC_MISC, stream);

@@ -8,8 +8,9 @@
 // an LDS histogram find the key T of the last entry kept and how many of the
 // entries equal to it stay, and a last pass writes the indices in ascending
 // order.  Each wavefront owns one contiguous sixteenth of the entries, so the
-// order needs one scan over 16 counts and no barrier inside the passes.  The
-// weights are read from L2 in each of the five passes.
+// order needs one scan over 16 counts and no barrier inside the passes.  Up to
+// 65536 entries are read once and stay in registers; more are read from L2 in
+// each of the five passes.
 //
 // Move: entry kept[j] of the source pages becomes entry j of the destination
 // pages, in the same pools; 64 entries of one head a workgroup, 16 bytes a
@@ -36,28 +37,57 @@ __device__ __forceinline__ uint32_t weight_key(float w, int i, int first,
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Calls f(i, key) for every entry of this wavefront's part, 64 a step in index
-// order, all lanes together (i >= hi: key 0 and no entry).
-template <typename Fn>
-__device__ __forceinline__ void for_entries(const float* w, int lo, int hi,
-                                            int first, int tail, Fn f) {
-  const int lane = threadIdx.x & 63;
-  for (int i0 = lo; i0 < hi; i0 += 512) {
-    float x[8];
+// The entries of one wavefront: [lo, hi), entry lo + 64 u + lane in slot u.  With
+// R slots or fewer they are read once and held in registers as keys; R = 0 reads
+// them again in every pass, 8 loads in flight.
+template <int R>
+struct Entries {
+  const float* w;
+  int lo, hi, first, tail;
+  uint32_t key[R ? R : 1];
+  __device__ __forceinline__ uint32_t key_of(float x, int i) const {
+    return i < hi ? weight_key(x, i, first, tail) : 0u;
+  }
+  __device__ __forceinline__ void load() {
+    if constexpr (R > 0) {
+      const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int i = i0 + u * 64 + lane;
-      x[u] = i < hi ? w[i] : 0.f;
-    }
+      for (int u = 0; u < R; ++u)       // (clamped: every slot's load is valid)
+        key[u] = hi > lo ? __float_as_uint(w[min(lo + u * 64 + lane, hi - 1)]) : 0u;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int i = i0 + u * 64 + lane;
-      if (i0 + u * 64 < hi)
-        f(i, i < hi, i < hi ? weight_key(x[u], i, first, tail) : 0u, x[u]);
+      for (int u = 0; u < R; ++u)
+        key[u] = key_of(__uint_as_float(key[u]), lo + u * 64 + lane);
     }
   }
-}
+  // f(index, inside, key) of 64 entries a step, in index order, all lanes at once
+  template <typename Fn>
+  __device__ __forceinline__ void each(Fn f) const {
+    const int lane = threadIdx.x & 63;
+    if constexpr (R > 0) {
+#pragma unroll
+      for (int u = 0; u < R; ++u) {
+        const int i = lo + u * 64 + lane;
+        if (lo + u * 64 < hi) f(i, i < hi, key[u]);
+      }
+    } else {
+      for (int i0 = lo; i0 < hi; i0 += 512) {
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int i = i0 + u * 64 + lane;
+          x[u] = i < hi ? w[i] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int i = i0 + u * 64 + lane;
+          if (i0 + u * 64 < hi) f(i, i < hi, key_of(x[u], i));
+        }
+      }
+    }
+  }
+};
 
+template <int R>
 __global__ void __launch_bounds__(kSelThreads)
 evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
                     int64_t ld_w, int first, int last, int32_t* __restrict__ kept,
@@ -69,11 +99,17 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
   const int s = blockIdx.x;
   const int n = sp.n[s], keep = sp.keep[s];
   if (keep == 0) return;
-  const int tail = n - last;
   const float* w = weights + (int64_t)s * ld_w;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per = ((n + kSelWaves - 1) / kSelWaves + 63) & ~63;
-  const int lo = min(n, wave * per), hi = min(n, lo + per);
+  Entries<R> en;
+  en.w = w;
+  en.lo = min(n, wave * per);
+  en.hi = min(n, en.lo + per);
+  en.first = first;
+  en.tail = n - last;
+  en.load();
 
   uint32_t prefix = 0, mask = 0;
   uint32_t need = keep;          // entries still to find among those matching
@@ -83,21 +119,19 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
     const uint32_t digit = pass == 2 ? 1023u : 2047u;
     for (int b = threadIdx.x; b < kBins; b += kSelThreads) hist[b] = 0;
     __syncthreads();
-    for_entries(w, lo, hi, first, tail,
-                [&](int, bool in, uint32_t key, float) {
-                  const bool on = in && (key & mask) == prefix;
-                  const uint64_t who = __ballot(on);
-                  if (!who) return;
-                  const uint32_t bin = (key >> shift) & digit;
-                  // equal weights would queue up at one counter
-                  const uint32_t lead = __shfl(bin, __ffsll((unsigned long long)who) - 1, 64);
-                  if (__ballot(on && bin != lead) == 0) {
-                    if (lane == __ffsll((unsigned long long)who) - 1)
-                      atomicAdd(&hist[lead], (uint32_t)__popcll(who));
-                  } else if (on) {
-                    atomicAdd(&hist[bin], 1u);
-                  }
-                });
+    en.each([&](int, bool in, uint32_t key) {
+      if (in && (key & mask) == prefix) {
+        const uint32_t bin = (key >> shift) & digit;
+        // one counter for all lanes would be added to 64 times in turn (equal
+        // weights do that in every pass)
+        const uint32_t lead = __builtin_amdgcn_readfirstlane(bin);
+        const uint64_t on = __ballot(1), same = __ballot(bin == lead);
+        if (same != on)
+          atomicAdd(&hist[bin], 1u);
+        else if (lane == __ffsll((unsigned long long)on) - 1)
+          atomicAdd(&hist[lead], (uint32_t)__popcll(on));
+      }
+    });
     __syncthreads();
     // from the top: thread t holds bins 2047 - 2t and 2046 - 2t
     const int b1 = kBins - 1 - 2 * (int)threadIdx.x;
@@ -126,7 +160,7 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
   }
   const uint32_t T = prefix;     // key of the last entry kept; `need` of them
   uint32_t gt = 0, eq = 0;
-  for_entries(w, lo, hi, first, tail, [&](int, bool in, uint32_t key, float) {
+  en.each([&](int, bool in, uint32_t key) {
     gt += (uint32_t)__popcll(__ballot(in && key > T));
     eq += (uint32_t)__popcll(__ballot(in && key == T));
   });
@@ -140,17 +174,20 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
     gt0 += wsum[i];
     eq0 += weq[i];
   }
-  const uint64_t below = (1ull << lane) - 1;
+  // bits of m below this lane
+  auto below = [](uint64_t m) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
+                                     __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+  };
   int32_t* ko = kept + (int64_t)s * ld_kept;
   float* wo = weights_out ? weights_out + (int64_t)s * ld_wo : nullptr;
-  for_entries(w, lo, hi, first, tail, [&](int i, bool in, uint32_t key, float x) {
+  en.each([&](int i, bool in, uint32_t key) {
     const uint64_t mg = __ballot(in && key > T), me = __ballot(in && key == T);
-    const uint32_t rg = gt0 + (uint32_t)__popcll(mg & below);
-    const uint32_t re = eq0 + (uint32_t)__popcll(me & below);
+    const uint32_t rg = gt0 + below(mg), re = eq0 + below(me);
     if (in && (key > T || (key == T && re < need))) {
       const uint32_t at = rg + min(re, need);
       ko[at] = i;
-      if (wo) wo[at] = x;
+      if (wo) wo[at] = w[i];
     }
     gt0 += (uint32_t)__popcll(mg);
     eq0 += (uint32_t)__popcll(me);
@@ -254,9 +291,17 @@ extern "C" int davet_evict_select(int32_t n_seqs, const int32_t* n,
       DAVET_EINVAL, "davet_evict_select: weights_out overlaps weights");
   if (most_keep == 0) return DAVET_OK;
   ProfScope ps(KC_MISC, stream);
-  hipLaunchKernelGGL(evict_select_kernel, dim3(n_seqs), dim3(kSelThreads), 0,
-                     stream, sp, weights, ld_weights, first, last, kept, ld_kept,
-                     weights_out, ld_weights_out);
+#define SELECT(R)                                                              \
+  hipLaunchKernelGGL((evict_select_kernel<R>), dim3(n_seqs), dim3(kSelThreads), \
+                     0, stream, sp, weights, ld_weights, first, last, kept,    \
+                     ld_kept, weights_out, ld_weights_out)
+  // slots a lane: the largest wavefront's sixteenth, in steps of 64 entries
+  const int64_t slots = (most_n + 1023) / 1024;
+  if (slots <= 8) SELECT(8);
+  else if (slots <= 32) SELECT(32);
+  else if (slots <= 64) SELECT(64);
+  else SELECT(0);
+#undef SELECT
   DAVET_HIP(hipGetLastError());
   return DAVET_OK;
 }

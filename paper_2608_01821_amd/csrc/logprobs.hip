@@ -1,20 +1,21 @@
 // Log probabilities of given tokens, entropy and the top alternatives of rows of
 // logits, in one pass over them.
 //
-// With m = max x, S = sum exp(x - m), A = sum exp(x - m) (x - m):
-//   log p(t) = x_t - m - ln S,      entropy = ln S - A / S
-// and the k largest logits in (value descending, id ascending) order.
+// With m the largest logit, c = log2(e) and t = c (x - m):
+//   S = sum 2^t,  B = sum 2^t t
+//   log p(w) = x_w - m - ln S,   entropy = ln S - B / (c S)
 //
-// A row is cut into slices of one workgroup; each of its four wavefronts walks
-// its part in batches of 16-byte loads and keeps (m, S, A) per lane, rescaled
-// when a batch moves the maximum.  The top k (at most 64) of a wavefront is a
-// sorted list with one entry a lane, as 64-bit keys whose order is the wanted
-// one.  A batch enters the list only where a lane's maximum beats the k-th
-// entry; the first batch starts from the k-th largest of the 64 lane maxima, so
-// that it enters about k values and not all.  Lists are joined in LDS at the end
-// of a workgroup, and a second launch joins the slices of a row where there are
-// several.  Bound by HBM (one read of the logits) for many rows, by two launches'
-// latency for few.
+// A row is cut into slices of one workgroup (one slice from 256 rows on); each of
+// its eight wavefronts walks its part in batches of 8 KB held in registers as
+// they came, the next batch on its way while one is worked on.  The top k (at
+// most 64) of a wavefront is a sorted list with one entry a lane, as 64-bit keys
+// whose order is the wanted one; values enter one by one.  So that few do, each of
+// the A wavefronts finds the ceil(k / A)-th largest of its lanes' maxima over its
+// first batch: the smallest of them bounds the row's k-th value from below.  Two
+// sorted lists join by one compare against the reversed other and six exchange
+// steps: in LDS between the wavefronts, and in a second launch between the slices
+// of a row where there are several.  Bound by HBM (one read of the logits) for
+// many rows, by the launches' latency for few.
 
 #include <math.h>
 
@@ -26,37 +27,38 @@ namespace davet {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxSlices = 64;
+constexpr int kMaxSlices = 16;
+constexpr int kWaves = 8;
 
-struct Stat { float m, S, A; };
+struct Stat { float m, S, B; };       // m = -inf: nothing yet
 
 __device__ __forceinline__ Stat stat_none() { return {-INFINITY, 0.f, 0.f}; }
-// exp(d) and exp(d) d for d = x - m <= 0 (0 and 0 for -inf)
-__device__ __forceinline__ void term(float x, float ref, float& S, float& A) {
-  const float d = x - ref;
-  const float e = __builtin_amdgcn_exp2f(d * kLog2e);
-  S += e;
-  if (e != 0.f) A = fmaf(e, d, A);
-}
 __device__ __forceinline__ Stat stat_to(const Stat& a, float m) {
   // nothing yet: its sums are 0 (or NaN, which stays)
-  const float d = a.m == -INFINITY ? 0.f : a.m - m;
-  const float e = __builtin_amdgcn_exp2f(d * kLog2e);
-  return {m, a.S * e, a.S != 0.f && e != 0.f ? e * fmaf(a.S, d, a.A) : 0.f * a.S};
+  const float d = a.m == -INFINITY ? 0.f : (a.m - m) * kLog2e;
+  const float e = __builtin_amdgcn_exp2f(d);
+  return {m, a.S * e, a.S != 0.f && e != 0.f ? e * fmaf(a.S, d, a.B) : 0.f * a.S};
 }
 __device__ __forceinline__ Stat stat_join(const Stat& a, const Stat& b) {
   const float m = fmaxf(a.m, b.m);
   const Stat x = stat_to(a, m), y = stat_to(b, m);
-  return {m, x.S + y.S, x.A + y.A};
+  return {m, x.S + y.S, x.B + y.B};
 }
 __device__ __forceinline__ Stat stat_wave(Stat s) {
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const Stat t = {__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64),
-                    __shfl_xor(s.A, o, 64)};
+                    __shfl_xor(s.B, o, 64)};
     s = stat_join(s, t);
   }
   return s;
+}
+// one logit; ref: s.m, or 0 while that is -inf
+__device__ __forceinline__ void term(float x, float ref, Stat& s) {
+  const float t = (x - ref) * kLog2e;
+  const float e = __builtin_amdgcn_exp2f(t);
+  s.S += e;
+  s.B = fmaf(e, fmaxf(t, -200.f), s.B);     // -inf: 0 times a finite number
 }
 
 // 64-bit key of a (value, id): larger value first, then lower id; never 0 for
@@ -80,24 +82,74 @@ __device__ __forceinline__ uint64_t lane64(uint64_t v, int l) {
 __device__ __forceinline__ void list_insert(uint64_t& list, uint64_t key) {
   const int at = (int)__popcll(__ballot(list > key));
   const int lane = threadIdx.x & 63;
+  // every lane's left neighbour (DPP wave_shr:1)
   const uint64_t up =
-      (uint64_t)(uint32_t)__shfl_up((int)(list >> 32), 1, 64) << 32 |
-      (uint32_t)__shfl_up((int)(uint32_t)list, 1, 64);
+      (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(list >> 32), 0x138,
+                                                      0xf, 0xf, false) << 32 |
+      (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)list, 0x138, 0xf, 0xf,
+                                            false);
   list = lane < at ? list : lane == at ? key : up;
 }
-// k-th largest (k in 1..64) of the 64 lanes' values; NaN lanes hold -inf
-__device__ __forceinline__ float kth_of_lanes(float x, int k) {
+__device__ __forceinline__ uint64_t xor64(uint64_t v, int o) {
+  return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, 64) << 32 |
+         (uint32_t)__shfl_xor((int)(uint32_t)v, o, 64);
+}
+// the 64 largest of two descending lists, the second one given in reverse
+__device__ __forceinline__ uint64_t list_join(uint64_t list, uint64_t reversed) {
+  const int lane = threadIdx.x & 63;
+  uint64_t v = list > reversed ? list : reversed;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint64_t y = xor64(v, o);
+    v = ((lane & o) == 0) == (v > y) ? v : y;
+  }
+  return v;
+}
+// The lists of W wavefronts (entries past k do not count) into wavefront 0's, in
+// log2 W steps; called by all.
+template <int W>
+__device__ __forceinline__ void join_waves(uint64_t& list, int k, int wave,
+                                           uint64_t (*s_list)[64]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-    for (int o = size >> 1; o > 0; o >>= 1) {
-      const float y = __shfl_xor(x, o, 64);
-      const bool desc = (lane & size) == 0;       // (size 64: always)
-      const bool low = (lane & o) == 0;
-      x = low == desc ? fmaxf(x, y) : fminf(x, y);
-    }
-  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), k - 1));
+  for (int o = 1; o < W; o <<= 1) {
+    if (lane >= k) list = 0;
+    if ((wave & (2 * o - 1)) == o) s_list[wave / (2 * o)][lane] = list;
+    __syncthreads();
+    if (k > 0 && (wave & (2 * o - 1)) == 0)
+      list = list_join(list, s_list[wave / (2 * o)][63 - lane]);
+    __syncthreads();
+  }
+}
+// largest of the 64 lanes' values, in every lane: DPP row shifts by 1, 2, 4, 8 and
+// the two row broadcasts leave it in lane 63
+__device__ __forceinline__ float max_of_lanes(float x) {
+  const int none = __float_as_int(-INFINITY);
+#define STEP(ctrl, rows)                                                       \
+  x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(                     \
+                   none, __float_as_int(x), ctrl, rows, 0xf, false)))
+  STEP(0x111, 0xf);
+  STEP(0x112, 0xf);
+  STEP(0x114, 0xf);
+  STEP(0x118, 0xf);
+  STEP(0x142, 0xa);
+  STEP(0x143, 0xc);
+#undef STEP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+// j-th largest of the 64 lanes' values, or -inf once there are none
+__device__ __forceinline__ float jth_of_lanes(float x, int j) {
+  float m = max_of_lanes(x);
+  for (; j > 1 && m > -INFINITY; --j) {
+    const uint64_t who = __ballot(x == m);
+    if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)who) - 1) x = -INFINITY;
+    m = max_of_lanes(x);
+  }
+  return m;
+}
+// the smallest float above x (finite)
+__device__ __forceinline__ float above(float x) {
+  return key_value(top_key(x, 0) + (1ull << 32));
 }
 
 // 16 bytes of logits as fp32
@@ -119,6 +171,20 @@ __device__ __forceinline__ void unpack(const u32x4& w, float* x) {
   }
 }
 
+// and back, values that came from unpack (or -inf)
+template <typename F>
+__device__ __forceinline__ u32x4 pack(const float* x) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F::dtype == DAVET_F32)
+      w[i] = __float_as_uint(x[i]);
+    else
+      w[i] = F::store2(x[2 * i], x[2 * i + 1]);
+  }
+  return w;
+}
+
 struct Out {
   float* logp;
   float* entropy;
@@ -134,36 +200,37 @@ __device__ __forceinline__ void finish(const Stat& s, uint64_t list, int row,
                                        const int32_t* targets, const Out& out) {
   const int lane = threadIdx.x & 63;
   const float lnS = logf(s.S);
+  const double z = (double)s.m + lnS;
   if (lane == 0) {
     if (out.logp) {
       const int t = targets[row];
       float v = -INFINITY;                        // no such token
       if ((unsigned)t < (unsigned)vocab && t != exclude && s.S != 0.f)
-        v = F::load(x[t]) - s.m - lnS;
+        v = (float)((double)F::load(x[t]) - z);
       out.logp[row] = v;
     }
-    if (out.entropy)
-      // nothing to choose from: 0; one certain token: not below 0
-      out.entropy[row] = s.S == 0.f ? 0.f : lnS - s.A / s.S;
+    if (out.entropy)                              // nothing to choose from: 0
+      out.entropy[row] = s.S == 0.f ? 0.f : lnS - s.B / s.S * (1.0f / kLog2e);
   }
   if (lane < k) {
     out.top_ids[(int64_t)row * k + lane] = list ? key_id(list) : -1;
     out.top_logp[(int64_t)row * k + lane] =
-        list ? key_value(list) - s.m - lnS : -INFINITY;
+        list ? (float)((double)key_value(list) - z) : -INFINITY;
   }
 }
 
-constexpr int kBatch = 4;     // 16-byte loads a lane in flight
+constexpr int kBatch = 8;     // 16-byte loads a lane and batch
 
 template <typename F>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(64 * kWaves)
 logprobs_kernel(const typename F::st* __restrict__ logits, int64_t ld, int vocab,
                 int exclude, int k, const int32_t* __restrict__ targets, Out out,
                 int slices, char* __restrict__ part) {
   using st = typename F::st;
   constexpr int N = Vec<F>::N;
-  __shared__ uint64_t s_list[4][64];
-  __shared__ Stat s_stat[4];
+  __shared__ uint64_t s_list[kWaves / 2][64];
+  __shared__ Stat s_stat[kWaves];
+  __shared__ float s_bound[kWaves];
   const int row = blockIdx.x / slices, slice = blockIdx.x % slices;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -175,103 +242,114 @@ logprobs_kernel(const typename F::st* __restrict__ logits, int64_t ld, int vocab
 
   Stat s = stat_none();
   uint64_t list = 0;
-  float thr = -INFINITY;        // value of the k-th entry
-  bool full = false;            // thr is an entry of the list, not a bound
+  float bound = -INFINITY;      // no value below it is among the row's top k
+  uint64_t kth = 0;             // the list's k-th entry
+  auto insert = [&](uint64_t who, uint64_t key) {
+    while (who) {
+      const int l = __ffsll((unsigned long long)who) - 1;
+      who &= who - 1;
+      list_insert(list, lane64(key, l));
+    }
+  };
 
-  // a batch of E values a lane; value e has id(e)
-  constexpr int E = kBatch * N;
-  auto take = [&](float (&v)[E], auto id) {
-    float mx = -INFINITY;
+  // this wavefront's 16-byte pieces; all have as many batches
+  const int parts = slices * kWaves, mine = slice * kWaves + wave;
+  const int per = ((nvec + parts - 1) / parts + 63) & ~63;
+  const int v0 = min(nvec, mine * per), v1 = min(nvec, v0 + per);
+  u32x4 w[kBatch], next[kBatch];
+  auto load = [&](int b, u32x4 (&d)[kBatch]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) mx = fmaxf(mx, v[e]);
+    for (int u = 0; u < kBatch; ++u)
+      if (b + u * 64 < v1) d[u] = xv[min(b + u * 64 + lane, v1 - 1)];
+  };
+  load(v0, next);
+  for (int b = v0, i = 0; i < per; i += 64 * kBatch, b += 64 * kBatch) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) w[u] = next[u];
+    load(b + 64 * kBatch, next);
+    float mx = -INFINITY, vmax[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      vmax[u] = -INFINITY;
+      if (b + u * 64 >= v1) continue;
+      const int first = head + (b + u * 64) * N;
+      // lanes past the end, and the excluded token, hold -inf
+      if (b + u * 64 + 64 > v1 || (exclude >= first && exclude < first + 64 * N)) {
+        float v[N];
+        unpack<F>(w[u], v);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (b + u * 64 + lane >= v1 || first + lane * N + e == exclude)
+            v[e] = -INFINITY;
+        w[u] = pack<F>(v);
+      }
+      float v[N];
+      unpack<F>(w[u], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) vmax[u] = fmaxf(vmax[u], v[e]);
+      mx = fmaxf(mx, vmax[u]);
+    }
     if (mx > s.m) s = stat_to(s, mx);
     const float ref = s.m == -INFINITY ? 0.f : s.m;
 #pragma unroll
-    for (int e = 0; e < E; ++e) term(v[e], ref, s.S, s.A);
-    if (k == 0) return;
-    if (!full) {
-      const float low = kth_of_lanes(mx, k);
-      thr = fmaxf(thr, low);
-    }
-    if (!__any(full ? mx > thr : mx >= thr && mx > -INFINITY)) return;
+    for (int u = 0; u < kBatch; ++u) {
+      if (b + u * 64 >= v1) continue;
+      float v[N];
+      unpack<F>(w[u], v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      // a later equal value has a higher id and loses to a full list
-      uint64_t who = __ballot(full ? v[e] > thr : v[e] >= thr && v[e] > -INFINITY);
-      const uint64_t key = top_key(v[e], id(e));
-      while (who) {
-        const int l = __ffsll((unsigned long long)who) - 1;
-        who &= who - 1;
-        list_insert(list, lane64(key, l));
-      }
+      for (int e = 0; e < N; ++e) term(v[e], ref, s);
     }
-    const uint64_t kth = lane64(list, k - 1);
-    full = kth != 0;
-    if (full) thr = key_value(kth);
-  };
-
-  // this wavefront's 16-byte pieces
-  const int parts = slices * 4, mine = slice * 4 + wave;
-  const int per = ((nvec + parts - 1) / parts + 63) & ~63;
-  const int v0 = min(nvec, mine * per), v1 = min(nvec, v0 + per);
-  for (int b = v0; b < v1; b += 64 * kBatch) {
-    u32x4 w[kBatch];
+    if (k == 0) continue;
+    if (i == 0) {
+      // (by the wavefronts whose lanes all have values; by the first, if none)
+      const int got = nvec - slice * kWaves * per;
+      const int A = max(1, min(kWaves, got / per + (got % per >= 64)));
+      const float j = wave < A ? jth_of_lanes(mx, (k + A - 1) / A) : INFINITY;
+      if (lane == 0) s_bound[wave] = j;
+      __syncthreads();
+      bound = s_bound[0];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      w[u] = xv[min(b + u * 64 + lane, v1 - 1)];
-    float v[E];
+      for (int o = 1; o < kWaves; ++o) bound = fminf(bound, s_bound[o]);
+    }
+    // wanted: above -inf, not below the bound, and above the list's k-th entry
+    // (a later equal value has a higher id)
+    const float least = fmaxf(fmaxf(bound, -3.402823466e38f),
+                              kth ? above(key_value(kth)) : -INFINITY);
+    if (!__any(mx >= least)) continue;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      unpack<F>(w[u], v + u * N);
-      if (b + u * 64 + lane >= v1)
+      if (!__any(vmax[u] >= least)) continue;
+      float v[N];
+      unpack<F>(w[u], v);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[u * N + e] = -INFINITY;
-    }
-    const int first = head + b * N;
-    if (exclude >= first && exclude < first + 64 * kBatch * N) {
-#pragma unroll
-      for (int e = 0; e < kBatch * N; ++e)
-        if (head + (b + (e / N) * 64 + lane) * N + e % N == exclude)
-          v[e] = -INFINITY;
-    }
-    take(v, [&](int e) { return head + (b + (e / N) * 64 + lane) * N + e % N; });
-  }
-  if (mine == parts - 1 && (head || tail < vocab)) {
-    // the edges: fewer than 16 values.  Lanes in id order within each edge; a
-    // head value has a lower id than any listed one and may equal the k-th.
-    const int ne = head + vocab - tail;
-    const int id = lane < head ? lane : tail + lane - head;
-    float v[1] = {lane < ne && id != exclude ? F::load(x[id]) : -INFINITY};
-    if (k > 0) {
-      uint64_t who = __ballot(v[0] > -INFINITY);
-      const uint64_t key = top_key(v[0], id);
-      while (who) {
-        const int l = __ffsll((unsigned long long)who) - 1;
-        who &= who - 1;
-        list_insert(list, lane64(key, l));
+      for (int e = 0; e < N; ++e) {
+        const uint64_t who = __ballot(v[e] >= least);
+        if (who)
+          insert(who, top_key(v[e], head + (b + u * 64 + lane) * N + e));
       }
     }
-    if (v[0] > s.m) s = stat_to(s, v[0]);
-    term(v[0], s.m == -INFINITY ? 0.f : s.m, s.S, s.A);
+    kth = lane64(list, k - 1);
+  }
+  if (mine == parts - 1 && (head || tail < vocab)) {
+    // the edges, fewer than 16 values (whole keys decide: their ids may be
+    // lower than those of equal values listed)
+    const int ne = head + vocab - tail;
+    const int id = lane < head ? lane : tail + lane - head;
+    const float v = lane < ne && id != exclude ? F::load(x[id]) : -INFINITY;
+    if (k > 0) insert(__ballot(v > -INFINITY), top_key(v, id));
+    if (v > s.m) s = stat_to(s, v);
+    term(v, s.m == -INFINITY ? 0.f : s.m, s);
   }
   s = stat_wave(s);
   if (lane == 0) s_stat[wave] = s;
-  if (lane < k) s_list[wave][lane] = list;
-  __syncthreads();
+  join_waves<kWaves>(list, k, wave, s_list);
   if (wave != 0) return;
-  for (int o = 1; o < 4; ++o) {
-    s = stat_join(s, s_stat[o]);
-    for (int i = 0; i < k; ++i) {
-      const uint64_t key = s_list[o][i];
-      if (key <= lane64(list, k - 1)) break;      // sorted: the rest is below
-      list_insert(list, key);
-    }
-  }
+  s = stat_wave(lane < kWaves ? s_stat[lane] : stat_none());
   if (slices == 1) {
     finish<F>(s, list, row, vocab, exclude, k, x, targets, out);
     return;
   }
-  // partial results: [rows][slices] Stat, then [rows][slices][k] keys
+  // partial results: [rows][slices][k] keys, then [rows][slices] Stat
   const int64_t at = (int64_t)row * slices + slice;
   const int64_t n_rows = gridDim.x / slices;
   uint64_t* pl = reinterpret_cast<uint64_t*>(part);
@@ -279,47 +357,46 @@ logprobs_kernel(const typename F::st* __restrict__ logits, int64_t ld, int vocab
   if (lane == 0) reinterpret_cast<Stat*>(pl + n_rows * slices * k)[at] = s;
 }
 
-// Joins the slices of one row: one wavefront a row, one slice a lane.  Every
-// round takes the largest of the slices' next keys.
+// Joins the slices of one row: four wavefronts take every fourth list each.
 template <typename F>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(256)
 logprobs_join_kernel(const typename F::st* __restrict__ logits, int64_t ld,
                      int vocab, int exclude, int k,
                      const int32_t* __restrict__ targets, Out out, int slices,
                      const char* __restrict__ part, int rows) {
-  extern __shared__ uint64_t keys[];     // [slices][k]
-  const int row = blockIdx.x, lane = threadIdx.x;
-  const uint64_t* pl = reinterpret_cast<const uint64_t*>(part);
-  const Stat* ps = reinterpret_cast<const Stat*>(pl + (int64_t)rows * slices * k);
-  for (int i = lane; i < slices * k; i += 64)
-    keys[i] = pl[(int64_t)row * slices * k + i];
+  __shared__ uint64_t s_list[2][64];
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t* pl = reinterpret_cast<const uint64_t*>(part) +
+                       (int64_t)row * slices * k;
+  const Stat* ps = reinterpret_cast<const Stat*>(
+                       reinterpret_cast<const uint64_t*>(part) +
+                       (int64_t)rows * slices * k) + (int64_t)row * slices;
   Stat s = stat_none();
-  if (lane < slices) s = ps[(int64_t)row * slices + lane];
-  s = stat_wave(s);
-  __syncthreads();
+  if (wave == 0 && lane < slices) s = ps[lane];
   uint64_t list = 0;
-  int next = 0;
-  for (int i = 0; i < k; ++i) {
-    const uint64_t mine =
-        lane < slices && next < k ? keys[lane * k + next] : 0;
-    uint64_t best = mine;
+  if (k > 0) {
+    uint64_t other[kMaxSlices / 4];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t y = (uint64_t)(uint32_t)__shfl_xor((int)(best >> 32), o, 64) << 32 |
-                         (uint32_t)__shfl_xor((int)(uint32_t)best, o, 64);
-      best = best > y ? best : y;
+    for (int i = 0; i < kMaxSlices / 4; ++i) {
+      const int j = i == 0 ? lane : 63 - lane, sl = wave + 4 * i;
+      other[i] = j < k && sl < slices ? pl[(int64_t)sl * k + j] : 0;
     }
-    if (best == 0) break;
-    if (mine == best) ++next;            // keys are distinct: ids are
-    if (lane == i) list = best;
+    list = other[0];
+#pragma unroll
+    for (int i = 1; i < kMaxSlices / 4; ++i)
+      if (wave + 4 * i < slices) list = list_join(list, other[i]);
   }
+  join_waves<4>(list, k, wave, s_list);
+  if (wave != 0) return;
+  s = stat_wave(s);
   finish<F>(s, list, row, vocab, exclude, k, logits + (int64_t)row * ld, targets, out);
 }
 
-// Slices a row: enough workgroups for the chip, at least 4096 logits each.
+// Slices a row: 256 workgroups fill the chip, at least 8192 logits each.
 int plan_slices(int rows, int vocab) {
-  const int want = (1024 + rows - 1) / rows;
-  return std::max(1, std::min({want, kMaxSlices, vocab / 4096}));
+  const int want = (256 + rows - 1) / rows;
+  return std::max(1, std::min({want, kMaxSlices, vocab / 8192}));
 }
 
 size_t part_bytes(int rows, int vocab, int k) {
@@ -379,15 +456,15 @@ extern "C" int davet_token_logprobs(int32_t rows, int32_t vocab,
     const auto* x = static_cast<const F::st*>(logits);                         \
     {                                                                          \
       ProfScope ps(KC_MISC, stream);                                           \
-      hipLaunchKernelGGL(logprobs_kernel<F>, dim3(rows * slices), dim3(256), 0, \
+      hipLaunchKernelGGL(logprobs_kernel<F>, dim3(rows * slices), dim3(64 * kWaves), 0, \
                          stream, x, ld, vocab, exclude, top, targets, out,     \
                          slices, part);                                        \
       DAVET_HIP(hipGetLastError());                                            \
     }                                                                          \
     if (slices > 1) {                                                          \
       ProfScope ps(KC_MISC, stream);                                           \
-      hipLaunchKernelGGL(logprobs_join_kernel<F>, dim3(rows), dim3(64),        \
-                         (size_t)slices * top * 8, stream, x, ld, vocab,       \
+      hipLaunchKernelGGL(logprobs_join_kernel<F>, dim3(rows), dim3(256), 0,    \
+                         stream, x, ld, vocab,                                 \
                          exclude, top, targets, out, slices, part, rows);      \
       DAVET_HIP(hipGetLastError());                                            \
     }                                                                          \
