@@ -564,7 +564,8 @@ typedef struct davet_kv_cache {
  *   qkv [rows, (n_heads + 2 n_kv_heads) * head_dim], stride ld_qkv: query heads,
  *   key heads, value heads (the row order of davet_layer_weights.wqkv).
  *   norm 1: queries and keys of each head become x / sqrt(mean x^2 + eps) * gain
- *   first (q_gain, k_gain: device float32 [head_dim], NULL for ones); 0: not.
+ *   first (q_gain, k_gain: device float32 [head_dim], 16-byte aligned, NULL for
+ *   ones); 0: not.
  *   Then the rotary embedding: elements (i, i + head_dim/2) turn by
  *   p * theta^(-2i/head_dim), p = pos[row] (device int32 [rows]) or, with pos
  *   NULL, the row's cache index.  Angles are exact for every int32 position.

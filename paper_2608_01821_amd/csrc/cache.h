@@ -23,6 +23,21 @@ struct ChunkPack {
   int32_t kv[DAVET_MAX_SEQS];
 };
 
+// Two values rounded (nearest even) into one word, a in the low half, in one
+// instruction of either 16-bit format.
+template <typename F>
+__device__ __forceinline__ uint32_t round2(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  const f2 v = {a, b};
+  if constexpr (F::dtype == DAVET_BF16) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
+  } else {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
+  }
+}
+
 constexpr int kCacheGroup = 16;   // smallest page: 16 aligned keys share one
 
 // Keys visible to query i of a chunk of n among kv cached tokens: all of them

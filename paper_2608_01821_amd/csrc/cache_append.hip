@@ -102,9 +102,8 @@ int check_heads(const davet_kv_cache* c, int32_t n_heads, const char* who) {
 
 namespace {
 
-constexpr int kThreads = 256;
-
-struct Freqs { double turns[64]; };   // theta^(-2 i / D) / (2 pi)
+constexpr int kMaxThreads = 512;
+constexpr int kMaxGroups = 512;       // workgroups
 
 // 8 elements as memory holds them
 template <typename F>
@@ -134,14 +133,14 @@ struct Piece {
       for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = __float_as_uint(v[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[0][i] = F::store2(v[2 * i], v[2 * i + 1]);
+      for (int i = 0; i < 4; ++i) w[0][i] = round2<F>(v[2 * i], v[2 * i + 1]);
     }
   }
 };
 
 template <typename F, int D>
-__global__ void __launch_bounds__(kThreads)
-cache_append_kernel(CacheView cv, ChunkPack cp, Freqs fr,
+__global__ void __launch_bounds__(kMaxThreads)
+cache_append_kernel(CacheView cv, ChunkPack cp, double log2_theta,
                     const typename F::st* qkv, int64_t ld_qkv,
                     int n_heads, const int32_t* __restrict__ pos, int norm,
                     const float* __restrict__ q_gain,
@@ -149,75 +148,94 @@ cache_append_kernel(CacheView cv, ChunkPack cp, Freqs fr,
                     typename F::st* q_out, int64_t ld_q, int rows_per_wg) {
   using st = typename F::st;
   constexpr int H = D / 2, TH = D / 16;       // threads a head
-  constexpr int UN = 2;
-  constexpr int kMaxRows = 4;
-  __shared__ float cs[kMaxRows][2][H];
-  const int total = cp.row0[cp.n_seqs];
+  __shared__ float cs[2][2][H];               // of even and odd rows
+  __shared__ int64_t slot[2];                 // cache row of key head 0; -1: hole
   const int r0 = blockIdx.x * rows_per_wg;
-  const int nr = min(rows_per_wg, total - r0);
+  const int r1 = min(r0 + rows_per_wg, cp.row0[cp.n_seqs]);
   const int heads = n_heads + 2 * cv.n_kv;
-  const int j = threadIdx.x % TH;
-  // Head rows threadIdx.x / TH, + 256 / TH, ... of the workgroup's rows, UN at a
-  // time; the first ones are on their way while the angles are computed.
-  Piece<F> a[UN], b[UN];
-  const int step = kThreads / TH;
-  auto load = [&](int u0) {
-#pragma unroll
-    for (int i = 0; i < UN; ++i) {
-      const int u = u0 + i * step;
-      if (u < nr * heads) {
-        const st* x = qkv + (int64_t)(r0 + u / heads) * ld_qkv +
-                      (int64_t)(u % heads) * D + 8 * j;
-        a[i].load(x);
-        b[i].load(x + H);
+  const int per = blockDim.x / TH, passes = (heads + per - 1) / per;
+  const int j = threadIdx.x % TH, h0 = threadIdx.x / TH;
+
+  // This thread's share of the angles: pair i turns theta^(-2 i / D) / (2 pi)
+  // times round per position.  (A table of them in the kernel's arguments would
+  // be read from host memory by every workgroup: 42 us where this takes 23.)
+  const int i = threadIdx.x % H;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const double freq = exp2(log2_theta * (-2.0 / D) * i) * 0.15915494309189533577;
+  auto angles = [&](int r) {
+    // one wavefront a row, in turn, so that no other waits for the same one
+    if (wave == r % (int)(blockDim.x >> 6) && (int)(threadIdx.x & 63) < H) {
+      const int s = owner(cp.row0, cp.n_seqs, r);
+      const int at = cp.kv[s] - cp.row0[s + 1] + r;
+      const double turns = (double)(pos ? pos[r] : at) * freq;
+      const float part = (float)(turns - rint(turns));
+      cs[r & 1][0][i] = cospif(2.f * part);
+      cs[r & 1][1][i] = sinpif(2.f * part);
+      if (i == 0) {
+        const int page = cv.table[(int64_t)s * cv.max_pages + (at >> cv.lg)];
+        slot[r & 1] = (unsigned)page < (unsigned)cv.n_pages
+                          ? (((int64_t)page * cv.n_kv) << cv.lg) +
+                                (at & ((1 << cv.lg) - 1))
+                          : -1;
       }
     }
   };
-  const int first = threadIdx.x / TH;
-  load(first);
-  for (int t = threadIdx.x; t < nr * H; t += kThreads) {
-    const int r = r0 + t / H, i = t % H;
-    const int s = owner(cp.row0, cp.n_seqs, r);
-    const int p = pos ? pos[r] : cp.kv[s] - cp.row0[s + 1] + r;
-    const double turns = (double)p * fr.turns[i];
-    const float part = (float)(turns - rint(turns));
-    cs[t / H][0][i] = cospif(2.f * part);
-    cs[t / H][1][i] = sinpif(2.f * part);
-  }
-  __syncthreads();
-  for (int u0 = first; u0 < nr * heads; u0 += UN * step) {
-    if (u0 != first) load(u0);
+  // item: one pass over the heads of one row; the next one's loads are out while
+  // one is worked on
+  Piece<F> a, b, na, nb;
+  auto load = [&](int r, int pass) {
+    const int h = pass * per + h0;
+    if (r < r1 && h < heads) {
+      const st* x = qkv + (int64_t)r * ld_qkv + (int64_t)h * D + 8 * j;
+      na.load(x);
+      nb.load(x + H);
+    }
+  };
+  load(r0, 0);
+  // the gains of this thread's elements
+  float gq[16], gk[16];
+  auto gains = [&](const float* g, float (&v)[16]) {
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-      const int u = u0 + i * step;
-      if (u >= nr * heads) break;
-      const int lr = u / heads, h = u % heads, r = r0 + lr;
+    for (int e = 0; e < 16; e += 4) {
+      f32x4 x = {1.f, 1.f, 1.f, 1.f};
+      if (norm && g)
+        x = *reinterpret_cast<const f32x4*>(g + 8 * j + (e & 7) + (e < 8 ? 0 : H));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[e + u] = x[u];
+    }
+  };
+  gains(q_gain, gq);
+  gains(k_gain, gk);
+  angles(r0);
+  for (int r = r0; r < r1; ++r) {
+    __syncthreads();
+    if (r + 1 < r1) angles(r + 1);
+    for (int pass = 0; pass < passes; ++pass) {
+      a = na;
+      b = nb;
+      load(pass + 1 < passes ? r : r + 1, pass + 1 < passes ? pass + 1 : 0);
+      const int h = pass * per + h0;
+      if (h >= heads) continue;
       st* out;
       if (h < n_heads) {
         out = q_out + (int64_t)r * ld_q + (int64_t)h * D + 8 * j;
       } else {
-        const int s = owner(cp.row0, cp.n_seqs, r);
-        const int at = cp.kv[s] - cp.row0[s + 1] + r;
-        const int page = cv.table[(int64_t)s * cv.max_pages + (at >> cv.lg)];
         const bool key = h - n_heads < cv.n_kv;
         const int kh = key ? h - n_heads : h - n_heads - cv.n_kv;
         st* base = static_cast<st*>(key ? cv.k : cv.v);
         // a hole in the page table takes nothing
-        out = (unsigned)page < (unsigned)cv.n_pages
-                  ? base + ((((int64_t)page * cv.n_kv + kh) << cv.lg) +
-                            (at & ((1 << cv.lg) - 1))) * D + 8 * j
-                  : nullptr;
+        const int64_t at = slot[r & 1];
+        if (at < 0) continue;
+        out = base + (at + ((int64_t)kh << cv.lg)) * D + 8 * j;
         if (!key) {                     // values, as they are
-          if (out) {
-            a[i].store(out);
-            b[i].store(out + H);
-          }
+          a.store(out);
+          b.store(out + H);
           continue;
         }
       }
       float x[8], y[8];
-      a[i].get(x);
-      b[i].get(y);
+      a.get(x);
+      b.get(y);
       if (norm) {
         float ss = 0.f;
 #pragma unroll
@@ -225,26 +243,24 @@ cache_append_kernel(CacheView cv, ChunkPack cp, Freqs fr,
 #pragma unroll
         for (int o = 1; o < TH; o <<= 1) ss += __shfl_xor(ss, o, 64);
         const float inv = 1.0f / sqrtf(ss * (1.0f / D) + eps);
-        const float* g = h < n_heads ? q_gain : k_gain;
+        const bool query = h < n_heads;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[e] *= inv * (g ? g[8 * j + e] : 1.f);
-          y[e] *= inv * (g ? g[H + 8 * j + e] : 1.f);
+          x[e] *= inv * (query ? gq[e] : gk[e]);
+          y[e] *= inv * (query ? gq[8 + e] : gk[8 + e]);
         }
       }
       float c[8], d[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float co = cs[lr][0][8 * j + e], si = cs[lr][1][8 * j + e];
+        const float co = cs[r & 1][0][8 * j + e], si = cs[r & 1][1][8 * j + e];
         c[e] = x[e] * co - y[e] * si;
         d[e] = y[e] * co + x[e] * si;
       }
-      if (out) {
-        a[i].put(c);
-        b[i].put(d);
-        a[i].store(out);
-        b[i].store(out + H);
-      }
+      a.put(c);
+      b.put(d);
+      a.store(out);
+      b.store(out + H);
     }
   }
 }
@@ -281,6 +297,10 @@ extern "C" int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
                       (!norm || (eps >= 0.f && std::isfinite(eps))),
                   DAVET_EINVAL,
                   "davet_cache_append: theta > 0 and eps >= 0 required, finite");
+  DAVET_CHECK_ARG((((uintptr_t)q_gain | (uintptr_t)k_gain) & 15) == 0 &&
+                      ((uintptr_t)pos & 3) == 0,
+                  DAVET_EINVAL,
+                  "davet_cache_append: q_gain and k_gain must be 16-byte aligned");
   if (total == 0) return DAVET_OK;
   const size_t es = dtype_size(cache->dtype);
   DAVET_CHECK_ARG((q_out == qkv && ld_q == ld_qkv) ||
@@ -289,22 +309,17 @@ extern "C" int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
                   DAVET_EINVAL,
                   "davet_cache_append: q_out overlaps qkv (in place needs the "
                   "same address and row stride)");
-  // 64 powers are 2 us of host time: the last table is kept, by its arguments
-  static thread_local Freqs fr;
-  static thread_local float fr_theta = 0.f;
-  static thread_local int fr_dim = 0;
-  if (fr_theta != theta || fr_dim != D) {
-    for (int i = 0; i < D / 2; ++i)
-      fr.turns[i] = pow((double)theta, -2.0 * i / D) / (2.0 * M_PI);
-    fr_theta = theta;
-    fr_dim = D;
-  }
-  const int rpw = total >= 2048 ? 2 : 1;
+  // threads for all heads of a row, or for equal passes over them; one row a
+  // workgroup while there are few, then runs of rows
+  const int units = (n_heads + 2 * cv.n_kv) * (D / 16);
+  const int passes = (units + kMaxThreads - 1) / kMaxThreads;
+  const int threads = (int)align_up((units + passes - 1) / passes, 64);  // >= D / 2
+  const int rpw = (total + kMaxGroups - 1) / kMaxGroups;
   const int grid = (total + rpw - 1) / rpw;
   ProfScope ps(KC_MISC, stream);
 #define APPEND(F, DIM)                                                         \
-  hipLaunchKernelGGL((cache_append_kernel<F, DIM>), dim3(grid), dim3(kThreads),\
-                     0, stream, cv, cp, fr, (const F::st*)qkv, ld_qkv, n_heads,\
+  hipLaunchKernelGGL((cache_append_kernel<F, DIM>), dim3(grid), dim3(threads), \
+                     0, stream, cv, cp, log2((double)theta), (const F::st*)qkv, ld_qkv, n_heads,\
                      pos, norm, q_gain, k_gain, eps, (F::st*)q_out, ld_q, rpw)
 #define APPEND_D(F) do { if (D == 128) APPEND(F, 128); else APPEND(F, 64); } while (0)
   if (cache->dtype == DAVET_F16) APPEND_D(F16S);

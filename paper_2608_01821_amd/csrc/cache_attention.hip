@@ -193,7 +193,7 @@ struct PageIds {
 // one eighth of the grid when the key heads divide by 8).
 struct AttnPlan {
   int32_t blk[DAVET_MAX_SEQS + 1];
-  uint8_t order[DAVET_MAX_SEQS];
+  int32_t order[DAVET_MAX_SEQS];   // (bytes would be vector loads)
   int32_t piece;        // keys a piece
   int32_t pieces;       // most pieces of a sequence; 1: no partials
   int32_t xcd;          // key heads dealt out to the 8 XCDs
@@ -405,10 +405,10 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
           hi[ps][e] = p[0];
           hi[ps][e + 1] = p[1];
         } else {
-          const uint32_t h = F::store2(p[0], p[1]);
+          const uint32_t h = round2<F>(p[0], p[1]);
           w[e / 2] = h;
           if constexpr (G == 1)
-            w2[e / 2] = F::store2(p[0] - F::load((uint16_t)(h & 0xffffu)),
+            w2[e / 2] = round2<F>(p[0] - F::load((uint16_t)(h & 0xffffu)),
                                   p[1] - F::load((uint16_t)(h >> 16)));
         }
       }
@@ -614,7 +614,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
             op[i + 1] = acc[i + 1] * inv;
           } else {
             *reinterpret_cast<uint32_t*>(op + i) =
-                F::store2(acc[i] * inv, acc[i + 1] * inv);
+                round2<F>(acc[i] * inv, acc[i + 1] * inv);
           }
         }
         if (lse && d0 == 0)
@@ -653,7 +653,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
                 f32x4{x[0], x[1], x[2], x[3]};
           else
             *reinterpret_cast<u32x2*>(op + dt * 32 + u * 8) =
-                u32x2{F::store2(x[0], x[1]), F::store2(x[2], x[3])};
+                u32x2{round2<F>(x[0], x[1]), round2<F>(x[2], x[3])};
         }
       if (lse && hhe == 0)
         lse[(int64_t)(row0 + qi) * n_heads + qh] =
@@ -698,45 +698,50 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 }
 
 // Joins the pieces of every row: with m the largest piece maximum and
-// w_p = 2^((m_p - m) c), o = sum w_p O_p / sum w_p l_p, in piece order.  D / 4
-// threads a row, four dims each.
+// w_p = 2^((m_p - m) c), o = sum w_p O_p / sum w_p l_p, in piece order.  One
+// wavefront a row, D / 64 dims a lane: the row, and so its sequence's entries in
+// the kernel's arguments, are scalar.
 template <typename F, int D>
 __global__ void __launch_bounds__(256)
 cache_merge_kernel(ChunkPack cp, const float* __restrict__ part, int part_rows,
                    int piece, int pieces, typename F::st* __restrict__ out,
                    int64_t ld_o, float* __restrict__ lse, int n_heads, Scale sc_) {
-  constexpr int TR = D / 4;
-  const int64_t row = (int64_t)blockIdx.x * (256 / TR) + threadIdx.x / TR;
+  constexpr int E = D / 64;
+  const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (row >= part_rows) return;
-  const int d0 = (threadIdx.x % TR) * 4;
-  const int tok = (int)(row / n_heads), h = (int)(row % n_heads);
+  const int d0 = (threadIdx.x & 63) * E;
+  const int tok = row / n_heads, h = row % n_heads;
   const int s = owner(cp.row0, cp.n_seqs, tok);
   const int np = (cp.kv[s] + piece - 1) / piece;
   const float* pm = part + (int64_t)pieces * part_rows * D;
   float m = -INFINITY;
+#pragma unroll 4
   for (int p = 0; p < np; ++p)
     m = fmaxf(m, pm[((int64_t)p * part_rows + row) * 2]);
-  float l = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f, acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll 4
   for (int p = 0; p < np; ++p) {
     const int64_t at = (int64_t)p * part_rows + row;
     const float mp = pm[at * 2], lp = pm[at * 2 + 1];
-    const f32x4 o = *reinterpret_cast<const f32x4*>(part + at * D + d0);
+    float o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = part[at * D + d0 + e];
     if (lp != 0.f) {
       const float w = __builtin_amdgcn_exp2f((mp - m) * sc_.c);
       l += w * lp;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] += w * o[i];
+      for (int e = 0; e < E; ++e) acc[e] += w * o[e];
     }
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   typename F::st* op = out + (int64_t)tok * ld_o + (int64_t)h * D + d0;
-  if constexpr (F::dtype == DAVET_F32)
-    *reinterpret_cast<f32x4*>(op) = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+  if constexpr (F::dtype != DAVET_F32 && E == 2)
+    *reinterpret_cast<uint32_t*>(op) = round2<F>(acc[0] * inv, acc[1] * inv);
   else
-    *reinterpret_cast<u32x2*>(op) = u32x2{F::store2(acc[0] * inv, acc[1] * inv),
-                                          F::store2(acc[2] * inv, acc[3] * inv)};
+#pragma unroll
+    for (int e = 0; e < E; ++e) op[e] = F::store(acc[e] * inv);
   if (lse && d0 == 0)
     lse[row] = l == 0.f
                    ? -INFINITY
@@ -916,10 +921,10 @@ AttnPlan plan_attn(const ChunkPack& cp, int n_kv, int g, int rows, int want,
     const int64_t nt = ((int64_t)(cp.row0[s + 1] - cp.row0[s]) * g + rows - 1) / rows;
     work += nt * n_kv * cp.kv[s];
     if (nt) longest = std::max(longest, cp.kv[s]);
-    ap.order[s] = (uint8_t)s;
+    ap.order[s] = s;
   }
   std::stable_sort(ap.order, ap.order + cp.n_seqs,
-                   [&](uint8_t a, uint8_t b) { return cp.kv[a] > cp.kv[b]; });
+                   [&](int32_t a, int32_t b) { return cp.kv[a] > cp.kv[b]; });
   int64_t piece = std::max<int64_t>((work + want - 1) / want,
                                     ((int64_t)longest + cap - 1) / cap);
   piece = std::max<int64_t>(align_up(piece, unit), 4 * unit);
@@ -981,9 +986,8 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   }
   if (ap.pieces > 1) {
     ProfScope ps(KC_MISC, stream);
-    const int per = 256 / (D / 4);
     hipLaunchKernelGGL((cache_merge_kernel<F, D>),
-                       dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0,
+                       dim3((unsigned)((rows + 3) / 4)), dim3(256), 0,
                        stream, cp, part, (int)rows, ap.piece, ap.pieces, (st*)out,
                        ld_o, lse, n_heads, sc);
     DAVET_HIP(hipGetLastError());

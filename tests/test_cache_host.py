@@ -25,11 +25,11 @@ def _i(*v):
 
 
 def _append(cache=None, n=1, cu=(0, 3), kv=(10,), qkv=A << 1, ldx=512, heads=4,
-            norm=0, eps=1e-6, theta=1e4, q=A << 2, ldq=256):
+            norm=0, eps=1e-6, theta=1e4, q=A << 2, ldq=256, gq=None, gk=None):
     c = cache if cache is not None else _cache()
     return dv.raw().davet_cache_append(
         C.byref(c), n, _i(*cu) if cu else None, _i(*kv) if kv else None, qkv, ldx,
-        heads, None, norm, None, None, eps, theta, q, ldq, None)
+        heads, None, norm, gq, gk, eps, theta, q, ldq, None)
 
 
 def _attend(cache=None, n=1, cu=(0, 3), kv=(10,), q=A << 1, ldq=256, heads=4,
@@ -75,6 +75,7 @@ def test_append_refusals():
     assert _append(norm=2) == EINVAL and _append(theta=0.0) == EINVAL
     assert _append(theta=float("inf")) == EINVAL
     assert _append(norm=1, eps=-1.0) == EINVAL
+    assert _append(norm=1, gq=A + 4) == EINVAL and _append(gk=A + 8) == EINVAL
     # q_out inside qkv at another stride or place
     assert _append(qkv=A << 1, q=A << 1, ldq=256) == EINVAL
     assert _append(qkv=A << 1, q=(A << 1) + 512, ldq=512) == EINVAL
