@@ -44,7 +44,7 @@ constexpr int kCacheGroup = 16;   // smallest page: 16 aligned keys share one
 // (block 0), or those up to the end of the query's block.
 __host__ __device__ inline int visible_end(int i, int n, int kv, int block) {
   if (block == 0) return kv;
-  const int64_t e = ((int64_t)i / block + 1) * block;
+  const int64_t e = ((int64_t)(i / block) + 1) * block;
   return kv - n + (int)(e < n ? e : n);
 }
 

@@ -38,6 +38,7 @@ namespace davet {
 namespace {
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s* lds_v4s_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
@@ -766,16 +767,19 @@ __global__ void __launch_bounds__(256, 2)
 cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                      const typename F::st* __restrict__ q, int64_t ld_q,
                      const float* __restrict__ lse, int n_heads, int block,
-                     float scale, const float* __restrict__ prev,
+                     Scale sc_, const float* __restrict__ prev,
                      float* __restrict__ weights, int64_t ld_w,
                      float* __restrict__ part) {
   using st = typename F::st;
   using T = Tile<F, D>;
   using v8 = typename Frag<F>::v8;
   constexpr int QB = 32 * T::RB;
-  constexpr int NI = 32 / T::RPI / 4;             // loads a wave
-  __shared__ __attribute__((aligned(1024))) char qs[2][QB];
-  __shared__ __attribute__((aligned(16))) float ls[2][32];
+  constexpr int NI = 32 / T::RPI / 4;             // loads of rows a wave
+  constexpr int NBUF = 4;                         // tiles of rows under way
+  __shared__ __attribute__((aligned(1024))) char qs[NBUF][QB];
+  // each wave's: lse of the 32 rows (and again), the keys each row sees
+  __shared__ __attribute__((aligned(16))) float ls[NBUF][4][64];
+  __shared__ __attribute__((aligned(16))) int lim[NBUF][4][32];
   const int nblk = wp.blk[cp.n_seqs];
   const int blk = blockIdx.x % nblk, chunk = blockIdx.x / nblk;
   const int s = owner(wp.blk, cp.n_seqs, blk);
@@ -801,42 +805,75 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
     h1 = min(h0 + wp.heads, cv.n_kv);
   }
   const int nb = b1 - b0, steps = (h1 - h0) * nb;
-  float next_lse = INFINITY;      // of the step whose rows are under way
-  auto issue = [&](int step, int b) {
-    const int h = h0 + step / nb, qb = b0 + step % nb;
+  // Token and head of the group of this lane's NI rows, and of the row whose lse
+  // it moves, kept as the rows advance (a division each would cost more than the
+  // products): row r is token r / g, head r % g.
+  int tok[NI + 1], hd[NI + 1];
+  auto lane_row = [&](int i) {
+    return i < NI ? (wave * NI + i) * T::RPI + lane / T::C : l32;
+  };
+  auto start = [&]() {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int lr = (wave * NI + i) * T::RPI + lane / T::C;
-      const int r = min(qb * 32 + lr, rows - 1);
-      const st* src = q + (int64_t)(row0 + r / g) * ld_q +
-                      (int64_t)(h * g + r % g) * D;
-      dma16(reinterpret_cast<const char*>(src) + T::k_slot(lr, lane % T::C) * 16,
-            qs[b] + (wave * NI + i) * 1024);
+    for (int i = 0; i <= NI; ++i) {
+      const int r = b0 * 32 + lane_row(i);
+      tok[i] = r / g;
+      hd[i] = r - tok[i] * g;
     }
-    if (threadIdx.x < 32) {
-      // rows past the last, and rows that saw nothing, give 0: exp(x - inf)
-      const int r = qb * 32 + threadIdx.x;
-      next_lse = INFINITY;
-      if (r < rows)
-        next_lse = lse[(int64_t)(row0 + r / g) * n_heads + h * g + r % g];
+  };
+  const int t32 = 32 / g, h32 = 32 - t32 * g;
+  int ih = h0, iqb = b0, ib = 0;        // the step to issue next, its buffer
+  // its rows and their lse: NI + 1 loads a wave; rows past the last repeat it
+  auto issue = [&]() {
+    if (iqb == b0) start();
+#pragma unroll
+    for (int i = 0; i <= NI; ++i) {
+      const bool past = iqb * 32 + lane_row(i) >= rows;
+      const int64_t tk = row0 + (past ? n - 1 : tok[i]);
+      const int hq = ih * g + (past ? g - 1 : hd[i]);
+      if (i < NI) {
+        const int lr = lane_row(i);
+        dma16(reinterpret_cast<const char*>(q + tk * ld_q + (int64_t)hq * D) +
+                  T::k_slot(lr, lane % T::C) * 16,
+              qs[ib] + (wave * NI + i) * 1024);
+      } else {
+        __builtin_amdgcn_global_load_lds(lse + tk * n_heads + hq,
+                                         (lds_ptr)ls[ib][wave], 4, 0, 0);
+        if (hh == 0)
+          lim[ib][wave][l32] = past ? 0 : visible_end(tok[i], n, kv, block);
+      }
+      tok[i] += t32;
+      hd[i] += h32;
+      if (hd[i] >= g) { hd[i] -= g; ++tok[i]; }
     }
+    ib = (ib + 1) % NBUF;
+    if (++iqb == b1) { iqb = b0; ++ih; }
   };
   v8 kf[D / 16];
   float acc = 0.f;
-  if (steps > 0) issue(0, 0);
+  for (int i = 0; i < min(NBUF - 1, steps); ++i) issue();
+  int h = h0, qb = b0;
   for (int step = 0; step < steps; ++step) {
-    const int h = h0 + step / nb, qb = b0 + step % nb;
     if (qb == b0) {
       const st* kp = static_cast<const st*>(cv.k) + (kbase + ((int64_t)h << cv.lg)) * D + hh * 8;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) kf[ks] = load_frag<F>(kp + ks * 16);
     }
-    if (threadIdx.x < 32)
-      ls[step & 1][threadIdx.x] = next_lse == -INFINITY ? INFINITY : next_lse;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // the loads of up to two later steps may stay out
+    static_assert(NBUF == 4, "the waits below");
+    if (steps - step > 2)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (NI + 1)) : "memory");
+    else if (steps - step == 2)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NI + 1) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     sync_lds();
-    if (step + 1 < steps) issue(step + 1, (step + 1) & 1);
-    const char* Qb = qs[step & 1];
+    // into the buffer that every wave has done with
+    if (step + NBUF - 1 < steps) issue();
+    // lse in units of log2; a row that saw nothing gives 0: exp(x - inf)
+    float* lw = ls[step % NBUF][wave];
+    const float le = lw[lane];
+    lw[lane] = le == -INFINITY ? INFINITY : le * kLog2e;
+    const char* Qb = qs[step % NBUF];
     f32x16 sc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.f;
@@ -844,23 +881,35 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
     for (int ks = 0; ks < D / 16; ++ks)
       sc = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[ks], sc);
     const int first_lim = visible_end(min(qb * 32, rows - 1) / g, n, kv, block);
-    const bool masked = (blk - wp.blk[s] + 1) * kWeightKeys > first_lim;
-    float sum = 0.f;
+    const bool masked = (blk - wp.blk[s] + 1) * kWeightKeys > first_lim ||
+                        qb * 32 + 32 > rows;
+    float p[16];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const f32x4 lv = *reinterpret_cast<const f32x4*>(&ls[step & 1][u * 8 + hh * 4]);
+      const f32x4 lv = *reinterpret_cast<const f32x4*>(lw + u * 8 + hh * 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float p = __builtin_amdgcn_exp2f(fmaf(sc[u * 4 + e], scale, -lv[e]) * kLog2e);
-        if (masked) {
-          const int r = qb * 32 + u * 8 + hh * 4 + e;
-          if (r >= rows || key >= visible_end(r / g, n, kv, block)) p = 0.f;
-        }
-        // (a row past the last repeats one: its lse is +inf, its weight 0)
-        sum += p;
+        const float x = sc[u * 4 + e];
+        p[u * 4 + e] = __builtin_amdgcn_exp2f(
+            F::dtype == DAVET_F32 ? fmaf(x, sc_.c, fmaf(x, sc_.c_lo, -lv[e]))
+                                  : fmaf(x, sc_.c, -lv[e]));
       }
     }
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const i32x4 end = *reinterpret_cast<const i32x4*>(
+            &lim[step % NBUF][wave][u * 8 + hh * 4]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          p[u * 4 + e] = key < end[e] ? p[u * 4 + e] : 0.f;
+      }
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum += p[e];
     acc += sum;
+    if (++qb == b1) { qb = b0; ++h; }
   }
   acc = pair_sum32(acc);
   if (hole) acc = 0.f;
@@ -998,7 +1047,7 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
 template <typename F, int D>
 int run_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
                 int64_t ld_q, const float* lse, int n_heads, int block,
-                float scale, const float* prev, float* weights, int64_t ld_w,
+                Scale scale, const float* prev, float* weights, int64_t ld_w,
                 float* part, hipStream_t stream) {
   WeightPlan wp{};
   int most = 0;
@@ -1154,7 +1203,7 @@ extern "C" int davet_cache_weights(const davet_kv_cache* cache, int32_t n_seqs,
                   "davet_cache_weights: too many query rows");
   rc = check_workspace(workspace, ws_bytes, total, n_heads, D, who);
   if (rc) return rc;
-  const float sc = make_scale(scale, D).scale;
+  const Scale sc = make_scale(scale, D);
   float* part = static_cast<float*>(workspace);
 #define WGT(F, DIM) run_weights<F, DIM>(cv, cp, q, ld_q, lse, n_heads, block, sc, \
                                         prev, weights, ld_weights, part, stream)
