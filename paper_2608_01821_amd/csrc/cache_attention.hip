@@ -157,6 +157,39 @@ struct Tile {
   }
 };
 
+// LDS reads with their wait.  Written as plain loads they would wait for every
+// DMA load under way: the compiler cannot tell which buffer one is for.
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+__device__ __forceinline__ void lds_read4(const uint32_t (&a)[4], u32x4 (&x)[4]) {
+  asm volatile("ds_read_b128 %0, %4\n\t"
+               "ds_read_b128 %1, %5\n\t"
+               "ds_read_b128 %2, %6\n\t"
+               "ds_read_b128 %3, %7\n\t"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3])
+               : "memory");
+}
+// both halves (keys +0 and +8: 8 RB bytes on) of four transposed fragments
+template <int HALF>
+__device__ __forceinline__ void lds_read_tr4(const uint32_t (&a)[4], u32x2 (&x)[8]) {
+  asm volatile("ds_read_b64_tr_b16 %0, %8\n\t"
+               "ds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+               "ds_read_b64_tr_b16 %2, %9\n\t"
+               "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+               "ds_read_b64_tr_b16 %4, %10\n\t"
+               "ds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+               "ds_read_b64_tr_b16 %6, %11\n\t"
+               "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]),
+                 "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(HALF)
+               : "memory");
+}
+
 // 8 consecutive elements of global memory as a fragment
 template <typename F>
 __device__ __forceinline__ typename Frag<F>::v8 load_frag(const typename F::st* p) {
@@ -257,6 +290,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   constexpr int OWN = KT / G;                     // tile rows a wave moves
   constexpr int NI = OWN / T::RPI;                // its loads, of K and of V
   constexpr float BIAS = Frag<F>::kBias;
+  constexpr bool STREAM = G == 1 && F::dtype != DAVET_F32;   // the next tile's loads stay out
   __shared__ __attribute__((aligned(1024))) char smem[LDS];
   __shared__ int s_bad;         // some value of a masked tile is not finite
 
@@ -311,25 +345,27 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     char* vd = kd + TILE;
     // one 16-key group: its rows of K and of V
     auto move = [&](int gi, int key, int page, bool hole) {
+      char* kl = kd + gi * 16 * T::RB;
+      char* vl = vd + gi * 16 * T::RB;
+      if (hole) {
+#pragma unroll
+        for (int j = 0; j < 16 / T::RPI; ++j) {
+          *reinterpret_cast<u32x4*>(kl + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+          *reinterpret_cast<u32x4*>(vl + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        }
+        return;
+      }
       const int64_t base =
-          ((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * D;
+          ((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * T::RB;
+      const char* kg = static_cast<const char*>(cv.k) + base;    // scalar
+      const char* vg = static_cast<const char*>(cv.v) + base;
       const int last = kv - 1 - key;              // last valid row of the group
 #pragma unroll
       for (int j = 0; j < 16 / T::RPI; ++j) {
-        const int lr = j * T::RPI + lane / T::C, tr = gi * 16 + lr;
-        char* kl = kd + (gi * 16 + j * T::RPI) * T::RB;
-        char* vl = vd + (gi * 16 + j * T::RPI) * T::RB;
-        if (hole) {
-          *reinterpret_cast<u32x4*>(kl + lane * 16) = u32x4{0, 0, 0, 0};
-          *reinterpret_cast<u32x4*>(vl + lane * 16) = u32x4{0, 0, 0, 0};
-        } else {
-          const int64_t row = base + (int64_t)min(lr, last) * D;
-          const int c = lane % T::C;
-          dma16(reinterpret_cast<const char*>(static_cast<const st*>(cv.k) + row) +
-                    T::k_slot(tr, c) * 16, kl);
-          dma16(reinterpret_cast<const char*>(static_cast<const st*>(cv.v) + row) +
-                    T::v_slot(tr, c) * 16, vl);
-        }
+        const int lr = j * T::RPI + lane / T::C, tr = gi * 16 + lr, c = lane % T::C;
+        const uint32_t row = (uint32_t)min(lr, last) * T::RB;
+        dma16(kg + (row + T::k_slot(tr, c) * 16), kl + j * 1024);
+        dma16(vg + (row + T::v_slot(tr, c) * 16), vl + j * 1024);
       }
     };
     int holes = 0, my_key = 0, my_page = 0;
@@ -356,9 +392,24 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[mt][e] = 0.f;
+      if constexpr (STREAM) {
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-        sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
+        for (int k4 = 0; k4 < D / 16; k4 += 4) {
+          uint32_t at[4];
+          u32x4 x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            at[i] = lds_at(Kb) + l32 * T::RB + (T::k_slot(l32, (k4 + i) * 2 + hh) << 4);
+          lds_read4(at, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sc[mt] = mm<F>(__builtin_bit_cast(v8, x[i]), qf[k4 + i], sc[mt]);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
+      }
     }
     // keys past a row's limit, or in a hole, score -inf
     const bool masked = k0 + KT > lim_all || holes;
@@ -426,6 +477,30 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+    }
+    if constexpr (STREAM) {
+      // fragments ps * (D / 32) + dt, four at a time
+#pragma unroll
+      for (int f4 = 0; f4 < KT / 16 * (D / 32); f4 += 4) {
+        uint32_t at[4];
+        u32x2 x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int ps = (f4 + i) / (D / 32), dt = (f4 + i) % (D / 32), j = lane & 15;
+          at[i] = lds_at(T::v_at(Vb, ps * 16 + hh * 4 + (j >> 2),
+                                 dt * 32 + 16 * ((lane >> 4) & 1) + 4 * (j & 3)));
+        }
+        lds_read_tr4<8 * T::RB>(at, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int ps = (f4 + i) / (D / 32), dt = (f4 + i) % (D / 32);
+          const v8 vf = __builtin_bit_cast(
+              v8, u32x4{x[2 * i][0], x[2 * i][1], x[2 * i + 1][0], x[2 * i + 1][1]});
+          o[dt] = mm<F>(vf, hi[ps], o[dt]);
+          o[dt] = mm<F>(vf, lo[ps], o[dt]);
+        }
+      }
+      return;
     }
 #pragma unroll
     for (int ps = 0; ps < KT / 16; ++ps)
