@@ -41,7 +41,6 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s* lds_v4s_ptr;
-typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxPieces = 64;
@@ -73,8 +72,36 @@ __device__ __forceinline__ f32x16 mm(typename Frag<F>::v8 a,
   }
 }
 
-__device__ __forceinline__ void dma16(const void* g, void* lds) {
-  __builtin_amdgcn_global_load_lds(g, (lds_ptr)lds, 16, 0, 0);
+// Global -> LDS DMA: lane l's 16 (or 4) bytes at base + offset go to lds + 16 l
+// (4 l); base and lds are the wavefront's.  In asm, so that the compiler does not
+// count it: it cannot tell the buffer that a load fills from the one an LDS read
+// takes, and would wait for every load before each read.  Every use waits for
+// its own loads (s_waitcnt vmcnt) and then for the other wavefronts'.  No register
+// is written; what the compiler counts itself it only waits for longer.
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+__device__ __forceinline__ void dma16(const void* base, uint32_t offset, void* lds) {
+  asm volatile("s_mov_b32 m0, %0\n\t"
+               "s_nop 0\n\t"
+               "global_load_lds_dwordx4 %1, %2"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds_at(lds))), "v"(offset),
+                  "s"(base)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma16_at(const void* g, void* lds) {
+  asm volatile("s_mov_b32 m0, %0\n\t"
+               "s_nop 0\n\t"
+               "global_load_lds_dwordx4 %1, off"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds_at(lds))), "v"(g)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma4_at(const void* g, void* lds) {
+  asm volatile("s_mov_b32 m0, %0\n\t"
+               "s_nop 0\n\t"
+               "global_load_lds_dword %1, off"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds_at(lds))), "v"(g)
+               : "memory", "m0");
 }
 __device__ __forceinline__ void sync_lds() {
   asm volatile("" ::: "memory");
@@ -156,39 +183,6 @@ struct Tile {
     }
   }
 };
-
-// LDS reads with their wait.  Written as plain loads they would wait for every
-// DMA load under way: the compiler cannot tell which buffer one is for.
-__device__ __forceinline__ uint32_t lds_at(const void* p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
-}
-__device__ __forceinline__ void lds_read4(const uint32_t (&a)[4], u32x4 (&x)[4]) {
-  asm volatile("ds_read_b128 %0, %4\n\t"
-               "ds_read_b128 %1, %5\n\t"
-               "ds_read_b128 %2, %6\n\t"
-               "ds_read_b128 %3, %7\n\t"
-               "s_waitcnt lgkmcnt(0)"
-               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3])
-               : "memory");
-}
-// both halves (keys +0 and +8: 8 RB bytes on) of four transposed fragments
-template <int HALF>
-__device__ __forceinline__ void lds_read_tr4(const uint32_t (&a)[4], u32x2 (&x)[8]) {
-  asm volatile("ds_read_b64_tr_b16 %0, %8\n\t"
-               "ds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
-               "ds_read_b64_tr_b16 %2, %9\n\t"
-               "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
-               "ds_read_b64_tr_b16 %4, %10\n\t"
-               "ds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
-               "ds_read_b64_tr_b16 %6, %11\n\t"
-               "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
-               "s_waitcnt lgkmcnt(0)"
-               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]),
-                 "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
-               : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(HALF)
-               : "memory");
-}
 
 // 8 consecutive elements of global memory as a fragment
 template <typename F>
@@ -290,7 +284,6 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   constexpr int OWN = KT / G;                     // tile rows a wave moves
   constexpr int NI = OWN / T::RPI;                // its loads, of K and of V
   constexpr float BIAS = Frag<F>::kBias;
-  constexpr bool STREAM = G == 1 && F::dtype != DAVET_F32;   // the next tile's loads stay out
   __shared__ __attribute__((aligned(1024))) char smem[LDS];
   __shared__ int s_bad;         // some value of a masked tile is not finite
 
@@ -364,8 +357,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       for (int j = 0; j < 16 / T::RPI; ++j) {
         const int lr = j * T::RPI + lane / T::C, tr = gi * 16 + lr, c = lane % T::C;
         const uint32_t row = (uint32_t)min(lr, last) * T::RB;
-        dma16(kg + (row + T::k_slot(tr, c) * 16), kl + j * 1024);
-        dma16(vg + (row + T::v_slot(tr, c) * 16), vl + j * 1024);
+        dma16(kg, row + T::k_slot(tr, c) * 16, kl + j * 1024);
+        dma16(vg, row + T::v_slot(tr, c) * 16, vl + j * 1024);
       }
     };
     int holes = 0, my_key = 0, my_page = 0;
@@ -392,24 +385,9 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[mt][e] = 0.f;
-      if constexpr (STREAM) {
 #pragma unroll
-        for (int k4 = 0; k4 < D / 16; k4 += 4) {
-          uint32_t at[4];
-          u32x4 x[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            at[i] = lds_at(Kb) + l32 * T::RB + (T::k_slot(l32, (k4 + i) * 2 + hh) << 4);
-          lds_read4(at, x);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            sc[mt] = mm<F>(__builtin_bit_cast(v8, x[i]), qf[k4 + i], sc[mt]);
-        }
-      } else {
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-          sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
-      }
+      for (int ks = 0; ks < D / 16; ++ks)
+        sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
     }
     // keys past a row's limit, or in a hole, score -inf
     const bool masked = k0 + KT > lim_all || holes;
@@ -477,30 +455,6 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-    }
-    if constexpr (STREAM) {
-      // fragments ps * (D / 32) + dt, four at a time
-#pragma unroll
-      for (int f4 = 0; f4 < KT / 16 * (D / 32); f4 += 4) {
-        uint32_t at[4];
-        u32x2 x[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ps = (f4 + i) / (D / 32), dt = (f4 + i) % (D / 32), j = lane & 15;
-          at[i] = lds_at(T::v_at(Vb, ps * 16 + hh * 4 + (j >> 2),
-                                 dt * 32 + 16 * ((lane >> 4) & 1) + 4 * (j & 3)));
-        }
-        lds_read_tr4<8 * T::RB>(at, x);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ps = (f4 + i) / (D / 32), dt = (f4 + i) % (D / 32);
-          const v8 vf = __builtin_bit_cast(
-              v8, u32x4{x[2 * i][0], x[2 * i][1], x[2 * i + 1][0], x[2 * i + 1][1]});
-          o[dt] = mm<F>(vf, hi[ps], o[dt]);
-          o[dt] = mm<F>(vf, lo[ps], o[dt]);
-        }
-      }
-      return;
     }
 #pragma unroll
     for (int ps = 0; ps < KT / 16; ++ps)
@@ -907,12 +861,11 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
       const int hq = ih * g + (past ? g - 1 : hd[i]);
       if (i < NI) {
         const int lr = lane_row(i);
-        dma16(reinterpret_cast<const char*>(q + tk * ld_q + (int64_t)hq * D) +
-                  T::k_slot(lr, lane % T::C) * 16,
-              qs[ib] + (wave * NI + i) * 1024);
+        dma16_at(reinterpret_cast<const char*>(q + tk * ld_q + (int64_t)hq * D) +
+                     T::k_slot(lr, lane % T::C) * 16,
+                 qs[ib] + (wave * NI + i) * 1024);
       } else {
-        __builtin_amdgcn_global_load_lds(lse + tk * n_heads + hq,
-                                         (lds_ptr)ls[ib][wave], 4, 0, 0);
+        dma4_at(lse + tk * n_heads + hq, ls[ib][wave]);
         if (hh == 0)
           lim[ib][wave][l32] = past ? 0 : visible_end(tok[i], n, kv, block);
       }
@@ -1086,8 +1039,8 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
     most = std::max(most, cp.row0[s + 1] - cp.row0[s]);
   const bool wide = (int64_t)most * g > 64;
   constexpr bool f32 = F::dtype == DAVET_F32;
-  constexpr int WB = F::dtype == DAVET_BF16 ? 2 : 1;    // wide: buffers
-  constexpr int WM = F::dtype == DAVET_F16 ? 3 : 2;     // workgroups a CU
+  constexpr int WB = f32 ? 1 : 2;                       // wide: buffers
+  constexpr int WM = 2;                                 // workgroups a CU
   constexpr int NB = f32 && D == 128 ? 1 : 2;           // narrow
   constexpr int NM = !f32 && D == 64 ? 2 : 1;
   const AttnPlan ap = plan_attn(cp, cv.n_kv, g, wide ? 128 : 32,
