@@ -382,12 +382,24 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     const char* Vb = Kb + TILE;
     f32x16 sc[MT];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[mt][e] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
         sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
+    if constexpr (G == 4 && F::dtype != DAVET_F32) {
+      // eight reads of K ahead of the matrix ops (left alone: two)
+      constexpr int NF = MT * D / 16;
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+      for (int i = 0; i < NF - 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
     }
     // keys past a row's limit, or in a hole, score -inf
     const bool masked = k0 + KT > lim_all || holes;
@@ -465,6 +477,16 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         if constexpr (G == 1 && F::dtype != DAVET_F32)
           o[dt] = mm<F>(vf, lo[ps], o[dt]);
       }
+    if constexpr (G == 4 && F::dtype != DAVET_F32) {
+      constexpr int NF = KT / 16 * (D / 32);      // fragments, two reads each
+      __builtin_amdgcn_sched_group_barrier(0x100, 12, 1);
+#pragma unroll
+      for (int i = 0; i < NF - 6; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 6, 1);
+    }
   };
 
   // A masked weight of 0 times an infinite (or NaN) value would be NaN.  Where
