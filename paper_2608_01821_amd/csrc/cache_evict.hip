@@ -8,9 +8,7 @@
 // an LDS histogram find the key T of the last entry kept and how many of the
 // entries equal to it stay, and a last pass writes the indices in ascending
 // order.  Each wavefront owns one contiguous sixteenth of the entries, so the
-// order needs one scan over 16 counts and no barrier inside the passes.  Up to
-// 65536 entries are read once and stay in registers; more are read from L2 in
-// each of the five passes.
+// order needs one scan over 16 counts and no barrier inside the passes.
 //
 // Move: entry kept[j] of the source pages becomes entry j of the destination
 // pages, in the same pools; 64 entries of one head a workgroup, 16 bytes a
@@ -37,62 +35,97 @@ __device__ __forceinline__ uint32_t weight_key(float w, int i, int first,
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The entries of one wavefront: [lo, hi), entry lo + 64 u + lane in slot u.  With
-// R slots or fewer they are read once and held in registers as keys; R = 0 reads
-// them again in every pass, 8 loads in flight.
-template <int R>
+// The entries of one wavefront: [lo, hi), lo a multiple of 256.  Counting takes
+// 256 a step, four neighbours a lane, so that LDS reads and ballots overlap; what
+// goes to or comes from memory goes 64 neighbours an instruction.  Up to kLdsKeys
+// entries of a sequence are read once and stay in LDS as keys; more are read from
+// L2 in every pass.  (Held in registers, 32 or 64 a lane, the five unrolled
+// passes are 40 KB of code, and its fetch took twice the work's time.)  Places
+// past hi have key 0, below that of any entry, so no pass asks.
+constexpr int kStep = 256;
+constexpr int kLdsKeys = 36 * 1024;
+
+template <bool LDS>
 struct Entries {
   const float* w;
+  uint32_t* keys;       // LDS: of the sequence
   int lo, hi, first, tail;
-  uint32_t key[R ? R : 1];
-  __device__ __forceinline__ uint32_t key_of(float x, int i) const {
-    return i < hi ? weight_key(x, i, first, tail) : 0u;
-  }
-  __device__ __forceinline__ void load() {
-    if constexpr (R > 0) {
-      const int lane = threadIdx.x & 63;
+  // f(index, key, weight) of 64 places a step, in index order, U steps of loads
+  // in flight; with `weigh` false the weight is not read where keys are in LDS
+  template <int U, typename Fn>
+  __device__ __forceinline__ void each64(bool fresh, bool weigh, Fn f) const {
+    const int lane = threadIdx.x & 63;
+    for (int i0 = lo; i0 < hi; i0 += U * 64) {
+      float x[U];
 #pragma unroll
-      for (int u = 0; u < R; ++u)       // (clamped: every slot's load is valid)
-        key[u] = hi > lo ? __float_as_uint(w[min(lo + u * 64 + lane, hi - 1)]) : 0u;
+      for (int u = 0; u < U; ++u)
+        x[u] = fresh || weigh ? w[min(i0 + u * 64 + lane, hi - 1)] : 0.f;
 #pragma unroll
-      for (int u = 0; u < R; ++u)
-        key[u] = key_of(__uint_as_float(key[u]), lo + u * 64 + lane);
+      for (int u = 0; u < U; ++u) {
+        if (i0 + u * 64 >= hi) break;
+        const int i = i0 + u * 64 + lane;
+        if (fresh)
+          f(i, i < hi ? weight_key(x[u], i, first, tail) : 0u, x[u]);
+        else
+          f(i, keys[i], x[u]);
+      }
     }
   }
-  // f(index, inside, key) of 64 entries a step, in index order, all lanes at once
+  __device__ __forceinline__ void load() {
+    if constexpr (LDS) {
+      each64<16>(true, true, [&](int i, uint32_t key, float) { keys[i] = key; });
+      // the rest of the last step
+      for (int i = (hi + 63) / 64 * 64 + (int)(threadIdx.x & 63);
+           i < (hi + kStep - 1) / kStep * kStep; i += 64)
+        if (hi > lo) keys[i] = 0;
+    }
+  }
+  // f(four keys), any order
   template <typename Fn>
-  __device__ __forceinline__ void each(Fn f) const {
+  __device__ __forceinline__ void count(Fn f) const {
     const int lane = threadIdx.x & 63;
-    if constexpr (R > 0) {
-#pragma unroll
-      for (int u = 0; u < R; ++u) {
-        const int i = lo + u * 64 + lane;
-        if (lo + u * 64 < hi) f(i, i < hi, key[u]);
-      }
+    if constexpr (LDS) {
+#pragma unroll 2
+      for (int i0 = lo; i0 < hi; i0 += kStep)
+        f(*reinterpret_cast<const u32x4*>(keys + i0 + lane * 4));
     } else {
-      for (int i0 = lo; i0 < hi; i0 += 512) {
-        float x[8];
+      for (int i0 = lo; i0 < hi; i0 += 4 * kStep) {
+        float x[4][4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int i = i0 + u * 64 + lane;
-          x[u] = i < hi ? w[i] : 0.f;
-        }
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int i = i0 + u * 64 + lane;
-          if (i0 + u * 64 < hi) f(i, i < hi, key_of(x[u], i));
+          for (int e = 0; e < 4; ++e)
+            x[u][e] = w[min(i0 + u * kStep + e * 64 + lane, hi - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          u32x4 k;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = i0 + u * kStep + e * 64 + lane;
+            k[e] = i < hi ? weight_key(x[u][e], i, first, tail) : 0u;
+          }
+          f(k);
         }
       }
     }
   }
 };
 
-template <int R>
+// sum of the first n of 16 counts
+__device__ __forceinline__ uint32_t sum_before(const uint32_t (&c)[kSelWaves], int n) {
+  uint32_t s = 0;
+#pragma unroll
+  for (int i = 0; i < kSelWaves; ++i) s += i < n ? c[i] : 0u;
+  return s;
+}
+
+template <bool LDS>
 __global__ void __launch_bounds__(kSelThreads)
 evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
                     int64_t ld_w, int first, int last, int32_t* __restrict__ kept,
                     int64_t ld_kept, float* __restrict__ weights_out,
                     int64_t ld_wo) {
+  __shared__ __attribute__((aligned(16))) uint32_t s_keys[LDS ? kLdsKeys : 4];
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t wsum[kSelWaves], weq[kSelWaves];
   __shared__ uint32_t s_bin, s_need;
@@ -102,9 +135,10 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
   const float* w = weights + (int64_t)s * ld_w;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = ((n + kSelWaves - 1) / kSelWaves + 63) & ~63;
-  Entries<R> en;
+  const int per = ((n + kSelWaves - 1) / kSelWaves + kStep - 1) / kStep * kStep;
+  Entries<LDS> en;
   en.w = w;
+  en.keys = s_keys;
   en.lo = min(n, wave * per);
   en.hi = min(n, en.lo + per);
   en.first = first;
@@ -119,18 +153,25 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
     const uint32_t digit = pass == 2 ? 1023u : 2047u;
     for (int b = threadIdx.x; b < kBins; b += kSelThreads) hist[b] = 0;
     __syncthreads();
-    en.each([&](int, bool in, uint32_t key) {
-      if (in && (key & mask) == prefix) {
-        const uint32_t bin = (key >> shift) & digit;
-        // one counter for all lanes would be added to 64 times in turn (equal
-        // weights do that in every pass)
-        const uint32_t lead = __builtin_amdgcn_readfirstlane(bin);
-        const uint64_t on = __ballot(1), same = __ballot(bin == lead);
-        if (same != on)
-          atomicAdd(&hist[bin], 1u);
-        else if (lane == __ffsll((unsigned long long)on) - 1)
-          atomicAdd(&hist[lead], (uint32_t)__popcll(on));
+    en.count([&](u32x4 key) {
+      bool on[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) on[e] = (key[e] & mask) == prefix;
+      if (!__any(on[0] || on[1] || on[2] || on[3])) return;
+      uint32_t bin[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bin[e] = (key[e] >> shift) & digit;
+      // One counter for all would be added to 256 times in turn (equal weights
+      // do that in every pass).
+      const uint32_t one = __builtin_amdgcn_readfirstlane(bin[0]);
+      if (__all(on[0] && on[1] && on[2] && on[3] && bin[0] == one &&
+                bin[1] == one && bin[2] == one && bin[3] == one)) {
+        if (lane == 0) atomicAdd(&hist[one], (uint32_t)kStep);
+        return;
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (on[e]) atomicAdd(&hist[bin[e]], 1u);
     });
     __syncthreads();
     // from the top: thread t holds bins 2047 - 2t and 2046 - 2t
@@ -144,8 +185,7 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
     }
     if (lane == 63) wsum[wave] = sum;
     __syncthreads();
-    uint32_t before = sum - c1 - c0;
-    for (int i = 0; i < wave; ++i) before += wsum[i];
+    const uint32_t before = sum - c1 - c0 + sum_before(wsum, wave);
     if (before < need && need <= before + c1) {
       s_bin = b1;
       s_need = need - before;
@@ -160,20 +200,19 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
   }
   const uint32_t T = prefix;     // key of the last entry kept; `need` of them
   uint32_t gt = 0, eq = 0;
-  en.each([&](int, bool in, uint32_t key) {
-    gt += (uint32_t)__popcll(__ballot(in && key > T));
-    eq += (uint32_t)__popcll(__ballot(in && key == T));
+  en.count([&](u32x4 key) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      gt += (uint32_t)__popcll(__ballot(key[e] > T));
+      eq += (uint32_t)__popcll(__ballot(key[e] == T));
+    }
   });
   if (lane == 0) {
     wsum[wave] = gt;
     weq[wave] = eq;
   }
   __syncthreads();
-  uint32_t gt0 = 0, eq0 = 0;
-  for (int i = 0; i < wave; ++i) {
-    gt0 += wsum[i];
-    eq0 += weq[i];
-  }
+  uint32_t gt0 = sum_before(wsum, wave), eq0 = sum_before(weq, wave);
   // bits of m below this lane
   auto below = [](uint64_t m) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
@@ -181,13 +220,15 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
   };
   int32_t* ko = kept + (int64_t)s * ld_kept;
   float* wo = weights_out ? weights_out + (int64_t)s * ld_wo : nullptr;
-  en.each([&](int i, bool in, uint32_t key) {
-    const uint64_t mg = __ballot(in && key > T), me = __ballot(in && key == T);
+  en.template each64<8>(!LDS, wo, [&](int i, uint32_t key, float x) {
+    const uint64_t mg = __ballot(key > T), me = __ballot(key == T);
+    // entries above T, and equal to it, before this one; of the latter the first
+    // `need` of the sequence stay
     const uint32_t rg = gt0 + below(mg), re = eq0 + below(me);
-    if (in && (key > T || (key == T && re < need))) {
+    if (key > T || (key == T && re < need)) {
       const uint32_t at = rg + min(re, need);
       ko[at] = i;
-      if (wo) wo[at] = w[i];
+      if (wo) wo[at] = x;
     }
     gt0 += (uint32_t)__popcll(mg);
     eq0 += (uint32_t)__popcll(me);
@@ -291,16 +332,12 @@ extern "C" int davet_evict_select(int32_t n_seqs, const int32_t* n,
       DAVET_EINVAL, "davet_evict_select: weights_out overlaps weights");
   if (most_keep == 0) return DAVET_OK;
   ProfScope ps(KC_MISC, stream);
-#define SELECT(R)                                                              \
-  hipLaunchKernelGGL((evict_select_kernel<R>), dim3(n_seqs), dim3(kSelThreads), \
-                     0, stream, sp, weights, ld_weights, first, last, kept,    \
-                     ld_kept, weights_out, ld_weights_out)
-  // slots a lane: the largest wavefront's sixteenth, in steps of 64 entries
-  const int64_t slots = (most_n + 1023) / 1024;
-  if (slots <= 8) SELECT(8);
-  else if (slots <= 32) SELECT(32);
-  else if (slots <= 64) SELECT(64);
-  else SELECT(0);
+#define SELECT(LDS)                                                            \
+  hipLaunchKernelGGL((evict_select_kernel<LDS>), dim3(n_seqs),                 \
+                     dim3(kSelThreads), 0, stream, sp, weights, ld_weights,    \
+                     first, last, kept, ld_kept, weights_out, ld_weights_out)
+  if ((most_n + kStep - 1) / kStep * kStep <= kLdsKeys) SELECT(true);
+  else SELECT(false);
 #undef SELECT
   DAVET_HIP(hipGetLastError());
   return DAVET_OK;
