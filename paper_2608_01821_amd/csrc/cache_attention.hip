@@ -385,11 +385,26 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[mt][e] = 0.f;
+    if constexpr (F::dtype == DAVET_F32) {
+      // two sums of half the length: a chain of D roundings would show in lse
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
+      for (int mt = 0; mt < MT; ++mt) {
+        f32x16 half = sc[mt];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
+        for (int ks = 0; ks < D / 16; ks += 2) {
+          sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
+          half = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks + 1, hh), qf[ks + 1], half);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[mt][e] += half[e];
+      }
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
+    }
     if constexpr (G == 4 && F::dtype != DAVET_F32) {
       // eight reads of K ahead of the matrix ops (left alone: two)
       constexpr int NF = MT * D / 16;
@@ -927,9 +942,20 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
     f32x16 sc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+    if constexpr (F::dtype == DAVET_F32) {
+      f32x16 half = sc;                 // two sums of half the length
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      sc = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[ks], sc);
+      for (int ks = 0; ks < D / 16; ks += 2) {
+        sc = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[ks], sc);
+        half = mm<F>(T::k_frag(Qb, l32, ks + 1, hh), kf[ks + 1], half);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[e] += half[e];
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+        sc = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[ks], sc);
+    }
     const int first_lim = visible_end(min(qb * 32, rows - 1) / g, n, kv, block);
     const bool masked = (blk - wp.blk[s] + 1) * kWeightKeys > first_lim ||
                         qb * 32 + 32 > rows;

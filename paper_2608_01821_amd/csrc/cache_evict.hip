@@ -11,8 +11,8 @@
 // order needs one scan over 16 counts and no barrier inside the passes.
 //
 // Move: entry kept[j] of the source pages becomes entry j of the destination
-// pages, in the same pools; 64 entries of one head a workgroup, 16 bytes a
-// thread and load.  Bound by HBM.
+// pages, in the same pools; 16 KB of one head's keys and of its values a
+// workgroup, 16 bytes a thread and load.  Bound by HBM.
 
 #include <algorithm>
 
@@ -237,17 +237,19 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
 
 struct GatherPack {
   int32_t n_seqs;
-  int32_t blk[DAVET_MAX_SEQS + 1];    // first 64-entry block of each sequence
+  int32_t blk[DAVET_MAX_SEQS + 1];    // first block of entries of each sequence
   int32_t keep[DAVET_MAX_SEQS];
 };
 
-constexpr int kRows = 64;
+// 16 KB of K and of V a workgroup: four loads of each a thread
+constexpr int gather_rows(int row_bytes) { return 16384 / row_bytes; }
 
 template <int RB>     // bytes of a row
 __global__ void __launch_bounds__(256)
 cache_gather_kernel(CacheView cv, GatherPack gp, const int32_t* __restrict__ kept,
                     int64_t ld_kept, const int32_t* __restrict__ dst_table,
                     int32_t dst_max_pages) {
+  constexpr int kRows = gather_rows(RB);
   constexpr int C = RB / 16, PER = kRows * C / 256;   // loads a thread, of K or V
   __shared__ int64_t src[kRows], dst[kRows];
   const int nblk = gp.blk[gp.n_seqs];
@@ -358,6 +360,8 @@ extern "C" int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
                   "davet_cache_gather: null pointer");
   GatherPack gp{};
   gp.n_seqs = n_seqs;
+  const int rb = cache->head_dim * (int)dtype_size(cache->dtype);
+  const int rows = gather_rows(rb);
   int64_t at = 0;
   for (int s = 0; s < n_seqs; ++s) {
     DAVET_CHECK_ARG(keep[s] >= 0 && keep[s] <= ld_kept &&
@@ -366,7 +370,7 @@ extern "C" int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
                     "davet_cache_gather: keep out of range of ld_kept or of "
                     "dst_max_pages * page_size");
     gp.keep[s] = keep[s];
-    at += (keep[s] + kRows - 1) / kRows;
+    at += (keep[s] + rows - 1) / rows;
     DAVET_CHECK_ARG(at * cv.n_kv < (1ll << 31), DAVET_ESHAPE,
                     "davet_cache_gather: too many entries");
     gp.blk[s + 1] = (int)at;
@@ -374,7 +378,6 @@ extern "C" int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
   if (at == 0) return DAVET_OK;
   ProfScope ps(KC_MISC, stream);
   const dim3 grid((unsigned)(at * cv.n_kv));
-  const int rb = cache->head_dim * (int)dtype_size(cache->dtype);
 #define GATHER(RB)                                                             \
   hipLaunchKernelGGL((cache_gather_kernel<RB>), grid, dim3(256), 0, stream, cv, \
                      gp, kept, ld_kept, dst_table, dst_max_pages)
