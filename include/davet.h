@@ -598,7 +598,7 @@ int davet_cache_workspace_bytes(int32_t n_heads, int32_t head_dim,
  * chunk's first token (B = 1: causal).  Holes hold no keys.  What is not visible
  * never contributes, whatever it holds (NaN and infinities included).  A row
  * that sees no key, or whose every score is -inf, gets zeros and lse -inf.
- *   scale: positive, or 0 for 1 / sqrt(head_dim).
+ *   scale: in [1e-30, 1e30], or 0 for 1 / sqrt(head_dim).
  *   q, out [rows, n_heads * head_dim] with strides, not overlapping; lse float32
  *   [rows, n_heads] or NULL.
  * The 16-bit modes round probabilities to 16 bits before they meet the values

@@ -528,7 +528,7 @@ def _rows(t, width, n_rows, size, name):
     if one != 1 and w > 1:
         raise ValueError("davet: the rows of %s must be dense" % name)
     if n < 2:
-        ld = w
+        ld = width              # one row: whatever its tensor's stride
     elif ld < width:
         raise ValueError("davet: the rows of %s overlap" % name)
     return t.data_ptr(), ld

@@ -256,11 +256,9 @@ struct Scale {
 };
 
 // (x - m) scale log2(e) for fp32 operands, where the rounding of the constant
-// would show; far differences stop at a weight of 0 (-inf times its rest might
-// be +inf).
+// would show (-inf apart: times the constant's rest it might be +inf)
 __device__ __forceinline__ float exact_arg(float d, const Scale& s) {
-  d = d < -1e4f / s.c ? -1e4f / s.c : d;
-  return fmaf(d, s.c, d * s.c_lo);
+  return d == -INFINITY ? d : fmaf(d, s.c, d * s.c_lo);
 }
 
 // G wavefronts share a tile (4: wide, 1: narrow); BUFS buffers a tile stream.
@@ -319,7 +317,14 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  // Scores are kept as differences from `ref`, near the row's largest: the matrix
+  // ops start from -ref, so the subtraction is free, and a difference keeps its
+  // bits however large the scores are.
+  float ref = 0.f, l_run = 0.f;
+  bool seen = false;                // some score above -inf so far
+  f32x16 start;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) start[e] = 0.f;
 
   if (threadIdx.x == 0) s_bad = 0;
   __syncthreads();
@@ -382,14 +387,14 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     const char* Vb = Kb + TILE;
     f32x16 sc[MT];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[mt][e] = 0.f;
+    for (int mt = 0; mt < MT; ++mt) sc[mt] = start;
     if constexpr (F::dtype == DAVET_F32) {
       // two sums of half the length: a chain of D roundings would show in lse
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        f32x16 half = sc[mt];
+        f32x16 half;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) half[e] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ks += 2) {
           sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
@@ -433,13 +438,27 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 #pragma unroll
       for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, sc[mt][e]);
     tmax = pair_max32(tmax);
-    // the maximum moves only when it is 2^8 behind: O is rescaled rarely
-    const float m_new =
-        m_run == -INFINITY || (tmax - m_run) * sc_.c > 8.0f ? tmax : m_run;
-    // while nothing is visible every weight is 0, not exp(-inf + inf)
-    const float ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * sc_.c);
-    const float neg_m = BIAS - ref * sc_.c;
+    // ref moves only when it is 2^8 behind the largest score (or with the first
+    // one): O is rescaled rarely
+    const bool move = seen ? tmax * sc_.c > 8.0f : tmax > -INFINITY;
+    if (__any(move)) {
+      const float to = move ? ref + tmax : ref;
+      const float by = move ? to - ref : 0.f;
+      const float alpha = seen ? __builtin_amdgcn_exp2f(-by * sc_.c) : 0.f;
+      ref = to;
+      seen = seen || move;
+      l_run *= alpha;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) start[e] = -ref;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[mt][e] -= by;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+    }
     float psum = 0.f;
     // probabilities as operands of 16 keys each; lo: what rounding to 16 bits
     // took off them (few rows wait for memory, not for the matrix cores)
@@ -454,8 +473,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         for (int u = 0; u < 2; ++u) {
           const float x = sc[ps >> 1][(ps & 1) * 8 + e + u];
           p[u] = __builtin_amdgcn_exp2f(F::dtype == DAVET_F32
-                                            ? exact_arg(x - ref, sc_)
-                                            : fmaf(x, sc_.c, neg_m));
+                                            ? exact_arg(x, sc_)
+                                            : fmaf(x, sc_.c, BIAS));
           psum += p[u];
         }
         if constexpr (F::dtype == DAVET_F32) {
@@ -475,14 +494,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       }
     }
     psum = pair_sum32(psum);
-    l_run = l_run * alpha + psum;
-    m_run = m_new;
-    if (__any(alpha != 1.0f)) {
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-    }
+    l_run += psum;
 #pragma unroll
     for (int ps = 0; ps < KT / 16; ++ps)
 #pragma unroll
@@ -617,6 +629,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int re = min(wrow + l32e, rows - 1);
   const int qi = re / g, qh = hk * g + re % g;
   const float bias_ln = BIAS * kLn2;
+  const float m_run = l_run == 0.f ? -INFINITY : ref;
   if constexpr (G == 1) {
     // join the four streams: O as [wave][dim][32 rows], then max and sum
     __syncthreads();
@@ -1016,6 +1029,9 @@ cache_weights_join_kernel(ChunkPack cp, WeightPlan wp,
   weights[at] = (prev ? prev[at] : 0.f) + acc;
 }
 
+// (its product with log2(e) and the rest of that stay normal numbers)
+bool good_scale(float s) { return s == 0.f || (s >= 1e-30f && s <= 1e30f); }
+
 Scale make_scale(float scale, int D) {
   const double s = scale == 0.f ? 1.0 / sqrt((double)D) : (double)scale;
   const double c = s * 1.4426950408889634074;
@@ -1048,8 +1064,10 @@ AttnPlan plan_attn(const ChunkPack& cp, int n_kv, int g, int rows, int want,
     if (nt) longest = std::max(longest, cp.kv[s]);
     ap.order[s] = s;
   }
-  std::stable_sort(ap.order, ap.order + cp.n_seqs,
-                   [&](int32_t a, int32_t b) { return cp.kv[a] > cp.kv[b]; });
+  // longest first: what is left for the last round is short
+  std::sort(ap.order, ap.order + cp.n_seqs, [&](int32_t a, int32_t b) {
+    return cp.kv[a] != cp.kv[b] ? cp.kv[a] > cp.kv[b] : a < b;
+  });
   int64_t piece = std::max<int64_t>((work + want - 1) / want,
                                     ((int64_t)longest + cap - 1) / cap);
   piece = std::max<int64_t>(align_up(piece, unit), 4 * unit);
@@ -1225,8 +1243,8 @@ extern "C" int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs
   if (!rc && total > 0)
     rc = check_rows(out, ld_out, (int64_t)n_heads * D, cache->dtype, who, "out");
   if (rc) return rc;
-  DAVET_CHECK_ARG(scale >= 0.f && std::isfinite(scale), DAVET_EINVAL,
-                  "davet_cache_attention: scale must be positive and finite, or 0");
+  DAVET_CHECK_ARG(good_scale(scale), DAVET_EINVAL,
+                  "davet_cache_attention: scale must be 0 or in [1e-30, 1e30]");
   DAVET_CHECK_ARG(block >= 0, DAVET_EINVAL,
                   "davet_cache_attention: block must not be negative");
   if (total == 0) return DAVET_OK;
@@ -1269,9 +1287,9 @@ extern "C" int davet_cache_weights(const davet_kv_cache* cache, int32_t n_seqs,
   if (rc) return rc;
   DAVET_CHECK_ARG((lse || total == 0) && weights, DAVET_EINVAL,
                   "davet_cache_weights: null pointer");
-  DAVET_CHECK_ARG(scale >= 0.f && std::isfinite(scale) && block >= 0, DAVET_EINVAL,
-                  "davet_cache_weights: scale must be positive and finite, or 0, "
-                  "and block not negative");
+  DAVET_CHECK_ARG(good_scale(scale) && block >= 0, DAVET_EINVAL,
+                  "davet_cache_weights: scale must be 0 or in [1e-30, 1e30], "
+                  "block not negative");
   for (int s = 0; s < n_seqs; ++s)
     DAVET_CHECK_ARG(kv_len[s] <= ld_weights, DAVET_ESHAPE,
                     "davet_cache_weights: kv_len beyond ld_weights");

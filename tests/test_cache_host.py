@@ -86,6 +86,7 @@ def test_append_refusals():
 def test_attention_and_weights_refusals():
     assert _attend(cache=_cache(v=None)) == EINVAL
     for kw in (dict(scale=-1.0), dict(scale=float("nan")), dict(block=-1),
+               dict(scale=1e-38), dict(scale=float("inf")),
                dict(q=None), dict(out=None), dict(q=A + 8), dict(ldq=260),
                dict(out=A << 1)):
         assert _attend(**kw) == EINVAL, kw

@@ -216,6 +216,37 @@ def test_attention_strided_rows_stay_inside():
         assert bool((out == 7).all()) and bool((lse[new:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-30, 1e-3, 1e4, 1e30])
+def test_scales_to_the_limits(dtype, scale):
+    """Uniform weights at one end, the largest score alone at the other (keys
+    that are one dim each: scores are exact and apart)."""
+    t = Setup(13, dtype, [3], [40], 2, 1, 64, 16)
+    for j in range(40):
+        p, o = oc.slot(t.host, 0, j)
+        t.k[p, 0, o] = 0
+        t.k[p, 0, o, j] = 1
+    ref = oc.attention(t.host, t.cu, t.kv, f64(t.q), 2, scale=scale, block=1)
+    out, lse = t.attend(scale=scale, block=1)
+    u = half_step(dtype)
+    tol = u * np.abs(ref["out"]) + ref["mass"] * (u + 1e-5)
+    assert np.all(np.abs(out - ref["out"]) <= tol)
+    assert np.all(np.abs(lse - ref["lse"]) <= 1e-5 + 4e-7 * np.abs(ref["lse"]))
+
+
+def test_one_row_of_any_tensor():
+    """A single row has no stride to align: a slice of odd width is taken."""
+    t = Setup(14, "f16", [1], [20], 2, 1, 64, 16)
+    q = torch.zeros(1, 128 + 5, dtype=torch.float16, device="cuda")
+    q[:, :128] = t.q.cuda()
+    out = torch.zeros(1, 128 + 3, dtype=torch.float16, device="cuda")
+    dv.davet_cache_attention(t.device(), t.cu, t.kv, q, 2, out,
+                             workspace=t.workspace())
+    torch.cuda.synchronize()
+    assert np.array_equal(f64(out[:, :128]).reshape(1, 2, 64), t.attend()[0])
+    assert bool((out[:, 128:] == 0).all())
+
+
 def test_far_pages_need_64_bit_offsets():
     """A pool of more than 2^31 elements, pages at its end."""
     t = Setup(4, "f16", [3], [100], 2, 2, 128, 16)
