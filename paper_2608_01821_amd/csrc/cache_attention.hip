@@ -47,6 +47,7 @@ constexpr int kMaxPieces = 64;
 constexpr int kMaxPartRows = 1 << 17;     // rows x pieces in the workspace
 constexpr int kWeightKeys = 128;          // keys a workgroup of the weights
 constexpr int kWeightParts = 2048;        // workgroups that leave partial sums
+constexpr int kAhead = 4;                 // fragments read ahead of the matrix ops
 
 // Fragments of 8 elements along the contracted axis and the op that takes them.
 template <typename S> struct Frag;
@@ -87,6 +88,31 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t offset, void* l
                "global_load_lds_dwordx4 %1, %2"
                :: "s"(__builtin_amdgcn_readfirstlane(lds_at(lds))), "v"(offset),
                   "s"(base)
+               : "memory", "m0");
+}
+// 2 or 4 of them in a row, 1024 bytes apart (the instruction's offset counts for
+// both addresses)
+__device__ __forceinline__ void dma16_run(const void* base, const uint32_t (&o)[2],
+                                          void* lds) {
+  asm volatile("s_mov_b32 m0, %0\n\t"
+               "s_nop 0\n\t"
+               "global_load_lds_dwordx4 %1, %3\n\t"
+               "global_load_lds_dwordx4 %2, %3 offset:%4"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds_at(lds))), "v"(o[0]),
+                  "v"(o[1]), "s"(base), "n"(1024)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma16_run(const void* base, const uint32_t (&o)[4],
+                                          void* lds) {
+  asm volatile("s_mov_b32 m0, %0\n\t"
+               "s_nop 0\n\t"
+               "global_load_lds_dwordx4 %1, %5\n\t"
+               "global_load_lds_dwordx4 %2, %5 offset:%6\n\t"
+               "global_load_lds_dwordx4 %3, %5 offset:%7\n\t"
+               "global_load_lds_dwordx4 %4, %5 offset:%8"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds_at(lds))), "v"(o[0]),
+                  "v"(o[1]), "v"(o[2]), "v"(o[3]), "s"(base), "n"(1 * 1024),
+                  "n"(2 * 1024), "n"(3 * 1024)
                : "memory", "m0");
 }
 __device__ __forceinline__ void dma16_at(const void* g, void* lds) {
@@ -311,6 +337,10 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
                    (int64_t)(hk * g + r % g) * D + hh * 8;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = load_frag<F>(qp + ks * 16);
+    // waited for here: in the key loop the compiler's waits for them would be
+    // for tiles on their way as well
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
   }
   f32x16 o[D / 32];
 #pragma unroll
@@ -334,58 +364,96 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   pages.init(cv.table + (int64_t)s * cv.max_pages, cv.max_pages);
   const int lg = cv.lg, psz = 1 << lg;
 
-  // Moves this wave's rows of the tile at key k0 into buffer b; returns the
-  // 16-key groups of the whole tile that lie in holes.  Keys past the last
-  // cached one repeat it; rows of holes are zeroed (their scores are masked,
-  // but a NaN left in LDS would meet a weight of 0).
-  auto issue = [&](int k0, int b) -> int {
-    char* kd = gbuf + b * 2 * TILE;
-    char* vd = kd + TILE;
-    // one 16-key group: its rows of K and of V
-    auto move = [&](int gi, int key, int page, bool hole) {
-      char* kl = kd + gi * 16 * T::RB;
-      char* vl = vd + gi * 16 * T::RB;
-      if (hole) {
-#pragma unroll
-        for (int j = 0; j < 16 / T::RPI; ++j) {
-          *reinterpret_cast<u32x4*>(kl + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-          *reinterpret_cast<u32x4*>(vl + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-        }
-        return;
-      }
-      const int64_t base =
-          ((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * T::RB;
-      const char* kg = static_cast<const char*>(cv.k) + base;    // scalar
-      const char* vg = static_cast<const char*>(cv.v) + base;
-      const int last = kv - 1 - key;              // last valid row of the group
-#pragma unroll
-      for (int j = 0; j < 16 / T::RPI; ++j) {
-        const int lr = j * T::RPI + lane / T::C, tr = gi * 16 + lr, c = lane % T::C;
-        const uint32_t row = (uint32_t)min(lr, last) * T::RB;
-        dma16(kg, row + T::k_slot(tr, c) * 16, kl + j * 1024);
-        dma16(vg, row + T::v_slot(tr, c) * 16, vl + j * 1024);
-      }
+  // A 16-key group on its way to LDS.  A page holds whole groups.
+  struct Group {
+    int64_t at;         // byte of its first row in the pools; -1: in a hole
+    int last;           // its last valid row
+  };
+  auto group = [&](int k0, int gi, int page) {
+    const int key = min(k0 + gi * 16, (kv - 1) & ~15);
+    Group r;
+    r.at = (unsigned)page < (unsigned)cv.n_pages
+               ? ((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * T::RB
+               : -1;
+    r.last = kv - 1 - key;
+    return r;
+  };
+  // Moves its rows of K or V.  Rows past the last valid one repeat it; rows of
+  // holes are zeroed (their scores are masked, but a NaN left in LDS would meet a
+  // weight of 0).  Row r = j RPI + lane / C of chunk lane % C comes from slot
+  // lane % C ^ f(r), and f(r) = f(j RPI) ^ f(lane / C).
+  auto move16 = [&](bool of_k, char* to, const Group& r) {
+    constexpr int N = 16 / T::RPI, RUN = N < 4 ? N : 4;
+    auto slot = [&](int row, int c) {
+      return of_k ? T::k_slot(row, c) : T::v_slot(row, c);
     };
-    int holes = 0, my_key = 0, my_page = 0;
+    if (r.at < 0) {
 #pragma unroll
-    for (int gi = 0; gi < KT / 16; ++gi) {
-      const int key = min(k0 + gi * 16, (kv - 1) & ~15);
-      const int page = pages.at(key >> lg);
-      const bool hole = (unsigned)page >= (unsigned)cv.n_pages;
-      holes |= hole << gi;
-      if constexpr (G == 4) {
-        if (gi == wave) { my_key = key; my_page = page; }
-      } else {
-        move(gi, key, page, hole);
+      for (int j = 0; j < N; ++j)
+        *reinterpret_cast<u32x4*>(to + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+      return;
+    }
+    const char* from = static_cast<const char*>(of_k ? cv.k : cv.v) + r.at;  // scalar
+    if (r.last >= 15) {
+      const uint32_t first = (uint32_t)(lane * 16) ^ (slot(lane / T::C, 0) * 16);
+#pragma unroll
+      for (int j = 0; j < N; j += RUN) {
+        uint32_t at[RUN];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) at[i] = first ^ (slot((j + i) * T::RPI, 0) * 16);
+        dma16_run(from + j * 1024, at, to + j * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int lr = j * T::RPI + lane / T::C, c = lane % T::C;
+        dma16(from, (uint32_t)min(lr, r.last) * T::RB + slot(lr, c) * 16, to + j * 1024);
       }
     }
-    if constexpr (G == 4) move(wave, my_key, my_page, (holes >> wave) & 1);
+  };
+  // G = 4: the 16-key groups of the tile at k0 that lie in holes, and the one
+  // that this wave moves
+  struct Tag { int holes; Group mine; };
+  auto tag = [&](int k0) {
+    Tag r = {};
+    int page;
+    if (lg >= 6) {                      // the tile is in one page
+      page = pages.at(k0 >> lg);
+      r.holes = (unsigned)page >= (unsigned)cv.n_pages ? (1 << KT / 16) - 1 : 0;
+    } else {
+      page = 0;
+#pragma unroll
+      for (int gi = 0; gi < KT / 16; ++gi) {
+        const int p = pages.at(min(k0 + gi * 16, kv - 1) >> lg);
+        r.holes |= ((unsigned)p >= (unsigned)cv.n_pages) << gi;
+        if (gi == wave) page = p;
+      }
+    }
+    r.mine = group(k0, wave, page);
+    return r;
+  };
+  auto move_k = [&](const Tag& r, int b) {
+    move16(true, gbuf + b * 2 * TILE + wave * 16 * T::RB, r.mine);
+  };
+  auto move_v = [&](const Tag& r, int b) {
+    move16(false, gbuf + b * 2 * TILE + TILE + wave * 16 * T::RB, r.mine);
+  };
+  // G = 1: the whole tile; returns its holes
+  auto issue = [&](int k0, int b) -> int {
+    char* kd = gbuf + b * 2 * TILE;
+    int holes = 0;
+#pragma unroll
+    for (int gi = 0; gi < KT / 16; ++gi) {
+      const Group r = group(k0, gi, pages.at(min(k0 + gi * 16, kv - 1) >> lg));
+      holes |= (r.at < 0) << gi;
+      move16(true, kd + gi * 16 * T::RB, r);
+      move16(false, kd + TILE + gi * 16 * T::RB, r);
+    }
     return holes;
   };
 
-  auto compute = [&](int k0, const char* Kb, int holes) {
-    const char* Vb = Kb + TILE;
-    f32x16 sc[MT];
+  // S^T - ref of a tile's keys
+  auto scores = [&](const char* Kb, f32x16 (&sc)[MT]) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) sc[mt] = start;
     if constexpr (F::dtype == DAVET_F32) {
@@ -410,17 +478,17 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         for (int mt = 0; mt < MT; ++mt)
           sc[mt] = mm<F>(T::k_frag(Kb, mt * 32 + l32, ks, hh), qf[ks], sc[mt]);
     }
-    if constexpr (G == 4 && F::dtype != DAVET_F32) {
-      // eight reads of K ahead of the matrix ops (left alone: two)
-      constexpr int NF = MT * D / 16;
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+  };
+  auto largest = [&](const f32x16 (&sc)[MT]) {
+    float m = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < NF - 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
-    }
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, sc[mt][e]);
+    return m;
+  };
+  // Masks a tile's scores and moves ref if need be; tmax: the largest unmasked
+  auto settle = [&](int k0, int holes, f32x16 (&sc)[MT], float tmax) {
     // keys past a row's limit, or in a hole, score -inf
     const bool masked = k0 + KT > lim_all || holes;
     if (masked) {
@@ -431,12 +499,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
           const int at = mt * 32 + (e >> 2) * 8 + hh * 4 + (e & 3);
           if (k0 + at >= lim || ((holes >> (at >> 4)) & 1)) sc[mt][e] = -INFINITY;
         }
+      tmax = largest(sc);
     }
-    float tmax = -INFINITY;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, sc[mt][e]);
     tmax = pair_max32(tmax);
     // ref moves only when it is 2^8 behind the largest score (or with the first
     // one): O is rescaled rarely
@@ -459,10 +523,11 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
     }
+  };
+  // Probabilities as operands of 16 keys each; lo: what rounding to 16 bits
+  // took off them (few rows wait for memory, not for the matrix cores).
+  auto weigh = [&](const f32x16 (&sc)[MT], v8 (&hi)[KT / 16], v8 (&lo)[KT / 16]) {
     float psum = 0.f;
-    // probabilities as operands of 16 keys each; lo: what rounding to 16 bits
-    // took off them (few rows wait for memory, not for the matrix cores)
-    v8 hi[KT / 16], lo[KT / 16];
 #pragma unroll
     for (int ps = 0; ps < KT / 16; ++ps) {
       u32x4 w, w2;
@@ -493,8 +558,9 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         if constexpr (G == 1) lo[ps] = __builtin_bit_cast(v8, w2);
       }
     }
-    psum = pair_sum32(psum);
     l_run += psum;
+  };
+  auto values = [&](const char* Vb, const v8 (&hi)[KT / 16], const v8 (&lo)[KT / 16]) {
 #pragma unroll
     for (int ps = 0; ps < KT / 16; ++ps)
 #pragma unroll
@@ -504,16 +570,14 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         if constexpr (G == 1 && F::dtype != DAVET_F32)
           o[dt] = mm<F>(vf, lo[ps], o[dt]);
       }
-    if constexpr (G == 4 && F::dtype != DAVET_F32) {
-      constexpr int NF = KT / 16 * (D / 32);      // fragments, two reads each
-      __builtin_amdgcn_sched_group_barrier(0x100, 12, 1);
-#pragma unroll
-      for (int i = 0; i < NF - 6; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 6, 1);
-    }
+  };
+  auto compute = [&](int k0, const char* Kb, int holes) {
+    f32x16 sc[MT];
+    scores(Kb, sc);
+    settle(k0, holes, sc, largest(sc));
+    v8 hi[KT / 16], lo[KT / 16];
+    weigh(sc, hi, lo);
+    values(Kb + TILE, hi, lo);
   };
 
   // A masked weight of 0 times an infinite (or NaN) value would be NaN.  Where
@@ -554,7 +618,13 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     if constexpr (BUFS == 1) {
       // one buffer, refilled once every wave is done with it; the other
       // workgroups of the CU hide the load
-      int holes = nt > 0 ? issue(begin, 0) : 0;
+      auto load = [&](int it) {
+        const Tag r = tag(begin + it * KT);
+        move_k(r, 0);
+        move_v(r, 0);
+        return r.holes;
+      };
+      int holes = nt > 0 ? load(0) : 0;
       for (int it = 0; it < nt; ++it) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         sync_lds();
@@ -566,21 +636,111 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         if (live) compute(begin + it * KT, gbuf, holes);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         sync_lds();
-        if (it + 1 < nt) holes = issue(begin + (it + 1) * KT, 0);
+        if (it + 1 < nt) holes = load(it + 1);
       }
     } else {
-      int holes = nt > 0 ? issue(begin, 0) : 0;
-      for (int it = 0; it < nt; ++it) {
+      // Two waves a SIMD do not fill each other's gaps by themselves: the matrix
+      // ops of a tile and its exponentials took turns.  So the scores of tile
+      // it + 1 are multiplied between the exponentials of tile it (K is loaded a
+      // tile further ahead than V), in an order fixed by hand.  Four ragged
+      // prompts, 32 x 128 heads, fp16: 0.77 PFLOP/s (before: 0.72), 0.87 in bf16.
+      static_assert(F::dtype != DAVET_F32, "16-bit probabilities");
+      f32x16 even[MT], odd[MT];
+      float tmax = -INFINITY;
+      Tag cur = {}, nxt = {};
+      if (nt > 0) {
+        cur = tag(begin);
+        move_k(cur, 0);
+        move_v(cur, 0);
+        if (nt > 1) {
+          nxt = tag(begin + KT);
+          move_k(nxt, 1);
+        }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         sync_lds();
-        const int cur = holes;
-        if (it + 1 < nt) holes = issue(begin + (it + 1) * KT, (it + 1) & 1);
-        if (tile_masked(begin + it * KT, cur)) {
-          clean(gbuf + (it & 1) * 2 * TILE + TILE);
+        if (live) {
+          scores(gbuf, even);
+          tmax = largest(even);
+        }
+      }
+      // tile `it`, whose K and V are in buffer b, with the scores `sc`
+      auto step = [&](int it, int b, f32x16 (&sc)[MT], f32x16 (&ahead)[MT]) {
+        const int k0 = begin + it * KT;
+        char* Vb = gbuf + b * 2 * TILE + TILE;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        sync_lds();
+        Tag far = {};
+        if (it + 2 < nt) {
+          far = tag(k0 + 2 * KT);
+          move_k(far, b);
+        }
+        if (it + 1 < nt) move_v(nxt, b ^ 1);
+        if (tile_masked(k0, cur.holes)) {
+          clean(Vb);
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           sync_lds();
         }
-        if (live) compute(begin + it * KT, gbuf + (it & 1) * 2 * TILE, cur);
+        if (live) {
+          settle(k0, cur.holes, sc, tmax);
+          // NK products S^T of the next tile (behind the last one: of what the
+          // buffer holds, for nothing), then NV products O^T of this one, each
+          // with kAhead fragments read ahead; pairs of probabilities between
+          // the first NK + NV / 2 of them, just before their products.
+          const char* Kn = gbuf + (b ^ 1) * 2 * TILE;
+          constexpr int NK = MT * D / 16, DT = D / 32, NV = KT / 16 * DT;
+          constexpr int PAIRS = KT / 4, SLOTS = NK + NV / 2;
+          v8 f[kAhead], hi[KT / 16];
+          auto read = [&](int i) {
+            f[i % kAhead] =
+                i < NK ? T::k_frag(Kn, (i % MT) * 32 + l32, i / MT, hh)
+                       : T::v_frag(Vb, (i - NK) / DT, (i - NK) % DT, lane);
+          };
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) read(i);
+          float sum[2] = {0.f, 0.f};
+          u32x4 w = {};
+          auto pairs = [&](int slot) {
+#pragma unroll
+            for (int pr = 0; pr < PAIRS; ++pr) {
+              if (pr * SLOTS / PAIRS != slot) continue;
+              const int ps = pr / 4, e = pr % 4 * 2;
+              float p[2];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                p[u] = __builtin_amdgcn_exp2f(
+                    fmaf(sc[ps >> 1][(ps & 1) * 8 + e + u], sc_.c, BIAS));
+                sum[u] += p[u];
+              }
+              w[pr % 4] = round2<F>(p[0], p[1]);
+              if (pr % 4 == 3) hi[ps] = __builtin_bit_cast(v8, w);
+            }
+          };
+          __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+          for (int i = 0; i < NK; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            ahead[i % MT] = mm<F>(f[i % kAhead], qf[i / MT],
+                                  i < MT ? start : ahead[i % MT]);
+            read(i + kAhead);
+            pairs(i);
+          }
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            o[i % DT] = mm<F>(f[(NK + i) % kAhead], hi[i / DT], o[i % DT]);
+            if (i + kAhead < NV) read(NK + i + kAhead);
+            pairs(NK + i);
+          }
+          __builtin_amdgcn_s_setprio(0);
+          l_run += sum[0] + sum[1];
+          tmax = largest(ahead);
+        }
+        cur = nxt;
+        nxt = far;
+      };
+      for (int it = 0; it < nt; it += 2) {
+        step(it, 0, even, odd);
+        if (it + 1 < nt) step(it + 1, 1, odd, even);
       }
     }
   } else {
@@ -629,6 +789,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int re = min(wrow + l32e, rows - 1);
   const int qi = re / g, qh = hk * g + re % g;
   const float bias_ln = BIAS * kLn2;
+  l_run = pair_sum32(l_run);
   const float m_run = l_run == 0.f ? -INFINITY : ref;
   if constexpr (G == 1) {
     // join the four streams: O as [wave][dim][32 rows], then max and sum
