@@ -14,8 +14,15 @@
 // first batch: the smallest of them bounds the row's k-th value from below.  Two
 // sorted lists join by one compare against the reversed other and six exchange
 // steps: in LDS between the wavefronts, and in a second launch between the slices
-// of a row where there are several.  Bound by HBM (one read of the logits) for
-// many rows, by the launches' latency for few.
+// of a row where there are several.
+//
+// Measured with 126,464 logits a row.  256 fp32 rows: 27 us without a list (4.7
+// TB/s of logits), 32 with the top 20; bf16 18 and 27 us (3.5 and 2.4 TB/s): bound
+// by HBM and, in 16 bits, by the eight instructions and one exponential a logit,
+// then by the inserts of the list (one value in about 100 cycles; sorting the
+// candidates of a wavefront at once instead took 64 kept ones from 19 to 17 us in
+// two rows, but 20 of 256 rows from 27 to 31).  Two rows, 15 slices each: 7.5 us
+// and 4 to join them, the latency of two launches; one slice a row takes 22.
 
 #include <math.h>
 
@@ -29,6 +36,38 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxSlices = 16;
 constexpr int kWaves = 8;
+
+// The value of lane ^ O without a trip through LDS: half-wave and row swaps (which
+// leave the lower and the upper ones), a rotation by 8 in rows of 16, mirrored
+// halves of 8, permuted fours.  Two rows of 126,464 logits, top 5: 12.6 us by way
+// of LDS, 11.5 so.
+template <int O>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+#define DPP(v, ctrl) \
+  (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v), ctrl, 0xf, 0xf, false)
+  if constexpr (O == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  } else if constexpr (O == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  } else if constexpr (O == 8) {
+    return DPP(x, 0x128);
+  } else if constexpr (O == 4) {
+    return DPP(DPP(x, 0x141), 0x1b);
+  } else {
+    return DPP(x, O == 2 ? 0x4e : 0xb1);
+  }
+#undef DPP
+}
+template <int O>
+__device__ __forceinline__ float lane_xor(float x) {
+  return __uint_as_float(lane_xor<O>(__float_as_uint(x)));
+}
+template <int O>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t x) {
+  return (uint64_t)lane_xor<O>((uint32_t)(x >> 32)) << 32 | lane_xor<O>((uint32_t)x);
+}
 
 struct Stat { float m, S, B; };       // m = -inf: nothing yet
 
@@ -44,14 +83,17 @@ __device__ __forceinline__ Stat stat_join(const Stat& a, const Stat& b) {
   const Stat x = stat_to(a, m), y = stat_to(b, m);
   return {m, x.S + y.S, x.B + y.B};
 }
+template <int O>
+__device__ __forceinline__ Stat stat_step(const Stat& s) {
+  return stat_join(s, {lane_xor<O>(s.m), lane_xor<O>(s.S), lane_xor<O>(s.B)});
+}
 __device__ __forceinline__ Stat stat_wave(Stat s) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const Stat t = {__shfl_xor(s.m, o, 64), __shfl_xor(s.S, o, 64),
-                    __shfl_xor(s.B, o, 64)};
-    s = stat_join(s, t);
-  }
-  return s;
+  s = stat_step<1>(s);
+  s = stat_step<2>(s);
+  s = stat_step<4>(s);
+  s = stat_step<8>(s);
+  s = stat_step<16>(s);
+  return stat_step<32>(s);
 }
 // one logit; ref: s.m, or 0 while that is -inf
 __device__ __forceinline__ void term(float x, float ref, Stat& s) {
@@ -90,20 +132,20 @@ __device__ __forceinline__ void list_insert(uint64_t& list, uint64_t key) {
                                             false);
   list = lane < at ? list : lane == at ? key : up;
 }
-__device__ __forceinline__ uint64_t xor64(uint64_t v, int o) {
-  return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, 64) << 32 |
-         (uint32_t)__shfl_xor((int)(uint32_t)v, o, 64);
+template <int O>
+__device__ __forceinline__ uint64_t exchange(uint64_t v) {
+  const uint64_t y = lane_xor<O>(v);
+  return ((threadIdx.x & O) == 0) == (v > y) ? v : y;
 }
 // the 64 largest of two descending lists, the second one given in reverse
 __device__ __forceinline__ uint64_t list_join(uint64_t list, uint64_t reversed) {
-  const int lane = threadIdx.x & 63;
   uint64_t v = list > reversed ? list : reversed;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const uint64_t y = xor64(v, o);
-    v = ((lane & o) == 0) == (v > y) ? v : y;
-  }
-  return v;
+  v = exchange<32>(v);
+  v = exchange<16>(v);
+  v = exchange<8>(v);
+  v = exchange<4>(v);
+  v = exchange<2>(v);
+  return exchange<1>(v);
 }
 // The lists of W wavefronts (entries past k do not count) into wavefront 0's, in
 // log2 W steps; called by all.
