@@ -16,6 +16,10 @@
 // number), which keeps far positions exact; what is left, at most half a turn,
 // goes through the fp32 sine and cosine.  A rotary table would be read instead,
 // but bounds the positions and is one more buffer to own.
+//
+// Bound by HBM: a row is read once and written once.  Measured: 3092 bf16 rows of
+// (32 + 8 + 8) x 128, 76 MB in all, 15.3 us (5.0 TB/s; a copy of 76 MB takes 15.0);
+// one row 3.3 us, a launch's latency.
 
 #include <math.h>
 
@@ -158,7 +162,8 @@ cache_append_kernel(CacheView cv, ChunkPack cp, double log2_theta,
 
   // This thread's share of the angles: pair i turns theta^(-2 i / D) / (2 pi)
   // times round per position.  (A table of them in the kernel's arguments would
-  // be read from host memory by every workgroup: 42 us where this takes 23.)
+  // be read from host memory by every workgroup: 3092 rows took 42 us with it, 23
+  // without, before the loads ahead.)
   const int i = threadIdx.x % H;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const double freq = exp2(log2_theta * (-2.0 / D) * i) * 0.15915494309189533577;

@@ -13,6 +13,11 @@
 // Move: entry kept[j] of the source pages becomes entry j of the destination
 // pages, in the same pools; 16 KB of one head's keys and of its values a
 // workgroup, 16 bytes a thread and load.  Bound by HBM.
+//
+// Measured: 2964 entries cut to half, 8.5 us to select (the latency of five passes
+// in one workgroup) and 10.9 to move them, 49 MB read and written (4.5 TB/s); eight
+// sequences of up to 32,700, 26.7 us and 157 for 750 MB (4.8 TB/s; a copy of that
+// size reaches 5.1).
 
 #include <algorithm>
 
@@ -338,6 +343,8 @@ extern "C" int davet_evict_select(int32_t n_seqs, const int32_t* n,
   hipLaunchKernelGGL((evict_select_kernel<LDS>), dim3(n_seqs),                 \
                      dim3(kSelThreads), 0, stream, sp, weights, ld_weights,    \
                      first, last, kept, ld_kept, weights_out, ld_weights_out)
+  // keys in LDS where they fit: 36,000 entries 33 us with the move of one head,
+  // 50 read from L2 in every pass; 2964 the same within 1 us
   if ((most_n + kStep - 1) / kStep * kStep <= kLdsKeys) SELECT(true);
   else SELECT(false);
 #undef SELECT

@@ -112,7 +112,15 @@ ATTEND = [  # dtype, new, kv, heads, kv_heads, dim, page, block
     ("f32", [32], [192], 4, 4, 64, 16, 0),
     ("bf16", [32, 32], [100, 77], 2, 2, 128, 16, 4),
     ("f16", [9], [9], 28, 4, 64, 32, 3),                # 63 rows a key head
-    ("f16", [65], [65], 1, 1, 128, 16, 1),              # wide from here
+    ("f16", [32], [90], 1, 1, 128, 16, 1),              # narrow's last
+    ("f16", [33], [90], 1, 1, 128, 16, 1),              # wide from here
+    ("f32", [64], [90], 1, 1, 128, 16, 1),
+    ("f32", [65], [90], 1, 1, 128, 16, 1),              # wide from here
+    ("bf16", [40], [64], 1, 1, 128, 64, 0),             # one tile, whole
+    ("f16", [40], [65], 2, 2, 64, 64, 0),               # two, the last of one key
+    ("bf16", [40], [193], 2, 1, 128, 128, 1),           # four
+    ("f16", [40, 36], [320, 130], 2, 2, 128, 256, 4),   # five and three
+    ("f16", [65], [65], 1, 1, 128, 16, 1),
     ("f16", [33], [200], 4, 2, 128, 64, 0),
     ("bf16", [130, 4], [300, 40], 2, 1, 128, 16, 1),
     ("bf16", [70], [600], 3, 1, 64, 32, 32),
@@ -148,6 +156,20 @@ def test_holes_and_empty_rows(dtype, new, kv, block):
     got = t.attend(block=block)
     check_attention(got, ref, dtype, 64, kv[0])
     assert np.all(got[0][new[0]:] == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("page", [32, 64, 256])
+@pytest.mark.parametrize("new", [3, 40, 90])
+def test_holes_of_whole_tiles(dtype, page, new):
+    """Pages as large as a tile of keys, and larger: every second one a hole."""
+    kv = 3 * page + 150
+    t = Setup(17, dtype, [new, 1], [kv, page + 1], 2, 2, 128, page,
+              fill=float("nan"))
+    t.table[0, ::2] = -1
+    t.table[1, 0] = t.k.shape[0]
+    ref = oc.attention(t.host, t.cu, t.kv, f64(t.q), 2, block=1)
+    check_attention(t.attend(block=1), ref, dtype, 128, kv)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
