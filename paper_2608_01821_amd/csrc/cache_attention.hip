@@ -948,41 +948,70 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 }
 
 // Joins the pieces of every row: with m the largest piece maximum and
-// w_p = 2^((m_p - m) c), o = sum w_p O_p / sum w_p l_p, in piece order.  One
-// wavefront a row, D / 64 dims a lane: the row, and so its sequence's entries in
-// the kernel's arguments, are scalar.
+// w_p = 2^((m_p - m) c), o = sum w_p O_p / sum w_p l_p.  One wavefront a row: the
+// row, and so its sequence's entries in the kernel's arguments, are scalar; piece p's
+// maximum and sum are lane p's (there are at most 64), a lane adds D / 64 dims in
+// piece order.  Nothing is loaded twice or one after the other: it is all latency.
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, lane_xor<1>(x));
+  x = fmaxf(x, lane_xor<2>(x));
+  x = fmaxf(x, lane_xor<4>(x));
+  x = fmaxf(x, lane_xor<8>(x));
+  x = fmaxf(x, lane_xor<16>(x));
+  return fmaxf(x, lane_xor<32>(x));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x += lane_xor<1>(x);
+  x += lane_xor<2>(x);
+  x += lane_xor<4>(x);
+  x += lane_xor<8>(x);
+  x += lane_xor<16>(x);
+  return x + lane_xor<32>(x);
+}
 template <typename F, int D>
 __global__ void __launch_bounds__(256)
 cache_merge_kernel(ChunkPack cp, const float* __restrict__ part, int part_rows,
                    int piece, int pieces, typename F::st* __restrict__ out,
                    int64_t ld_o, float* __restrict__ lse, int n_heads, Scale sc_) {
   constexpr int E = D / 64;
+  constexpr int U = 8;                  // pieces' loads at a time
+  typedef float vec __attribute__((ext_vector_type(E)));
   const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (row >= part_rows) return;
-  const int d0 = (threadIdx.x & 63) * E;
+  const int lane = threadIdx.x & 63, d0 = lane * E;
   const int tok = row / n_heads, h = row % n_heads;
   const int s = owner(cp.row0, cp.n_seqs, tok);
   const int np = (cp.kv[s] + piece - 1) / piece;
-  const float* pm = part + (int64_t)pieces * part_rows * D;
-  float m = -INFINITY;
-#pragma unroll 4
-  for (int p = 0; p < np; ++p)
-    m = fmaxf(m, pm[((int64_t)p * part_rows + row) * 2]);
-  float l = 0.f, acc[E];
+  const float* pm = part + (int64_t)pieces * part_rows * D +
+                    ((int64_t)min(lane, np - 1) * part_rows + row) * 2;
+  const float mp = pm[0], lp = lane < np ? pm[1] : 0.f;
+  vec o[U];
+  auto load = [&](int p0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      o[u] = *reinterpret_cast<const vec*>(
+          part + ((int64_t)min(p0 + u, np - 1) * part_rows + row) * D + d0);
+  };
+  load(0);
+  // a piece that saw nothing: sum 0, maximum -inf (NaN scores: sum NaN)
+  const bool use = lp != 0.f;
+  const float m = wave_max(use ? mp : -INFINITY);
+  const float w = use ? __builtin_amdgcn_exp2f((mp - m) * sc_.c) : 0.f;
+  const float l = wave_sum(use ? w * lp : 0.f);
+  const uint64_t used = __ballot(use);
+  float acc[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < np; ++p) {
-    const int64_t at = (int64_t)p * part_rows + row;
-    const float mp = pm[at * 2], lp = pm[at * 2 + 1];
-    float o[E];
+  for (int p0 = 0; p0 < np; p0 += U) {
+    if (p0 > 0) load(p0);
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = part[at * D + d0 + e];
-    if (lp != 0.f) {
-      const float w = __builtin_amdgcn_exp2f((mp - m) * sc_.c);
-      l += w * lp;
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + u;
+      if (p >= np || !(used >> p & 1)) continue;
+      const float wp = __uint_as_float(
+          (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), p));
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += w * o[e];
+      for (int e = 0; e < E; ++e) acc[e] += wp * o[u][e];
     }
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -992,7 +1021,7 @@ cache_merge_kernel(ChunkPack cp, const float* __restrict__ part, int part_rows,
   else
 #pragma unroll
     for (int e = 0; e < E; ++e) op[e] = F::store(acc[e] * inv);
-  if (lse && d0 == 0)
+  if (lse && lane == 0)
     lse[row] = l == 0.f
                    ? -INFINITY
                    : m * sc_.scale + (logf(l) - Frag<F>::kBias * kLn2);

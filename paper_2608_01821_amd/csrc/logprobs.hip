@@ -37,38 +37,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxSlices = 16;
 constexpr int kWaves = 8;
 
-// The value of lane ^ O without a trip through LDS: half-wave and row swaps (which
-// leave the lower and the upper ones), a rotation by 8 in rows of 16, mirrored
-// halves of 8, permuted fours.  Two rows of 126,464 logits, top 5: 12.6 us by way
-// of LDS, 11.5 so.
-template <int O>
-__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
-#define DPP(v, ctrl) \
-  (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v), ctrl, 0xf, 0xf, false)
-  if constexpr (O == 32) {
-    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return threadIdx.x & 32 ? r[0] : r[1];
-  } else if constexpr (O == 16) {
-    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    return threadIdx.x & 16 ? r[0] : r[1];
-  } else if constexpr (O == 8) {
-    return DPP(x, 0x128);
-  } else if constexpr (O == 4) {
-    return DPP(DPP(x, 0x141), 0x1b);
-  } else {
-    return DPP(x, O == 2 ? 0x4e : 0xb1);
-  }
-#undef DPP
-}
-template <int O>
-__device__ __forceinline__ float lane_xor(float x) {
-  return __uint_as_float(lane_xor<O>(__float_as_uint(x)));
-}
-template <int O>
-__device__ __forceinline__ uint64_t lane_xor(uint64_t x) {
-  return (uint64_t)lane_xor<O>((uint32_t)(x >> 32)) << 32 | lane_xor<O>((uint32_t)x);
-}
-
 struct Stat { float m, S, B; };       // m = -inf: nothing yet
 
 __device__ __forceinline__ Stat stat_none() { return {-INFINITY, 0.f, 0.f}; }
