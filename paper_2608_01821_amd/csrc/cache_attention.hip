@@ -1255,10 +1255,11 @@ int max_pieces(int64_t rows) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxPieces, kMaxPartRows / rows));
 }
 
-// Cuts the keys into pieces so that the workgroups fill the chip once: `want`
-// of them run at a time.
+// Cuts the keys into pieces, multiples of `unit`, so that the workgroups fill the
+// chip once: `want` of them run at a time.  No piece is shorter than `least`, and
+// up to `whole` keys stay in one (no second launch).
 AttnPlan plan_attn(const ChunkPack& cp, int n_kv, int g, int rows, int want,
-                   int unit, int cap) {
+                   int unit, int least, int whole, int cap) {
   AttnPlan ap{};
   ap.xcd = n_kv % 8 == 0;
   int64_t work = 0;
@@ -1275,7 +1276,7 @@ AttnPlan plan_attn(const ChunkPack& cp, int n_kv, int g, int rows, int want,
   });
   int64_t piece = std::max<int64_t>((work + want - 1) / want,
                                     ((int64_t)longest + cap - 1) / cap);
-  piece = std::max<int64_t>(align_up(piece, unit), 4 * unit);
+  piece = std::max<int64_t>(align_up(piece, unit), longest <= whole ? whole : least);
   auto blocks = [&](int64_t p, int s) {
     const int64_t nt = ((int64_t)(cp.row0[s + 1] - cp.row0[s]) * g + rows - 1) / rows;
     return nt * n_kv * ((cp.kv[s] + p - 1) / p);
@@ -1319,8 +1320,14 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   constexpr int WM = 2;                                 // workgroups a CU
   constexpr int NB = f32 && D == 128 ? 1 : 2;           // narrow
   constexpr int NM = !f32 && D == 64 ? 2 : 1;
+  // Shortest pieces.  narrow, one tile a wave: one token, 8 key heads of 128 dims,
+  // 2964 keys 15.1 us in pieces of 128, 16.1 of 256, 19.1 of 512; 640 keys 13.1, and
+  // 18 in one piece; 250 keys 13.9, and 12.3 in one.  fp32, 64 dims: 250 keys 13.0
+  // and 16.3 in one, 200 the same.  wide: 128 queries, 8 heads, 2964 keys 24.6 us in
+  // pieces of 64, 20.2 of 128, 19.3 of 256.
   const AttnPlan ap = plan_attn(cp, cv.n_kv, g, wide ? 128 : 32,
                                 256 * (wide ? WM : NM), wide ? 64 : 128,
+                                wide ? 256 : 128, wide ? 256 : f32 ? 256 : 384,
                                 max_pieces(rows));
   const int64_t grid = (int64_t)ap.blk[cp.n_seqs] * (ap.xcd ? 8 : 1);
   DAVET_CHECK_ARG(grid < (1ll << 31), DAVET_ESHAPE,
