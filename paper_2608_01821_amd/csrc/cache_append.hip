@@ -107,7 +107,11 @@ int check_heads(const davet_kv_cache* c, int32_t n_heads, const char* who) {
 namespace {
 
 constexpr int kMaxThreads = 512;
-constexpr int kMaxGroups = 512;       // workgroups
+// Threads of all workgroups, which then take runs of rows.  32,000 rows of 9 x 64:
+// 85 us with 512 workgroups of their 128 threads, 25 with 1536; rows of 48 x 128
+// (384 threads) gain nothing from more than 512 (3092 of them 15.3 us, 16-18 with
+// 768 to 2048).
+constexpr int kMaxInFlight = 512 * 384;
 
 // 8 elements as memory holds them
 template <typename F>
@@ -319,7 +323,8 @@ extern "C" int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
   const int units = (n_heads + 2 * cv.n_kv) * (D / 16);
   const int passes = (units + kMaxThreads - 1) / kMaxThreads;
   const int threads = (int)align_up((units + passes - 1) / passes, 64);  // >= D / 2
-  const int rpw = (total + kMaxGroups - 1) / kMaxGroups;
+  const int groups = kMaxInFlight / threads;
+  const int rpw = (total + groups - 1) / groups;
   const int grid = (total + rpw - 1) / rpw;
   ProfScope ps(KC_MISC, stream);
 #define APPEND(F, DIM)                                                         \

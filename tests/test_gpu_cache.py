@@ -23,7 +23,9 @@ APPEND = [  # dtype, new, kv, heads, kv_heads, dim, page, norm
     ("f32", [9, 3], [9, 67], 4, 4, 64, 32, True),
     ("f32", [7], [300], 7, 1, 128, 256, False),
     ("f16", [33, 30], [33, 61], 28, 4, 64, 128, True),
-    ("bf16", [2100], [2110], 2, 1, 64, 32, True),     # two rows a workgroup
+    ("bf16", [2100], [2110], 2, 1, 64, 32, True),
+    ("f16", [3050, 3200, 0, 1], [3050, 3207, 0, 1], 1, 1, 64, 64, True),  # three rows
+    ("bf16", [401], [410], 32, 16, 128, 64, True),    # a workgroup, or two, of 512
 ]
 
 
