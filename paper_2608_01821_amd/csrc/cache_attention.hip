@@ -54,8 +54,8 @@ typedef __attribute__((address_space(3))) v4s* lds_v4s_ptr;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxPieces = 64;
 constexpr int kMaxPartRows = 1 << 17;     // rows x pieces in the workspace
-constexpr int kWeightKeys = 128;          // keys a workgroup of the weights
-constexpr int kWeightParts = 2048;        // workgroups that leave partial sums
+constexpr int kWeightKeys = 128;          // keys a workgroup of the weights (or twice)
+constexpr int kWeightGroups = 4096;       // most workgroups that leave partial sums
 constexpr int kAhead = 4;                 // fragments read ahead of the matrix ops
 
 // Fragments of 8 elements along the contracted axis and the op that takes them.
@@ -1029,8 +1029,8 @@ cache_merge_kernel(ChunkPack cp, const float* __restrict__ part, int part_rows,
 
 // Weights: w_j = prev_j + sum over the rows r that see key j of
 // exp(scale q_r.k_j - lse_r).  S = Q K^T this time: a lane holds 16 rows' scores
-// of ONE key and adds them in registers.  A workgroup takes 128 keys (32 a wave,
-// held as fragments) and walks the rows of its key heads in tiles of 32 that the
+// of ONE key and adds them in registers.  A workgroup takes 128 keys (32 a wave, or
+// 64, held as fragments) and walks the rows of its key heads in tiles of 32 that the
 // four waves share through LDS.  Chunks of (key head, row range) leave partial
 // sums that a second kernel adds in order.
 //
@@ -1038,15 +1038,18 @@ cache_merge_kernel(ChunkPack cp, const float* __restrict__ part, int part_rows,
 // heads: 74.5 us for 376 MB of keys (5.0 TB/s), bound by HBM.  128 queries, 32 heads,
 // 3092 keys: 14.4 us and 4 to add the partial sums, where 26 MB take 5: bound by the
 // chain of page, keys, rows and four tiles, gone through once with the whole chip's
-// workgroups at it (loading the keys ahead of the rows: 16.1 us).
+// workgroups at it (loading the keys ahead of the rows: 16.1 us).  Four prompts of up
+// to 3092 in full, 163 GFLOP: 270 us (0.6 PFLOP/s), bound by the vector ops and
+// waits of four waves at one tile of rows.
 struct WeightPlan {
-  int32_t blk[DAVET_MAX_SEQS + 1];    // first 128-key block of each sequence
+  int32_t blk[DAVET_MAX_SEQS + 1];    // first block of keys of each sequence
   int32_t heads;                      // key heads a chunk
   int32_t qsplit;                     // row ranges a key head (heads = 1)
   int32_t chunks;
 };
 
-template <typename F, int D>
+// KW: tiles of 32 keys a wave
+template <typename F, int D, int KW>
 __global__ void __launch_bounds__(256, 2)
 cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                      const typename F::st* __restrict__ q, int64_t ld_q,
@@ -1072,11 +1075,20 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
   const int rows = n * g, nqb = (rows + 31) / 32;
   const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int key = (blk - wp.blk[s]) * kWeightKeys + wave * 32 + l32;
-  const int kc = min(key, kv - 1);
-  const int page = cv.table[(int64_t)s * cv.max_pages + (kc >> cv.lg)];
-  const bool hole = (unsigned)page >= (unsigned)cv.n_pages;
-  const int64_t kbase = hole ? 0 : (((int64_t)page * cv.n_kv) << cv.lg) + (kc & ((1 << cv.lg) - 1));
+  constexpr int KEYS = kWeightKeys * KW;          // of the workgroup
+  int key[KW];
+  bool hole[KW];
+  int64_t kbase[KW];
+#pragma unroll
+  for (int t = 0; t < KW; ++t) {
+    key[t] = (blk - wp.blk[s]) * KEYS + (wave * KW + t) * 32 + l32;
+    const int kc = min(key[t], kv - 1);
+    const int page = cv.table[(int64_t)s * cv.max_pages + (kc >> cv.lg)];
+    hole[t] = (unsigned)page >= (unsigned)cv.n_pages;
+    kbase[t] = hole[t] ? 0
+                       : (((int64_t)page * cv.n_kv) << cv.lg) +
+                             (kc & ((1 << cv.lg) - 1));
+  }
   int h0, h1, b0 = 0, b1 = nqb;
   if (wp.qsplit > 1) {
     h0 = chunk / wp.qsplit;
@@ -1131,15 +1143,19 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
     ib = (ib + 1) % NBUF;
     if (++iqb == b1) { iqb = b0; ++ih; }
   };
-  v8 kf[D / 16];
-  float acc = 0.f;
+  v8 kf[KW][D / 16];
+  float acc[KW] = {};
   for (int i = 0; i < min(NBUF - 1, steps); ++i) issue();
   int h = h0, qb = b0;
   for (int step = 0; step < steps; ++step) {
     if (qb == b0) {
-      const st* kp = static_cast<const st*>(cv.k) + (kbase + ((int64_t)h << cv.lg)) * D + hh * 8;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) kf[ks] = load_frag<F>(kp + ks * 16);
+      for (int t = 0; t < KW; ++t) {
+        const st* kp = static_cast<const st*>(cv.k) +
+                       (kbase[t] + ((int64_t)h << cv.lg)) * D + hh * 8;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) kf[t][ks] = load_frag<F>(kp + ks * 16);
+      }
     }
     // the loads of up to two later steps may stay out
     static_assert(NBUF == 4, "the waits below");
@@ -1157,37 +1173,46 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
     const float le = lw[lane];
     lw[lane] = le == -INFINITY ? INFINITY : le * kLog2e;
     const char* Qb = qs[step % NBUF];
-    f32x16 sc;
+    f32x16 sc[KW];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+    for (int t = 0; t < KW; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[t][e] = 0.f;
     if constexpr (F::dtype == DAVET_F32) {
-      f32x16 half = sc;                 // two sums of half the length
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ks += 2) {
-        sc = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[ks], sc);
-        half = mm<F>(T::k_frag(Qb, l32, ks + 1, hh), kf[ks + 1], half);
+      for (int t = 0; t < KW; ++t) {
+        f32x16 half = sc[t];            // two sums of half the length
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ks += 2) {
+          sc[t] = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[t][ks], sc[t]);
+          half = mm<F>(T::k_frag(Qb, l32, ks + 1, hh), kf[t][ks + 1], half);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[t][e] += half[e];
       }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[e] += half[e];
     } else {
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-        sc = mm<F>(T::k_frag(Qb, l32, ks, hh), kf[ks], sc);
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const v8 qf = T::k_frag(Qb, l32, ks, hh);
+#pragma unroll
+        for (int t = 0; t < KW; ++t) sc[t] = mm<F>(qf, kf[t][ks], sc[t]);
+      }
     }
     const int first_lim = visible_end(min(qb * 32, rows - 1) / g, n, kv, block);
-    const bool masked = (blk - wp.blk[s] + 1) * kWeightKeys > first_lim ||
+    const bool masked = (blk - wp.blk[s] + 1) * KEYS > first_lim ||
                         qb * 32 + 32 > rows;
-    float p[16];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const f32x4 lv = *reinterpret_cast<const f32x4*>(lw + u * 8 + hh * 4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = sc[u * 4 + e];
-        p[u * 4 + e] = __builtin_amdgcn_exp2f(
-            F::dtype == DAVET_F32 ? fmaf(x, sc_.c, fmaf(x, sc_.c_lo, -lv[e]))
-                                  : fmaf(x, sc_.c, -lv[e]));
-      }
+      for (int t = 0; t < KW; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = sc[t][u * 4 + e];
+          sc[t][u * 4 + e] = __builtin_amdgcn_exp2f(
+              F::dtype == DAVET_F32 ? fmaf(x, sc_.c, fmaf(x, sc_.c_lo, -lv[e]))
+                                    : fmaf(x, sc_.c, -lv[e]));
+        }
     }
     if (masked) {
 #pragma unroll
@@ -1195,41 +1220,49 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
         const i32x4 end = *reinterpret_cast<const i32x4*>(
             &lim[step % NBUF][wave][u * 8 + hh * 4]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          p[u * 4 + e] = key < end[e] ? p[u * 4 + e] : 0.f;
+        for (int t = 0; t < KW; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sc[t][u * 4 + e] = key[t] < end[e] ? sc[t][u * 4 + e] : 0.f;
       }
     }
-    float sum = 0.f;
+    float sum[KW] = {};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sum += p[e];
-    acc += sum;
+    for (int t = 0; t < KW; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum[t] += sc[t][e];
+#pragma unroll
+    for (int t = 0; t < KW; ++t) acc[t] += sum[t];
     if (++qb == b1) { qb = b0; ++h; }
   }
-  acc = pair_sum32(acc);
-  if (hole) acc = 0.f;
-  if (hh == 0) {
+#pragma unroll
+  for (int t = 0; t < KW; ++t) {
+    float w = pair_sum32(acc[t]);
+    if (hole[t]) w = 0.f;
+    if (hh != 0) continue;
     if (wp.chunks > 1) {
-      part[((int64_t)chunk * nblk + blk) * kWeightKeys + wave * 32 + l32] = acc;
-    } else if (key < kv) {
-      const int64_t at = (int64_t)s * ld_w + key;
-      weights[at] = (prev ? prev[at] : 0.f) + acc;
+      part[((int64_t)chunk * nblk + blk) * KEYS + (wave * KW + t) * 32 + l32] = w;
+    } else if (key[t] < kv) {
+      const int64_t at = (int64_t)s * ld_w + key[t];
+      weights[at] = (prev ? prev[at] : 0.f) + w;
     }
   }
 }
 
-__global__ void __launch_bounds__(kWeightKeys)
+// one thread a key; blockDim.x: keys of a block
+__global__ void __launch_bounds__(2 * kWeightKeys)
 cache_weights_join_kernel(ChunkPack cp, WeightPlan wp,
                           const float* __restrict__ part,
                           const float* __restrict__ prev,
                           float* __restrict__ weights, int64_t ld_w) {
   const int nblk = wp.blk[cp.n_seqs], blk = blockIdx.x;
   const int s = owner(wp.blk, cp.n_seqs, blk);
-  const int key = (blk - wp.blk[s]) * kWeightKeys + threadIdx.x;
+  const int keys = blockDim.x, key = (blk - wp.blk[s]) * keys + threadIdx.x;
   if (key >= cp.kv[s]) return;
   float acc = 0.f;
 #pragma unroll 8
   for (int c = 0; c < wp.chunks; ++c)
-    acc += part[((int64_t)c * nblk + blk) * kWeightKeys + threadIdx.x];
+    acc += part[((int64_t)c * nblk + blk) * keys + threadIdx.x];
   const int64_t at = (int64_t)s * ld_w + key;
   weights[at] = (prev ? prev[at] : 0.f) + acc;
 }
@@ -1355,24 +1388,33 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   return DAVET_OK;
 }
 
-template <typename F, int D>
-int run_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
+template <typename F, int D, int KW>
+int launch_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
                 int64_t ld_q, const float* lse, int n_heads, int block,
                 Scale scale, const float* prev, float* weights, int64_t ld_w,
                 float* part, hipStream_t stream) {
+  constexpr int KEYS = kWeightKeys * KW;
   WeightPlan wp{};
   int most = 0;
   for (int s = 0; s < cp.n_seqs; ++s) {
     const int n = cp.row0[s + 1] - cp.row0[s];
     most = std::max(most, n);
-    wp.blk[s + 1] = wp.blk[s] + (cp.kv[s] + kWeightKeys - 1) / kWeightKeys;
+    wp.blk[s + 1] = wp.blk[s] + (cp.kv[s] + KEYS - 1) / KEYS;
   }
   const int nblk = wp.blk[cp.n_seqs];
   if (nblk == 0) return DAVET_OK;
   const int g = n_heads / cv.n_kv;
   const int64_t nqb = ((int64_t)most * g + 31) / 32;
-  // 1024 workgroups fill the chip twice
-  const int want = std::max(1, kWeightParts / 2 / nblk);
+  int64_t steps = 0;
+  for (int s = 0; s < cp.n_seqs; ++s)
+    steps += (int64_t)(wp.blk[s + 1] - wp.blk[s]) * cv.n_kv *
+             (((int64_t)(cp.row0[s + 1] - cp.row0[s]) * g + 31) / 32);
+  // Workgroups: the chip twice over (1024), or with more work up to kWeightGroups of
+  // at least 16 tiles of rows each (four prompts of up to 3092 in full, unequal:
+  // 390 us with 1024, 270 so).
+  const int groups = (int)std::max<int64_t>(
+      1024, std::min<int64_t>(kWeightGroups, steps / 16));
+  const int want = std::max(1, groups / nblk);
   wp.qsplit = 1;
   if (want >= cv.n_kv) {
     wp.heads = 1;
@@ -1387,18 +1429,37 @@ int run_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
                   "davet_cache_weights: too many key blocks");
   {
     ProfScope ps(KC_MISC, stream);
-    hipLaunchKernelGGL((cache_weights_kernel<F, D>), dim3((unsigned)grid), dim3(256),
+    hipLaunchKernelGGL((cache_weights_kernel<F, D, KW>), dim3((unsigned)grid), dim3(256),
                        0, stream, cv, cp, wp, (const typename F::st*)q, ld_q, lse,
                        n_heads, block, scale, prev, weights, ld_w, part);
     DAVET_HIP(hipGetLastError());
   }
   if (wp.chunks > 1) {
     ProfScope ps(KC_MISC, stream);
-    hipLaunchKernelGGL(cache_weights_join_kernel, dim3(nblk), dim3(kWeightKeys),
+    hipLaunchKernelGGL(cache_weights_join_kernel, dim3(nblk), dim3(KEYS),
                        0, stream, cp, wp, part, prev, weights, ld_w);
     DAVET_HIP(hipGetLastError());
   }
   return DAVET_OK;
+}
+
+template <typename F, int D>
+int run_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
+                int64_t ld_q, const float* lse, int n_heads, int block,
+                Scale scale, const float* prev, float* weights, int64_t ld_w,
+                float* part, hipStream_t stream) {
+  int64_t tiles = 0;                    // 32 rows x 128 keys, of all key heads
+  for (int s = 0; s < cp.n_seqs; ++s)
+    tiles += ((int64_t)(cp.row0[s + 1] - cp.row0[s]) * n_heads + 31) / 32 *
+             ((cp.kv[s] + kWeightKeys - 1) / kWeightKeys);
+  // Two tiles of keys a wave (half the LDS reads and waits) from enough work on:
+  // 30,000 tiles 62 us, 66 with one; 14,000 tiles 42.5 and 38; fp32 has no room.
+  if constexpr (F::dtype != DAVET_F32)
+    if (tiles > 20000)
+      return launch_weights<F, D, 2>(cv, cp, q, ld_q, lse, n_heads, block, scale,
+                                     prev, weights, ld_w, part, stream);
+  return launch_weights<F, D, 1>(cv, cp, q, ld_q, lse, n_heads, block, scale, prev,
+                                 weights, ld_w, part, stream);
 }
 
 size_t workspace_bytes(int64_t total_q, int n_heads, int D) {
@@ -1406,7 +1467,7 @@ size_t workspace_bytes(int64_t total_q, int n_heads, int D) {
   size_t b = 0;
   if (rows > 0 && max_pieces(rows) > 1)
     b = attn_part_floats(rows, max_pieces(rows), D) * sizeof(float);
-  const size_t w = (size_t)kWeightParts * kWeightKeys * sizeof(float);
+  const size_t w = (size_t)kWeightGroups * 2 * kWeightKeys * sizeof(float);
   return align_up(std::max(b, w), 256);
 }
 

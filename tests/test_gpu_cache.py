@@ -331,6 +331,46 @@ def test_weights(case, accumulate):
     assert torch.equal(w[-1], keep[-1])
 
 
+@pytest.mark.parametrize("dtype,heads,hk,dim,page,block", [
+    ("f16", 32, 8, 128, 64, 0), ("bf16", 32, 32, 64, 16, 1), ("f16", 32, 4, 64, 256, 48)])
+def test_weights_of_long_chunks(dtype, heads, hk, dim, page, block):
+    """Enough rows and keys that a wavefront takes two tiles of keys; a hole, and a
+    short sequence beside."""
+    new, kv = [700, 20], [5003, 290]
+    t = Setup(31, dtype, new, kv, heads, hk, dim, page, fill=float("nan"))
+    t.table[0, 1] = -1
+    scale, want, most = dim ** -0.5, np.zeros((2, max(kv))), 0.0
+    lse = np.zeros((sum(new), heads))
+    q = t.q.cuda().double().reshape(-1, heads, dim)
+    for s, (n, m) in enumerate(zip(new, kv)):
+        ids = torch.from_numpy(t.table[s, :-(-m // page)].astype(np.int64))
+        k = t.k[ids.clamp(min=0)].cuda().double().permute(1, 0, 2, 3)
+        k = k.reshape(hk, -1, dim)[:, :m]
+        i, j = torch.arange(n)[:, None], torch.arange(m)[None]
+        end = m if block == 0 else m - n + ((i // block + 1) * block).clamp(max=n)
+        seen = ((j < end) & (ids >= 0).repeat_interleave(page)[:m]).cuda()
+        rows = slice(t.cu[s], t.cu[s + 1])
+        for h in range(heads):
+            kh, qh = k[h * hk // heads].nan_to_num(), q[rows, h]
+            x = (scale * (qh @ kh.T.contiguous())).masked_fill(~seen, -np.inf)
+            z = x.logsumexp(1).float().double()
+            want[s, :m] += (x - z[:, None]).exp().sum(0).cpu().numpy()
+            lse[rows, h] = z.cpu().numpy()
+            most = max(most, float(scale * (qh.abs() @ kh.abs().T.contiguous()).max()))
+    w = torch.full((2, max(kv) + 1), 7.0, device="cuda")
+    dv.davet_cache_weights(t.device(), t.cu, t.kv, t.q.cuda(), heads,
+                           torch.from_numpy(lse).float().cuda(), w, block=block,
+                           workspace=t.workspace())
+    torch.cuda.synchronize()
+    rel = (dim + 8) * 2.0 ** -24 * (most + np.abs(lse).max() + 1) + \
+        (max(new) * heads + 8) * 2.0 ** -24         # as in test_weights
+    for s, m in enumerate(kv):
+        got = f64(w[s, :m])
+        assert np.all(np.abs(got - want[s, :m]) <= rel * want[s, :m] + 1e-30)
+        assert torch.all(w[s, m:] == 7.0)
+    assert np.all(f64(w[0, page:2 * page]) == 0)
+
+
 def test_weights_sum_to_the_rows():
     """Every row and head gives 1 in all."""
     t = Setup(5, "f16", [50], [300], 4, 2, 128, 32)
