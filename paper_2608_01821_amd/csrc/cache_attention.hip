@@ -877,6 +877,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       const int64_t at = (int64_t)pl.piece * part_rows +
                          (int64_t)(row0 + qi) * n_heads + qh;
       float* po = part + at * D + hhe * 4;
+      // (the join does not use the O of a piece that saw nothing)
+      if (l_run != 0.f)
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -1089,12 +1091,17 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                        : (((int64_t)page * cv.n_kv) << cv.lg) +
                              (kc & ((1 << cv.lg) - 1));
   }
+  // the row tiles from the first one that sees any of the keys
   int h0, h1, b0 = 0, b1 = nqb;
+  if (block > 0) {
+    const int own = (blk - wp.blk[s]) * KEYS - (kv - n);
+    if (own > 0) b0 = min(nqb, (int)((int64_t)(own / block) * block * g / 32));
+  }
   if (wp.qsplit > 1) {
     h0 = chunk / wp.qsplit;
     h1 = h0 + 1;
-    const int per = (nqb + wp.qsplit - 1) / wp.qsplit;
-    b0 = min(nqb, (chunk % wp.qsplit) * per);
+    const int per = (nqb - b0 + wp.qsplit - 1) / wp.qsplit;
+    b0 = min(nqb, b0 + (chunk % wp.qsplit) * per);
     b1 = min(nqb, b0 + per);
   } else {
     h0 = chunk * wp.heads;
@@ -1357,10 +1364,13 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   // 2964 keys 15.1 us in pieces of 128, 16.1 of 256, 19.1 of 512; 640 keys 13.1, and
   // 18 in one piece; 250 keys 13.9, and 12.3 in one.  fp32, 64 dims: 250 keys 13.0
   // and 16.3 in one, 200 the same.  wide: 128 queries, 8 heads, 2964 keys 24.6 us in
-  // pieces of 64, 20.2 of 128, 19.3 of 256.
+  // pieces of 64, 20.2 of 128, 19.3 of 256; fp32, whose tile of 64 keys takes 4 to 8
+  // us, 194 queries over 272 keys 23 us in pieces of 64, 32 of 128, 48 of 256.
+  constexpr int NH = f32 ? 256 : 384;
+  constexpr int WL = f32 ? 64 : 256, WH = f32 ? 128 : 256;
   const AttnPlan ap = plan_attn(cp, cv.n_kv, g, wide ? 128 : 32,
                                 256 * (wide ? WM : NM), wide ? 64 : 128,
-                                wide ? 256 : 128, wide ? 256 : f32 ? 256 : 384,
+                                wide ? WL : 128, wide ? WH : NH,
                                 max_pieces(rows));
   const int64_t grid = (int64_t)ap.blk[cp.n_seqs] * (ap.xcd ? 8 : 1);
   DAVET_CHECK_ARG(grid < (1ll << 31), DAVET_ESHAPE,
