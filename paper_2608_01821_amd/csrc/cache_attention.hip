@@ -1091,12 +1091,15 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                        : (((int64_t)page * cv.n_kv) << cv.lg) +
                              (kc & ((1 << cv.lg) - 1));
   }
-  // the row tiles from the first one that sees any of the keys
-  int h0, h1, b0 = 0, b1 = nqb;
+  // the row tiles from the first one that sees any of the keys; rows from `all` on
+  // see them all
+  int h0, h1, b0 = 0, b1 = nqb, all = 0;
   if (block > 0) {
-    const int own = (blk - wp.blk[s]) * KEYS - (kv - n);
+    const int own = (blk - wp.blk[s]) * KEYS - (kv - n), end = min(own + KEYS, n);
     if (own > 0) b0 = min(nqb, (int)((int64_t)(own / block) * block * g / 32));
+    if (end > 0) all = (end - 1) / block * block * g;
   }
+  auto masked = [&](int qb) { return qb * 32 < all || qb * 32 + 32 > rows; };
   if (wp.qsplit > 1) {
     h0 = chunk / wp.qsplit;
     h1 = h0 + 1;
@@ -1140,7 +1143,7 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                  qs[ib] + (wave * NI + i) * 1024);
       } else {
         dma4_at(lse + tk * n_heads + hq, ls[ib][wave]);
-        if (hh == 0)
+        if (masked(iqb) && hh == 0)
           lim[ib][wave][l32] = past ? 0 : visible_end(tok[i], n, kv, block);
       }
       tok[i] += t32;
@@ -1205,9 +1208,6 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
         for (int t = 0; t < KW; ++t) sc[t] = mm<F>(qf, kf[t][ks], sc[t]);
       }
     }
-    const int first_lim = visible_end(min(qb * 32, rows - 1) / g, n, kv, block);
-    const bool masked = (blk - wp.blk[s] + 1) * KEYS > first_lim ||
-                        qb * 32 + 32 > rows;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const f32x4 lv = *reinterpret_cast<const f32x4*>(lw + u * 8 + hh * 4);
@@ -1221,7 +1221,7 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                                     : fmaf(x, sc_.c, -lv[e]));
         }
     }
-    if (masked) {
+    if (masked(qb)) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const i32x4 end = *reinterpret_cast<const i32x4*>(
