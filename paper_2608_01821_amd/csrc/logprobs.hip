@@ -14,7 +14,8 @@
 // first batch: the smallest of them bounds the row's k-th value from below.  Two
 // sorted lists join by one compare against the reversed other and six exchange
 // steps: in LDS between the wavefronts, and in a second launch between the slices
-// of a row where there are several.
+// of a row where there are several.  Rows of up to 1024 logits have a kernel of their
+// own, below.
 //
 // Measured with 126,464 logits a row.  256 fp32 rows: 27 us without a list (4.7
 // TB/s of logits), 32 with the top 20; bf16 18 and 27 us (3.5 and 2.4 TB/s): bound
@@ -100,20 +101,42 @@ __device__ __forceinline__ void list_insert(uint64_t& list, uint64_t key) {
                                             false);
   list = lane < at ? list : lane == at ? key : up;
 }
-template <int O>
+// One step of a bitonic network: of each pair (l, l ^ O) the larger to the lower
+// lane, or, where lane & S, to the upper one.
+template <int O, int S>
 __device__ __forceinline__ uint64_t exchange(uint64_t v) {
   const uint64_t y = lane_xor<O>(v);
-  return ((threadIdx.x & O) == 0) == (v > y) ? v : y;
+  const bool larger = ((threadIdx.x & O) == 0) == ((threadIdx.x & S & 63) == 0);
+  return larger == (v > y) ? v : y;
+}
+// steps O, O / 2, .. 1
+template <int O, int S>
+__device__ __forceinline__ uint64_t exchanges(uint64_t v) {
+  v = exchange<O, S>(v);
+  if constexpr (O > 1) v = exchanges<O / 2, S>(v);
+  return v;
 }
 // the 64 largest of two descending lists, the second one given in reverse
 __device__ __forceinline__ uint64_t list_join(uint64_t list, uint64_t reversed) {
-  uint64_t v = list > reversed ? list : reversed;
-  v = exchange<32>(v);
-  v = exchange<16>(v);
-  v = exchange<8>(v);
-  v = exchange<4>(v);
-  v = exchange<2>(v);
-  return exchange<1>(v);
+  return exchanges<32, 64>(list > reversed ? list : reversed);
+}
+// 64 keys into ascending order (descending order of the complements)
+__device__ __forceinline__ uint64_t sort_up(uint64_t v) {
+  v = exchanges<1, 2>(~v);
+  v = exchanges<2, 4>(v);
+  v = exchanges<4, 8>(v);
+  v = exchanges<8, 16>(v);
+  v = exchanges<16, 32>(v);
+  return ~exchanges<32, 64>(v);
+}
+// lane l's value in lane 63 - l
+__device__ __forceinline__ uint64_t lane_reverse(uint64_t v) {
+  v = lane_xor<1>(v);
+  v = lane_xor<2>(v);
+  v = lane_xor<4>(v);
+  v = lane_xor<8>(v);
+  v = lane_xor<16>(v);
+  return lane_xor<32>(v);
 }
 // The lists of W wavefronts (entries past k do not count) into wavefront 0's, in
 // log2 W steps; called by all.
@@ -367,6 +390,52 @@ logprobs_kernel(const typename F::st* __restrict__ logits, int64_t ld, int vocab
   if (lane == 0) reinterpret_cast<Stat*>(pl + n_rows * slices * k)[at] = s;
 }
 
+// A row of at most 64 kWaves kShort logits, one workgroup: a lane holds up to kShort
+// of them, wavefront w the runs of 64 w, w + 8, ..; each run is sorted and joined to
+// the wavefront's list.  Batches of 8 KB would give such a row to one wavefront, and
+// a list of its inserts: 98 rows of 326, top 64, 28 us, 7.2 so; 4096 rows of 1000,
+// top 20, 74 and 44 us.  From about 2000 logits on the sorts are the slower ones (98
+// rows of 4096, top 20: 13.4 us, 8.0 by inserts).
+constexpr int kShort = 2;
+template <typename F>
+__global__ void __launch_bounds__(64 * kWaves)
+logprobs_short_kernel(const typename F::st* __restrict__ logits, int64_t ld,
+                      int vocab, int exclude, int k,
+                      const int32_t* __restrict__ targets, Out out) {
+  __shared__ uint64_t s_list[kWaves / 2][64];
+  __shared__ Stat s_stat[kWaves];
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const typename F::st* x = logits + (int64_t)row * ld;
+  float v[kShort];
+#pragma unroll
+  for (int i = 0; i < kShort; ++i) {
+    const int id = (i * kWaves + wave) * 64 + lane;
+    v[i] = id < vocab ? F::load(x[id]) : -INFINITY;
+    if (id == exclude) v[i] = -INFINITY;
+  }
+  Stat s = stat_none();
+#pragma unroll
+  for (int i = 0; i < kShort; ++i) s.m = fmaxf(s.m, v[i]);
+  const float ref = s.m == -INFINITY ? 0.f : s.m;
+  uint64_t list = 0;
+#pragma unroll
+  for (int i = 0; i < kShort; ++i) {
+    const int first = (i * kWaves + wave) * 64;
+    if (first >= vocab) break;
+    term(v[i], ref, s);
+    if (k == 0) continue;
+    const uint64_t run = sort_up(v[i] > -INFINITY ? top_key(v[i], first + lane) : 0);
+    list = i == 0 ? lane_reverse(run) : list_join(list, run);
+  }
+  s = stat_wave(s);
+  if (lane == 0) s_stat[wave] = s;
+  join_waves<kWaves>(list, k, wave, s_list);
+  if (wave != 0) return;
+  s = stat_wave(lane < kWaves ? s_stat[lane] : stat_none());
+  finish<F>(s, list, row, vocab, exclude, k, x, targets, out);
+}
+
 // Joins the slices of one row: four wavefronts take every fourth list each.
 template <typename F>
 __global__ void __launch_bounds__(256)
@@ -464,6 +533,13 @@ extern "C" int davet_token_logprobs(int32_t rows, int32_t vocab,
 #define LOGP(F)                                                                \
   do {                                                                         \
     const auto* x = static_cast<const F::st*>(logits);                         \
+    if (vocab <= 64 * kWaves * kShort) {                                       \
+      ProfScope ps(KC_MISC, stream);                                           \
+      hipLaunchKernelGGL(logprobs_short_kernel<F>, dim3(rows), dim3(64 * kWaves), 0, \
+                         stream, x, ld, vocab, exclude, top, targets, out);    \
+      DAVET_HIP(hipGetLastError());                                            \
+      break;                                                                   \
+    }                                                                          \
     {                                                                          \
       ProfScope ps(KC_MISC, stream);                                           \
       hipLaunchKernelGGL(logprobs_kernel<F>, dim3(rows * slices), dim3(64 * kWaves), 0, \

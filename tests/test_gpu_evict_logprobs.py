@@ -181,6 +181,29 @@ def test_logprobs_orders():
     _check_logprobs(q.half().cuda(), "f16", [1, 2, 3, 4], 33, exclude=0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [1, 2, 63, 65, 512, 513, 1000, 1024, 1025, 1100])
+def test_logprobs_short_rows(dtype, vocab):
+    """Rows that one workgroup holds whole, and the first that it does not: random,
+    equal, quantised, ascending, masked to one, to none; strided, any start."""
+    rng = np.random.default_rng(vocab)
+    big = values(rng, (7, vocab + 5), dtype, 3.0).cuda()
+    x = big[:, 3:3 + vocab]
+    x[1] = 0.25
+    x[2] = torch.from_numpy(rng.integers(0, 4, vocab).astype(np.float32)).to(x.dtype)
+    x[3] = torch.linspace(-6, 6, vocab).to(x.dtype)
+    x[4] = -np.inf
+    x[4, vocab // 2] = 1.0
+    x[5] = -np.inf
+    x[6, ::2] = torch.finfo(x.dtype).min
+    big[:, :3], big[:, 3 + vocab:] = 100.0, 100.0
+    last = vocab - 1
+    for top in (0, 1, 33, 64):
+        _check_logprobs(x, dtype, [last, 0, last // 2, 0, vocab // 2, 0, vocab], top)
+    _check_logprobs(x, dtype, [last, 0, last // 2, 0, vocab // 2, 0, -1], 20,
+                    exclude=vocab // 2)
+
+
 def test_logprobs_masked_rows():
     """-inf, the type's lowest value, rows with nothing, targets out of range."""
     rng = np.random.default_rng(2)
