@@ -519,10 +519,11 @@ def davet_run_schedule(cfg, weights: Weights, geoms, visual, view_bufs,
 def _rows(t, width, n_rows, size, name):
     """(address, row stride in elements) of a 2-D tensor of `size`-byte elements
     whose rows are dense and hold `width` of them."""
-    if t.dim() != 2 or t.element_size() != size:
+    shape = t.shape
+    if len(shape) != 2 or t.element_size() != size:
         raise ValueError("davet: %s must be 2-D with %d-byte elements"
                          % (name, size))
-    n, w = t.shape
+    n, w = shape
     if n < n_rows or w < width:
         raise ValueError("davet: %s must hold [%d, %d]" % (name, n_rows, width))
     ld, one = t.stride()
@@ -588,7 +589,7 @@ def _launch(dev, stream, fn, *args):
     global _torch
     if _torch is None:
         import torch as _torch
-    if dev != _torch.cuda.current_device():
+    if dev != _torch._C._cuda_getDevice():      # (a tensor is there: initialised)
         with _torch.cuda.device(dev):
             return _launch(dev, stream, fn, *args)
     if stream is None:
