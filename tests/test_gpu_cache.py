@@ -130,6 +130,11 @@ ATTEND = [  # dtype, new, kv, heads, kv_heads, dim, page, block
     ("f32", [129], [129], 2, 2, 64, 64, 0),
     ("f16", [200], [1400], 8, 8, 64, 128, 7),           # wide with pieces
     ("f16", [300, 257, 0, 1], [300, 700, 5, 64], 2, 2, 128, 64, 0),
+    # pieces of many rows, several a wavefront: heads in whole and broken groups
+    ("f16", [280, 21], [1300, 700], 28, 4, 64, 64, 0),
+    ("bf16", [1180], [1300], 7, 1, 64, 32, 5),
+    ("f16", [2740], [2760], 3, 1, 128, 64, 0),
+    ("f32", [520], [900], 16, 2, 64, 16, 1),
 ]
 
 
