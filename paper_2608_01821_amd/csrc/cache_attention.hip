@@ -1104,7 +1104,7 @@ cache_merge_rows_kernel(ChunkPack cp, const float* __restrict__ part, int part_r
 // 3092 keys: 14.4 us and 4 to add the partial sums, where 26 MB take 5: bound by the
 // chain of page, keys, rows and four tiles, gone through once with the whole chip's
 // workgroups at it (loading the keys ahead of the rows: 16.1 us).  Four prompts of up
-// to 3092 in full, 163 GFLOP: 270 us (0.6 PFLOP/s), bound by the vector ops and
+// to 3092 in full, 163 GFLOP: 256 us (0.64 PFLOP/s), bound by the vector ops and
 // waits of four waves at one tile of rows.
 struct WeightPlan {
   int32_t blk[DAVET_MAX_SEQS + 1];    // first block of keys of each sequence
@@ -1495,7 +1495,7 @@ int launch_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
              (((int64_t)(cp.row0[s + 1] - cp.row0[s]) * g + 31) / 32);
   // Workgroups: the chip twice over (1024), or with more work up to kWeightGroups of
   // at least 16 tiles of rows each (four prompts of up to 3092 in full, unequal:
-  // 390 us with 1024, 270 so).
+  // 390 us with 1024, 270 so, both before later steps).
   const int groups = (int)std::max<int64_t>(
       1024, std::min<int64_t>(kWeightGroups, steps / 16));
   const int want = std::max(1, groups / nblk);

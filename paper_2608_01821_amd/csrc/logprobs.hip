@@ -472,7 +472,8 @@ logprobs_join_kernel(const typename F::st* __restrict__ logits, int64_t ld,
   finish<F>(s, list, row, vocab, exclude, k, logits + (int64_t)row * ld, targets, out);
 }
 
-// Slices a row: 256 workgroups fill the chip, at least 8192 logits each.
+// Slices a row: 256 workgroups fill the chip, at least 8192 logits each (two rows of
+// 126,464 take 22 us in one slice each, 11.5 in 15; 256 rows 27 in one, 31 in two).
 int plan_slices(int rows, int vocab) {
   const int want = (256 + rows - 1) / rows;
   return std::max(1, std::min({want, kMaxSlices, vocab / 8192}));
