@@ -14,9 +14,9 @@
 // pages, in the same pools; 16 KB of one head's keys and of its values a
 // workgroup, 16 bytes a thread and load.  Bound by HBM.
 //
-// Measured: 2964 entries cut to half, 8.5 us to select (the latency of five passes
+// Measured: 2964 entries cut to half, 7.9 us to select (the latency of five passes
 // in one workgroup) and 10.9 to move them, 49 MB read and written (4.5 TB/s); eight
-// sequences of up to 32,700, 26.7 us and 157 for 750 MB (4.8 TB/s; a copy of that
+// sequences of up to 32,700, 26 us and 157 for 750 MB (4.8 TB/s; a copy of that
 // size reaches 5.1).
 
 #include <algorithm>
@@ -124,6 +124,21 @@ __device__ __forceinline__ uint32_t sum_before(const uint32_t (&c)[kSelWaves], i
   return s;
 }
 
+// sum over the lanes up to each: DPP row shifts by 1, 2, 4, 8 and the two row
+// broadcasts
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
+#define STEP(ctrl, rows) \
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false)
+  STEP(0x111, 0xf);
+  STEP(0x112, 0xf);
+  STEP(0x114, 0xf);
+  STEP(0x118, 0xf);
+  STEP(0x142, 0xa);
+  STEP(0x143, 0xc);
+#undef STEP
+  return x;
+}
+
 template <bool LDS>
 __global__ void __launch_bounds__(kSelThreads)
 evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
@@ -182,12 +197,7 @@ evict_select_kernel(SelectPack sp, const float* __restrict__ weights,
     // from the top: thread t holds bins 2047 - 2t and 2046 - 2t
     const int b1 = kBins - 1 - 2 * (int)threadIdx.x;
     const uint32_t c1 = hist[b1], c0 = hist[b1 - 1];
-    uint32_t sum = c1 + c0;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t y = __shfl_up(sum, o, 64);
-      if (lane >= o) sum += y;
-    }
+    const uint32_t sum = scan_lanes(c1 + c0);
     if (lane == 63) wsum[wave] = sum;
     __syncthreads();
     const uint32_t before = sum - c1 - c0 + sum_before(wsum, wave);
