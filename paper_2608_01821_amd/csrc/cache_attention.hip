@@ -267,8 +267,9 @@ struct AttnPlan {
 // so the tiles and pieces of a key head share one L2 and every XCD has the same
 // work.
 struct Place { int s, hk, piece, tile; };
+// The last tile comes first under a causal mask: it sees the most keys.
 __device__ __forceinline__ Place place(const AttnPlan& ap, const ChunkPack& cp,
-                                       int n_kv, int g, int rows) {
+                                       int n_kv, int g, int rows, bool causal) {
   const int b = ap.xcd ? (int)blockIdx.x >> 3 : (int)blockIdx.x;
   const int i = owner(ap.blk, cp.n_seqs, b);
   Place p;
@@ -282,6 +283,7 @@ __device__ __forceinline__ Place place(const AttnPlan& ap, const ChunkPack& cp,
   p.hk = ap.xcd ? ((int)blockIdx.x & 7) + 8 * h : h;
   p.piece = rem / nt;
   p.tile = rem - p.piece * nt;
+  if (causal) p.tile = nt - 1 - p.tile;
   return p;
 }
 
@@ -321,14 +323,18 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   __shared__ int s_bad;         // some value of a masked tile is not finite
 
   const int g = n_heads / cv.n_kv;
-  const Place pl = place(ap, cp, cv.n_kv, g, 32 * G);
+  const Place pl = place(ap, cp, cv.n_kv, g, 32 * G, block > 0);
   const int s = pl.s, hk = pl.hk;
   const int row0 = cp.row0[s], n = cp.row0[s + 1] - row0, kv = cp.kv[s];
   const int rows = n * g;
   const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wrow = pl.tile * 32 * G + (G == 4 ? wave * 32 : 0);
-  const bool live = wrow < rows;                  // of the wave
+  // keys up to the last one that any row of the wave sees (the rest of the tiles
+  // that the workgroup moves are nothing to it)
+  const int wave_end = wrow < rows
+                           ? visible_end(min(wrow + 31, rows - 1) / g, n, kv, block)
+                           : 0;
   // keys of this piece, up to the last one that any row of the tile sees
   const int tile_last = min(pl.tile * 32 * G + 32 * G, rows) - 1;
   const int end = min((pl.piece + 1) * ap.piece,
@@ -642,7 +648,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           sync_lds();
         }
-        if (live) compute(begin + it * KT, gbuf, holes);
+        if (begin + it * KT < wave_end) compute(begin + it * KT, gbuf, holes);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         sync_lds();
         if (it + 1 < nt) holes = load(it + 1);
@@ -667,7 +673,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         sync_lds();
-        if (live) {
+        if (begin < wave_end) {
           scores(gbuf, even);
           tmax = largest(even);
         }
@@ -689,7 +695,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           sync_lds();
         }
-        if (live) {
+        if (k0 < wave_end) {
           settle(k0, cur.holes, sc, tmax);
           // NK products S^T of the next tile (behind the last one: of what the
           // buffer holds, for nothing), then NV products O^T of this one, each
