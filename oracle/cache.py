@@ -89,6 +89,8 @@ def attention(cache, cu_q, kv_len, q, n_heads, scale=0.0, block=0):
                 row = cu_q[s] + i
                 x = scale * (k[:m] @ q[row, h])
                 top = x.max()
+                if top == -np.inf:              # zeros, lse -inf
+                    continue
                 e = np.exp(x - top)
                 p = e / e.sum()
                 r["out"][row, h] = p @ v[:m]

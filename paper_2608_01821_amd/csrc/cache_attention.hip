@@ -293,9 +293,13 @@ struct Scale {
 };
 
 // (x - m) scale log2(e) for fp32 operands, where the rounding of the constant
-// would show (-inf apart: times the constant's rest it might be +inf)
+// would show (-inf apart: times the constant's rest it might be +inf); the same
+// less l
 __device__ __forceinline__ float exact_arg(float d, const Scale& s) {
   return d == -INFINITY ? d : fmaf(d, s.c, d * s.c_lo);
+}
+__device__ __forceinline__ float exact_arg(float d, const Scale& s, float l) {
+  return d == -INFINITY ? d : fmaf(d, s.c, fmaf(d, s.c_lo, -l));
 }
 
 // G wavefronts share a tile (4: wide, 1: narrow); BUFS buffers a tile stream.
@@ -1286,7 +1290,7 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
         for (int e = 0; e < 4; ++e) {
           const float x = sc[t][u * 4 + e];
           sc[t][u * 4 + e] = __builtin_amdgcn_exp2f(
-              F::dtype == DAVET_F32 ? fmaf(x, sc_.c, fmaf(x, sc_.c_lo, -lv[e]))
+              F::dtype == DAVET_F32 ? exact_arg(x, sc_, lv[e])
                                     : fmaf(x, sc_.c, -lv[e]));
         }
     }
