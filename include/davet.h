@@ -570,8 +570,8 @@ typedef struct davet_kv_cache {
  *   p * theta^(-2i/head_dim), p = pos[row] (device int32 [rows]) or, with pos
  *   NULL, the row's cache index.  Angles are exact for every int32 position.
  * Queries go to q_out [rows, n_heads * head_dim], stride ld_q, which may be qkv
- * itself (same address and stride: the query columns in place) and must not
- * overlap it otherwise; keys to the cache; values are copied to it bit for bit.
+ * itself (same address and, with more than one row, stride: the query columns in
+ * place) and must not overlap it otherwise; keys to the cache; values are copied to it bit for bit.
  * Norm and rotation run in float32 and round once.  The chunk's cache slots must
  * be distinct (no page shared among the sequences that write it). */
 int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,

@@ -312,12 +312,13 @@ extern "C" int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
                   "davet_cache_append: q_gain and k_gain must be 16-byte aligned");
   if (total == 0) return DAVET_OK;
   const size_t es = dtype_size(cache->dtype);
-  DAVET_CHECK_ARG((q_out == qkv && ld_q == ld_qkv) ||
+  // (a single row has no stride)
+  DAVET_CHECK_ARG((q_out == qkv && (ld_q == ld_qkv || total == 1)) ||
                       !overlap(q_out, ((total - 1) * ld_q + n_heads * D) * es, qkv,
                                ((total - 1) * ld_qkv + width) * es),
                   DAVET_EINVAL,
                   "davet_cache_append: q_out overlaps qkv (in place needs the "
-                  "same address and row stride)");
+                  "same address and, of several rows, stride)");
   // threads for all heads of a row, or for equal passes over them; one row a
   // workgroup while there are few, then runs of rows
   const int units = (n_heads + 2 * cv.n_kv) * (D / 16);

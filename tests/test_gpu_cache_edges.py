@@ -63,3 +63,24 @@ def test_weights_of_scores_of_minus_infinity(dtype, dim, scale):
     assert np.all(np.abs(added - want - 0.5) <= rel * (want + 0.5))
     lse = t.attend(block=1, scale=scale)[1]
     assert np.isneginf(lse[0]).all() and np.isfinite(lse[1:]).all()
+
+
+# --------------------------------------------------------------- single rows --
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("spare", [0, 5])
+def test_append_of_one_row_in_place(dtype, spare):
+    """A tensor of exactly one row, its queries in place: what separate outputs
+    give, bit for bit; columns past the query heads stay."""
+    t = Setup(25, dtype, [1], [20], 4, 2, 64, 16)
+    qkv = torch.from_numpy(t.rng.standard_normal((1, 8 * 64 + spare))).to(
+        TORCH[dtype]).cuda()
+    got, want = qkv.clone(), torch.zeros(1, 4 * 64, dtype=TORCH[dtype], device="cuda")
+    k = []
+    for x, out in ((qkv, want), (got, got)):
+        cache = t.device()
+        dv.davet_cache_append(cache, t.cu, t.kv, x, 4, out, norm=True)
+        torch.cuda.synchronize()
+        k.append(t.dk)
+    assert torch.equal(got[:, :256], want) and torch.equal(got[:, 256:], qkv[:, 256:])
+    assert torch.equal(k[0], k[1])
