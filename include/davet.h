@@ -571,9 +571,10 @@ typedef struct davet_kv_cache {
  *   NULL, the row's cache index.  Angles are exact for every int32 position.
  * Queries go to q_out [rows, n_heads * head_dim], stride ld_q, which may be qkv
  * itself (same address and, with more than one row, stride: the query columns in
- * place) and must not overlap it otherwise; keys to the cache; values are copied to it bit for bit.
- * Norm and rotation run in float32 and round once.  The chunk's cache slots must
- * be distinct (no page shared among the sequences that write it). */
+ * place) and must not overlap it otherwise; keys to the cache; values are copied
+ * to it bit for bit.  Norm and rotation run in float32 and round once.  The
+ * chunk's cache slots must be distinct (no page shared among the sequences that
+ * write it). */
 int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
                        const int32_t* cu_q, const int32_t* kv_len,
                        const void* qkv, int64_t ld_qkv, int32_t n_heads,
@@ -597,7 +598,9 @@ int davet_cache_workspace_bytes(int32_t n_heads, int32_t head_dim,
  * chunk's own up to the end of the query's block, blocks of B counted from the
  * chunk's first token (B = 1: causal).  Holes hold no keys.  What is not visible
  * never contributes, whatever it holds (NaN and infinities included).  A row
- * that sees no key, or whose every score is -inf, gets zeros and lse -inf.
+ * that sees no key, or whose every score is -inf, gets zeros and lse -inf,
+ * whatever the values; in any other row a visible value that is not finite makes
+ * its element of out an infinity or NaN (it may not where its key scores -inf).
  *   scale: in [1e-30, 1e30], or 0 for 1 / sqrt(head_dim).
  *   q, out [rows, n_heads * head_dim] with strides, not overlapping; lse float32
  *   [rows, n_heads] or NULL.

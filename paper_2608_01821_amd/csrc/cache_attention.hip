@@ -325,6 +325,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   constexpr float BIAS = Frag<F>::kBias;
   __shared__ __attribute__((aligned(1024))) char smem[LDS];
   __shared__ int s_bad;         // some value of a masked tile is not finite
+  __shared__ uint32_t s_dead[G];          // rows without a score above -inf, a bit each
 
   const int g = n_heads / cv.n_kv;
   const Place pl = place(ap, cp, cv.n_kv, g, 32 * G, block > 0);
@@ -841,6 +842,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       wt[w] = use[w] ? __builtin_amdgcn_exp2f((mw - m) * sc_.c) : 0.f;
       if (use[w]) l += wt[w] * lw;
     }
+    const uint32_t dead = (uint32_t)__ballot(l == 0.f);
+    if (wave == 0 && lane_e == 0) s_dead[0] = dead;
     float acc[DP];
 #pragma unroll
     for (int i = 0; i < DP; ++i) {
@@ -882,19 +885,29 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
               l == 0.f ? -INFINITY : m * sc_.scale + (logf(l) - bias_ln);
       }
     }
-  } else if (wrow + l32e < rows) {
-    if (ap.pieces > 1) {
+  } else {
+    const uint32_t dead = (uint32_t)__ballot(l_run == 0.f);
+    if (lane_e == 0) s_dead[wave] = dead;
+    if (l_run == 0.f) {         // (their O may be 0 times an infinity)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+    }
+    if (wrow + l32e >= rows) {
+      // nothing to write
+    } else if (ap.pieces > 1) {
       const int64_t at = (int64_t)pl.piece * part_rows +
                          (int64_t)(row0 + qi) * n_heads + qh;
       float* po = part + at * D + hhe * 4;
       // (the join does not use the O of a piece that saw nothing)
       if (l_run != 0.f)
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
+        for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          *reinterpret_cast<f32x4*>(po + dt * 32 + u * 8) =
-              f32x4{o[dt][u * 4], o[dt][u * 4 + 1], o[dt][u * 4 + 2], o[dt][u * 4 + 3]};
+          for (int u = 0; u < 4; ++u)
+            *reinterpret_cast<f32x4*>(po + dt * 32 + u * 8) =
+                f32x4{o[dt][u * 4], o[dt][u * 4 + 1], o[dt][u * 4 + 2], o[dt][u * 4 + 3]};
       if (hhe == 0) {
         float* pm = part + (int64_t)ap.pieces * part_rows * D + at * 2;
         pm[0] = m_run;
@@ -924,8 +937,9 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     }
   }
 
-  // Values that `clean` took out, for the rows that see them: a positive weight
-  // times an infinity (or NaN) is that, whatever the weight.  One thread a dim;
+  // Values that `clean` took out, for the rows that see them and have a score: a
+  // positive weight times an infinity (or NaN) is that.  (The join may multiply a
+  // piece by a weight that underflowed: NaN for an infinity.)  One thread a dim;
   // speed does not matter here.
   __syncthreads();
   if (s_bad && wave * 64 + lane_e < D) {
@@ -946,6 +960,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         if (fabsf(x) < INFINITY) continue;
         for (int rr = pl.tile * 32 * G; rr <= tile_last; ++rr) {
           if (key >= visible_end(rr / g, n, kv, block)) continue;
+          const int own = rr - pl.tile * 32 * G;
+          if (s_dead[own >> 5] >> (own & 31) & 1) continue;
           const int tok = row0 + rr / g, hd = hk * g + rr % g;
           if (ap.pieces > 1) {
             part[((int64_t)pl.piece * part_rows + (int64_t)tok * n_heads + hd) * D + d] += x;

@@ -84,3 +84,25 @@ def test_append_of_one_row_in_place(dtype, spare):
         k.append(t.dk)
     assert torch.equal(got[:, :256], want) and torch.equal(got[:, 256:], qkv[:, 256:])
     assert torch.equal(k[0], k[1])
+
+
+# ---------------------------------------------------- values of no importance --
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("new,kv", [(3, 90), (3, 1300), (80, 200), (80, 1600)])
+def test_rows_of_minus_infinity_are_zeros(dtype, new, kv):
+    """A row whose every score is -inf gets zeros and lse -inf whatever the values
+    it sees hold: in tiles that all rows see, in the last ones, in pieces."""
+    t = Setup(27, dtype, [new], [kv], 2, 2, 64, 16)
+    t.q.view(new, 2, 64)[:, :, 9] = -1.0
+    put(t, "k", 0, range(kv - new + 2), 9, np.inf)   # all that rows 0 and 1 see
+    put(t, "v", 0, (2, kv - new, kv - new + 1), 5, np.inf)
+    put(t, "v", 0, (3, kv - new), 6, np.nan)
+    out, lse = t.attend(block=1)
+    assert np.isneginf(lse[:2]).all() and np.all(out[:2] == 0)
+    assert np.isfinite(lse[2:]).all()
+    rest = [d for d in range(64) if d not in (5, 6)]
+    ref = oc.attention(t.host, t.cu, t.kv, f64(t.q), 2, block=1)
+    ref["dot"] = np.full_like(ref["dot"], np.abs(f64(t.q)).max() * 5 * 64 ** 0.5)
+    ref = {k: x[2:] if x.ndim == 2 else x[2:][..., rest] for k, x in ref.items()}
+    check_attention((out[2:][..., rest], lse[2:]), ref, dtype, 64, kv)
