@@ -106,3 +106,125 @@ def test_rows_of_minus_infinity_are_zeros(dtype, new, kv):
     ref["dot"] = np.full_like(ref["dot"], np.abs(f64(t.q)).max() * 5 * 64 ** 0.5)
     ref = {k: x[2:] if x.ndim == 2 else x[2:][..., rest] for k, x in ref.items()}
     check_attention((out[2:][..., rest], lse[2:]), ref, dtype, 64, kv)
+
+
+# --------------------------------------------------- work over many workgroups --
+
+def launches(call):
+    """Kernels that a call launches."""
+    dv.prof_enable(64)
+    dv.prof_reset()
+    call()
+    n = sum(c for c, _ in dv.prof_read().values())
+    dv.prof_enable(0)
+    return n
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), -float("inf")])
+@pytest.mark.parametrize("new,kv,heads,hk", [
+    (9, 1400, 2, 2),            # few rows, joined a wavefront a row
+    (90, 1400, 2, 1),           # tiles of many
+    (1100, 1900, 8, 8)])        # joined many rows a wavefront
+def test_values_that_are_not_finite_in_pieces(dtype, bad, new, kv, heads, hk):
+    """Keys cut into pieces, a value of NaN or infinity late in a causal chunk and
+    one that every row sees: the first reaches the rows that see it and no other,
+    each its own dim only."""
+    t = Setup(29, dtype, [new], [kv], heads, hk, 64, 16)
+    cut = new - 3
+    ref = exact_attention(t, 1)
+    put(t, "v", 0, [kv - new + cut], 5, bad)
+    put(t, "v", 0, [7], 6, bad)
+    out = []
+    assert launches(lambda: out.append(t.attend(block=1))) == 2
+    out, lse = out[0]
+    assert not np.isfinite(out[cut:, :, 5]).any()
+    assert not np.isfinite(out[:, :, 6]).any()
+    late = [d for d in range(64) if d != 6]
+    both = [d for d in range(64) if d not in (5, 6)]
+    for rows, dims in ((slice(0, cut), late), (slice(cut, new), both)):
+        part = {k: x[rows] if x.ndim == 2 else x[rows][..., dims]
+                for k, x in ref.items()}
+        check_attention((out[rows][..., dims], lse[rows]), part, dtype, 64, kv)
+
+
+@pytest.mark.parametrize("dtype,new,kv,heads,hk,dim,page,block,n", [
+    # key heads a workgroup, chunks of them: 2 in 4
+    ("f16", [3], [17000], 16, 8, 128, 64, 0, 2),
+    ("f32", [40], [17000], 8, 8, 64, 32, 1, 2),
+    ("bf16", [5, 70], [20000, 20500], 8, 8, 64, 16, 1, 2),      # 3 in 3
+    ("f16", [6], [17000], 32, 32, 64, 128, 4, 2),               # 5 in 7
+    ("f16", [64], [40000], 32, 8, 64, 64, 1, 2),                # two tiles a wave
+    ("bf16", [1] * 4, [20000, 19000, 20011, 17], 8, 8, 128, 256, 0, 2),
+    ("f16", [1, 2, 1, 40], [20000, 19000, 20011, 20300], 8, 8, 64, 64, 1, 1),
+    ("f32", [2, 1, 1, 9], [20000, 19000, 20011, 20300], 2, 2, 128, 64, 0, 1),
+])
+def test_weights_of_many_keys(dtype, new, kv, heads, hk, dim, page, block, n):
+    """Workgroups that walk over several key heads, with partial sums (two
+    launches) and without (one); a hole, pages' ends without a token."""
+    t = Setup(33, dtype, new, kv, heads, hk, dim, page)
+    t.table[0, 1] = -1
+    want, lse, rel = exact_weights(t, block)
+    w = torch.full((len(kv), max(kv) + 1), 7.0, device="cuda")
+    args = (t.device(), t.cu, t.kv, t.q.cuda(), heads, torch.from_numpy(
+        lse).float().cuda(), w)
+    ws = t.workspace()
+    assert launches(lambda: dv.davet_cache_weights(
+        *args, block=block, workspace=ws)) == n
+    torch.cuda.synchronize()
+    for s, m in enumerate(kv):
+        got = f64(w[s, :m])
+        assert np.all(np.abs(got - want[s, :m]) <= rel * want[s, :m] + 1e-30)
+        assert torch.all(w[s, m:] == 7.0)
+    assert np.all(f64(w[0, page:2 * page]) == 0)
+
+
+def heads_of(t, block):
+    """For each sequence and head of a Setup: its number, rows, head, keys and
+    values [n, dim] on the GPU in float64, scores with -inf where not visible."""
+    _, hk, page, dim = t.k.shape
+    q = t.q.cuda().double().reshape(-1, t.heads, dim)
+    for s, m in enumerate(t.kv):
+        n = t.cu[s + 1] - t.cu[s]
+        ids = torch.from_numpy(t.table[s, :-(-m // page)].astype(np.int64))
+        k, v = (x[ids.clamp(min=0)].cuda().double().permute(1, 0, 2, 3).reshape(
+            hk, -1, dim)[:, :m] for x in (t.k, t.v))
+        i, j = torch.arange(n)[:, None], torch.arange(m)[None]
+        end = m if block == 0 else m - n + ((i // block + 1) * block).clamp(max=n)
+        seen = ((j < end) & (ids >= 0).repeat_interleave(page)[:m]).cuda()
+        rows = slice(t.cu[s], t.cu[s + 1])
+        for h in range(t.heads):
+            g = h * hk // t.heads
+            x = dim ** -0.5 * (q[rows, h] @ k[g].T.contiguous())
+            yield s, rows, h, q[rows, h], k[g], v[g], x.masked_fill(~seen, -np.inf)
+
+
+def exact_attention(t, block):
+    """As the oracle's, which goes one row at a time."""
+    dim, shape = t.k.shape[3], (t.cu[-1], t.heads)
+    r = dict(out=np.zeros(shape + (dim,)), mass=np.zeros(shape + (dim,)),
+             lse=np.zeros(shape), dot=np.zeros(shape))
+    for _, rows, h, q, k, v, x in heads_of(t, block):
+        z = x.logsumexp(1)
+        p = (x - z[:, None]).exp()
+        r["out"][rows, h], r["mass"][rows, h] = f64(p @ v), f64(p @ v.abs())
+        r["lse"][rows, h] = f64(z)
+        r["dot"][rows, h] = dim ** -0.5 * f64(
+            (q.abs() @ k.abs().T.contiguous()).amax(1))
+    return r
+
+
+def exact_weights(t, block):
+    """(weights, lse, relative tolerance)."""
+    dim = t.k.shape[3]
+    want, lse, most = np.zeros((len(t.kv), max(t.kv))), np.zeros((t.cu[-1], t.heads)), 0
+    for s, rows, h, q, k, _, x in heads_of(t, block):
+        z = x.logsumexp(1).float().double()
+        want[s, :t.kv[s]] += f64((x - z[:, None]).exp().sum(0))
+        lse[rows, h] = f64(z)
+        most = max(most, float(dim ** -0.5 * q.abs().amax() * k.abs().sum(1).amax()))
+    # each term: a score off by dim 2^-24 of its magnitudes, the argument's
+    # roundings, the exponential; then fp32 sums of rows x heads terms
+    rel = (dim + 8) * 2.0 ** -24 * (most + np.abs(lse).max() + 1) + \
+        (t.cu[-1] * t.heads + 8) * 2.0 ** -24
+    return want, lse, rel
