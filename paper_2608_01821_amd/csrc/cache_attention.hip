@@ -1139,14 +1139,13 @@ struct WeightPlan {
   int32_t chunks;
 };
 
-// KW: tiles of 32 keys a wave
+// KW: tiles of 32 keys a wave.  prev may be weights: neither is __restrict__.
 template <typename F, int D, int KW>
 __global__ void __launch_bounds__(256, 2)
 cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                      const typename F::st* __restrict__ q, int64_t ld_q,
                      const float* __restrict__ lse, int n_heads, int block,
-                     Scale sc_, const float* __restrict__ prev,
-                     float* __restrict__ weights, int64_t ld_w,
+                     Scale sc_, const float* prev, float* weights, int64_t ld_w,
                      float* __restrict__ part) {
   using st = typename F::st;
   using T = Tile<F, D>;
@@ -1349,8 +1348,7 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
 __global__ void __launch_bounds__(2 * kWeightKeys)
 cache_weights_join_kernel(ChunkPack cp, WeightPlan wp,
                           const float* __restrict__ part,
-                          const float* __restrict__ prev,
-                          float* __restrict__ weights, int64_t ld_w) {
+                          const float* prev, float* weights, int64_t ld_w) {
   const int nblk = wp.blk[cp.n_seqs], blk = blockIdx.x;
   const int s = owner(wp.blk, cp.n_seqs, blk);
   const int keys = blockDim.x, key = (blk - wp.blk[s]) * keys + threadIdx.x;

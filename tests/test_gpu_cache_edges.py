@@ -228,3 +228,21 @@ def exact_weights(t, block):
     rel = (dim + 8) * 2.0 ** -24 * (most + np.abs(lse).max() + 1) + \
         (t.cu[-1] * t.heads + 8) * 2.0 ** -24
     return want, lse, rel
+
+
+@pytest.mark.parametrize("kv,n", [([17000], 2), ([20000, 19000, 20011, 20300], 1)])
+def test_weights_add_up_in_place(kv, n):
+    """prev is weights itself, with partial sums and without: three layers."""
+    t = Setup(37, "f16", [2] * len(kv), kv, 8, 8, 64, 64)
+    want, lse, rel = exact_weights(t, 1)
+    w = torch.zeros(len(kv), max(kv), device="cuda")
+    args = (t.device(), t.cu, t.kv, t.q.cuda(), 8, torch.from_numpy(
+        lse).float().cuda(), w)
+    ws = t.workspace()
+    for turn in range(1, 4):
+        assert launches(lambda: dv.davet_cache_weights(
+            *args, prev=w, block=1, workspace=ws)) == n
+        torch.cuda.synchronize()
+        for s, m in enumerate(kv):
+            err = np.abs(f64(w[s, :m]) - turn * want[s, :m])
+            assert np.all(err <= turn * (rel + 2.0 ** -24) * want[s, :m] + 1e-30)
