@@ -671,7 +671,10 @@ int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
  * entropy 0.  A NaN or +inf logit makes the row's probabilities NaN; ids are
  * ranked all the same, NaN never listed.  logp (with targets), entropy may be
  * NULL.  workspace: davet_logprobs_workspace_bytes, 256-byte aligned (NULL / 0
- * where that is 0).
+ * where that is 0).  It says what exactly `rows` rows need, and fewer rows, each cut
+ * into more slices, may need MORE (256 need nothing): a workspace kept for every
+ * count of up to N rows holds (min(N, 255) + 255) * (8 * top + 12) bytes, which is
+ * enough for each of them and for any vocab.
  * Errors: EINVAL, ESHAPE (rows, vocab, ld, top), EDTYPE, ENOMEM. */
 int davet_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top,
                                    size_t* bytes /*host*/);

@@ -479,6 +479,8 @@ int plan_slices(int rows, int vocab) {
   return std::max(1, std::min({want, kMaxSlices, vocab / 8192}));
 }
 
+// Not monotonic in the rows: r rows of ceil(256 / r) slices each are at most r + 255
+// slices, and from 256 rows on there are none.
 size_t part_bytes(int rows, int vocab, int k) {
   const int sl = plan_slices(rows, vocab);
   if (sl == 1) return 0;
