@@ -512,17 +512,47 @@ def davet_run_schedule(cfg, weights: Weights, geoms, visual, view_bufs,
 
 
 # ---- paged cache and token log probabilities.  These take row-strided tensors
-# (last dimension dense) and check that each holds what the call reads or
-# writes; without `stream` they run on the current stream of their tensors'
-# device, whichever device is current.
+# (last dimension dense) and check that each is of the type that the call takes
+# and holds what it reads or writes; without `stream` they run on the current
+# stream of their tensors' device, whichever device is current.
 
-def _rows(t, width, n_rows, size, name):
-    """(address, row stride in elements) of a 2-D tensor of `size`-byte elements
-    whose rows are dense and hold `width` of them."""
+_torch = None
+_FLOAT = _INT = ()          # torch types of float32 and int32 arguments
+_KINDS = {}                 # of a davet_dtype's: 16 bits also as bit patterns
+
+
+def _load_torch():
+    global _torch, _FLOAT, _INT
+    import torch
+    _FLOAT, _INT = (torch.float32,), (torch.int32,)
+    bits = (torch.int16,) + ((torch.uint16,) if hasattr(torch, "uint16") else ())
+    _KINDS.update({DAVET_F32: _FLOAT, DAVET_BF16: (torch.bfloat16,) + bits,
+                   DAVET_F16: (torch.float16,) + bits})
+    _torch = torch
+
+
+def _kinds(dtype):
+    """The torch types that hold a davet_dtype."""
+    if _torch is None:
+        _load_torch()
+    if dtype not in _KINDS:
+        raise DavetError(-3, "dtype must be DAVET_F32, DAVET_BF16 or DAVET_F16")
+    return _KINDS[dtype]
+
+
+def _wrong_type(t, kinds, name):
+    return ValueError("davet: %s is of %s, not of %s"
+                      % (name, t.dtype, " or ".join(str(k) for k in kinds)))
+
+
+def _rows(t, width, n_rows, kinds, name):
+    """(address, row stride in elements) of a 2-D tensor of a type in `kinds` whose
+    rows are dense and hold `width` elements."""
+    if t.dtype not in kinds:
+        raise _wrong_type(t, kinds, name)
     shape = t.shape
-    if len(shape) != 2 or t.element_size() != size:
-        raise ValueError("davet: %s must be 2-D with %d-byte elements"
-                         % (name, size))
+    if len(shape) != 2:
+        raise ValueError("davet: %s must be 2-D" % name)
     n, w = shape
     if n < n_rows or w < width:
         raise ValueError("davet: %s must hold [%d, %d]" % (name, n_rows, width))
@@ -536,13 +566,15 @@ def _rows(t, width, n_rows, size, name):
     return t.data_ptr(), ld
 
 
-def _dense(t, n, name, size=4):
-    """Address of a dense tensor of at least `n` `size`-byte elements, or None."""
+def _dense(t, n, kinds, name):
+    """Address of a dense tensor of at least `n` elements of a type in `kinds`, or
+    None."""
     if t is None:
         return None
-    if t.numel() < n or t.element_size() != size or not t.is_contiguous():
-        raise ValueError("davet: %s must be dense, with %d elements of %d bytes"
-                         % (name, n, size))
+    if t.dtype not in kinds:
+        raise _wrong_type(t, kinds, name)
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError("davet: %s must be dense, with %d elements" % (name, n))
     return t.data_ptr()
 
 
@@ -580,15 +612,9 @@ def _gpu(first, *tensors):
     return dev
 
 
-_torch = None
-
-
 def _launch(dev, stream, fn, *args):
     """fn(*args, stream handle) with GPU `dev` current; without `stream`, on its
     current one."""
-    global _torch
-    if _torch is None:
-        import torch as _torch
     if dev != _torch._C._cuda_getDevice():      # (a tensor is there: initialised)
         with _torch.cuda.device(dev):
             return _launch(dev, stream, fn, *args)
@@ -608,16 +634,16 @@ class KvCache:
     int32 [n_seqs, max_pages], dense device tensors, which it keeps alive."""
 
     def __init__(self, k, v, page_table, dtype):
-        size = 4 if dtype == DAVET_F32 else 2
+        kinds = _kinds(dtype)
         if k.dim() != 4 or (v is not None and v.shape != k.shape) or \
                 page_table.dim() != 2:
             raise ValueError("davet: k and v must be [n_pages, n_kv_heads, "
                              "page_size, head_dim] alike, page_table [n_seqs, "
                              "max_pages]")
-        addr = (_dense(k, 0, "k", size), _dense(v, 0, "v", size),
-                _dense(page_table, 0, "page_table"))
+        addr = (_dense(k, 0, kinds, "k"), _dense(v, 0, kinds, "v"),
+                _dense(page_table, 0, _INT, "page_table"))
         self.k, self.v, self.page_table = k, v, page_table
-        self.n_seqs, self.head_dim, self.size = len(page_table), k.shape[3], size
+        self.n_seqs, self.head_dim, self.kinds = len(page_table), k.shape[3], kinds
         self.n_kv_heads, self.page_size = k.shape[1], k.shape[2]
         self.struct = KvCacheT(*addr, page_table.shape[1], k.shape[0], k.shape[2],
                                k.shape[1], k.shape[3], int(dtype))
@@ -638,11 +664,11 @@ def davet_cache_append(cache: KvCache, cu_q, kv_len, qkv, n_heads, q_out,
                        pos=None, norm=False, q_gain=None, k_gain=None, eps=1e-6,
                        theta=10000.0, stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
-    D, size = cache.head_dim, cache.size
-    x, ldx = _rows(qkv, (n_heads + 2 * cache.n_kv_heads) * D, rows, size, "qkv")
-    q, ldq = _rows(q_out, n_heads * D, rows, size, "q_out")
-    p = _dense(pos, rows, "pos")
-    gq, gk = _dense(q_gain, D, "q_gain"), _dense(k_gain, D, "k_gain")
+    D, kinds = cache.head_dim, cache.kinds
+    x, ldx = _rows(qkv, (n_heads + 2 * cache.n_kv_heads) * D, rows, kinds, "qkv")
+    q, ldq = _rows(q_out, n_heads * D, rows, kinds, "q_out")
+    p = _dense(pos, rows, _INT, "pos")
+    gq, gk = _dense(q_gain, D, _FLOAT, "q_gain"), _dense(k_gain, D, _FLOAT, "k_gain")
     _launch(cache._gpu(qkv, q_out, pos, q_gain, k_gain), stream,
             _L.davet_cache_append, cache._ref, n, cu, kv, x, ldx, n_heads, p,
             1 if norm else 0, gq, gk, eps, theta, q, ldq)
@@ -660,9 +686,9 @@ def davet_cache_attention(cache: KvCache, cu_q, kv_len, q, n_heads, out,
                           stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
     width = n_heads * cache.head_dim
-    x, ldx = _rows(q, width, rows, cache.size, "q")
-    o, ldo = _rows(out, width, rows, cache.size, "out")
-    e, (ws, nb) = _dense(lse, rows * n_heads, "lse"), _space(workspace)
+    x, ldx = _rows(q, width, rows, cache.kinds, "q")
+    o, ldo = _rows(out, width, rows, cache.kinds, "out")
+    e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
     _launch(cache._gpu(q, out, lse, workspace), stream, _L.davet_cache_attention,
             cache._ref, n, cu, kv, x, ldx, n_heads, scale, block, o, ldo, e, ws, nb)
 
@@ -672,14 +698,14 @@ def davet_cache_weights(cache: KvCache, cu_q, kv_len, q, n_heads, lse, weights,
                         stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
     most = max(kv)
-    x, ldx = _rows(q, n_heads * cache.head_dim, rows, cache.size, "q")
-    w, ldw = _rows(weights, most, n, 4, "weights")
+    x, ldx = _rows(q, n_heads * cache.head_dim, rows, cache.kinds, "q")
+    w, ldw = _rows(weights, most, n, _FLOAT, "weights")
     p = None
     if prev is not None:
-        p, ldp = _rows(prev, most, n, 4, "prev")
+        p, ldp = _rows(prev, most, n, _FLOAT, "prev")
         if ldp != ldw and n > 1:
             raise ValueError("davet: prev and weights need one row stride")
-    e, (ws, nb) = _dense(lse, rows * n_heads, "lse"), _space(workspace)
+    e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
     _launch(cache._gpu(q, lse, weights, prev, workspace), stream,
             _L.davet_cache_weights, cache._ref, n, cu, kv, x, ldx, n_heads, scale,
             block, e, p, w, ldw, ws, nb)
@@ -692,10 +718,12 @@ def davet_evict_select(n, keep, weights, kept, first=0, last=0,
     if seqs != len(keep) or seqs == 0:
         raise ValueError("davet: n and keep need one entry a sequence")
     most = max(keep)
-    w, ldw = _rows(weights, max(n), seqs, 4, "weights")
-    k, ldk = _rows(kept, most, seqs, 4, "kept")
+    if _torch is None:
+        _load_torch()
+    w, ldw = _rows(weights, max(n), seqs, _FLOAT, "weights")
+    k, ldk = _rows(kept, most, seqs, _INT, "kept")
     o, ldo = (None, 0) if weights_out is None else \
-        _rows(weights_out, most, seqs, 4, "weights_out")
+        _rows(weights_out, most, seqs, _FLOAT, "weights_out")
     _launch(_gpu(weights, kept, weights_out), stream, _L.davet_evict_select, seqs,
             _ints(n), _ints(keep), w, ldw, first, last, k, ldk, o, ldo)
 
@@ -705,8 +733,8 @@ def davet_cache_gather(cache: KvCache, kept, keep, dst_table, stream=None):
     n = len(keep)
     if n == 0 or n > cache.n_seqs or dst_table.dim() != 2 or len(dst_table) < n:
         raise ValueError("davet: the page tables need a row a sequence")
-    k, ldk = _rows(kept, max(keep), n, 4, "kept")
-    dst = _dense(dst_table, 0, "dst_table")
+    k, ldk = _rows(kept, max(keep), n, _INT, "kept")
+    dst = _dense(dst_table, 0, _INT, "dst_table")
     _launch(cache._gpu(kept, dst_table), stream, _L.davet_cache_gather, cache._ref,
             n, _ints(keep), k, ldk, dst, dst_table.shape[1])
 
@@ -724,17 +752,17 @@ def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
     """``logits`` [rows, vocab]; ``top_logp`` and ``top_ids`` [rows, top], dense
     (both or neither)."""
     rows, vocab = logits.shape
-    x, ld = _rows(logits, vocab, rows, 4 if dtype == DAVET_F32 else 2, "logits")
-    g, lp, en = _dense(targets, rows, "targets"), _dense(logp, rows, "logp"), \
-        _dense(entropy, rows, "entropy")
+    x, ld = _rows(logits, vocab, rows, _kinds(dtype), "logits")
+    g, lp = _dense(targets, rows, _INT, "targets"), _dense(logp, rows, _FLOAT, "logp")
+    en = _dense(entropy, rows, _FLOAT, "entropy")
     top, tl, ti = 0, None, None
     if top_ids is not None or top_logp is not None:
         if top_ids is None or top_logp is None or top_ids.dim() != 2 or \
                 top_ids.shape != top_logp.shape:
             raise ValueError("davet: top_logp and top_ids must be [rows, top]")
         top = top_ids.shape[1]
-        tl = _dense(top_logp, rows * top, "top_logp")
-        ti = _dense(top_ids, rows * top, "top_ids")
+        tl = _dense(top_logp, rows * top, _FLOAT, "top_logp")
+        ti = _dense(top_ids, rows * top, _INT, "top_ids")
     ws, nb = _space(workspace)
     _launch(_gpu(logits, targets, logp, entropy, top_logp, top_ids, workspace),
             stream, _L.davet_token_logprobs, rows, vocab, x, int(dtype), ld,

@@ -35,3 +35,71 @@ def test_fewer_rows_than_the_workspace_was_asked_for():
     need = dv.davet_logprobs_workspace_bytes(255, 126464, 5)
     assert f(255, need - 1) == ENOMEM
     assert "%d bytes" % need in dv.raw().davet_last_error().decode()
+
+
+# ------------------------------------------------------------- types of tensors --
+
+K16 = torch.zeros(4, 2, 16, 64, dtype=torch.float16)
+TABLE = torch.zeros(2, 3, dtype=torch.int32)
+Q16 = torch.zeros(3, 256, dtype=torch.float16)
+F = torch.zeros(3, 256)
+I = torch.zeros(3, 256, dtype=torch.int32)
+CHUNK = ([0, 3], [3])
+
+
+def _wrong_types():
+    c = dv.KvCache(K16, K16, TABLE, dv.DAVET_F16)
+    qkv = torch.zeros(3, 512, dtype=torch.float16)
+    b = torch.bfloat16
+
+    def append(x=qkv, q=Q16, **kw):
+        return lambda: dv.davet_cache_append(c, *CHUNK, x, 4, q, **kw)
+
+    def attend(q=Q16, out=Q16, **kw):
+        return lambda: dv.davet_cache_attention(c, *CHUNK, q, 4, out, **kw)
+
+    def weigh(q=Q16, lse=F, w=F, **kw):
+        return lambda: dv.davet_cache_weights(c, *CHUNK, q, 4, lse, w, **kw)
+
+    def select(w=F, kept=I, **kw):
+        return lambda: dv.davet_evict_select([5], [2], w, kept, **kw)
+
+    def score(x=F, dt=dv.DAVET_F32, **kw):
+        return lambda: dv.davet_token_logprobs(x, dt, **kw)
+    return [
+        lambda: dv.KvCache(K16.to(b), K16, TABLE, dv.DAVET_F16),
+        lambda: dv.KvCache(K16, K16.to(b), TABLE, dv.DAVET_F16),
+        lambda: dv.KvCache(K16, K16, TABLE, dv.DAVET_BF16),
+        lambda: dv.KvCache(K16, K16, TABLE.float(), dv.DAVET_F16),
+        append(qkv.to(b)), append(q=Q16.to(b)), append(pos=F), append(q_gain=I),
+        append(k_gain=I),
+        attend(Q16.to(b)), attend(out=Q16.to(b)), attend(lse=I),
+        weigh(Q16.to(b)), weigh(lse=I), weigh(w=I), weigh(prev=I),
+        select(I), select(kept=F), select(weights_out=I),
+        lambda: dv.davet_cache_gather(c, F, [2], TABLE),
+        lambda: dv.davet_cache_gather(c, I, [2], TABLE.float()),
+        score(I), score(Q16, dv.DAVET_BF16), score(targets=F, logp=F),
+        score(targets=I, logp=I), score(entropy=I),
+        score(top_logp=I, top_ids=I), score(top_logp=F, top_ids=F),
+    ]
+
+
+@pytest.mark.parametrize("i", range(28))
+def test_a_tensor_of_another_type_of_the_same_width_is_refused(i):
+    calls = _wrong_types()
+    assert len(calls) == 28
+    with pytest.raises(ValueError, match="is of torch"):
+        calls[i]()
+
+
+def test_sixteen_bits_may_come_as_bit_patterns():
+    """As elsewhere in the binding; these get as far as the check of the device."""
+    bits = K16.view(torch.int16)
+    for dt in (dv.DAVET_F16, dv.DAVET_BF16):
+        c = dv.KvCache(bits, bits, TABLE, dt)
+        with pytest.raises(ValueError, match="on a GPU"):
+            dv.davet_cache_attention(c, *CHUNK, Q16.view(torch.int16), 4,
+                                     Q16.view(torch.int16))
+    with pytest.raises(dv.DavetError) as e:
+        dv.KvCache(K16, K16, TABLE, 7)
+    assert e.value.status == EDTYPE
