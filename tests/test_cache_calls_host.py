@@ -103,3 +103,27 @@ def test_sixteen_bits_may_come_as_bit_patterns():
     with pytest.raises(dv.DavetError) as e:
         dv.KvCache(K16, K16, TABLE, 7)
     assert e.value.status == EDTYPE
+
+
+# ----------------------------------------------------------------- host lists --
+
+@pytest.mark.parametrize("bad", [2 ** 32 + 3, 2 ** 31, -2 ** 31 - 1, -2 ** 32 + 3,
+                                 3.0, None])
+@pytest.mark.parametrize("n", [1, 2, 64, 65, 100])
+def test_lengths_beyond_32_bits_are_refused(bad, n):
+    """Not taken modulo 2^32, whatever the list's length."""
+    with pytest.raises(ValueError, match="32-bit"):
+        dv._lib._ints([3] * (n - 1) + [bad])
+    if n <= 64:
+        table = TABLE[:1].expand(n, 3).contiguous()
+        c = dv.KvCache(K16, K16, table, dv.DAVET_F16)
+        with pytest.raises(ValueError, match="32-bit"):
+            dv.davet_cache_attention(c, [0] * n + [3], [3] * (n - 1) + [bad], Q16, 4,
+                                     Q16)
+
+
+def test_lists_reach_the_library_whole():
+    for vals in ([], [5], list(range(-3, 62)), list(range(100))):
+        got = dv._lib._ints(vals)
+        assert isinstance(got, C.Array) and list(got) == vals
+        assert dv._lib._ints(got) is got
