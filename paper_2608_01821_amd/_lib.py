@@ -519,11 +519,17 @@ def davet_run_schedule(cfg, weights: Weights, geoms, visual, view_bufs,
 _torch = None
 _FLOAT = _INT = ()          # torch types of float32 and int32 arguments
 _KINDS = {}                 # of a davet_dtype's: 16 bits also as bit patterns
+_device = _raw_stream = None    # the current device; a device's current stream
 
 
 def _load_torch():
-    global _torch, _FLOAT, _INT
+    global _torch, _FLOAT, _INT, _device, _raw_stream
     import torch
+    # torch's own short cuts where it has them: torch.cuda.current_stream() builds
+    # an object, 2 us
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                          lambda dev: torch.cuda.current_stream(dev).cuda_stream)
     _FLOAT, _INT = (torch.float32,), (torch.int32,)
     bits = (torch.int16,) + ((torch.uint16,) if hasattr(torch, "uint16") else ())
     _KINDS.update({DAVET_F32: _FLOAT, DAVET_BF16: (torch.bfloat16,) + bits,
@@ -620,12 +626,11 @@ def _gpu(first, *tensors):
 def _launch(dev, stream, fn, *args):
     """fn(*args, stream handle) with GPU `dev` current; without `stream`, on its
     current one."""
-    if dev != _torch._C._cuda_getDevice():      # (a tensor is there: initialised)
+    if dev != _device():                # (a tensor is there: initialised)
         with _torch.cuda.device(dev):
             return _launch(dev, stream, fn, *args)
     if stream is None:
-        # the handle alone: torch.cuda.current_stream() builds an object, 2 us
-        stream = _torch._C._cuda_getCurrentRawStream(dev)
+        stream = _raw_stream(dev)
     elif not isinstance(stream, int):
         stream = stream.cuda_stream
     status = fn(*args, stream)

@@ -127,3 +127,22 @@ def test_lists_reach_the_library_whole():
         got = dv._lib._ints(vals)
         assert isinstance(got, C.Array) and list(got) == vals
         assert dv._lib._ints(got) is got
+
+
+def test_streams_by_public_names(monkeypatch):
+    """A torch without the short cuts that the binding takes."""
+    class Stream:
+        cuda_stream = 77
+    monkeypatch.delattr(torch._C, "_cuda_getDevice", raising=False)
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: Stream())
+    try:
+        dv._lib._load_torch()
+        calls = []
+        for stream in (None, 5, Stream()):
+            dv._lib._launch(3, stream, lambda *a: calls.append(a) or 0, 1, 2)
+        assert calls == [(1, 2, 77), (1, 2, 5), (1, 2, 77)]
+    finally:
+        monkeypatch.undo()
+        dv._lib._load_torch()
