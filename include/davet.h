@@ -543,7 +543,8 @@ int davet_run_schedule(const davet_model_cfg* cfg, const davet_weights* w,
  * kv_len[s] - n + i.  A sequence may have no new tokens, and no tokens at all.
  * Lengths are taken when the call is made: a captured graph replays those of
  * its capture.  Tensor rows have strides (ld, in elements) and start at 16-byte
- * boundaries; query head h of [.., n_heads * head_dim] reads key head
+ * boundaries; tensors that must not overlap may be columns side by side of one
+ * buffer (one stride); query head h of [.., n_heads * head_dim] reads key head
  * h / (n_heads / n_kv_heads).  Rows past cu_q[n_seqs] are left as they are.
  * Errors of all: EINVAL (null, misaligned, bad scalar), ESHAPE (n_seqs, lengths,
  * strides, page or head counts; kv_len beyond max_pages * page_size), EDTYPE,

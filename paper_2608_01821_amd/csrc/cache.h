@@ -105,5 +105,16 @@ inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return an && bn && x < y + bn && y < x + an;
 }
+// whether n rows of aw elements from a, every lda, share one with n rows of bw from
+// b, every ldb: rows of one stride may lie side by side, others are taken as whole
+// ranges (widths at most the strides)
+inline bool rows_overlap(const void* a, int64_t lda, int64_t aw, const void* b,
+                         int64_t ldb, int64_t bw, int64_t n, size_t es) {
+  if (!overlap(a, ((n - 1) * lda + aw) * es, b, ((n - 1) * ldb + bw) * es)) return false;
+  if (n == 1 || lda != ldb) return true;
+  const uintptr_t row = lda * es;
+  const uintptr_t d = ((uintptr_t)b % row + row - (uintptr_t)a % row) % row;
+  return d < aw * es || d + bw * es > row;
+}
 
 }  // namespace davet

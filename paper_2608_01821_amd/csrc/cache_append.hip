@@ -314,8 +314,8 @@ extern "C" int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
   const size_t es = dtype_size(cache->dtype);
   // (a single row has no stride)
   DAVET_CHECK_ARG((q_out == qkv && (ld_q == ld_qkv || total == 1)) ||
-                      !overlap(q_out, ((total - 1) * ld_q + n_heads * D) * es, qkv,
-                               ((total - 1) * ld_qkv + width) * es),
+                      !rows_overlap(q_out, ld_q, (int64_t)n_heads * D, qkv, ld_qkv,
+                                    width, total, es),
                   DAVET_EINVAL,
                   "davet_cache_append: q_out overlaps qkv (in place needs the "
                   "same address and, of several rows, stride)");

@@ -1639,8 +1639,8 @@ extern "C" int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs
   rc = check_workspace(workspace, ws_bytes, total, n_heads, D, who);
   if (rc) return rc;
   const size_t es = dtype_size(cache->dtype);
-  DAVET_CHECK_ARG(!overlap(out, ((total - 1) * ld_out + n_heads * D) * es, q,
-                           ((total - 1) * ld_q + n_heads * D) * es),
+  DAVET_CHECK_ARG(!rows_overlap(out, ld_out, n_heads * D, q, ld_q, n_heads * D, total,
+                                es),
                   DAVET_EINVAL, "davet_cache_attention: out overlaps q");
   const Scale sc = make_scale(scale, D);
   float* part = static_cast<float*>(workspace);

@@ -344,8 +344,8 @@ extern "C" int davet_evict_select(int32_t n_seqs, const int32_t* n,
                   DAVET_ESHAPE, "davet_evict_select: row stride below a length");
   DAVET_CHECK_ARG(
       !weights_out ||
-          !overlap(weights_out, ((n_seqs - 1) * ld_weights_out + most_keep) * 4,
-                   weights, ((n_seqs - 1) * ld_weights + most_n) * 4),
+          !rows_overlap(weights_out, ld_weights_out, most_keep, weights, ld_weights,
+                        most_n, n_seqs, 4),
       DAVET_EINVAL, "davet_evict_select: weights_out overlaps weights");
   if (most_keep == 0) return DAVET_OK;
   ProfScope ps(KC_MISC, stream);

@@ -146,3 +146,28 @@ def test_streams_by_public_names(monkeypatch):
     finally:
         monkeypatch.undo()
         dv._lib._load_torch()
+
+
+# ------------------------------------------------------------- memory in common --
+
+def _attend(q, ldq, out, ldo, n=3):
+    cache = dv.KvCacheT(A, A << 4, A << 8, 8, 32, 16, 2, 64, dv.DAVET_F16)
+    f = dv.raw().davet_cache_attention
+    return f(C.byref(cache), 1, (C.c_int32 * 2)(0, n), (C.c_int32 * 1)(10), q, ldq, 4,
+             0.0, 0, out, ldo, None, A << 3, 1 << 30, None)
+
+
+def test_rows_that_share_memory_are_refused():
+    """Of 256 fp16 elements (512 bytes) each: columns that meet, rows that run into
+    the next ones, strides that differ."""
+    x = A << 1
+    for d in (0, 256, 496, 528 - 1024, -496, 1024, 1024 + 16, 1024 * 2 - 16, 528):
+        assert _attend(x, 512, x + d, 512) == EINVAL, d     # 1024-byte rows
+    assert _attend(x, 512, x + 512, 520) == EINVAL          # drift into each other
+    assert _attend(x, 256, x + 512, 256) == EINVAL          # one row on
+    assert _attend(x, 256, x + 256, 256, n=1) == EINVAL
+    # what stays of weights beside them, too wide by one
+    i = lambda *v: (C.c_int32 * len(v))(*v)
+    for d in (0, 9, 27, 30):
+        assert dv.raw().davet_evict_select(2, i(10, 8), i(4, 3), A, 30, 0, 0, A << 1,
+                                           8, A + 4 * d, 30, None) == EINVAL, d

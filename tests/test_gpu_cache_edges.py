@@ -246,3 +246,44 @@ def test_weights_add_up_in_place(kv, n):
         for s, m in enumerate(kv):
             err = np.abs(f64(w[s, :m]) - turn * want[s, :m])
             assert np.all(err <= turn * (rel + 2.0 ** -24) * want[s, :m] + 1e-30)
+
+
+# ----------------------------------------------------------- columns of a buffer --
+
+@pytest.mark.parametrize("new", [1, 5, 70])
+def test_columns_side_by_side_of_one_buffer(new):
+    """Queries and outputs, projected rows and queries, weights and what stays of
+    them: the results of buffers of their own, and no other column touched."""
+    t = Setup(39, "f16", [new, 2], [150, 40], 4, 2, 64, 16)
+    rows, w = new + 2, 4 * 64
+    want = t.attend(block=1)
+    for first, second in ((0, 1), (1, 0)):      # either may be the left one
+        buf = torch.full((rows, 2 * w + 8), 7.0, dtype=torch.float16, device="cuda")
+        q, out = (buf[:, i * w:i * w + w] for i in (first, second))
+        q.copy_(t.q.cuda())
+        dv.davet_cache_attention(t.device(), t.cu, t.kv, q, 4, out, block=1,
+                                 workspace=t.workspace())
+        torch.cuda.synchronize()
+        assert np.array_equal(f64(out).reshape(rows, 4, 64), want[0])
+        assert torch.equal(q, t.q.cuda()) and bool((buf[:, 2 * w:] == 7).all())
+    qkv = torch.from_numpy(t.rng.standard_normal((rows, 2 * w))).half().cuda()
+    own = torch.empty(rows, w, dtype=torch.float16, device="cuda")
+    dv.davet_cache_append(t.device(), t.cu, t.kv, qkv, 4, own)
+    k = t.dk
+    buf = torch.zeros(rows, 3 * w, dtype=torch.float16, device="cuda")
+    buf[:, w:] = qkv
+    dv.davet_cache_append(t.device(), t.cu, t.kv, buf[:, w:], 4, buf)
+    torch.cuda.synchronize()
+    assert torch.equal(buf[:, :w], own) and torch.equal(buf[:, w:], qkv)
+    assert torch.equal(t.dk, k)
+    x = torch.from_numpy(t.rng.random((2, 150 + 60))).float().cuda()
+    kept = torch.zeros(2, 60, dtype=torch.int32, device="cuda")
+    before = x.clone()
+    dv.davet_evict_select(t.kv, [60, 30], x, kept, weights_out=x[:, 150:])
+    torch.cuda.synchronize()
+    assert torch.equal(x[:, :150], before[:, :150])
+    for s, keep in enumerate((60, 30)):
+        idx = oc.select(t.kv[s], keep, f64(before[s]))
+        assert kept[s, :keep].tolist() == idx
+        assert torch.equal(x[s, 150:150 + keep], before[s, idx])
+        assert torch.equal(x[s, 150 + keep:], before[s, 150 + keep:])
