@@ -546,6 +546,7 @@ int davet_run_schedule(const davet_model_cfg* cfg, const davet_weights* w,
  * boundaries; tensors that must not overlap may be columns side by side of one
  * buffer (one stride); query head h of [.., n_heads * head_dim] reads key head
  * h / (n_heads / n_kv_heads).  Rows past cu_q[n_seqs] are left as they are.
+ * float32 and int32 arrays are aligned to their elements.
  * Errors of all: EINVAL (null, misaligned, bad scalar), ESHAPE (n_seqs, lengths,
  * strides, page or head counts; kv_len beyond max_pages * page_size), EDTYPE,
  * ENOMEM (workspace). */

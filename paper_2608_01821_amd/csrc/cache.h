@@ -2,6 +2,8 @@
 // kernels see it, the packed chunk of new tokens, and the host's checks.
 #pragma once
 
+#include <initializer_list>
+
 #include "common.h"
 
 namespace davet {
@@ -100,6 +102,12 @@ int check_rows(const void* p, int64_t ld, int64_t width, int dtype,
                const char* who, const char* what);
 // n_heads a multiple of the cache's heads, at most 1024
 int check_heads(const davet_kv_cache* c, int32_t n_heads, const char* who);
+// whether all start at 4-byte boundaries (NULL does)
+inline bool aligned4(std::initializer_list<const void*> ps) {
+  uintptr_t x = 0;
+  for (const void* p : ps) x |= (uintptr_t)p;
+  return (x & 3) == 0;
+}
 // whether [a, a + an) and [b, b + bn) bytes overlap
 inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;

@@ -1633,6 +1633,8 @@ extern "C" int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs
                   "davet_cache_attention: scale must be 0 or in [1e-30, 1e30]");
   DAVET_CHECK_ARG(block >= 0, DAVET_EINVAL,
                   "davet_cache_attention: block must not be negative");
+  DAVET_CHECK_ARG(aligned4({lse}), DAVET_EINVAL,
+                  "davet_cache_attention: lse must be 4-byte aligned");
   if (total == 0) return DAVET_OK;
   DAVET_CHECK_ARG(total * n_heads <= (1ll << 30), DAVET_ESHAPE,
                   "davet_cache_attention: too many query rows");
@@ -1673,6 +1675,8 @@ extern "C" int davet_cache_weights(const davet_kv_cache* cache, int32_t n_seqs,
   if (rc) return rc;
   DAVET_CHECK_ARG((lse || total == 0) && weights, DAVET_EINVAL,
                   "davet_cache_weights: null pointer");
+  DAVET_CHECK_ARG(aligned4({lse, prev, weights}), DAVET_EINVAL,
+                  "davet_cache_weights: lse, prev and weights must be 4-byte aligned");
   DAVET_CHECK_ARG(good_scale(scale) && block >= 0, DAVET_EINVAL,
                   "davet_cache_weights: scale must be 0 or in [1e-30, 1e30], "
                   "block not negative");

@@ -324,6 +324,9 @@ extern "C" int davet_evict_select(int32_t n_seqs, const int32_t* n,
                   "davet_evict_select: n_seqs out of range [1, 64]");
   DAVET_CHECK_ARG(n && keep && weights && kept, DAVET_EINVAL,
                   "davet_evict_select: null pointer");
+  DAVET_CHECK_ARG(aligned4({weights, kept, weights_out}), DAVET_EINVAL,
+                  "davet_evict_select: weights, kept and weights_out must be 4-byte "
+                  "aligned");
   DAVET_CHECK_ARG(first >= 0 && last >= 0, DAVET_EINVAL,
                   "davet_evict_select: first and last must not be negative");
   SelectPack sp{};
@@ -375,6 +378,8 @@ extern "C" int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
                   "davet_cache_gather: n_seqs out of range [1, 64]");
   DAVET_CHECK_ARG(keep && kept && dst_table, DAVET_EINVAL,
                   "davet_cache_gather: null pointer");
+  DAVET_CHECK_ARG(aligned4({kept, dst_table}), DAVET_EINVAL,
+                  "davet_cache_gather: kept and dst_table must be 4-byte aligned");
   GatherPack gp{};
   gp.n_seqs = n_seqs;
   const int rb = cache->head_dim * (int)dtype_size(cache->dtype);

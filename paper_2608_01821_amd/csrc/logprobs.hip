@@ -524,6 +524,8 @@ extern "C" int davet_token_logprobs(int32_t rows, int32_t vocab,
                   DAVET_EINVAL, "davet_token_logprobs: null pointer");
   DAVET_CHECK_ARG(((uintptr_t)logits & (dtype_size(dtype) - 1)) == 0, DAVET_EINVAL,
                   "davet_token_logprobs: logits misaligned for their type");
+  DAVET_CHECK_ARG(aligned4({targets, logp, entropy, top_logp, top_ids}), DAVET_EINVAL,
+                  "davet_token_logprobs: targets and outputs must be 4-byte aligned");
   const int slices = plan_slices(rows, vocab);
   const size_t need = part_bytes(rows, vocab, top);
   DAVET_CHECK_ARG(need == 0 || (workspace && ((uintptr_t)workspace & 255) == 0 &&

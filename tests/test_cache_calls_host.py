@@ -171,3 +171,36 @@ def test_rows_that_share_memory_are_refused():
     for d in (0, 9, 27, 30):
         assert dv.raw().davet_evict_select(2, i(10, 8), i(4, 3), A, 30, 0, 0, A << 1,
                                            8, A + 4 * d, 30, None) == EINVAL, d
+
+
+def test_arrays_are_aligned_to_their_elements():
+    """Every float32 and int32 argument, off by two bytes."""
+    L, cache = dv.raw(), dv.KvCacheT(A, A << 4, A << 8, 8, 32, 16, 2, 64, dv.DAVET_F16)
+    c, i = C.byref(cache), lambda *v: (C.c_int32 * len(v))(*v)
+    cu, kv = i(0, 3), i(10)
+
+    def attend(lse):
+        return L.davet_cache_attention(c, 1, cu, kv, A << 1, 256, 4, 0.0, 0, A << 2,
+                                       256, lse, A << 3, 1 << 30, None)
+
+    def weigh(lse=A, prev=A, w=A):
+        return L.davet_cache_weights(c, 1, cu, kv, A << 1, 256, 4, 0.0, 0, lse, prev,
+                                     w, 16, A << 3, 1 << 30, None)
+
+    def select(w=A, kept=A << 1, out=A << 2):
+        return L.davet_evict_select(1, i(10), i(4), w, 16, 0, 0, kept, 8, out, 8, None)
+
+    def gather(kept=A, dst=A):
+        return L.davet_cache_gather(c, 1, i(4), kept, 8, dst, 2, None)
+
+    def score(tgt=A, lp=A, en=A, tl=A, ti=A):
+        return L.davet_token_logprobs(2, 100, A, dv.DAVET_F16, 100, -1, tgt, lp, en, 2,
+                                      tl, ti, None, 0, None)
+    b = A + 2
+    for call in (lambda: attend(b), lambda: weigh(lse=b), lambda: weigh(prev=b),
+                 lambda: weigh(w=b), lambda: select(w=b), lambda: select(kept=b),
+                 lambda: select(out=b), lambda: gather(kept=b), lambda: gather(dst=b),
+                 lambda: score(tgt=b), lambda: score(lp=b), lambda: score(en=b),
+                 lambda: score(tl=b), lambda: score(ti=b)):
+        assert call() == EINVAL
+        assert "4-byte aligned" in L.davet_last_error().decode()
