@@ -622,8 +622,11 @@ int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs,
  * for j < kv_len[s], with q, scale and block as given to the
  * davet_cache_attention call that wrote lse (rows with lse -inf give nothing).
  * prev and weights: device float32 rows of stride ld_weights; prev may be NULL
- * (zeros) or weights itself, to accumulate over layers and steps.  Entries
- * past kv_len[s] are left as they are; keys in holes receive nothing. */
+ * (zeros) or weights itself, to accumulate over layers and steps.  Entries past
+ * kv_len[s] are left as they are; keys in holes receive nothing.
+ * A term carries the roundings of its score and of the float32 lse: about 2^-22 of
+ * their sizes, relative (0.5 % at 10^4, nothing to rely on beyond 10^6); where
+ * |lse| is above 65536 no term counts more than 1. */
 int davet_cache_weights(const davet_kv_cache* cache, int32_t n_seqs,
                         const int32_t* cu_q, const int32_t* kv_len,
                         const void* q, int64_t ld_q, int32_t n_heads,

@@ -56,6 +56,7 @@ constexpr int kMaxPieces = 64;
 constexpr int kMaxPartRows = 1 << 17;     // rows x pieces in the workspace
 constexpr int kWeightKeys = 128;          // keys a workgroup of the weights (or twice)
 constexpr int kWeightGroups = 4096;       // most workgroups that leave partial sums
+constexpr float kLargeLse = 65536.f;      // terms are off by 1 % and more
 constexpr int kAhead = 4;                 // fragments read ahead of the matrix ops
 
 // Fragments of 8 elements along the contracted axis and the op that takes them.
@@ -1270,6 +1271,7 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
     float* lw = ls[step % NBUF][wave];
     const float le = lw[lane];
     lw[lane] = le == -INFINITY ? INFINITY : le * kLog2e;
+    const bool large = __any(fabsf(le) > kLargeLse && le != -INFINITY);
     const char* Qb = qs[step % NBUF];
     f32x16 sc[KW];
 #pragma unroll
@@ -1308,6 +1310,14 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
               F::dtype == DAVET_F32 ? exact_arg(x, sc_, lv[e])
                                     : fmaf(x, sc_.c, -lv[e]));
         }
+    }
+    // no term is above 1 but for the roundings of its score and lse, which are past
+    // any bound once those are (a branch: as a minimum in every term 4 % slower)
+    if (large) {
+#pragma unroll
+      for (int t = 0; t < KW; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[t][e] = sc[t][e] > 1.f ? 1.f : sc[t][e];
     }
     if (masked(qb)) {
 #pragma unroll

@@ -287,3 +287,48 @@ def test_columns_side_by_side_of_one_buffer(new):
         assert kept[s, :keep].tolist() == idx
         assert torch.equal(x[s, 150:150 + keep], before[s, idx])
         assert torch.equal(x[s, 150 + keep:], before[s, 150 + keep:])
+
+
+# -------------------------------------------------------------- large scores --
+
+def one_hot(dtype):
+    """Keys of one dim each: the scores are the queries' elements, exactly."""
+    t = Setup(35, dtype, [3], [40], 2, 1, 64, 16)
+    for j in range(40):
+        p, o = oc.slot(t.host, 0, j)
+        t.k[p, 0, o] = 0
+        t.k[p, 0, o, j] = 1
+    return t
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-30, 1e-3, 30.0, 1e3, 1e4, 1e5])
+def test_weights_of_large_scores(dtype, scale):
+    """What the header says of scores of any size: a term is off by 2^-22 of the
+    sizes of its score and lse together.  (The argument is x c - lse c', c and c' =
+    log2(e) rounded to fp32, so are the second product and the result: 2 |x c| + 3
+    |lse c'| times 2^-24; then the exponential's 2^-23 and the sums of six.)"""
+    t = one_hot(dtype)
+    scale = float(np.float32(scale))
+    ref = oc.attention(t.host, t.cu, t.kv, f64(t.q), 2, scale=scale, block=1)
+    lse = f64(torch.from_numpy(ref["lse"]).float())
+    want = oc.weights(t.host, t.cu, t.kv, f64(t.q), 2, lse, scale=scale, block=1)
+    got = received(t, lse, 1, scale)
+    top = scale * np.abs(f64(t.q)).max()
+    rel = np.expm1(2.0 ** -22 * (top + np.abs(lse).max() + 4))
+    assert np.all(np.abs(got - want) <= rel * want + 6 * 1e-37)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("block", [0, 1])
+@pytest.mark.parametrize("scale", [1e7, 1e9, 1e18, 1e30])
+def test_no_term_of_huge_scores_is_above_one(dtype, block, scale):
+    """Their lse says less than its own rounding: a term may be anything in [0, 1],
+    and a key far below every row's largest score still receives nothing."""
+    t = one_hot(dtype)
+    lse = oc.attention(t.host, t.cu, t.kv, f64(t.q), 2, scale=scale, block=block)["lse"]
+    got = received(t, lse, block, scale)
+    assert np.all((got >= 0) & (got <= 6))
+    q = f64(t.q).reshape(6, 64)[:, :40]
+    low = (q < q.max(1, keepdims=True) - 0.1).all(0)        # 2^-22 of q is far less
+    assert low.sum() > 20 and np.all(got[0, low] == 0)
