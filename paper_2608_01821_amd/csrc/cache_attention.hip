@@ -294,13 +294,9 @@ struct Scale {
 };
 
 // (x - m) scale log2(e) for fp32 operands, where the rounding of the constant
-// would show (-inf apart: times the constant's rest it might be +inf); the same
-// less l
+// would show (-inf apart: times the constant's rest it might be +inf)
 __device__ __forceinline__ float exact_arg(float d, const Scale& s) {
   return d == -INFINITY ? d : fmaf(d, s.c, d * s.c_lo);
-}
-__device__ __forceinline__ float exact_arg(float d, const Scale& s, float l) {
-  return d == -INFINITY ? d : fmaf(d, s.c, fmaf(d, s.c_lo, -l));
 }
 
 // G wavefronts share a tile (4: wide, 1: narrow); BUFS buffers a tile stream.
@@ -1305,9 +1301,10 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
       for (int t = 0; t < KW; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+          // (fp32: c_lo > 0, so that a score of -inf gives 0)
           const float x = sc[t][u * 4 + e];
           sc[t][u * 4 + e] = __builtin_amdgcn_exp2f(
-              F::dtype == DAVET_F32 ? exact_arg(x, sc_, lv[e])
+              F::dtype == DAVET_F32 ? fmaf(x, sc_.c, fmaf(x, sc_.c_lo, -lv[e]))
                                     : fmaf(x, sc_.c, -lv[e]));
         }
     }
@@ -1381,6 +1378,17 @@ Scale make_scale(float scale, int D) {
   r.c = (float)c;
   r.c_lo = (float)(c - (double)r.c);
   r.scale = (float)s;
+  return r;
+}
+
+// The same with a positive second float: a score of -inf times both is -inf (plus an
+// infinity of the other sign it would be NaN).  For arguments that use both.
+Scale lower_scale(Scale r) {
+  if (r.c_lo <= 0.f) {
+    const float below = nextafterf(r.c, 0.f);
+    r.c_lo += r.c - below;
+    r.c = below;
+  }
   return r;
 }
 
@@ -1697,7 +1705,8 @@ extern "C" int davet_cache_weights(const davet_kv_cache* cache, int32_t n_seqs,
                   "davet_cache_weights: too many query rows");
   rc = check_workspace(workspace, ws_bytes, total, n_heads, D, who);
   if (rc) return rc;
-  const Scale sc = make_scale(scale, D);
+  Scale sc = make_scale(scale, D);
+  if (cache->dtype == DAVET_F32) sc = lower_scale(sc);
   float* part = static_cast<float*>(workspace);
 #define WGT(F, DIM) run_weights<F, DIM>(cv, cp, q, ld_q, lse, n_heads, block, sc, \
                                         prev, weights, ld_weights, part, stream)
