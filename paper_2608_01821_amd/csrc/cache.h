@@ -118,6 +118,7 @@ inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
 // ranges (widths at most the strides)
 inline bool rows_overlap(const void* a, int64_t lda, int64_t aw, const void* b,
                          int64_t ldb, int64_t bw, int64_t n, size_t es) {
+  if (n == 0 || aw == 0 || bw == 0) return false;
   if (!overlap(a, ((n - 1) * lda + aw) * es, b, ((n - 1) * ldb + bw) * es)) return false;
   if (n == 1 || lda != ldb) return true;
   const uintptr_t row = lda * es;

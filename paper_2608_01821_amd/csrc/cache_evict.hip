@@ -345,6 +345,9 @@ extern "C" int davet_evict_select(int32_t n_seqs, const int32_t* n,
   DAVET_CHECK_ARG(most_n <= ld_weights && most_keep <= ld_kept &&
                       (!weights_out || most_keep <= ld_weights_out),
                   DAVET_ESHAPE, "davet_evict_select: row stride below a length");
+  DAVET_CHECK_ARG(std::max({ld_weights, ld_kept, weights_out ? ld_weights_out : 0}) <
+                      (1ll << 40),
+                  DAVET_ESHAPE, "davet_evict_select: row stride of 2^40 or more");
   DAVET_CHECK_ARG(
       !weights_out ||
           !rows_overlap(weights_out, ld_weights_out, most_keep, weights, ld_weights,

@@ -204,3 +204,18 @@ def test_arrays_are_aligned_to_their_elements():
                  lambda: score(tl=b), lambda: score(ti=b)):
         assert call() == EINVAL
         assert "4-byte aligned" in L.davet_last_error().decode()
+
+
+def test_selection_of_nothing_and_strides_past_any_memory():
+    """Nothing kept shares no memory with the weights; a stride whose last row's
+    address would not fit 64 bits is refused before it is computed."""
+    i = lambda *v: (C.c_int32 * len(v))(*v)
+
+    def select(keep, ldw=16, ldk=8, ldo=16):
+        return dv.raw().davet_evict_select(2, i(10, 10), i(keep, keep), A, ldw, 0, 0,
+                                           A << 1, ldk, A, ldo, None)
+    assert select(0) == 0
+    assert select(4) == EINVAL
+    for kw in (dict(ldw=2 ** 62), dict(ldk=2 ** 62), dict(ldo=2 ** 62),
+               dict(ldw=2 ** 62, ldo=2 ** 62), dict(ldw=2 ** 40)):
+        assert select(4, **kw) == ESHAPE, kw
