@@ -570,7 +570,8 @@ typedef struct davet_kv_cache {
  *   ones); 0: not.
  *   Then the rotary embedding: elements (i, i + head_dim/2) turn by
  *   p * theta^(-2i/head_dim), p = pos[row] (device int32 [rows]) or, with pos
- *   NULL, the row's cache index.  Angles are exact for every int32 position.
+ *   NULL, the row's cache index.  Angles are reduced in float64: every int32
+ *   position is turned as exactly as a small one (theta >= 1).
  * Queries go to q_out [rows, n_heads * head_dim], stride ld_q, which may be qkv
  * itself (same address and, with more than one row, stride: the query columns in
  * place) and must not overlap it otherwise; keys to the cache; values are copied
@@ -606,9 +607,11 @@ int davet_cache_workspace_bytes(int32_t n_heads, int32_t head_dim,
  *   scale: in [1e-30, 1e30], or 0 for 1 / sqrt(head_dim).
  *   q, out [rows, n_heads * head_dim] with strides, not overlapping; lse float32
  *   [rows, n_heads] or NULL.
- * The 16-bit modes round probabilities to 16 bits before they meet the values
- * (with few rows, to twice 16); scores, sums and outputs are float32 until the
- * store.  Results do not depend on timing. */
+ * The 16-bit modes round probabilities to 16 bits before they meet the values, or
+ * to twice 16 where no chunk of the call has more than 32 rows a key head (queries
+ * times heads that share it; so a sequence's results may differ by that rounding with
+ * the chunks beside it).  Scores, sums and outputs are float32 until the store.  Results
+ * do not depend on timing. */
 int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs,
                           const int32_t* cu_q, const int32_t* kv_len,
                           const void* q, int64_t ld_q, int32_t n_heads,

@@ -32,10 +32,11 @@
 // eight histories of up to 32,700, 8 key heads, 16 bits, 748 MB, 135 us with the
 // join's 5 (5.5 TB/s); 16 sequences of 32 queries over up to 3773, 32 key heads, 638
 // MB, 121 us (5.3 TB/s).  wide, bound by the matrix ops and exponentials of two
-// waves a SIMD: four prompts of up to 3092 in full, 325 GFLOP, 370 us in fp16 (0.88
-// PFLOP/s; 0.77 when it runs for long and the clock falls; a large product reaches
-// 1.34).  fp32: 92 TFLOP/s (a large product 154).  A call of a few keys takes 11 us
-// in fp32, the latency of its chain.
+// waves a SIMD: four prompts of up to 3092 in full, 325 GFLOP, 363 to 402 us in fp16
+// (0.81 to 0.89 PFLOP/s with the clock, 0.77 when it runs for long; a large product
+// reaches 1.34).  fp32: 92 TFLOP/s (a large product 154).  A call of 192 keys takes
+// 12 us in fp32: the chain of its loads, and two tiles of 64 matrix ops in series a
+// wavefront.
 
 #include <math.h>
 
@@ -365,8 +366,8 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   // Scores are kept as differences from `ref`, near the row's largest: the matrix
-  // ops start from -ref, so the subtraction is free, and a difference keeps its
-  // bits however large the scores are.
+  // ops start from -ref, so the subtraction costs neither an op nor a rounding of
+  // its own (the sums' error still grows with the scores' size).
   float ref = 0.f, l_run = 0.f;
   bool seen = false;                // some score above -inf so far
   f32x16 start;
@@ -1127,8 +1128,9 @@ cache_merge_rows_kernel(ChunkPack cp, const float* __restrict__ part, int part_r
 // 3092 keys: 14.4 us and 4 to add the partial sums, where 26 MB take 5: bound by the
 // chain of page, keys, rows and four tiles, gone through once with the whole chip's
 // workgroups at it (loading the keys ahead of the rows: 16.1 us).  Four prompts of up
-// to 3092 in full, 163 GFLOP: 256 us (0.64 PFLOP/s), bound by the vector ops and
-// waits of four waves at one tile of rows.
+// to 3092 in full, 163 GFLOP: 231 to 256 us (0.64 to 0.71 PFLOP/s), bound by the
+// vector ops and waits of four waves at one tile of rows.  fp32, the 128 queries: 50
+// us (65 TFLOP/s).
 struct WeightPlan {
   int32_t blk[DAVET_MAX_SEQS + 1];    // first block of keys of each sequence
   int32_t heads;                      // key heads a chunk
@@ -1454,7 +1456,10 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   int most = 0;
   for (int s = 0; s < cp.n_seqs; ++s)
     most = std::max(most, cp.row0[s + 1] - cp.row0[s]);
-  // Rows from which the wide form is taken.  16 bits: sixteen sequences over up to
+  // Rows from which the wide form is taken, by the longest chunk of the batch (one
+  // launch): a short one beside it has its probabilities rounded once too.  Error of
+  // the output against 64 bits, its own rounding included: 2.1e-4 narrow, 2.8e-4 wide
+  // in fp16; 1.7e-3 and 2.2e-3 in bf16.  16 bits: sixteen sequences over up to
   // 3000 keys, 32 heads of 128, take 109 us with 48 rows where narrow takes 161, and
   // 100 both with 32, where narrow keeps more of the probabilities.  fp32 (one
   // buffer): four sequences, 8 heads, 58 us with 64 rows where narrow takes 43, and

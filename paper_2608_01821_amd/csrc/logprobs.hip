@@ -19,11 +19,12 @@
 //
 // Measured with 126,464 logits a row.  256 fp32 rows: 27 us without a list (4.7
 // TB/s of logits), 32 with the top 20; bf16 18 and 27 us (3.5 and 2.4 TB/s): bound
-// by HBM and, in 16 bits, by the eight instructions and one exponential a logit,
-// then by the inserts of the list (one value in about 100 cycles; sorting the
-// candidates of a wavefront at once instead took 64 kept ones from 19 to 17 us in
-// two rows, but 20 of 256 rows from 27 to 31).  Two rows, 15 slices each: 7.5 us
-// and 4 to join them, the latency of two launches; one slice a row takes 22.
+// by HBM and, in 16 bits, by the eight instructions and one exponential a logit; what
+// of the list's 9 us is finding candidates and what inserting them (about 100 cycles
+// each) is not measured.  (Sorting the candidates of a wavefront at once instead took
+// 64 kept ones from 19 to 17 us in two rows, but 20 of 256 rows from 27 to 31.)  Two
+// rows, 15 slices each: 7.5 us and 4 to join them, the latency of two launches; one
+// slice a row takes 22.
 
 #include <math.h>
 

@@ -32,6 +32,7 @@ def put(t, name, s, js, dim, value):
 
 # ------------------------------------------------------------ scores of -inf --
 
+@pytest.mark.filterwarnings("ignore:invalid value")      # (the oracle's 0 inf)
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("scale", [0.0, 0.2, 0.25])
@@ -88,6 +89,7 @@ def test_append_of_one_row_in_place(dtype, spare):
 
 # ---------------------------------------------------- values of no importance --
 
+@pytest.mark.filterwarnings("ignore:invalid value")      # (the oracle's 0 inf)
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("new,kv", [(3, 90), (3, 1300), (80, 200), (80, 1600)])
 def test_rows_of_minus_infinity_are_zeros(dtype, new, kv):
