@@ -612,6 +612,13 @@ def _ints(vals):
         raise ValueError("davet: host lists must hold 32-bit integers (%s)" % e)
 
 
+def _small(v, name):
+    """A host integer that fits int32 (ctypes would keep its low 32 bits)."""
+    if not -0x80000000 <= v <= 0x7fffffff:
+        raise ValueError("davet: %s must be a 32-bit integer" % name)
+    return v
+
+
 def _gpu(first, *tensors):
     """Index of the GPU that holds all tensors (None entries aside)."""
     dev = first.get_device()
@@ -674,7 +681,7 @@ def davet_cache_append(cache: KvCache, cu_q, kv_len, qkv, n_heads, q_out,
                        pos=None, norm=False, q_gain=None, k_gain=None, eps=1e-6,
                        theta=10000.0, stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
-    D, kinds = cache.head_dim, cache.kinds
+    n_heads, D, kinds = _small(n_heads, "n_heads"), cache.head_dim, cache.kinds
     x, ldx = _rows(qkv, (n_heads + 2 * cache.n_kv_heads) * D, rows, kinds, "qkv")
     q, ldq = _rows(q_out, n_heads * D, rows, kinds, "q_out")
     p = _dense(pos, rows, _INT, "pos")
@@ -686,8 +693,9 @@ def davet_cache_append(cache: KvCache, cu_q, kv_len, qkv, n_heads, q_out,
 
 def davet_cache_workspace_bytes(n_heads, head_dim, max_q):
     out = C.c_size_t(0)
-    _check(_L.davet_cache_workspace_bytes(int(n_heads), int(head_dim),
-                                          int(max_q), C.byref(out)))
+    _check(_L.davet_cache_workspace_bytes(
+        _small(int(n_heads), "n_heads"), _small(int(head_dim), "head_dim"),
+        _small(int(max_q), "max_q"), C.byref(out)))
     return out.value
 
 
@@ -695,6 +703,7 @@ def davet_cache_attention(cache: KvCache, cu_q, kv_len, q, n_heads, out,
                           lse=None, scale=0.0, block=0, workspace=None,
                           stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    n_heads, block = _small(n_heads, "n_heads"), _small(block, "block")
     width = n_heads * cache.head_dim
     x, ldx = _rows(q, width, rows, cache.kinds, "q")
     o, ldo = _rows(out, width, rows, cache.kinds, "out")
@@ -707,6 +716,7 @@ def davet_cache_weights(cache: KvCache, cu_q, kv_len, q, n_heads, lse, weights,
                         prev=None, scale=0.0, block=0, workspace=None,
                         stream=None):
     n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    n_heads, block = _small(n_heads, "n_heads"), _small(block, "block")
     most = max(kv)
     x, ldx = _rows(q, n_heads * cache.head_dim, rows, cache.kinds, "q")
     w, ldw = _rows(weights, most, n, _FLOAT, "weights")
@@ -734,6 +744,7 @@ def davet_evict_select(n, keep, weights, kept, first=0, last=0,
     k, ldk = _rows(kept, most, seqs, _INT, "kept")
     o, ldo = (None, 0) if weights_out is None else \
         _rows(weights_out, most, seqs, _FLOAT, "weights_out")
+    first, last = _small(first, "first"), _small(last, "last")
     _launch(_gpu(weights, kept, weights_out), stream, _L.davet_evict_select, seqs,
             _ints(n), _ints(keep), w, ldw, first, last, k, ldk, o, ldo)
 
@@ -751,8 +762,9 @@ def davet_cache_gather(cache: KvCache, kept, keep, dst_table, stream=None):
 
 def davet_logprobs_workspace_bytes(rows, vocab, top):
     out = C.c_size_t(0)
-    _check(_L.davet_logprobs_workspace_bytes(int(rows), int(vocab), int(top),
-                                             C.byref(out)))
+    _check(_L.davet_logprobs_workspace_bytes(
+        _small(int(rows), "rows"), _small(int(vocab), "vocab"),
+        _small(int(top), "top"), C.byref(out)))
     return out.value
 
 
@@ -773,7 +785,7 @@ def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
         top = top_ids.shape[1]
         tl = _dense(top_logp, rows * top, _FLOAT, "top_logp")
         ti = _dense(top_ids, rows * top, _INT, "top_ids")
-    ws, nb = _space(workspace)
+    exclude, (ws, nb) = _small(exclude, "exclude"), _space(workspace)
     _launch(_gpu(logits, targets, logp, entropy, top_logp, top_ids, workspace),
             stream, _L.davet_token_logprobs, rows, vocab, x, int(dtype), ld,
             exclude, g, lp, en, top, tl, ti, ws, nb)

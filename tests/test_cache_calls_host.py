@@ -219,3 +219,25 @@ def test_selection_of_nothing_and_strides_past_any_memory():
     for kw in (dict(ldw=2 ** 62), dict(ldk=2 ** 62), dict(ldo=2 ** 62),
                dict(ldw=2 ** 62, ldo=2 ** 62), dict(ldw=2 ** 40)):
         assert select(4, **kw) == ESHAPE, kw
+
+
+@pytest.mark.parametrize("bad", [2 ** 32, 2 ** 32 + 1, -2 ** 32, 2 ** 31])
+def test_integers_beyond_32_bits_are_refused(bad):
+    """exclude 2^32 is not token 0, block 2^32 not the bidirectional mask."""
+    c = dv.KvCache(K16, K16, TABLE, dv.DAVET_F16)
+    qkv = torch.zeros(3, 512, dtype=torch.float16)
+    for call in (
+            lambda: dv.davet_cache_append(c, *CHUNK, qkv, bad + 4, Q16),
+            lambda: dv.davet_cache_attention(c, *CHUNK, Q16, bad + 4, Q16),
+            lambda: dv.davet_cache_weights(c, *CHUNK, Q16, bad + 4, F, F),
+            lambda: dv.davet_cache_attention(c, *CHUNK, Q16, 4, Q16, block=bad),
+            lambda: dv.davet_cache_weights(c, *CHUNK, Q16, 4, F, F, block=bad),
+            lambda: dv.davet_evict_select([5], [2], F, I, first=bad),
+            lambda: dv.davet_evict_select([5], [2], F, I, last=bad),
+            lambda: dv.davet_token_logprobs(F, dv.DAVET_F32, exclude=bad),
+            lambda: dv.davet_cache_workspace_bytes(4, 64, bad),
+            lambda: dv.davet_cache_workspace_bytes(bad + 4, 64, 1),
+            lambda: dv.davet_logprobs_workspace_bytes(bad + 2, 50000, 5),
+            lambda: dv.davet_logprobs_workspace_bytes(2, bad + 50000, 5)):
+        with pytest.raises(ValueError, match="32-bit"):
+            call()
