@@ -21,6 +21,7 @@
  *                        and with davet_evict_select eviction by weight
  *   davet_token_logprobs log probabilities, entropy and top alternatives of
  *                        rows of logits
+ *   davet_rotary         rotary positions of any layout and scaling
  *
  * Conventions, for every entry point:
  *   - Pointers are DEVICE pointers unless the comment says host.  Arrays are
@@ -691,6 +692,57 @@ int davet_token_logprobs(int32_t rows, int32_t vocab, const void* logits,
                          const int32_t* targets, float* logp, float* entropy,
                          int32_t top, float* top_logp, int32_t* top_ids,
                          void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ----------------------------------------------------- rotary positions -- */
+
+/* davet_cache_append turns whole heads in halves by unscaled frequencies.  For
+ * models with another layout these calls turn queries and keys first; the append
+ * then gets pos all zero, which turns nothing (cos 0 = 1, sin 0 = 0, exactly). */
+typedef enum davet_rotary_layout {
+  DAVET_ROTARY_HALVES = 0,   /* pair i: elements i and i + dim / 2 */
+  DAVET_ROTARY_PAIRS = 1     /* pair i: elements 2 i and 2 i + 1   */
+} davet_rotary_layout;
+
+/* Frequencies f_i of pair i, from f = theta^(-2 i / dim): */
+typedef enum davet_rotary_scaling {
+  DAVET_ROTARY_PLAIN = 0,    /* f                                                */
+  DAVET_ROTARY_LINEAR = 1,   /* f / factor: positions interpolated               */
+  DAVET_ROTARY_BASE = 2,     /* theta times factor^(dim / (dim - 2)): the fastest
+                                pair as it was, the slowest one / factor         */
+  DAVET_ROTARY_RAMP = 3      /* w f + (1 - w) f / factor, w the turns that the pair
+                                makes in `trained` positions, from `slow` (0) to
+                                `fast` (1), clamped: fast pairs as they were, slow
+                                ones interpolated                                */
+} davet_rotary_scaling;
+
+/* turns[i] = f_i / (2 pi), the turns pair i makes a position (HOST, dim / 2 doubles;
+ * copy them to the device once).  factor, trained, fast and slow are read by the
+ * scalings that name them.  dim even in [2, 512]; theta >= 1, factor >= 1, trained
+ * > 0, fast > slow >= 0.  Errors: EINVAL, ESHAPE. */
+int davet_rotary_turns(int32_t dim, double theta, int32_t scaling, double factor,
+                       double trained, double fast, double slow,
+                       double* turns /*host*/);
+
+/* Turns the first `dim` elements of each head of x [rows, n_heads * head_dim] (row
+ * stride ld_x) to out (ld_out): pair (a, b) by t = 2 pi pos[row] turns[i],
+ *   a' = gain (a cos t - b sin t),  b' = gain (b cos t + a sin t),
+ * and copies the others.  inverse 1: by -t, which makes it the gradient of the call
+ * with inverse 0 (dx from dout, the same gain).
+ *   pos: device int32 [rows], any values, or NULL for the row numbers; turns: device
+ *   double [dim / 2].  Whole turns are taken off in float64, so that every int32
+ *   position is turned as exactly as a small one.
+ *   gain: finite (1; a scaled model's attention factor, once on queries and keys).
+ *   out may be x (same address and, of several rows, stride) and must not overlap
+ *   it otherwise.  Strides and addresses need no more than the elements' alignment;
+ *   16-byte ones are the fastest.
+ * Products run in float32 and round once.
+ * Errors: EINVAL, ESHAPE (rows up to 2^24, n_heads in [1, 4096], head_dim even in
+ * [2, 512], dim even in [2, head_dim], strides), EDTYPE. */
+int davet_rotary(int32_t rows, int32_t n_heads, int32_t head_dim, int32_t dim,
+                 int32_t layout, const void* x, int64_t ld_x, void* out,
+                 int64_t ld_out, int32_t dtype, const int32_t* pos,
+                 const double* turns, float gain, int32_t inverse,
+                 hipStream_t stream);
 
 /* ------------------------------------------------------------ profiling -- */
 

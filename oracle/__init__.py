@@ -22,6 +22,7 @@ Contents (each function cites the passage of the paper it follows):
   loop    -- the full schedule loop (Sec. 3.1 and Fig. 2's procedure)
   cache   -- a paged key/value cache: entry, attention, eviction; token log
              probabilities
+  rotary  -- rotary positions of any layout and scaling
 
 Precision: the denoiser runs in float64 on bf16-rounded (or fp32) inputs;
 the policy runs in IEEE double with the operation order printed in the
@@ -29,4 +30,4 @@ equations.  Readings of silent or ambiguous passages are listed in the
 design notes of the repository and restated where each is used.
 """
 
-from . import views, realizers, policy, model, decode, stats, loop, cache  # noqa: F401
+from . import views, realizers, policy, model, decode, stats, loop, cache, rotary  # noqa: F401

@@ -17,6 +17,8 @@ from ._lib import (  # noqa: F401
     davet_logprobs_workspace_bytes, davet_set_attention_split,
     davet_head_tiled_elems, davet_pack_head, davet_parse_operation,
     davet_policy_envelope, davet_policy_step, davet_policy_step_device,
+    DAVET_ROTARY_BASE, DAVET_ROTARY_HALVES, DAVET_ROTARY_LINEAR, DAVET_ROTARY_PAIRS,
+    DAVET_ROTARY_PLAIN, DAVET_ROTARY_RAMP, davet_rotary, davet_rotary_turns,
     davet_realizer_key_count,
     davet_realizer_keys, davet_realizer_maps, davet_run_schedule,
     davet_step_stats, davet_token_logprobs, davet_unmask, davet_version, davet_view_map_sizes,

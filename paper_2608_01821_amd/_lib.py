@@ -79,6 +79,12 @@ class KvCacheT(C.Structure):
 
 MAX_PAGE_SIZE = 256
 MAX_TOP = 64
+DAVET_ROTARY_HALVES = 0
+DAVET_ROTARY_PAIRS = 1
+DAVET_ROTARY_PLAIN = 0
+DAVET_ROTARY_LINEAR = 1
+DAVET_ROTARY_BASE = 2
+DAVET_ROTARY_RAMP = 3
 
 
 if not os.path.exists(LIB_PATH):
@@ -156,6 +162,11 @@ _SIGS = {
     "davet_cache_weights": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _P_i32,
                                       _vp, _i64, _i32, C.c_float, _i32, _vp,
                                       _vp, _vp, _i64, _vp, C.c_size_t, _vp]),
+    "davet_rotary_turns": (C.c_int, [_i32, C.c_double, _i32, C.c_double,
+                                     C.c_double, C.c_double, C.c_double,
+                                     _P_f64]),
+    "davet_rotary": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp,
+                               _i64, _i32, _vp, _vp, C.c_float, _i32, _vp]),
     "davet_evict_select": (C.c_int, [_i32, _P_i32, _P_i32, _vp, _i64, _i32,
                                      _i32, _vp, _i64, _vp, _i64, _vp]),
     "davet_cache_gather": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _vp,
@@ -517,20 +528,20 @@ def davet_run_schedule(cfg, weights: Weights, geoms, visual, view_bufs,
 # stream of their tensors' device, whichever device is current.
 
 _torch = None
-_FLOAT = _INT = ()          # torch types of float32 and int32 arguments
+_FLOAT = _INT = _DOUBLE = ()    # torch types of float32, int32, float64 arguments
 _KINDS = {}                 # of a davet_dtype's: 16 bits also as bit patterns
 _device = _raw_stream = None    # the current device; a device's current stream
 
 
 def _load_torch():
-    global _torch, _FLOAT, _INT, _device, _raw_stream
+    global _torch, _FLOAT, _INT, _DOUBLE, _device, _raw_stream
     import torch
     # torch's own short cuts where it has them: torch.cuda.current_stream() builds
     # an object, 2 us
     _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                           lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-    _FLOAT, _INT = (torch.float32,), (torch.int32,)
+    _FLOAT, _INT, _DOUBLE = (torch.float32,), (torch.int32,), (torch.float64,)
     bits = (torch.int16,) + ((torch.uint16,) if hasattr(torch, "uint16") else ())
     _KINDS.update({DAVET_F32: _FLOAT, DAVET_BF16: (torch.bfloat16,) + bits,
                    DAVET_F16: (torch.float16,) + bits})
@@ -789,6 +800,34 @@ def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
     _launch(_gpu(logits, targets, logp, entropy, top_logp, top_ids, workspace),
             stream, _L.davet_token_logprobs, rows, vocab, x, int(dtype), ld,
             exclude, g, lp, en, top, tl, ti, ws, nb)
+
+
+# ---- rotary positions
+
+def davet_rotary_turns(dim, theta, scaling=DAVET_ROTARY_PLAIN, factor=1.0,
+                       trained=0.0, fast=0.0, slow=0.0):
+    """The turns a position of each pair, a list of dim / 2 floats."""
+    dim, scaling = _small(int(dim), "dim"), _small(scaling, "scaling")
+    out = (C.c_double * max(1, min(dim, 512) // 2))()
+    _check(_L.davet_rotary_turns(dim, theta, scaling, factor, trained, fast, slow,
+                                 out))
+    return list(out)
+
+
+def davet_rotary(x, n_heads, head_dim, turns, out, dtype, pos=None,
+                 layout=DAVET_ROTARY_HALVES, gain=1.0, inverse=False, stream=None):
+    """``x`` and ``out`` [rows, n_heads * head_dim] or wider; ``turns`` a dense
+    float64 device tensor: twice its length is the part of a head that turns."""
+    kinds, rows = _kinds(dtype), len(x)
+    n_heads, head_dim = _small(n_heads, "n_heads"), _small(head_dim, "head_dim")
+    width = _small(n_heads * head_dim, "n_heads * head_dim")
+    a, lda = _rows(x, width, rows, kinds, "x")
+    o, ldo = _rows(out, width, rows, kinds, "out")
+    t, p = _dense(turns, 1, _DOUBLE, "turns"), _dense(pos, rows, _INT, "pos")
+    layout = _small(layout, "layout")
+    _launch(_gpu(x, out, turns, pos), stream, _L.davet_rotary, rows, n_heads,
+            head_dim, 2 * turns.numel(), layout, a, lda, o, ldo, int(dtype), p, t,
+            gain, 1 if inverse else 0)
 
 
 def prof_enable(max_launches):

@@ -1,0 +1,204 @@
+"""davet_rotary against the float64 oracle: types, layouts, parts of heads, odd
+sizes, strides and alignments, far positions, in place, backwards; its gradient; and
+a cache whose keys it turned."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_01821_amd as dv
+from cache_util import CODE, TORCH, f64, half_step, page_table, values
+from oracle import cache as oc
+from oracle import rotary as orot
+
+pytestmark = pytest.mark.gpu
+LAYOUT = {False: dv.DAVET_ROTARY_HALVES, True: dv.DAVET_ROTARY_PAIRS}
+
+
+def tolerance(x, ref, dim, pos, per, pairs, gain, dtype):
+    """Of an element of a turned pair (a, b): the argument's rounding (at most 2^-26
+    turns, and those of pos * turns in float64), the fp32 sine and cosine (2 units of
+    2^-24 each) times the gain, two products and a sum (3 more): relative to |gain|
+    (|a| + |b|); then the store."""
+    size = np.zeros_like(ref)
+    for i in range(dim // 2):
+        a, b = (2 * i, 2 * i + 1) if pairs else (i, i + dim // 2)
+        t = 2 * np.pi * (2.0 ** -26 + np.abs(np.asarray(pos, np.float64)) * per[i] *
+                         2.0 ** -51)
+        s = abs(gain) * (np.abs(x[:, :, a]) + np.abs(x[:, :, b]))
+        size[:, :, a] = size[:, :, b] = s * (t[:, None] + 6 * 2.0 ** -24)
+    u = half_step(dtype)
+    return u * np.abs(ref) + (1 + u) * size + (2.0 ** -25 if dtype == "f16" else 1e-37)
+
+
+CASES = [  # dtype, rows, heads, width, dim, pairs, inverse, beside, shift
+    ("f16", 1, 1, 2, 2, False, False, 0, 0),
+    ("f16", 1, 40, 128, 128, False, False, 1024, 0),
+    ("bf16", 3, 5, 64, 64, True, False, 0, 0),
+    ("f32", 7, 3, 80, 20, False, True, 16, 0),         # vectors of 2
+    ("f32", 5, 3, 96, 24, False, False, 0, 0),         # of 4
+    ("bf16", 9, 2, 96, 62, False, False, 0, 0),        # of 1
+    ("f16", 9, 2, 96, 62, True, True, 8, 0),           # the border inside a vector
+    ("f16", 4, 3, 66, 34, True, False, 0, 0),
+    ("bf16", 4, 3, 66, 34, False, True, 0, 0),
+    ("f32", 6, 2, 512, 512, False, False, 0, 0),
+    ("bf16", 6, 1, 512, 510, True, False, 3, 1),       # odd stride and address
+    ("f16", 33, 4, 128, 64, False, False, 5, 3),
+    ("f32", 33, 4, 64, 64, True, True, 2, 2),
+    ("f16", 3, 300, 64, 64, False, False, 0, 0),       # several passes a row
+    ("bf16", 2, 9, 256, 64, True, False, 0, 4),
+    ("f16", 1300, 9, 64, 64, True, False, 0, 0),       # runs of rows
+    ("f32", 2111, 2, 64, 32, False, False, 24, 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rotary(case, in_place):
+    dtype, rows, heads, width, dim, pairs, inverse, beside, shift = case
+    rng = np.random.default_rng(rows + 7 * dim)
+    cols = heads * width + beside
+    flat = values(rng, (shift + (rows + 2) * cols,), dtype)
+    store = flat.cuda()
+    x = store[shift:].view(rows + 2, cols)
+    host = f64(flat)[shift:].reshape(rows + 2, cols)[:rows, :heads * width]
+    host = host.reshape(rows, heads, width)
+    pos = rng.integers(-2 ** 31, 2 ** 31, rows)
+    pos[0] = 5
+    per = dv.davet_rotary_turns(dim, 1e4, dv.DAVET_ROTARY_RAMP, factor=4.0,
+                                trained=4096, fast=32, slow=1)
+    gain = 1.25
+    out = x if in_place else torch.full((rows + 2, heads * width + 3), 7.0,
+                                        dtype=TORCH[dtype], device="cuda")
+    before = out.clone()
+    dv.davet_rotary(x[:rows], heads, width,
+                    torch.tensor(per, dtype=torch.float64, device="cuda"), out[:rows],
+                    CODE[dtype], pos=torch.from_numpy(pos.astype(np.int32)).cuda(),
+                    layout=LAYOUT[pairs], gain=gain, inverse=inverse)
+    torch.cuda.synchronize()
+    ref = orot.rotate(host, dim, pos, per, pairs, gain, inverse)
+    got = f64(out)[:rows, :heads * width].reshape(ref.shape)
+    tol = tolerance(host, ref, dim, pos, per, pairs, gain, dtype)
+    assert np.all(np.abs(got - ref) <= tol), (np.abs(got - ref) / tol).max()
+    assert np.array_equal(got[:, :, dim:], host[:, :, dim:])      # bit for bit
+    assert torch.equal(out[rows:], before[rows:])
+    assert torch.equal(out[:, heads * width:], before[:, heads * width:])
+    if not in_place:
+        assert np.array_equal(f64(store), f64(flat))
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_row_numbers_without_positions(pairs):
+    rng = np.random.default_rng(3)
+    x = values(rng, (700, 2 * 64), "f32")
+    per = dv.davet_rotary_turns(64, 1e4)
+    dx, out = x.cuda(), torch.empty(700, 128, device="cuda")
+    turns = torch.tensor(per, dtype=torch.float64, device="cuda")
+    dv.davet_rotary(dx, 2, 64, turns, out, dv.DAVET_F32, layout=LAYOUT[pairs])
+    ref = orot.rotate(f64(x).reshape(700, 2, 64), 64, range(700), per, pairs)
+    tol = tolerance(f64(x).reshape(700, 2, 64), ref, 64, range(700), per, pairs, 1.0,
+                    "f32")
+    assert np.all(np.abs(f64(out).reshape(ref.shape) - ref) <= tol)
+    # a position of 0 changes nothing, whatever the others
+    dv.davet_rotary(dx, 2, 64, turns, out, dv.DAVET_F32, layout=LAYOUT[pairs],
+                    pos=torch.zeros(700, dtype=torch.int32, device="cuda"))
+    assert torch.equal(out, dx)
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_infinities_stay_in_their_pairs(pairs):
+    x = torch.ones(2, 3 * 64)
+    x[0, 64 + 5], x[1, 2 * 64 + 60] = float("nan"), float("inf")
+    per = torch.tensor(dv.davet_rotary_turns(32, 1e4), dtype=torch.float64).cuda()
+    out = torch.empty(2, 192, device="cuda")
+    dv.davet_rotary(x.cuda(), 3, 64, per, out, dv.DAVET_F32, layout=LAYOUT[pairs],
+                    pos=torch.tensor([3, 9], dtype=torch.int32).cuda())
+    bad = ~torch.isfinite(out.cpu())
+    where = [64 + 5, 64 + (4 if pairs else 21)]
+    assert bad[0].nonzero().flatten().tolist() == sorted(where)
+    assert bad[1].nonzero().flatten().tolist() == [2 * 64 + 60]   # not turned: itself
+    assert out[1, 2 * 64 + 60].item() == float("inf")
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dim", [128, 40])
+def test_gradient(pairs, dim):
+    """The call backwards against the formula's gradient and against differences of
+    the forward call (which is linear: any step will do)."""
+    rng = np.random.default_rng(dim)
+    rows, heads, width, gain = 37, 3, 128, 0.75
+    per = dv.davet_rotary_turns(dim, 1e4, dv.DAVET_ROTARY_LINEAR, factor=2.0)
+    turns = torch.tensor(per, dtype=torch.float64, device="cuda")
+    pos_h = rng.integers(0, 100000, rows)
+    pos = torch.from_numpy(pos_h.astype(np.int32)).cuda()
+    x, d, g = (values(rng, (rows, heads * width), "f32") for _ in range(3))
+
+    def turn(t, back=False):
+        out = torch.empty_like(t, device="cuda")
+        dv.davet_rotary(t.cuda(), heads, width, turns, out, dv.DAVET_F32, pos=pos,
+                        layout=LAYOUT[pairs], gain=gain, inverse=back)
+        return f64(out)
+    grad = turn(g, back=True)
+    shape = (rows, heads, width)
+    ref = orot.rotate(f64(g).reshape(shape), dim, pos_h, per, pairs, gain, True)
+    tol = tolerance(f64(g).reshape(shape), ref, dim, pos_h, per, pairs, gain, "f32")
+    assert np.all(np.abs(grad.reshape(shape) - ref) <= tol)
+    step = (turn(x + d) - turn(x - d)) / 2
+    n = rows * heads * width
+    # every element of both sides is off by at most 16 roundings of numbers up to 12
+    assert abs((step * f64(g)).sum() - (f64(d) * grad).sum()) <= \
+        n * 16 * 2.0 ** -24 * 12
+
+
+def test_keys_turned_before_the_cache():
+    """Queries and keys turned in place in the projected rows, in neighbouring pairs
+    of half a head, then appended with positions of 0, which turn nothing: the cache
+    holds what the turn gave, and the queries come out as it left them."""
+    rng = np.random.default_rng(11)
+    heads, hk, dim, page, kv = 4, 2, 64, 16, [40, 9]
+    cu = [0, 7, 16]
+    total, table = page_table(rng, kv, page)
+    k, v = (values(rng, (total, hk, page, dim), "f16") for _ in range(2))
+    qkv = values(rng, (16, (heads + 2 * hk) * dim), "f16").cuda()
+    plain = f64(qkv).reshape(16, -1, dim)
+    pos = torch.tensor([33 + i for i in range(7)] + list(range(9)), dtype=torch.int32)
+    per = dv.davet_rotary_turns(32, 1e4, dv.DAVET_ROTARY_BASE, factor=4.0)
+    dv.davet_rotary(qkv, heads + hk, dim,
+                    torch.tensor(per, dtype=torch.float64, device="cuda"), qkv,
+                    dv.DAVET_F16, pos=pos.cuda(), layout=dv.DAVET_ROTARY_PAIRS)
+    turned = f64(qkv)
+    dk, dvv = k.cuda(), v.cuda()
+    cache = dv.KvCache(dk, dvv, torch.from_numpy(table).cuda(), dv.DAVET_F16)
+    q = torch.empty(16, heads * dim, dtype=torch.float16, device="cuda")
+    dv.davet_cache_append(cache, cu, kv, qkv, heads, q,
+                          pos=torch.zeros(16, dtype=torch.int32, device="cuda"))
+    assert np.array_equal(f64(q), turned[:, :heads * dim])
+    _, rk, rv = oc.append(dict(k=f64(k), v=f64(v), table=table), cu, kv, turned, heads,
+                          pos=[0] * 16)
+    assert np.array_equal(f64(dk), rk) and np.array_equal(f64(dvv), rv)
+    ref = orot.rotate(plain[:, :heads + hk], 32, pos.tolist(), per, True)
+    tol = tolerance(plain[:, :heads + hk], ref, 32, pos.tolist(), per, True, 1.0, "f16")
+    assert np.all(np.abs(turned.reshape(plain.shape)[:, :heads + hk] - ref) <= tol)
+
+
+def test_on_another_stream_and_captured():
+    rng = np.random.default_rng(2)
+    x = values(rng, (64, 5 * 64), "bf16").cuda()
+    turns = torch.tensor(dv.davet_rotary_turns(64, 1e4), dtype=torch.float64).cuda()
+    want, out = torch.empty_like(x), torch.zeros_like(x)
+    dv.davet_rotary(x, 5, 64, turns, want, dv.DAVET_BF16)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    dv.davet_rotary(x, 5, 64, turns, out, dv.DAVET_BF16, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dv.davet_rotary(x, 5, 64, turns, out, dv.DAVET_BF16)
+    for i in range(3):
+        x.copy_(values(rng, (64, 5 * 64), "bf16"))
+        dv.davet_rotary(x, 5, 64, turns, want, dv.DAVET_BF16)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
