@@ -19,6 +19,8 @@
  *                        keys and values in a paged cache and computes only a
  *                        chunk of new tokens: entry into the cache, attention,
  *                        and with davet_evict_select eviction by weight
+ *   davet_tree_plan      positions and ancestors of a tree of drafted tokens, and
+ *                        with davet_cache_tree_attention its attention
  *   davet_token_logprobs log probabilities, entropy and top alternatives of
  *                        rows of logits
  *   davet_rotary         rotary positions of any layout and scaling
@@ -82,6 +84,7 @@ typedef enum davet_dtype { DAVET_F32 = 0, DAVET_BF16 = 1, DAVET_F16 = 2 } davet_
 #define DAVET_MAX_RESP 1024      /* response length L                     */
 #define DAVET_MAX_PAGE_SIZE 256  /* tokens of a cache page                */
 #define DAVET_MAX_TOP 64         /* alternatives of davet_token_logprobs  */
+#define DAVET_MAX_TREE 256       /* drafted tokens of a sequence          */
 
 /* Evidence realizers (Sec. 4.3: any construction with an ordered
  * evidence-cost hierarchy; pooling is the paper's default, pruning varies
@@ -665,6 +668,42 @@ int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
                        const int32_t* keep, const int32_t* kept,
                        int64_t ld_kept, const int32_t* dst_table,
                        int32_t dst_max_pages, hipStream_t stream);
+
+/* ------------------------------------------- a tree of drafted tokens -- */
+
+/* Positions and ancestors of drafted tokens that form trees, several continuations
+ * of one history checked in one pass.  Rows cu_q[s] .. cu_q[s+1] (HOST, at most
+ * DAVET_MAX_TREE of a sequence) are the drafted tokens, the last ones of the kv_len[s]
+ * (HOST) cached ones; parent (device int32 [rows]) the token that each continues,
+ * counted from its sequence's first drafted one, or a negative number: the last token
+ * before the draft.  A parent comes before its children: an entry that is not below
+ * the token's own number counts as negative.
+ *   pos: device int32 [rows], or NULL: first_pos[s] (HOST, NULL for kv_len[s] less the
+ *   drafted tokens) plus the number of drafted tokens above the row's; the `pos` of
+ *   davet_cache_append.
+ *   mask: device uint32 [rows, DAVET_MAX_TREE / 32], or NULL: bit j % 32 of word j / 32
+ *   set where drafted token j is the row's own or above it.
+ * kv_len may be NULL with first_pos.  Errors: EINVAL, ESHAPE. */
+int davet_tree_plan(int32_t n_seqs, const int32_t* cu_q, const int32_t* kv_len,
+                    const int32_t* first_pos, const int32_t* parent, int32_t* pos,
+                    uint32_t* mask, hipStream_t stream);
+
+/* davet_cache_attention (its formulas, arguments, workspace and numerics) where row i
+ * of a sequence sees every cached token before the chunk, and of the chunk's own those
+ * j whose bit in its row of `mask` (as davet_tree_plan's, but any bits will do) is
+ * set; bits past the sequence's chunk are not looked at.  At most DAVET_MAX_TREE new
+ * tokens a sequence.
+ * The accepted tokens of a tree are moved to the front with davet_cache_gather: a
+ * cache whose page tables start with the page of the first drafted token, `kept` what
+ * of that page was there before and then the accepted ones, into fresh pages. */
+int davet_cache_tree_attention(const davet_kv_cache* cache, int32_t n_seqs,
+                               const int32_t* cu_q, const int32_t* kv_len,
+                               const void* q, int64_t ld_q, int32_t n_heads,
+                               float scale, const uint32_t* mask, void* out,
+                               int64_t ld_out, float* lse, void* workspace,
+                               size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------ token log probabilities -- */
 
 /* Log probabilities, entropy and top alternatives of rows of logits (for
  * instance davet_denoise_step's logits_out), temperature 1, natural logarithm:

@@ -100,6 +100,45 @@ def attention(cache, cu_q, kv_len, q, n_heads, scale=0.0, block=0):
     return r
 
 
+def attention_of(cache, cu_q, kv_len, q, n_heads, seen, scale=0.0):
+    """attention() where seen(s, i, h) lists the cache indices that row i of
+    sequence s sees of key head h (those in holes hold no keys)."""
+    _, hk, _, D = cache["k"].shape
+    q = np.asarray(q, np.float64).reshape(len(q), n_heads, D)
+    scale = scale or 1.0 / np.sqrt(D)
+    rows = cu_q[-1]
+    r = dict(out=np.zeros((rows, n_heads, D)), mass=np.zeros((rows, n_heads, D)),
+             lse=np.full((rows, n_heads), -np.inf), dot=np.zeros((rows, n_heads)))
+    for s in range(len(kv_len)):
+        for row in range(cu_q[s], cu_q[s + 1]):
+            for g in range(hk):
+                js = [j for j in seen(s, row - cu_q[s], g) if slot(cache, s, j)]
+                if not js:
+                    continue
+                k = gathered(cache, "k", s, g, js)
+                v = gathered(cache, "v", s, g, js)
+                for h in range(g * (n_heads // hk), (g + 1) * (n_heads // hk)):
+                    x = scale * (k @ q[row, h])
+                    top = x.max()
+                    if top == -np.inf:
+                        continue
+                    e = np.exp(x - top)
+                    p = e / e.sum()
+                    r["out"][row, h] = p @ v
+                    r["mass"][row, h] = p @ np.abs(v)
+                    r["lse"][row, h] = top + np.log(e.sum())
+                    r["dot"][row, h] = scale * (np.abs(k) @ np.abs(q[row, h])).max()
+    return r
+
+
+def above(parent):
+    """For each drafted token of one tree, those above it and itself, ascending."""
+    out = []
+    for i, p in enumerate(parent):
+        out.append((out[p] if 0 <= p < i else []) + [i])
+    return out
+
+
 def weights(cache, cu_q, kv_len, q, n_heads, lse, scale=0.0, block=0):
     """[n_seqs, max kv]: what each cached key received."""
     _, hk, _, D = cache["k"].shape

@@ -79,6 +79,8 @@ class KvCacheT(C.Structure):
 
 MAX_PAGE_SIZE = 256
 MAX_TOP = 64
+MAX_TREE = 256
+TREE_WORDS = MAX_TREE // 32
 DAVET_ROTARY_HALVES = 0
 DAVET_ROTARY_PAIRS = 1
 DAVET_ROTARY_PLAIN = 0
@@ -162,6 +164,12 @@ _SIGS = {
     "davet_cache_weights": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _P_i32,
                                       _vp, _i64, _i32, C.c_float, _i32, _vp,
                                       _vp, _vp, _i64, _vp, C.c_size_t, _vp]),
+    "davet_tree_plan": (C.c_int, [_i32, _P_i32, _P_i32, _P_i32, _vp, _vp, _vp,
+                                  _vp]),
+    "davet_cache_tree_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                             _P_i32, _vp, _i64, _i32, C.c_float,
+                                             _vp, _vp, _i64, _vp, _vp,
+                                             C.c_size_t, _vp]),
     "davet_rotary_turns": (C.c_int, [_i32, C.c_double, _i32, C.c_double,
                                      C.c_double, C.c_double, C.c_double,
                                      _P_f64]),
@@ -529,12 +537,13 @@ def davet_run_schedule(cfg, weights: Weights, geoms, visual, view_bufs,
 
 _torch = None
 _FLOAT = _INT = _DOUBLE = ()    # torch types of float32, int32, float64 arguments
+_BITS = ()                  # and of 32-bit masks
 _KINDS = {}                 # of a davet_dtype's: 16 bits also as bit patterns
 _device = _raw_stream = None    # the current device; a device's current stream
 
 
 def _load_torch():
-    global _torch, _FLOAT, _INT, _DOUBLE, _device, _raw_stream
+    global _torch, _FLOAT, _INT, _DOUBLE, _BITS, _device, _raw_stream
     import torch
     # torch's own short cuts where it has them: torch.cuda.current_stream() builds
     # an object, 2 us
@@ -542,6 +551,7 @@ def _load_torch():
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                           lambda dev: torch.cuda.current_stream(dev).cuda_stream)
     _FLOAT, _INT, _DOUBLE = (torch.float32,), (torch.int32,), (torch.float64,)
+    _BITS = _INT + ((torch.uint32,) if hasattr(torch, "uint32") else ())
     bits = (torch.int16,) + ((torch.uint16,) if hasattr(torch, "uint16") else ())
     _KINDS.update({DAVET_F32: _FLOAT, DAVET_BF16: (torch.bfloat16,) + bits,
                    DAVET_F16: (torch.float16,) + bits})
@@ -800,6 +810,39 @@ def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
     _launch(_gpu(logits, targets, logp, entropy, top_logp, top_ids, workspace),
             stream, _L.davet_token_logprobs, rows, vocab, x, int(dtype), ld,
             exclude, g, lp, en, top, tl, ti, ws, nb)
+
+
+# ---- a tree of drafted tokens
+
+def davet_tree_plan(cu_q, kv_len, parent, pos=None, mask=None, first_pos=None,
+                    stream=None):
+    """``cu_q``, ``kv_len`` and ``first_pos``: host lists; ``parent`` and ``pos``
+    dense int32 [rows], ``mask`` dense int32 (or uint32) [rows, TREE_WORDS]."""
+    n = len(cu_q) - 1
+    if n < 1 or (kv_len is None and first_pos is None) or \
+            any(x is not None and len(x) != n for x in (kv_len, first_pos)):
+        raise ValueError("davet: cu_q needs an entry more than kv_len and first_pos")
+    if _torch is None:
+        _load_torch()
+    rows = max(0, cu_q[n])
+    up, p = _dense(parent, rows, _INT, "parent"), _dense(pos, rows, _INT, "pos")
+    m = _dense(mask, rows * TREE_WORDS, _BITS, "mask")
+    cu, kv, first = (None if v is None else _ints(v) for v in (cu_q, kv_len, first_pos))
+    _launch(_gpu(parent, pos, mask), stream, _L.davet_tree_plan, n, cu, kv, first, up,
+            p, m)
+
+
+def davet_cache_tree_attention(cache: KvCache, cu_q, kv_len, q, n_heads, mask, out,
+                               lse=None, scale=0.0, workspace=None, stream=None):
+    n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    n_heads, width = _small(n_heads, "n_heads"), n_heads * cache.head_dim
+    x, ldx = _rows(q, width, rows, cache.kinds, "q")
+    o, ldo = _rows(out, width, rows, cache.kinds, "out")
+    m = _dense(mask, rows * TREE_WORDS, _BITS, "mask")
+    e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
+    _launch(cache._gpu(q, mask, out, lse, workspace), stream,
+            _L.davet_cache_tree_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
+            scale, m, o, ldo, e, ws, nb)
 
 
 # ---- rotary positions
