@@ -21,6 +21,8 @@
  *                        and with davet_evict_select eviction by weight
  *   davet_tree_plan      positions and ancestors of a tree of drafted tokens, and
  *                        with davet_cache_tree_attention its attention
+ *   davet_cache_page_*   attention over the pages of a long cache that a cheap
+ *                        score selects for each new token
  *   davet_token_logprobs log probabilities, entropy and top alternatives of
  *                        rows of logits
  *   davet_rotary         rotary positions of any layout and scaling
@@ -702,6 +704,56 @@ int davet_cache_tree_attention(const davet_kv_cache* cache, int32_t n_seqs,
                                float scale, const uint32_t* mask, void* out,
                                int64_t ld_out, float* lse, void* workspace,
                                size_t ws_bytes, hipStream_t stream);
+
+/* --------------------------------------- attention over selected pages -- */
+
+/* For caches of which a new token reads only the pages that matter to it.  Bounds:
+ * of every page and key head the smallest and the largest value of each element of
+ * its keys, as device array [n_pages, n_kv_heads, 2, head_dim] of the cache's type,
+ * 16-byte aligned, which the caller keeps beside the pools (a page's bounds go with
+ * the page: sequences that share one share them).
+ *
+ * This call brings up to date the bounds of the pages that hold the chunk's tokens,
+ * over their tokens below kv_len: call it after davet_cache_append.  (A chunk of the
+ * whole sequence, cu_q = 0, kv_len, does every page, for instance after
+ * davet_cache_gather.)  Holes are left out, other pages' bounds as they are; a NaN
+ * among the keys makes its bounds NaN.  A page must not belong to two sequences that
+ * have new tokens in it.  cache->v may be NULL.  Errors: as for a chunk. */
+int davet_cache_page_bounds(const davet_kv_cache* cache, int32_t n_seqs,
+                            const int32_t* cu_q, const int32_t* kv_len, void* bounds,
+                            hipStream_t stream);
+
+/* Which pages each new token reads, for each key head: of the pages with keys that are
+ * visible to it (as in davet_cache_attention, `block` too; holes apart) all, if there
+ * are no more than `top`; else its first `first` and last `last` ones and then those
+ * ranked first by (score descending, page ascending), NaN with -inf,
+ *   score = sum_{heads of the key head} sum_e max(q_e lo_e, q_e hi_e),
+ * no less than the sum of their scores (without the scale) with any key of the page.
+ * The sum is taken in float64 and rounded to float32, so what is selected depends on no
+ * order of summation.
+ *   pages: device int32 [rows, n_kv_heads, top]: indices in the sequence's page table,
+ *   ascending, then -1.
+ * top in [1, 32768], first + last <= top; sequences with new tokens have at most 32768
+ * pages.  cache->k and v are not read.  Errors: as for a chunk. */
+int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_seqs,
+                            const int32_t* cu_q, const int32_t* kv_len, const void* q,
+                            int64_t ld_q, int32_t n_heads, int32_t block,
+                            const void* bounds, int32_t first, int32_t last,
+                            int32_t top, int32_t* pages, hipStream_t stream);
+
+/* davet_cache_attention (its formulas, arguments, workspace and numerics; probabilities
+ * are rounded to twice 16 bits) where each new token and key head sees, of the keys
+ * that are visible there, those in the pages of its list: pages [rows, n_kv_heads, top]
+ * as davet_cache_page_select writes it, or any other.  Entries outside the sequence's
+ * pages are no pages, wherever they stand; of more entries than the sequence has pages
+ * only as many are read; an order other than ascending changes no more than the sums'
+ * order, and a page that is listed twice counts twice.  top in [1, 2^26]. */
+int davet_cache_page_attention(const davet_kv_cache* cache, int32_t n_seqs,
+                               const int32_t* cu_q, const int32_t* kv_len,
+                               const void* q, int64_t ld_q, int32_t n_heads,
+                               float scale, int32_t block, const int32_t* pages,
+                               int32_t top, void* out, int64_t ld_out, float* lse,
+                               void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------ token log probabilities -- */
 

@@ -139,6 +139,53 @@ def above(parent):
     return out
 
 
+def page_bounds(cache, cu_q, kv_len, bounds):
+    """bounds [n_pages, n_kv_heads, 2, D] with those of the chunk's pages brought up
+    to date: the elementwise smallest and largest of the keys below kv_len."""
+    b = np.array(bounds, np.float64)
+    _, hk, size, _ = cache["k"].shape
+    for s, kv in enumerate(kv_len):
+        n = cu_q[s + 1] - cu_q[s]
+        for page in sorted({j // size for j in range(kv - n, kv)}):
+            js = [j for j in range(page * size, min(kv, page * size + size))]
+            if slot(cache, s, js[0]):
+                for h in range(hk):
+                    k = gathered(cache, "k", s, h, js)
+                    b[cache["table"][s, page], h] = k.min(0), k.max(0)
+    return b
+
+
+def page_select(cache, cu_q, kv_len, q, n_heads, bounds, top, first=0, last=0,
+                block=0):
+    """[rows][n_kv_heads] lists of the pages that each new token reads."""
+    n_pages, hk, size, D = cache["k"].shape
+    q = np.asarray(q, np.float64).reshape(len(q), hk, n_heads // hk, D)
+    out = []
+    for s, kv in enumerate(kv_len):
+        n = cu_q[s + 1] - cu_q[s]
+        for i in range(n):
+            end = kv if block == 0 else kv - n + min(n, (i // block + 1) * block)
+            count = -(-end // size)
+            there = [p for p in range(count) if 0 <= cache["table"][s, p] < n_pages]
+            row = []
+            for h in range(hk):
+                score = {}
+                for p in there:
+                    lo, hi = bounds[cache["table"][s, p], h].astype(np.float64)
+                    x = np.float32(np.maximum(q[cu_q[s] + i, h] * lo,
+                                              q[cu_q[s] + i, h] * hi).sum())
+                    score[p] = np.float32(-np.inf) if np.isnan(x) else x
+                if count <= top:
+                    row.append(there)
+                    continue
+                sure = [p for p in there if p < first or p >= count - last]
+                rest = sorted((p for p in there if p not in sure),
+                              key=lambda p: (-score[p], p))
+                row.append(sorted(sure + rest[:top - len(sure)]))
+            out.append(row)
+    return out
+
+
 def weights(cache, cu_q, kv_len, q, n_heads, lse, scale=0.0, block=0):
     """[n_seqs, max kv]: what each cached key received."""
     _, hk, _, D = cache["k"].shape

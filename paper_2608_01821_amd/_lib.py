@@ -170,6 +170,15 @@ _SIGS = {
                                              _P_i32, _vp, _i64, _i32, C.c_float,
                                              _vp, _vp, _i64, _vp, _vp,
                                              C.c_size_t, _vp]),
+    "davet_cache_page_bounds": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                          _P_i32, _vp, _vp]),
+    "davet_cache_page_select": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                          _P_i32, _vp, _i64, _i32, _i32, _vp,
+                                          _i32, _i32, _i32, _vp, _vp]),
+    "davet_cache_page_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                             _P_i32, _vp, _i64, _i32, C.c_float,
+                                             _i32, _vp, _i32, _vp, _i64, _vp,
+                                             _vp, C.c_size_t, _vp]),
     "davet_rotary_turns": (C.c_int, [_i32, C.c_double, _i32, C.c_double,
                                      C.c_double, C.c_double, C.c_double,
                                      _P_f64]),
@@ -843,6 +852,58 @@ def davet_cache_tree_attention(cache: KvCache, cu_q, kv_len, q, n_heads, mask, o
     _launch(cache._gpu(q, mask, out, lse, workspace), stream,
             _L.davet_cache_tree_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
             scale, m, o, ldo, e, ws, nb)
+
+
+# ---- attention over selected pages
+
+def _page_bounds(cache, bounds):
+    """Address of a cache's bounds [n_pages, n_kv_heads, 2, head_dim]."""
+    s = cache.struct
+    return _dense(bounds, s.n_pages * s.n_kv_heads * 2 * s.head_dim, cache.kinds,
+                  "bounds")
+
+
+def _page_list(cache, pages, rows):
+    """(address, top) of pages [rows, n_kv_heads, top]."""
+    shape = pages.shape
+    if len(shape) != 3 or shape[0] < rows or shape[1] != cache.n_kv_heads:
+        raise ValueError("davet: pages must be [rows, n_kv_heads, top]")
+    return _dense(pages, 0, _INT, "pages"), shape[2]
+
+
+def davet_cache_page_bounds(cache: KvCache, cu_q, kv_len, bounds, stream=None):
+    """``bounds``: dense [n_pages, n_kv_heads, 2, head_dim] of the cache's type."""
+    n, cu, kv, _ = cache._chunk(cu_q, kv_len)
+    b = _page_bounds(cache, bounds)
+    _launch(cache._gpu(bounds), stream, _L.davet_cache_page_bounds, cache._ref, n, cu,
+            kv, b)
+
+
+def davet_cache_page_select(cache: KvCache, cu_q, kv_len, q, n_heads, bounds, pages,
+                            first=0, last=0, block=0, stream=None):
+    """``pages``: dense int32 [rows, n_kv_heads, top]."""
+    n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    n_heads, block = _small(n_heads, "n_heads"), _small(block, "block")
+    first, last = _small(first, "first"), _small(last, "last")
+    x, ldx = _rows(q, n_heads * cache.head_dim, rows, cache.kinds, "q")
+    b, (p, top) = _page_bounds(cache, bounds), _page_list(cache, pages, rows)
+    _launch(cache._gpu(q, bounds, pages), stream, _L.davet_cache_page_select,
+            cache._ref, n, cu, kv, x, ldx, n_heads, block, b, first, last, top, p)
+
+
+def davet_cache_page_attention(cache: KvCache, cu_q, kv_len, q, n_heads, pages, out,
+                               lse=None, scale=0.0, block=0, workspace=None,
+                               stream=None):
+    n, cu, kv, rows = cache._chunk(cu_q, kv_len)
+    n_heads, block = _small(n_heads, "n_heads"), _small(block, "block")
+    width = n_heads * cache.head_dim
+    x, ldx = _rows(q, width, rows, cache.kinds, "q")
+    o, ldo = _rows(out, width, rows, cache.kinds, "out")
+    p, top = _page_list(cache, pages, rows)
+    e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
+    _launch(cache._gpu(q, pages, out, lse, workspace), stream,
+            _L.davet_cache_page_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
+            scale, block, p, top, o, ldo, e, ws, nb)
 
 
 # ---- rotary positions

@@ -36,7 +36,7 @@ POLICY_FLAGS = [
 HIP_SOURCES = ["views.hip", "realizers.hip", "unmask.hip", "rowops.hip", "gemm16.hip",
                "gemm_f32.hip", "attention.hip", "step.hip", "policy_dev.hip",
                "cache_append.hip", "cache_attention.hip", "cache_evict.hip",
-               "cache_tree.hip",
+               "cache_tree.hip", "cache_pages.hip",
                "logprobs.hip", "rotary.hip",
                "runtime.cpp",
                "schedule.cpp"]
