@@ -25,6 +25,8 @@
  *                        score selects for each new token
  *   davet_token_logprobs log probabilities, entropy and top alternatives of
  *                        rows of logits
+ *   davet_beam_select    the best continuations over beams and vocabulary, and with
+ *                        davet_cache_reorder the cache that goes with them
  *   davet_rotary         rotary positions of any layout and scaling
  *
  * Conventions, for every entry point:
@@ -87,6 +89,7 @@ typedef enum davet_dtype { DAVET_F32 = 0, DAVET_BF16 = 1, DAVET_F16 = 2 } davet_
 #define DAVET_MAX_PAGE_SIZE 256  /* tokens of a cache page                */
 #define DAVET_MAX_TOP 64         /* alternatives of davet_token_logprobs  */
 #define DAVET_MAX_TREE 256       /* drafted tokens of a sequence          */
+#define DAVET_MAX_BEAMS 64       /* beams of a request                    */
 
 /* Evidence realizers (Sec. 4.3: any construction with an ordered
  * evidence-cost hierarchy; pooling is the paper's default, pruning varies
@@ -783,6 +786,52 @@ int davet_token_logprobs(int32_t rows, int32_t vocab, const void* logits,
                          const int32_t* targets, float* logp, float* entropy,
                          int32_t top, float* top_logp, int32_t* top_ids,
                          void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* -------------------------------------------------------------- beams -- */
+
+/* The best continuations of `groups` requests with `beams` beams each: row g beams + b
+ * of logits (as davet_token_logprobs takes them, `exclude` too) belongs to beam b of
+ * request g, which has the score scores[row] (device float32).  Candidates are the
+ * pairs of a row and a token with a logit above -inf, of value
+ *   scores[row] + logits[row, w] - logsumexp(logits[row, :]);
+ * a row with done[row] other than 0 (device int32, NULL: none) has one candidate
+ * instead, the token `pad` with the value scores[row], and its logits are not read.  A
+ * row whose score or logsumexp is not finite has none.
+ *   out_scores, out_rows, out_tokens [groups, top]: the values (rounded to float32),
+ *   rows and tokens of the `top` (1 .. 64) best, by (value descending, row ascending,
+ *   logit descending, token ascending); values are compared in float64, the sums of
+ *   exponentials under them are float32.  Where there are fewer candidates: -inf, -1,
+ *   -1.  out_scores may be scores where top is beams.
+ * beams 1 .. DAVET_MAX_BEAMS, at most 2^22 rows.  workspace:
+ * davet_beam_workspace_bytes for these sizes exactly (fewer requests may need more),
+ * 256-byte aligned; (rows + 255) * (8 * top + 12) + 255 bytes are enough for any vocab
+ * and fewer rows.
+ * Errors: EINVAL, ESHAPE (sizes, ld), EDTYPE, ENOMEM. */
+int davet_beam_workspace_bytes(int32_t groups, int32_t beams, int32_t vocab,
+                               int32_t top, size_t* bytes /*host*/);
+int davet_beam_select(int32_t groups, int32_t beams, int32_t vocab,
+                      const void* logits, int32_t dtype, int64_t ld,
+                      int32_t exclude, const float* scores, const int32_t* done,
+                      int32_t pad, int32_t top, float* out_scores,
+                      int32_t* out_rows, int32_t* out_tokens, void* workspace,
+                      size_t ws_bytes, hipStream_t stream);
+
+/* Moves the cache along with the beams: sequence s continues sequence parent[s]
+ * (device int32 [n_seqs], rows of cache->page_table, which has n_seqs of them; the same
+ * one may be continued several times).  Its row of dst_table (device [n_seqs,
+ * dst_max_pages], not overlapping page_table) takes the pages of parent[s] that
+ * kv_len[s] tokens (HOST: the parent's length) fill, which the two then share, and for
+ * a last page that they fill in part fresh[s] (device int32), into which the keys and
+ * values of its tokens are copied, every head.  Call it for each layer (the table comes
+ * out the same), then let go of pages that no table has.  Entries behind are left as
+ * they are.  Fresh pages must be distinct and hold no key that the call reads (fresh[s]
+ * may be the parent's own last page: then it stays there, uncopied).  A parent outside
+ * [0, n_seqs), a hole for a last page and a fresh page outside the pool make the
+ * entries concerned -1. */
+int davet_cache_reorder(const davet_kv_cache* cache, int32_t n_seqs,
+                        const int32_t* kv_len, const int32_t* parent,
+                        const int32_t* fresh, int32_t* dst_table,
+                        int32_t dst_max_pages, hipStream_t stream);
 
 /* ----------------------------------------------------- rotary positions -- */
 

@@ -234,3 +234,48 @@ def logprobs(x, target, exclude=-1, top=0):
     if 0 <= target < len(x) and target != exclude:
         out = lp[target]
     return out, ent, [(j, lp[j]) for j in order[:top]]
+
+
+def beam_select(x, scores, beams, top, exclude=-1, done=None, pad=0):
+    """For each request the `top` best (value, row, token); x [rows, vocab]."""
+    out = []
+    for g in range(len(x) // beams):
+        cands = []
+        for r in range(g * beams, (g + 1) * beams):
+            score = float(scores[r])
+            if done is not None and done[r]:
+                if np.isfinite(score):
+                    cands.append((-score, r, 0.0, pad))
+                continue
+            row = np.array(x[r], np.float64)
+            if 0 <= exclude < len(row):
+                row[exclude] = -np.inf
+            with np.errstate(invalid="ignore"):
+                m = row[row > -np.inf].max() if (row > -np.inf).any() else np.nan
+                lse = m + np.log(np.sum(np.exp(row - m)))
+            if not np.isfinite(score - lse):
+                continue
+            best = sorted((j for j in range(len(row)) if row[j] > -np.inf),
+                          key=lambda j: (-row[j], j))[:top]
+            cands += [(-(score + row[j] - lse), r, -row[j], j) for j in best]
+        out.append([(-v, r, j) for v, r, _, j in sorted(cands)[:top]])
+    return out
+
+
+def reorder(cache, kv_len, parent, fresh, dst):
+    """(k, v, dst) after the cache moved along, as copies."""
+    n_pages, _, size, _ = cache["k"].shape
+    k, v, dst = cache["k"].copy(), cache["v"].copy(), np.array(dst)
+    for s, kv in enumerate(kv_len):
+        known = 0 <= parent[s] < len(kv_len)
+        whole, rest = kv // size, kv % size
+        dst[s, :whole] = cache["table"][parent[s], :whole] if known else -1
+        if rest:
+            a = int(cache["table"][parent[s], whole]) if known else -1
+            b = int(fresh[s])
+            move = 0 <= a < n_pages and 0 <= b < n_pages
+            dst[s, whole] = b if move else -1
+            if move:
+                k[b, :, :rest] = cache["k"][a, :, :rest]
+                v[b, :, :rest] = cache["v"][a, :, :rest]
+    return k, v, dst

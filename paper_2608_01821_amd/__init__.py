@@ -12,6 +12,7 @@ from ._lib import (  # noqa: F401
     davet_set_wait_limit, default_mailbox,
     davet_build_views, davet_build_views_static,
     davet_cache_append, davet_cache_attention, davet_cache_gather,
+    davet_beam_select, davet_beam_workspace_bytes, davet_cache_reorder, MAX_BEAMS,
     davet_cache_page_attention, davet_cache_page_bounds, davet_cache_page_select,
     davet_cache_tree_attention, davet_cache_weights, davet_cache_workspace_bytes, davet_convert, davet_demand_prior, davet_denoise_step,
     davet_evict_select, davet_fp16_overflow_count,

@@ -80,6 +80,7 @@ class KvCacheT(C.Structure):
 MAX_PAGE_SIZE = 256
 MAX_TOP = 64
 MAX_TREE = 256
+MAX_BEAMS = 64
 TREE_WORDS = MAX_TREE // 32
 DAVET_ROTARY_HALVES = 0
 DAVET_ROTARY_PAIRS = 1
@@ -179,6 +180,13 @@ _SIGS = {
                                              _P_i32, _vp, _i64, _i32, C.c_float,
                                              _i32, _vp, _i32, _vp, _i64, _vp,
                                              _vp, C.c_size_t, _vp]),
+    "davet_beam_workspace_bytes": (C.c_int, [_i32, _i32, _i32, _i32,
+                                             C.POINTER(C.c_size_t)]),
+    "davet_beam_select": (C.c_int, [_i32, _i32, _i32, _vp, _i32, _i64, _i32, _vp,
+                                    _vp, _i32, _i32, _vp, _vp, _vp, _vp,
+                                    C.c_size_t, _vp]),
+    "davet_cache_reorder": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _vp, _vp,
+                                      _vp, _i32, _vp]),
     "davet_rotary_turns": (C.c_int, [_i32, C.c_double, _i32, C.c_double,
                                      C.c_double, C.c_double, C.c_double,
                                      _P_f64]),
@@ -904,6 +912,56 @@ def davet_cache_page_attention(cache: KvCache, cu_q, kv_len, q, n_heads, pages, 
     _launch(cache._gpu(q, pages, out, lse, workspace), stream,
             _L.davet_cache_page_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
             scale, block, p, top, o, ldo, e, ws, nb)
+
+
+# ---- beams
+
+def davet_beam_workspace_bytes(groups, beams, vocab, top):
+    out = C.c_size_t(0)
+    _check(_L.davet_beam_workspace_bytes(
+        _small(int(groups), "groups"), _small(int(beams), "beams"),
+        _small(int(vocab), "vocab"), _small(int(top), "top"), C.byref(out)))
+    return out.value
+
+
+def davet_beam_select(logits, dtype, scores, beams, out_scores, out_rows, out_tokens,
+                      exclude=-1, done=None, pad=0, workspace=None, stream=None):
+    """``logits`` [groups * beams, vocab]; ``out_scores``, ``out_rows`` and
+    ``out_tokens`` [groups, top], dense."""
+    rows, vocab = logits.shape
+    beams = _small(beams, "beams")
+    if beams < 1 or rows % beams:
+        raise ValueError("davet: logits needs a row a beam of every request")
+    groups = rows // beams
+    x, ld = _rows(logits, vocab, rows, _kinds(dtype), "logits")
+    sc, dn = _dense(scores, rows, _FLOAT, "scores"), _dense(done, rows, _INT, "done")
+    shape = out_scores.shape
+    if len(shape) != 2 or shape[0] < groups or out_rows.shape != shape or \
+            out_tokens.shape != shape:
+        raise ValueError("davet: out_scores, out_rows and out_tokens must be "
+                         "[groups, top]")
+    o = _dense(out_scores, 0, _FLOAT, "out_scores")
+    r, t = _dense(out_rows, 0, _INT, "out_rows"), _dense(out_tokens, 0, _INT,
+                                                         "out_tokens")
+    exclude, pad = _small(exclude, "exclude"), _small(pad, "pad")
+    ws, nb = _space(workspace)
+    _launch(_gpu(logits, scores, done, out_scores, out_rows, out_tokens, workspace),
+            stream, _L.davet_beam_select, groups, beams, vocab, x, int(dtype), ld,
+            exclude, sc, dn, pad, shape[1], o, r, t, ws, nb)
+
+
+def davet_cache_reorder(cache: KvCache, kv_len, parent, fresh, dst_table,
+                        stream=None):
+    """``kv_len``: host list, one entry a row of the cache's page table; ``parent`` and
+    ``fresh``: dense int32; ``dst_table``: dense int32 [n_seqs, pages]."""
+    n = len(kv_len)
+    if n == 0 or n != cache.n_seqs or dst_table.dim() != 2 or len(dst_table) < n:
+        raise ValueError("davet: kv_len needs an entry, and dst_table a row, for each "
+                         "of page_table's")
+    p, f = _dense(parent, n, _INT, "parent"), _dense(fresh, n, _INT, "fresh")
+    dst = _dense(dst_table, 0, _INT, "dst_table")
+    _launch(cache._gpu(parent, fresh, dst_table), stream, _L.davet_cache_reorder,
+            cache._ref, n, _ints(kv_len), p, f, dst, dst_table.shape[1])
 
 
 # ---- rotary positions

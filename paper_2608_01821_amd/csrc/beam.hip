@@ -1,0 +1,294 @@
+// Beams: the best continuations over all beams of a request and the vocabulary, and
+// the move of a paged cache along with them.
+//
+//   value(b, w) = score_b + x_bw - lse_b,  lse_b = m_b + ln S_b
+//
+// A beam's best continuations are its largest logits, so each row gives its `top` by
+// (logit, id) and its (m, S) in one pass over the logits (the kernels of logprobs.h),
+// and a second launch, a workgroup a request, joins them: its wavefronts turn the rows'
+// lists into float64 values (two beams' candidates may be closer than float32
+// roundings) and keep the best 64 in order, one a lane; then their lists are joined.
+//
+// Order: value, then row, then (logit, id): within a row values only ever tie where
+// logits do, or where the score is so large that they vanish beside it.
+
+#include "logprobs.h"
+
+namespace davet {
+namespace {
+
+// a candidate: ordered bits of its value (0: none), its row's key, its row
+struct Cand {
+  uint64_t v, key;
+  uint32_t row;
+};
+__device__ __forceinline__ bool better(const Cand& a, const Cand& b) {
+  if (a.v != b.v) return a.v > b.v;
+  if (a.row != b.row) return a.row < b.row;
+  return a.key > b.key;
+}
+// order of finite doubles (larger first), never 0
+__device__ __forceinline__ uint64_t value_key(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x == 0.0 ? 0.0 : x);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double value_of(uint64_t k) {
+  return __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
+}
+// steps O, O / 2, .. 1 of a bitonic join: of each pair of lanes the better one to the
+// lower lane
+template <int O>
+__device__ __forceinline__ void settle(Cand& c) {
+  const Cand o = {lane_xor<O>(c.v), lane_xor<O>(c.key), lane_xor<O>(c.row)};
+  const bool lower = (threadIdx.x & O) == 0;
+  if (lower != better(c, o)) c = o;
+  if constexpr (O > 1) settle<O / 2>(c);
+}
+// the 64 best of two lists in order, the second one given in reverse
+__device__ __forceinline__ void join(Cand& c, const Cand& reversed) {
+  if (better(reversed, c)) c = reversed;
+  settle<32>(c);
+}
+
+// Every (beam, slice) list is one item; the wavefronts take them in turn, the loads of
+// a few at a time.
+constexpr int kJoinWaves = 16, kItems = 4;
+__global__ void __launch_bounds__(64 * kJoinWaves)
+beam_join_kernel(int rows, int beams, int slices, int k,
+                 const char* __restrict__ part, const float* scores,
+                 const int32_t* __restrict__ done, int pad, float* out_scores,
+                 int32_t* __restrict__ out_rows, int32_t* __restrict__ out_tokens) {
+  __shared__ uint64_t s_v[kJoinWaves / 2][64], s_key[kJoinWaves / 2][64];
+  __shared__ uint32_t s_row[kJoinWaves / 2][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t* lists = reinterpret_cast<const uint64_t*>(part);
+  const Stat* stats = reinterpret_cast<const Stat*>(lists + (int64_t)rows * slices * k);
+  const int row0 = blockIdx.x * beams, items = beams * slices;
+  Cand best = {0, 0, 0xffffffffu};
+  for (int i0 = wave; i0 < items; i0 += kJoinWaves * kItems) {
+    uint64_t list[kItems];
+    Stat s[kItems];
+    float score[kItems];
+    int over[kItems];
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const int it = min(i0 + u * kJoinWaves, items - 1), row = row0 + it / slices;
+      score[u] = scores[row];
+      over[u] = done ? done[row] : 0;
+      // entry j in lane 63 - j: ascending, as the join takes it.  (What a row that is
+      // over left unwritten is not used.)
+      list[u] = 63 - lane < k ? lists[((int64_t)row0 * slices + it) * k + 63 - lane] : 0;
+      s[u] = lane < slices ? stats[(int64_t)row * slices + lane] : stat_none();
+    }
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const int it = i0 + u * kJoinWaves;
+      if (it >= items) break;
+      const uint32_t row = row0 + it / slices;
+      Cand c = {0, 0, 0xffffffffu};
+      if (over[u]) {
+        if (it % slices == 0 && lane == 63 && fabsf(score[u]) < INFINITY)
+          c = {value_key((double)score[u]), top_key(0.f, pad), row};
+      } else {
+        const Stat a = stat_wave(s[u]);
+        const double base = (double)score[u] - ((double)a.m + log((double)a.S));
+        if (list[u] && fabs(base) < INFINITY)
+          c = {value_key(base + (double)key_value(list[u])), list[u], row};
+      }
+      join(best, c);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < kJoinWaves; o <<= 1) {
+    const int at = wave / (2 * o);
+    if ((wave & (2 * o - 1)) == o) {
+      s_v[at][lane] = best.v;
+      s_key[at][lane] = best.key;
+      s_row[at][lane] = best.row;
+    }
+    __syncthreads();
+    if ((wave & (2 * o - 1)) == 0)
+      join(best, {s_v[at][63 - lane], s_key[at][63 - lane], s_row[at][63 - lane]});
+    __syncthreads();
+  }
+  if (wave != 0 || lane >= k) return;
+  const int64_t at = (int64_t)blockIdx.x * k + lane;
+  out_scores[at] = best.v ? (float)value_of(best.v) : -INFINITY;
+  out_rows[at] = best.v ? (int)best.row : -1;
+  out_tokens[at] = best.v ? key_id(best.key) : -1;
+}
+
+size_t beam_bytes(int64_t rows, int vocab, int k) {
+  const int64_t n = rows * plan_slices((int)rows, vocab);
+  return align_up((size_t)n * ((size_t)k * 8 + sizeof(Stat)), 256);
+}
+
+int check_beams(int32_t groups, int32_t beams, int32_t vocab, int32_t top,
+                const std::string& who) {
+  DAVET_CHECK_ARG(groups >= 0 && beams >= 1 && beams <= DAVET_MAX_BEAMS &&
+                      (int64_t)groups * beams <= (1 << 22) && vocab >= 1 &&
+                      vocab <= (1 << 30) && top >= 1 && top <= DAVET_MAX_TOP,
+                  DAVET_ESHAPE,
+                  who + ": beams and top in [1, 64], at most 2^22 rows, vocab in "
+                        "[1, 2^30]");
+  return DAVET_OK;
+}
+
+struct ReorderPack { int32_t kv[DAVET_MAX_SEQS]; };
+
+// One workgroup a (sequence, key head): its share of the last page, keys and values;
+// that of key head 0 also writes the sequence's table.
+__global__ void __launch_bounds__(256)
+cache_reorder_kernel(CacheView cv, ReorderPack rp, int n_seqs, int row_bytes,
+                     const int32_t* __restrict__ parent,
+                     const int32_t* __restrict__ fresh, int32_t* __restrict__ dst,
+                     int dst_max_pages) {
+  const int s = blockIdx.x / cv.n_kv, h = blockIdx.x % cv.n_kv;
+  const int from = parent[s], kv = rp.kv[s];
+  const int whole = kv >> cv.lg, rest = kv & ((1 << cv.lg) - 1);
+  const bool known = (unsigned)from < (unsigned)n_seqs;
+  const int32_t* src = cv.table + (int64_t)(known ? from : 0) * cv.max_pages;
+  int32_t* to = dst + (int64_t)s * dst_max_pages;
+  if (h == 0)
+    for (int i = threadIdx.x; i < whole; i += 256) to[i] = known ? src[i] : -1;
+  if (rest == 0) return;
+  const int a = known ? src[whole] : -1, b = fresh[s];
+  const bool move = (unsigned)a < (unsigned)cv.n_pages && (unsigned)b < (unsigned)cv.n_pages;
+  if (h == 0 && threadIdx.x == 0) to[whole] = move ? b : -1;
+  if (!move || a == b) return;
+  const int n = rest * row_bytes / 16;
+  const int64_t block = (int64_t)row_bytes << cv.lg;
+  const int64_t ao = ((int64_t)a * cv.n_kv + h) * block;
+  const int64_t bo = ((int64_t)b * cv.n_kv + h) * block;
+  const u32x4* ka = reinterpret_cast<const u32x4*>(static_cast<const char*>(cv.k) + ao);
+  const u32x4* va = reinterpret_cast<const u32x4*>(static_cast<const char*>(cv.v) + ao);
+  u32x4* kb = reinterpret_cast<u32x4*>(static_cast<char*>(cv.k) + bo);
+  u32x4* vb = reinterpret_cast<u32x4*>(static_cast<char*>(cv.v) + bo);
+  constexpr int U = 4;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 256 * U) {
+    u32x4 x[U], y[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      x[u] = ka[min(i0 + u * 256, n - 1)];
+      y[u] = va[min(i0 + u * 256, n - 1)];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * 256 < n) {
+        kb[i0 + u * 256] = x[u];
+        vb[i0 + u * 256] = y[u];
+      }
+  }
+}
+
+}  // namespace
+}  // namespace davet
+
+extern "C" int davet_beam_workspace_bytes(int32_t groups, int32_t beams, int32_t vocab,
+                                          int32_t top, size_t* bytes) {
+  using namespace davet;
+  DAVET_CHECK_ARG(bytes, DAVET_EINVAL, "davet_beam_workspace_bytes: bytes is null");
+  const int rc = check_beams(groups, beams, vocab, top, "davet_beam_workspace_bytes");
+  if (rc) return rc;
+  *bytes = groups ? beam_bytes((int64_t)groups * beams, vocab, top) : 0;
+  return DAVET_OK;
+}
+
+extern "C" int davet_beam_select(int32_t groups, int32_t beams, int32_t vocab,
+                                 const void* logits, int32_t dtype, int64_t ld,
+                                 int32_t exclude, const float* scores,
+                                 const int32_t* done, int32_t pad, int32_t top,
+                                 float* out_scores, int32_t* out_rows,
+                                 int32_t* out_tokens, void* workspace, size_t ws_bytes,
+                                 hipStream_t stream) {
+  using namespace davet;
+  DAVET_CHECK_ARG(dtype == DAVET_F32 || is16(dtype), DAVET_EDTYPE,
+                  "davet_beam_select: dtype must be DAVET_F32, DAVET_BF16 or DAVET_F16");
+  int rc = check_beams(groups, beams, vocab, top, "davet_beam_select");
+  if (rc) return rc;
+  const int rows = groups * beams;
+  DAVET_CHECK_ARG(ld >= vocab && ld < (1ll << 40), DAVET_ESHAPE,
+                  "davet_beam_select: row stride below vocab, or 2^40 and more");
+  if (groups == 0) return DAVET_OK;
+  DAVET_CHECK_ARG(logits && scores && out_scores && out_rows && out_tokens, DAVET_EINVAL,
+                  "davet_beam_select: null pointer");
+  DAVET_CHECK_ARG(((uintptr_t)logits & (dtype_size(dtype) - 1)) == 0, DAVET_EINVAL,
+                  "davet_beam_select: logits misaligned for their type");
+  DAVET_CHECK_ARG(aligned4({scores, done, out_scores, out_rows, out_tokens}),
+                  DAVET_EINVAL,
+                  "davet_beam_select: scores, done and outputs must be 4-byte aligned");
+  const size_t need = beam_bytes(rows, vocab, top);
+  DAVET_CHECK_ARG(workspace && ((uintptr_t)workspace & 255) == 0 && ws_bytes >= need,
+                  DAVET_ENOMEM,
+                  "davet_beam_select: workspace missing, misaligned or below " +
+                      std::to_string(need) + " bytes");
+  char* part = static_cast<char*>(workspace);
+  const bool brief = vocab <= 64 * kWaves * kShort;
+  const int slices = brief ? 1 : plan_slices(rows, vocab);
+#define ROWS(F)                                                                \
+  do {                                                                         \
+    const auto* x = static_cast<const F::st*>(logits);                         \
+    if (brief)                                                                 \
+      hipLaunchKernelGGL((logprobs_short_kernel<F, true>), dim3(rows),         \
+                         dim3(64 * kWaves), 0, stream, x, ld, vocab, exclude,  \
+                         top, nullptr, Out{}, part, done);                     \
+    else                                                                       \
+      hipLaunchKernelGGL((logprobs_kernel<F, true>), dim3(rows * slices),      \
+                         dim3(64 * kWaves), 0, stream, x, ld, vocab, exclude,  \
+                         top, nullptr, Out{}, slices, part, done);             \
+  } while (0)
+  {
+    ProfScope ps(KC_MISC, stream);
+    if (dtype == DAVET_F16) ROWS(F16S);
+    else if (dtype == DAVET_BF16) ROWS(BF16S);
+    else ROWS(F32S);
+    DAVET_HIP(hipGetLastError());
+  }
+#undef ROWS
+  ProfScope ps(KC_MISC, stream);
+  hipLaunchKernelGGL(beam_join_kernel, dim3(groups), dim3(64 * kJoinWaves), 0, stream,
+                     rows, beams, slices, top, part, scores, done, pad, out_scores,
+                     out_rows, out_tokens);
+  DAVET_HIP(hipGetLastError());
+  return DAVET_OK;
+}
+
+extern "C" int davet_cache_reorder(const davet_kv_cache* cache, int32_t n_seqs,
+                                   const int32_t* kv_len, const int32_t* parent,
+                                   const int32_t* fresh, int32_t* dst_table,
+                                   int32_t dst_max_pages, hipStream_t stream) {
+  using namespace davet;
+  static const char who[] = "davet_cache_reorder";
+  CacheView cv;
+  const int rc = check_cache(cache, true, who, &cv);
+  if (rc) return rc;
+  DAVET_CHECK_ARG(n_seqs >= 1 && n_seqs <= DAVET_MAX_SEQS, DAVET_ESHAPE,
+                  "davet_cache_reorder: n_seqs out of range [1, 64]");
+  DAVET_CHECK_ARG(kv_len && parent && fresh && dst_table, DAVET_EINVAL,
+                  "davet_cache_reorder: null pointer");
+  DAVET_CHECK_ARG(aligned4({parent, fresh, dst_table}), DAVET_EINVAL,
+                  "davet_cache_reorder: parent, fresh and dst_table must be 4-byte "
+                  "aligned");
+  ReorderPack rp{};
+  for (int s = 0; s < n_seqs; ++s) {
+    const int64_t pages = ((int64_t)kv_len[s] + cache->page_size - 1) >> cv.lg;
+    DAVET_CHECK_ARG(kv_len[s] >= 0 && kv_len[s] <= (1 << 30) &&
+                        pages <= cv.max_pages && pages <= dst_max_pages,
+                    DAVET_ESHAPE,
+                    "davet_cache_reorder: kv_len out of range of max_pages or "
+                    "dst_max_pages (or 2^30)");
+    rp.kv[s] = kv_len[s];
+  }
+  DAVET_CHECK_ARG(dst_max_pages >= 0 &&
+                      !overlap(dst_table, (size_t)n_seqs * dst_max_pages * 4,
+                               cache->page_table, (size_t)n_seqs * cv.max_pages * 4),
+                  DAVET_EINVAL, "davet_cache_reorder: dst_table overlaps page_table");
+  ProfScope ps(KC_MISC, stream);
+  hipLaunchKernelGGL(cache_reorder_kernel, dim3((unsigned)(n_seqs * cv.n_kv)), dim3(256),
+                     0, stream, cv, rp, n_seqs,
+                     cache->head_dim * (int)dtype_size(cache->dtype), parent, fresh,
+                     dst_table, dst_max_pages);
+  DAVET_HIP(hipGetLastError());
+  return DAVET_OK;
+}
