@@ -37,6 +37,7 @@ HIP_SOURCES = ["views.hip", "realizers.hip", "unmask.hip", "rowops.hip", "gemm16
                "gemm_f32.hip", "attention.hip", "step.hip", "policy_dev.hip",
                "cache_append.hip", "cache_attention.hip", "cache_evict.hip",
                "cache_tree.hip", "cache_pages.hip",
+               "cache_page_attention.hip",
                "logprobs.hip", "beam.hip", "rotary.hip",
                "runtime.cpp",
                "schedule.cpp"]

@@ -386,7 +386,7 @@ extern "C" int davet_cache_attention(const davet_kv_cache* cache, int32_t n_seqs
   float* part = static_cast<float*>(workspace);
 #define ATT(F, DIM)                                                            \
   run_attention<F, DIM, kChunk>(cv, cp, q, ld_q, out, ld_out, lse, n_heads, block, \
-                                sc, part, Extra{}, who, stream)
+                                sc, part, nullptr, who, stream)
   if (cache->dtype == DAVET_F16) return D == 128 ? ATT(F16S, 128) : ATT(F16S, 64);
   if (cache->dtype == DAVET_BF16) return D == 128 ? ATT(BF16S, 128) : ATT(BF16S, 64);
   return D == 128 ? ATT(F32S, 128) : ATT(F32S, 64);

@@ -1,6 +1,6 @@
 // The attention kernels over a paged key/value cache, for a chunk of new tokens
-// (cache_attention.hip), a tree of them (cache_tree.hip) and listed pages
-// (cache_pages.hip).
+// (cache_attention.hip) and a tree of them (cache_tree.hip); what they share with the
+// attention over listed pages (cache_pages.hip).
 //
 //   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),
 //   lse_i = ln sum_j exp(scale q_i.k_j)
@@ -239,22 +239,8 @@ __device__ __forceinline__ typename Frag<F>::v8 load_frag(const typename F::st* 
 // What a row sees of its sequence's keys:
 //   kChunk  all before the chunk, and the chunk's up to the end of its block
 //   kTree   all before the chunk, and those of the chunk that its mask names
-//   kPages  those of the pages that its own list names, as far as kChunk's.  Every
-//           token is a tile of its own (narrow form): its keys are the list's pages
-//           one after the other, and `page_size` times an entry's place in the list
-//           takes a key's index's place.
-enum Form { kChunk, kTree, kPages };
+enum Form { kChunk, kTree };
 constexpr int kTreeWords = DAVET_MAX_TREE / 32;
-struct Extra {
-  const uint32_t* mask;     // kTree: [rows, kTreeWords]
-  const int32_t* list;      // kPages: [rows, n_kv, top]
-  int top;
-};
-// keys of a sequence of kv as kPages counts them
-__host__ __device__ inline int listed_keys(int kv, int top, int lg) {
-  const int np = (kv + (1 << lg) - 1) >> lg;
-  return (top < np ? top : np) << lg;
-}
 
 // 64 consecutive entries of a sequence's page table row, one a lane; moves on
 // as the keys do (page numbers must not fall behind `base`).
@@ -277,34 +263,6 @@ struct PageIds {
   }
 };
 
-// The same of a token's list: the pages listed and where they are (-1: not below n).
-struct ListIds {
-  const int32_t* list;
-  const int32_t* row;
-  int top, n, base, ids, pages;
-  __device__ __forceinline__ void init(const int32_t* l, int t, const int32_t* r,
-                                       int np) {
-    list = l;
-    top = t;
-    row = r;
-    n = np;
-    base = -64;
-    ids = pages = -1;
-  }
-  __device__ __forceinline__ int at(int entry) {
-    if (entry - base >= 64) {
-      base = entry;
-      const int e = entry + (int)(threadIdx.x & 63);
-      pages = e < top ? list[e] : -1;
-      ids = (unsigned)pages < (unsigned)n ? row[pages] : -1;
-    }
-    return __builtin_amdgcn_readlane(ids, entry - base);
-  }
-  __device__ __forceinline__ int page(int entry) const {
-    return __builtin_amdgcn_readlane(pages, entry - base);
-  }
-};
-
 // Launch plan, by value: workgroups of sequence order[i] start at blk[i] (of
 // one eighth of the grid when the key heads divide by 8).
 struct AttnPlan {
@@ -321,25 +279,22 @@ struct AttnPlan {
 // work.
 struct Place { int s, hk, piece, tile; };
 // The last tile comes first under a causal mask: it sees the most keys.
-template <int FORM>
 __device__ __forceinline__ Place place(const AttnPlan& ap, const ChunkPack& cp,
-                                       const CacheView& cv, const Extra& ex, int g,
-                                       int rows, bool causal) {
+                                       int n_kv, int g, int rows, bool causal) {
   const int b = ap.xcd ? (int)blockIdx.x >> 3 : (int)blockIdx.x;
   const int i = owner(ap.blk, cp.n_seqs, b);
   Place p;
   p.s = ap.order[i];
   const int n = cp.row0[p.s + 1] - cp.row0[p.s];
-  const int nt = FORM == kPages ? n * ((g + rows - 1) / rows) : (n * g + rows - 1) / rows;
-  const int kv = FORM == kPages ? listed_keys(cp.kv[p.s], ex.top, cv.lg) : cp.kv[p.s];
-  const int np = (kv + ap.piece - 1) / ap.piece;
+  const int nt = (n * g + rows - 1) / rows;
+  const int np = (cp.kv[p.s] + ap.piece - 1) / ap.piece;
   int rem = b - ap.blk[i];
   const int h = rem / (nt * np);
   rem -= h * nt * np;
   p.hk = ap.xcd ? ((int)blockIdx.x & 7) + 8 * h : h;
   p.piece = rem / nt;
   p.tile = rem - p.piece * nt;
-  if (FORM == kChunk && causal) p.tile = nt - 1 - p.tile;
+  if (causal) p.tile = nt - 1 - p.tile;
   return p;
 }
 
@@ -361,11 +316,11 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
                   const typename F::st* __restrict__ q, int64_t ld_q,
                   typename F::st* __restrict__ out, int64_t ld_o,
                   float* __restrict__ lse, int n_heads, int block, Scale sc_,
-                  float* __restrict__ part, int part_rows, Extra ex) {
+                  float* __restrict__ part, int part_rows,
+                  const uint32_t* __restrict__ mask) {
   using st = typename F::st;
   using T = Tile<F, D>;
   using v8 = typename Frag<F>::v8;
-  static_assert(FORM != kPages || G == 1, "a token's rows are few");
   constexpr int KT = G == 4 ? 64 : 32;            // keys a tile
   constexpr int MT = KT / 32;
   constexpr int KG = 4 / G;                       // tile streams
@@ -385,17 +340,10 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 
   const int g = n_heads / cv.n_kv;
   const int lg = cv.lg, psz = 1 << lg;
-  Place pl = place<FORM>(ap, cp, cv, ex, g, 32 * G, block > 0);
+  const Place pl = place(ap, cp, cv.n_kv, g, 32 * G, block > 0);
   const int s = pl.s, hk = pl.hk;
-  const int n_all = cp.row0[s + 1] - cp.row0[s], kv_all = cp.kv[s];
-  // kPages: the token that this tile belongs to, by itself
-  const int tok0 = FORM == kPages ? pl.tile / ((g + 32 * G - 1) / (32 * G)) : 0;
-  if (FORM == kPages) pl.tile -= tok0 * ((g + 32 * G - 1) / (32 * G));
-  const int row0 = cp.row0[s] + tok0, n = FORM == kPages ? 1 : n_all;
-  const int kv = FORM == kPages ? listed_keys(kv_all, ex.top, lg) : kv_all;
-  // kPages: cache indices below it are visible
-  const int token_lim = visible_end(tok0, n_all, kv_all, block);
-  const int past = kv_all - n_all;
+  const int row0 = cp.row0[s], n = cp.row0[s + 1] - row0, kv = cp.kv[s];
+  const int past = kv - n;
   const int rows = n * g;
   const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -452,7 +400,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int i = threadIdx.x; i < 32 * G * kTreeWords; i += 256) {
       const int r = i / kTreeWords, w = i % kTreeWords, left = n - w * 32;
       const int tok = min(pl.tile * 32 * G + r, rows - 1) / g;
-      uint32_t m = left > 0 ? ex.mask[(int64_t)(row0 + tok) * kTreeWords + w] : 0u;
+      uint32_t m = left > 0 ? mask[(int64_t)(row0 + tok) * kTreeWords + w] : 0u;
       if (left < 32) m &= left > 0 ? (1u << left) - 1 : 0u;
       s_mask[r * MS + w] = m;
     }
@@ -463,16 +411,11 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int32_t* table = cv.table + (int64_t)s * cv.max_pages;
   PageIds pages;
   pages.init(table, cv.max_pages);
-  ListIds list;
-  const int32_t* list0 =
-      FORM == kPages ? ex.list + ((int64_t)row0 * cv.n_kv + hk) * ex.top : nullptr;
-  if (FORM == kPages) list.init(list0, ex.top, table, (kv_all + psz - 1) >> lg);
 
   // A 16-key group on its way to LDS.  A page holds whole groups.
   struct Group {
     int64_t at;         // byte of its first row in the pools; -1: in a hole
     int last;           // its last valid row
-    int hidden;         // kPages: rows from 16 - hidden on are not visible
   };
   auto group = [&](int k0, int gi, int page) {
     const int key = min(k0 + gi * 16, (kv - 1) & ~15);
@@ -481,19 +424,6 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
                ? ((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * T::RB
                : -1;
     r.last = kv - 1 - key;
-    r.hidden = 0;
-    return r;
-  };
-  // kPages: of the list's key `key`.  A group that nobody sees is as in a hole.
-  auto listed = [&](int key) {
-    Group r = {-1, 15, 16};
-    if (key >= kv) return r;
-    const int phys = list.at(key >> lg), off = key & (psz - 1);
-    const int first = (list.page(key >> lg) << lg) + off;
-    if ((unsigned)phys >= (unsigned)cv.n_pages || first >= token_lim) return r;
-    r.at = ((((int64_t)phys * cv.n_kv + hk) << lg) + off) * T::RB;
-    r.last = kv_all - 1 - first;
-    r.hidden = max(0, first + 16 - token_lim);
     return r;
   };
   // Moves its rows of K or V.  Rows past the last valid one repeat it; rows of
@@ -556,21 +486,14 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   auto move_v = [&](const Tag& r, int b) {
     move16(false, gbuf + b * 2 * TILE + TILE + wave * 16 * T::RB, r.mine);
   };
-  // G = 1: the whole tile; returns its holes (kPages: five bits a group, how many of
-  // its rows are hidden)
+  // G = 1: the whole tile; returns its holes
   auto issue = [&](int k0, int b) -> int {
     char* kd = gbuf + b * 2 * TILE;
     int holes = 0;
 #pragma unroll
     for (int gi = 0; gi < KT / 16; ++gi) {
-      Group r;
-      if constexpr (FORM == kPages) {
-        r = listed(k0 + gi * 16);
-        holes |= r.hidden << (5 * gi);
-      } else {
-        r = group(k0, gi, pages.at(min(k0 + gi * 16, kv - 1) >> lg));
-        holes |= (r.at < 0) << gi;
-      }
+      const Group r = group(k0, gi, pages.at(min(k0 + gi * 16, kv - 1) >> lg));
+      holes |= (r.at < 0) << gi;
       move16(true, kd + gi * 16 * T::RB, r);
       move16(false, kd + TILE + gi * 16 * T::RB, r);
     }
@@ -636,12 +559,9 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int c = mt * 32 + (e >> 2) * 8 + (e & 3), at = c + hh * 4;
-          const bool out =
-              FORM == kPages
-                  ? (at & 15) + ((holes >> (5 * (at >> 4))) & 31) >= 16
-                  : (FORM == kTree ? !((sees >> c) & 1) : k0 + at >= lim) ||
-                        ((holes >> (at >> 4)) & 1);
-          if (out) sc[mt][e] = -INFINITY;
+          if ((FORM == kTree ? !((sees >> c) & 1) : k0 + at >= lim) ||
+              ((holes >> (at >> 4)) & 1))
+            sc[mt][e] = -INFINITY;
         }
       tmax = largest(sc);
     }
@@ -1068,42 +988,21 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   __syncthreads();
   if (s_bad && wave * 64 + lane_e < D) {
     const int d = wave * 64 + lane_e;
-    // where key `key` lies (row of the pools, or -1), and its cache index
-    struct Row { int64_t at; int index; };
-    auto row_of = [&](int key) {
-      Row r = {-1, key};
-      int page = key >> lg;
-      if constexpr (FORM == kPages) {
-        page = key < kv ? list0[page] : -1;
-        if ((unsigned)page >= (unsigned)((kv_all + psz - 1) >> lg)) return r;
-        r.index = (page << lg) + (key & (psz - 1));
-        if (r.index >= kv_all) return r;
-      }
-      const int phys = table[page];
-      if ((unsigned)phys < (unsigned)cv.n_pages)
-        r.at = (((int64_t)phys * cv.n_kv + hk) << lg) + (key & (psz - 1));
-      return r;
-    };
     for (int k0 = begin; k0 < end; k0 += KT) {
       int holes = 0;
       for (int gi = 0; gi < KT / 16; ++gi) {
-        if constexpr (FORM == kPages) {       // (some row of the group is hidden)
-          const Row r = row_of(k0 + gi * 16);
-          holes |= r.at < 0 || r.index + 16 > token_lim;
-        } else {
-          holes |= row_of(min(k0 + gi * 16, (kv - 1) & ~15)).at < 0;
-        }
+        const int page = table[min(k0 + gi * 16, (kv - 1) & ~15) >> lg];
+        holes |= ((unsigned)page >= (unsigned)cv.n_pages) << gi;
       }
       if (!tile_masked(k0, holes)) continue;
       for (int key = k0; key < min(k0 + KT, end); ++key) {
-        const Row r = row_of(key);
-        if (r.at < 0) continue;
-        const float x = F::load(static_cast<const st*>(cv.v)[r.at * D + d]);
+        const int page = table[key >> lg];
+        if ((unsigned)page >= (unsigned)cv.n_pages) continue;
+        const float x = F::load(static_cast<const st*>(
+            cv.v)[((((int64_t)page * cv.n_kv + hk) << lg) + (key & (psz - 1))) * D + d]);
         if (fabsf(x) < INFINITY) continue;
         for (int rr = pl.tile * 32 * G; rr <= tile_last; ++rr) {
-          if constexpr (FORM == kPages) {
-            if (r.index >= token_lim) continue;
-          } else if constexpr (FORM == kTree) {
+          if constexpr (FORM == kTree) {
             const int j = key - past;
             if (j >= 0 &&
                 !(s_mask[(rr - pl.tile * 32 * G) * MS + (j >> 5)] >> (j & 31) & 1))
@@ -1334,10 +1233,36 @@ AttnPlan plan_attn(const ChunkPack& cp, int n_kv, Tiles tiles, int want, int uni
   return ap;
 }
 
+// The launch that joins the pieces; cp.kv: the keys that were cut into them.
+template <typename F, int D>
+int join_pieces(const ChunkPack& cp, const float* part, const AttnPlan& ap, void* out,
+                int64_t ld_o, float* lse, int n_heads, Scale sc, hipStream_t stream) {
+  using st = typename F::st;
+  const int64_t rows = (int64_t)cp.row0[cp.n_seqs] * n_heads;
+  ProfScope ps(KC_MISC, stream);
+  // 27,000 rows of 64 dims in two pieces 13 us a wavefront each, 5 packed (of 128
+  // dims 14 and 8); 4096 rows the same; 32 rows in 24 pieces 2.5 us more packed
+  if (rows < 8192) {
+    hipLaunchKernelGGL((cache_merge_kernel<F, D>),
+                       dim3((unsigned)((rows + 3) / 4)), dim3(256), 0,
+                       stream, cp, part, (int)rows, ap.piece, ap.pieces,
+                       (st*)out, ld_o, lse, n_heads, sc);
+  } else {
+    constexpr int R = 256 / D;                // rows a wavefront
+    const int64_t waves = (int64_t)cp.row0[cp.n_seqs] * ((n_heads + R - 1) / R);
+    hipLaunchKernelGGL((cache_merge_rows_kernel<F, D>),
+                       dim3((unsigned)((waves + 3) / 4)), dim3(256), 0,
+                       stream, cp, part, (int)rows, ap.piece, ap.pieces,
+                       (st*)out, ld_o, lse, n_heads, sc);
+  }
+  DAVET_HIP(hipGetLastError());
+  return DAVET_OK;
+}
+
 template <typename F, int D, int FORM>
 int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
                   int64_t ld_q, void* out, int64_t ld_o, float* lse,
-                  int n_heads, int block, Scale sc, float* part, const Extra& ex,
+                  int n_heads, int block, Scale sc, float* part, const uint32_t* mask,
                   const char* who, hipStream_t stream) {
   using st = typename F::st;
   const int g = n_heads / cv.n_kv;
@@ -1354,7 +1279,7 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   // buffer): four sequences, 8 heads, 58 us with 64 rows where narrow takes 43, and
   // 62 with 96 where it takes 63.
   constexpr bool f32 = F::dtype == DAVET_F32;
-  const bool wide = FORM != kPages && (int64_t)most * g > (f32 ? 64 : 32);
+  const bool wide = (int64_t)most * g > (f32 ? 64 : 32);
   constexpr int WB = f32 ? 1 : 2;                       // wide: buffers
   constexpr int WM = 2;                                 // workgroups a CU
   constexpr int NB = f32 && D == 128 ? 1 : 2;           // narrow
@@ -1367,16 +1292,11 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   // us, 194 queries over 272 keys 23 us in pieces of 64, 32 of 128, 48 of 256.
   constexpr int NH = f32 ? 256 : 384;
   constexpr int WL = f32 ? 64 : 256, WH = f32 ? 128 : 256;
-  ChunkPack keys = cp;                      // with the keys that the form goes through
-  if (FORM == kPages)
-    for (int s = 0; s < cp.n_seqs; ++s)
-      keys.kv[s] = listed_keys(cp.kv[s], ex.top, cv.lg);
   const int tile = wide ? 128 : 32;
-  auto tiles = [&](int s) -> int64_t {
-    const int64_t n = cp.row0[s + 1] - cp.row0[s];
-    return FORM == kPages ? n * ((g + tile - 1) / tile) : (n * g + tile - 1) / tile;
+  auto tiles = [&](int s) {
+    return ((int64_t)(cp.row0[s + 1] - cp.row0[s]) * g + tile - 1) / tile;
   };
-  const AttnPlan ap = plan_attn(keys, cv.n_kv, tiles,
+  const AttnPlan ap = plan_attn(cp, cv.n_kv, tiles,
                                 256 * (wide ? WM : NM), wide ? 64 : 128,
                                 wide ? WL : 128, wide ? WH : NH,
                                 max_pieces(rows));
@@ -1385,40 +1305,21 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
                   std::string(who) + ": too many row tiles");
   {
     ProfScope ps(KC_MISC, stream);
-    if constexpr (FORM != kPages) {
-      if (wide)
-        hipLaunchKernelGGL((cache_attn_kernel<F, D, 4, WB, WM, FORM>),
-                           dim3((unsigned)grid), dim3(256), 0, stream, cv, cp, ap,
-                           (const st*)q, ld_q, (st*)out, ld_o, lse, n_heads, block, sc,
-                           part, (int)rows, ex);
-    }
-    if (!wide)
+    if (wide)
+      hipLaunchKernelGGL((cache_attn_kernel<F, D, 4, WB, WM, FORM>),
+                         dim3((unsigned)grid), dim3(256), 0, stream, cv, cp, ap,
+                         (const st*)q, ld_q, (st*)out, ld_o, lse, n_heads, block, sc,
+                         part, (int)rows, mask);
+    else
       hipLaunchKernelGGL((cache_attn_kernel<F, D, 1, NB, NM, FORM>),
                          dim3((unsigned)grid), dim3(256), 0, stream, cv, cp, ap,
                          (const st*)q, ld_q, (st*)out, ld_o, lse, n_heads, block, sc,
-                         part, (int)rows, ex);
+                         part, (int)rows, mask);
     DAVET_HIP(hipGetLastError());
   }
-  if (ap.pieces > 1) {
-    ProfScope ps(KC_MISC, stream);
-    // 27,000 rows of 64 dims in two pieces 13 us a wavefront each, 5 packed (of 128
-    // dims 14 and 8); 4096 rows the same; 32 rows in 24 pieces 2.5 us more packed
-    if (rows < 8192) {
-      hipLaunchKernelGGL((cache_merge_kernel<F, D>),
-                         dim3((unsigned)((rows + 3) / 4)), dim3(256), 0,
-                         stream, keys, part, (int)rows, ap.piece, ap.pieces,
-                         (st*)out, ld_o, lse, n_heads, sc);
-    } else {
-      constexpr int R = 256 / D;                // rows a wavefront
-      const int64_t waves = (int64_t)cp.row0[cp.n_seqs] * ((n_heads + R - 1) / R);
-      hipLaunchKernelGGL((cache_merge_rows_kernel<F, D>),
-                         dim3((unsigned)((waves + 3) / 4)), dim3(256), 0,
-                         stream, keys, part, (int)rows, ap.piece, ap.pieces,
-                         (st*)out, ld_o, lse, n_heads, sc);
-    }
-    DAVET_HIP(hipGetLastError());
-  }
-  return DAVET_OK;
+  return ap.pieces > 1 ? join_pieces<F, D>(cp, part, ap, out, ld_o, lse, n_heads, sc,
+                                           stream)
+                       : DAVET_OK;
 }
 
 size_t workspace_bytes(int64_t total_q, int n_heads, int D) {

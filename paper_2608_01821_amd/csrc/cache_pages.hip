@@ -1,6 +1,6 @@
-// Sparse attention over pages that a cheap score selects: the elementwise bounds of
-// each page's keys, the choice of pages for each new token and key head, and the
-// attention over them (the kernels of cache_attn.h, narrow form, a token a tile).
+// Pages that a cheap score selects: the elementwise bounds of each page's keys, and the
+// choice of pages for each new token and key head.  (Their attention:
+// cache_page_attention.hip.)
 //
 // For a page with keys k_j, lo = min_j k_j and hi = max_j k_j, element by element:
 //   q.k_j = sum_e q_e k_je <= sum_e max(q_e lo_e, q_e hi_e) = q+.hi + q-.lo
@@ -19,7 +19,11 @@
 // the last page taken is found two bits at a time by counting, and the pages are
 // written in ascending order.
 
-#include "cache_attn.h"
+#include <math.h>
+
+#include <algorithm>
+
+#include "cache.h"
 
 namespace davet {
 namespace {
@@ -432,38 +436,4 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
 #undef SELECT
   DAVET_HIP(hipGetLastError());
   return DAVET_OK;
-}
-
-extern "C" int davet_cache_page_attention(
-    const davet_kv_cache* cache, int32_t n_seqs, const int32_t* cu_q,
-    const int32_t* kv_len, const void* q, int64_t ld_q, int32_t n_heads, float scale,
-    int32_t block, const int32_t* pages, int32_t top, void* out, int64_t ld_out,
-    float* lse, void* workspace, size_t ws_bytes, hipStream_t stream) {
-  using namespace davet;
-  static const char who[] = "davet_cache_page_attention";
-  CacheView cv;
-  ChunkPack cp;
-  int64_t total = 0;
-  const int rc = check_attention(cache, n_seqs, cu_q, kv_len, q, ld_q, n_heads, scale,
-                                 block, out, ld_out, lse, workspace, ws_bytes, who, &cv,
-                                 &cp, &total);
-  if (rc) return rc;
-  DAVET_CHECK_ARG(top >= 1 && top <= (1 << 26), DAVET_ESHAPE,
-                  "davet_cache_page_attention: top out of range [1, 2^26]");
-  if (total == 0) return DAVET_OK;
-  DAVET_CHECK_ARG(pages && aligned4({pages}), DAVET_EINVAL,
-                  "davet_cache_page_attention: pages null or not 4-byte aligned");
-  const int D = cache->head_dim;
-  const Scale sc = make_scale(scale, D);
-  float* part = static_cast<float*>(workspace);
-  Extra ex{};
-  ex.list = pages;
-  ex.top = top;
-#define ATT(F, DIM)                                                               \
-  run_attention<F, DIM, kPages>(cv, cp, q, ld_q, out, ld_out, lse, n_heads, block, \
-                                sc, part, ex, who, stream)
-  if (cache->dtype == DAVET_F16) return D == 128 ? ATT(F16S, 128) : ATT(F16S, 64);
-  if (cache->dtype == DAVET_BF16) return D == 128 ? ATT(BF16S, 128) : ATT(BF16S, 64);
-  return D == 128 ? ATT(F32S, 128) : ATT(F32S, 64);
-#undef ATT
 }

@@ -125,11 +125,9 @@ extern "C" int davet_cache_tree_attention(
   const int D = cache->head_dim;
   const Scale sc = make_scale(scale, D);
   float* part = static_cast<float*>(workspace);
-  Extra ex{};
-  ex.mask = mask;
 #define ATT(F, DIM)                                                               \
   run_attention<F, DIM, kTree>(cv, cp, q, ld_q, out, ld_out, lse, n_heads, 0, sc, \
-                               part, ex, who, stream)
+                               part, mask, who, stream)
   if (cache->dtype == DAVET_F16) return D == 128 ? ATT(F16S, 128) : ATT(F16S, 64);
   if (cache->dtype == DAVET_BF16) return D == 128 ? ATT(BF16S, 128) : ATT(BF16S, 64);
   return D == 128 ? ATT(F32S, 128) : ATT(F32S, 64);
