@@ -5,19 +5,22 @@
 //
 // The keys of a list are its pages' one after the other ("listed keys"); 16 aligned
 // ones share a page.  A wavefront takes 32 of them (fp32: 16) against up to 16 query
-// heads, all in registers:
+// heads:
 //
-//   S^T = K Q^T    16 x 16 matrix ops, a lane's rows of K straight from memory: lane l
-//                  holds the scores of query head l % 16 and keys 4 (l / 16) + 0 .. 3
+//   S^T = K Q^T    16 x 16 matrix ops: lane l holds the scores of query head l % 16 and
+//                  keys 4 (l / 16) + 0 .. 3 of each 16.  K goes through LDS by DMA, a
+//                  row's bytes side by side: as operands straight from memory, a
+//                  quarter of a load's lanes would touch 16 rows, and the sixteen
+//                  ragged blocks below took 86 us, bound by that.
 //   O^T = V^T P^T  which takes those probabilities where they are as its B operand;
 //                  for its A operand lane l loads 8 (fp32: 4) neighbouring dims,
 //                  8 (l % 16) on, of the same keys, so that matrix op d, which takes
 //                  element d of each, gives dims 8 m + d.  16 bits: the lane's 8 x 8
-//                  block is transposed by 32 byte permutes.
+//                  block is transposed by 32 byte permutes.  No LDS.
 //
-// No value passes through LDS, which leaves room for three wavefronts a SIMD, and each
-// has the next keys on their way while it weighs and adds the values, and the next
-// values while it multiplies keys.  Rows of Q past the last head repeat it.
+// Every wavefront goes its own way, with the next keys on their way while it adds up
+// values, and the next values while it multiplies keys.  Rows of Q past the last head
+// repeat it.
 //
 // Four wavefronts share a list's keys and are joined in LDS, or, where there are lists
 // enough to fill the chip, each has its own.  A list may also be cut into pieces, which
@@ -82,7 +85,7 @@ __device__ __forceinline__ f32x4 mm16(typename Frag<F>::v8 a, typename Frag<F>::
 
 // W: wavefronts that share a list (4, 1: each has its own).
 template <typename F, int D, int W>
-__global__ void __launch_bounds__(256, F::dtype == DAVET_F32 ? 2 : 3)
+__global__ void __launch_bounds__(256, F::dtype == DAVET_F32 && D == 128 ? 2 : 3)
 page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
                  const typename F::st* __restrict__ q, int64_t ld_q,
                  typename F::st* __restrict__ out, int64_t ld_o,
@@ -98,8 +101,11 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   constexpr int VD = F32 ? 4 : D / 16;          // dims each gives
   constexpr int NO = D / 16;                    // 16 x 16 tiles of O
   constexpr float BIAS = Frag<F>::kBias;
-  constexpr int LR = D + 4;
-  __shared__ __attribute__((aligned(16))) float s_o[W == 4 ? 4 * 16 * LR : 4];
+  using T = Tile<F, D>;
+  constexpr int KB = KT * RB;                   // a tile of keys, 4 or 8 KB
+  // each wavefront's keys; then O of its rows, as large
+  __shared__ __attribute__((aligned(1024))) char smem[4 * KB];
+  static_assert(KB == 16 * D * 4, "O takes the keys' place");
   __shared__ float s_m[4][16], s_l[4][16];
 
   const int g = n_heads / cv.n_kv, rt = (g + 15) / 16, lg = cv.lg, psz = 1 << lg;
@@ -153,17 +159,35 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int i = 0; i < GR; ++i) t.g[i] = group(k0 + i * 16);
     return t;
   };
-  u32x4 kr[GR][KC];
+  char* const kbuf = smem + wave * KB;
   typedef uint32_t vreg __attribute__((ext_vector_type(F32 ? 4 : VD / 2)));
   vreg vr[GR][4][VC];
+  // Row r = j RPI + lane / C of a group, chunk lane % C of its place in LDS, holds
+  // chunk k_slot(r, lane % C) of memory.  Rows past the last cached one repeat it.
   auto load_k = [&](const Tile16& t) {
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
       const char* p = static_cast<const char*>(cv.k) + t.g[i].at;
-      const uint32_t o = min(l16, t.g[i].last) * RB + quad * 16;
+      char* to = kbuf + i * 16 * RB;
+      constexpr int N = 16 / T::RPI, RUN = N < 4 ? N : 4;
+      if (t.g[i].last >= 15) {
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
-        kr[i][c] = *reinterpret_cast<const u32x4*>(p + (o + c * 64));
+        for (int j = 0; j < N; j += RUN) {
+          uint32_t at[RUN];
+#pragma unroll
+          for (int u = 0; u < RUN; ++u)
+            at[u] = (uint32_t)(lane * 16) ^
+                    (T::k_slot((j + u) * T::RPI + lane / T::C, 0) * 16);
+          dma16_run(p + j * 1024, at, to + j * 1024);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const int lr = j * T::RPI + lane / T::C;
+          dma16(p, (uint32_t)min(lr, t.g[i].last) * RB + T::k_slot(lr, lane % T::C) * 16,
+                to + j * 1024);
+        }
+      }
     }
   };
   auto load_v = [&](const Tile16& t) {
@@ -195,6 +219,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   float ref = 0.f, l_run = 0.f;
   bool seen = false;                // some score above -inf so far
 
+  constexpr int NV = GR * 4 * VC;       // loads of V a tile
   constexpr int STEP = W * KT;
   int k0 = begin + (W == 4 ? wave * KT : 0);
   Tile16 cur = {};
@@ -205,6 +230,15 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   }
   for (; k0 < end; k0 += STEP) {
     const bool more = k0 + STEP < end;
+    // the tile's keys are there; its values, loaded after them, may not be
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NV) : "memory");
+    u32x4 kr[GR][KC];
+#pragma unroll
+    for (int i = 0; i < GR; ++i)
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+        kr[i][c] = *reinterpret_cast<const u32x4*>(
+            kbuf + (i * 16 + l16) * RB + T::k_slot(l16, c * 4 + quad) * 16);
     f32x4 sc[GR];
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
@@ -231,11 +265,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       }
     }
     Tile16 next = {};
-    if (more) {
-      next = tile_at(k0 + STEP);
-      load_k(next);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    if (more) next = tile_at(k0 + STEP);
     // hidden keys: score -inf, and values of 0 (0 times an infinity would be NaN)
     bool some = false;
 #pragma unroll
@@ -251,6 +281,18 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
           for (int c = 0; c < VC; ++c) vr[i][e][c] = vreg{};
         }
     }
+    // The next keys, once this tile's are read and its values there (the compiler does
+    // not count the DMA: a wait for values behind it would be for both).
+    auto next_k = [&]() {
+#pragma unroll
+      for (int i = 0; i < GR; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int c = 0; c < VC; ++c) asm volatile("" : "+v"(vr[i][e][c]));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) load_k(next);
+    };
     if (some) {
       float tmax = -INFINITY;
 #pragma unroll
@@ -281,6 +323,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
         p[i] = __builtin_amdgcn_exp2f(F32 ? exact_arg(x, sc_) : fmaf(x, sc_.c, BIAS));
         l_run += p[i];
       }
+      next_k();
       if constexpr (F32) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -314,6 +357,8 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
           o[d] = mm16<F>(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, lo), o[d]);
         }
       }
+    } else {
+      next_k();
     }
     if (more) load_v(next);
     __builtin_amdgcn_sched_barrier(0);
@@ -357,10 +402,15 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       lse[head + l16] = l_run == 0.f ? -INFINITY
                                      : m_run * sc_.scale + (logf(l_run) - bias_ln);
   } else {
+    float* const s_o = reinterpret_cast<float*>(smem);
+    auto o_at = [&](int w, int r, int d) -> float& {
+      // (rows' 16-byte pieces in turn: 16 rows at a time are written at one dim)
+      return s_o[(w * 16 + r) * D + (d ^ ((r & 15) * 4))];
+    };
 #pragma unroll
     for (int t = 0; t < NO; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s_o[(wave * 16 + l16) * LR + dim_of(t, i)] = o[t][i];
+      for (int i = 0; i < 4; ++i) o_at(wave, l16, dim_of(t, i)) = o[t][i];
     if (quad == 0) {
       s_m[wave][l16] = m_run;
       s_l[wave][l16] = l_run;
@@ -385,7 +435,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       acc[i] = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w)
-        if (use[w]) acc[i] += wt[w] * s_o[(w * 16 + r) * LR + d0 + i];
+        if (use[w]) acc[i] += wt[w] * o_at(w, r, d0 + i);
     }
     if (ap.pieces > 1) {
       const int64_t at = (int64_t)piece * part_rows + head + r;
