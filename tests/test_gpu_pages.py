@@ -88,6 +88,12 @@ SELECT = [  # dtype, new, kv, heads, kv_heads, dim, page, block, top, first, las
     ("bf16", [1], [16 * 5000], 2, 1, 64, 16, 0, 300, 1, 1),  # more than 4096 pages
     ("f32", [1], [16 * 4200], 1, 1, 64, 16, 0, 7, 0, 0),
     ("f16", [40], [60], 32, 1, 64, 16, 1, 2, 1, 1),
+    # many tokens and key heads: a wavefront each
+    ("f16", [140, 3], [700, 333], 8, 8, 64, 16, 1, 6, 1, 1),
+    ("bf16", [33], [1600], 64, 32, 128, 16, 4, 40, 0, 2),
+    ("f32", [70], [16 * 64], 16, 16, 64, 16, 1, 63, 0, 0),
+    ("f32", [34], [530], 32, 32, 128, 16, 0, 5, 2, 0),
+    ("f16", [2], [16 * 512], 1024, 1024, 64, 16, 0, 7, 0, 1),
 ]
 
 
@@ -173,6 +179,12 @@ ATTEND = [  # dtype, new, kv, heads, kv_heads, dim, page, block, top
     ("f16", [2], [2000], 4, 1, 128, 16, 1, 64),             # pieces
     ("bf16", [1], [3000], 2, 1, 64, 256, 0, 11),
     ("f32", [40], [90], 2, 2, 64, 16, 1, 3),
+    # lists enough for a wavefront each
+    ("f16", [260, 1], [300, 40], 8, 8, 64, 16, 1, 4),
+    ("bf16", [33], [400], 128, 64, 128, 32, 0, 5),
+    ("f32", [70], [100], 64, 32, 64, 16, 4, 3),
+    ("f32", [66], [90], 32, 32, 128, 16, 1, 2),
+    ("f16", [130], [140], 320, 16, 64, 16, 0, 3),           # two row tiles each
 ]
 
 
