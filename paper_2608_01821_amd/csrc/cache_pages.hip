@@ -12,14 +12,17 @@
 // and their sum almost, so the order of summation does not decide which of two close
 // pages is taken, and equal scores go to the lower page.
 //
-// A page's bounds are 256 to 1024 bytes, read 16 a lane by 16 to 64 lanes; a lane keeps
-// its elements of Q in registers and multiplies as many pages as there are such lanes,
-// whose sums are then added and dealt out at once, a page a lane (31 additions for 32
-// pages of 32 lanes).  So a wavefront's step is 64 pages, one a lane.
+// Three forms:
+//   tiles  chunks of 8 tokens and more: 16 tokens x 16 pages by float64 matrix ops,
+//          which read a page's bounds once for all 16
+//   waves  many (token, key head): a wavefront each, by vector ops, no LDS
+//   group  few of them: a workgroup each
+// In the last two a page's bounds are read 16 bytes a lane by 16 to 64 lanes, which keep
+// their elements of Q in registers; the sums of several pages are added over the lanes
+// and dealt out to them at once.
 //
-// Selection: the key of the last page taken is found two bits at a time by counting,
-// and the pages are written in ascending order.  Either a workgroup takes one (token,
-// key head), or, where there are many, a wavefront does, by itself and without LDS.
+// Then the key of the last page taken is found from its highest bit down, by counting,
+// and the pages are written in ascending order.
 
 #include <math.h>
 
@@ -119,9 +122,9 @@ page_bounds_kernel(CacheView cv, BoundsPack bp, typename F::st* __restrict__ bou
 
 // ---- selection
 
-constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kMaxPages = 32768;        // of a sequence: their keys fill the LDS
-constexpr int kManyItems = 1024;
+constexpr int kManyItems = 1024;        // of them a wavefront each
 
 // order of a score: larger first; NaN with -inf, -0 with +0; never 0
 __device__ __forceinline__ uint32_t score_key(float x) {
@@ -176,12 +179,17 @@ struct Scorer {
     else
       return F::load((uint16_t)(w[e >> 1] >> (16 * (e & 1))));
   }
-  // heads: the g query heads' rows
-  __device__ __forceinline__ void init(const st* heads, int g, const st* b, int n_kv,
-                                       int hk) {
-    const int l = threadIdx.x & (LP - 1);
-    bounds = b + (int64_t)hk * 2 * D + l * N;
+  // what a query's element adds to Q- or Q+ (a NaN to both)
+  __device__ __forceinline__ static double part(float v, bool lower) {
+    return (double)(lower ? (v > 0.f ? 0.f : v) : (v < 0.f ? 0.f : v));
+  }
+  __device__ __forceinline__ void prepare(const st* b, int n_kv, int hk) {
+    bounds = b + (int64_t)hk * 2 * D + (threadIdx.x & (LP - 1)) * N;
     page = (int64_t)n_kv * 2 * D;
+  }
+  // heads: the g query heads' rows
+  __device__ __forceinline__ void init(const st* heads, int g) {
+    const int l = threadIdx.x & (LP - 1);
 #pragma unroll
     for (int e = 0; e < N; ++e) q[e] = 0.0;
     for (int h = 0; h < g; ++h) {
@@ -189,23 +197,20 @@ struct Scorer {
                                                       (l & (H - 1)) * N);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float v = elem(w, e);             // (a NaN makes both sums NaN)
-        q[e] += (double)(l < H ? (v > 0.f ? 0.f : v) : (v < 0.f ? 0.f : v));
+        q[e] += part(elem(w, e), l < H);
       }
     }
   }
   // of the 64 pages whose places the lanes hold (0 for none): lane l's score is its own
   // page's
-  __device__ __forceinline__ float score(int phys) const {
+  __device__ __forceinline__ float score64(int phys) const {
     const int lane = threadIdx.x & 63;
     // page u 4 + j + b H of each LP lanes' share: b the highest bit of a lane's number
     // in it, j the lowest two
     auto load = [&](int u, u32x4 (&w)[8]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int ph = __shfl(phys, (lane & ~(LP - 1)) + u * 4 + (i & 3) + (i >> 2) * H, 64);
-        w[i] = *reinterpret_cast<const u32x4*>(bounds + (int64_t)ph * page);
-      }
+      for (int i = 0; i < 8; ++i)
+        w[i] = read(__shfl(phys, (lane & ~(LP - 1)) + u * 4 + (i & 3) + (i >> 2) * H, 64));
     };
     u32x4 w[2][8];
     load(0, w[0]);
@@ -214,16 +219,7 @@ struct Scorer {
     for (int u = 0; u < LP / 8; ++u) {
       if (u + 1 < LP / 8) load(u + 1, w[(u + 1) & 1]);
       __builtin_amdgcn_sched_barrier(0);
-      double x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = 0.0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[i] = fma((double)elem(w[u & 1][i], e), q[e], x[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = deal<H>(x[i], x[i + 4]);
-      sum[u] = deal<2>(deal<1>(x[0], x[1]), deal<1>(x[2], x[3]));
+      sum[u] = eight(w[u & 1]);
     }
     if constexpr (LP >= 64)
 #pragma unroll
@@ -232,6 +228,36 @@ struct Scorer {
 #pragma unroll
       for (int u = 0; u < 2; ++u) sum[u] = deal<8>(sum[u], sum[u + 2]);
     return (float)deal<4>(sum[0], sum[1]);
+  }
+  // of 8 pages for each LP lanes: theirs is page (lane & 3) + (lane & H ? 4 : 0)
+  static constexpr int PAGES = 8 * 64 / LP;         // of a wavefront
+  __device__ __forceinline__ float score8(const u32x4 (&w)[8]) const {
+    double x = eight(w);
+    x += swapped<4>(x);
+    if constexpr (LP >= 32) x += swapped<8>(x);
+    if constexpr (LP >= 64) x += swapped<16>(x);
+    return (float)x;
+  }
+  __device__ __forceinline__ u32x4 read(int phys) const {
+    return *reinterpret_cast<const u32x4*>(bounds + (int64_t)phys * page);
+  }
+
+ private:
+  template <int O>
+  __device__ __forceinline__ static double swapped(double x) {
+    return __builtin_bit_cast(double, lane_xor<O>(__builtin_bit_cast(uint64_t, x)));
+  }
+  __device__ __forceinline__ double eight(const u32x4 (&w)[8]) const {
+    double x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = 0.0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[i] = fma((double)elem(w[i], e), q[e], x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = deal<H>(x[i], x[i + 4]);
+    return deal<2>(deal<1>(x[0], x[1]), deal<1>(x[2], x[3]));
   }
 };
 
@@ -259,62 +285,140 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t m) {
                                    __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
 }
 
-// One workgroup an item.  Wavefront w takes a run of whole 64s: their keys stay in
-// registers (LDS false: up to 4096 pages) or in LDS.
-template <typename F, int D, bool LDS>
+// The pages of one item by one wavefront: lane l's kr[i] is the key of page 64 i + l, in
+// the first `steps` of R.
+template <int R>
+__device__ __forceinline__ void choose(const uint32_t (&kr)[R], int steps, int top,
+                                       bool all, int32_t* out) {
+const int lane = threadIdx.x & 63;
+  uint32_t there = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < steps) there += (uint32_t)__popcll(__ballot(kr[i] != 0));
+  const uint32_t keep = min((uint32_t)top, there);
+  uint32_t T = 1;
+  if (!all && keep > 0) {
+    T = 0;
+    for (int b = 31; b >= 0; --b) {
+      const uint32_t x = T | 1u << b;
+      uint32_t n = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (i < steps) n += (uint32_t)__popcll(__ballot(kr[i] >= x));
+      if (n >= keep) T = x;
+    }
+  }
+  uint32_t gts = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < steps) gts += (uint32_t)__popcll(__ballot(kr[i] > T));
+  const uint32_t need = keep - gts;
+  uint32_t gt0 = 0, eq0 = 0;
+  if (keep > 0)
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (i >= steps) break;
+      const uint64_t mg = __ballot(kr[i] > T), me = __ballot(kr[i] == T);
+      const uint32_t rg = gt0 + lanes_below(mg), re = eq0 + lanes_below(me);
+      if (kr[i] > T || (kr[i] == T && re < need))
+        out[rg + min(re, need)] = i * 64 + lane;
+      gt0 += (uint32_t)__popcll(mg);
+      eq0 += (uint32_t)__popcll(me);
+    }
+  for (int i = (int)keep + lane; i < top; i += 64) out[i] = -1;
+}
+
+// One workgroup an item.  CAP: pages that the LDS holds keys of.
+template <typename F, int D, int CAP>
 __global__ void __launch_bounds__(kSelThreads)
 page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict__ q,
                    int64_t ld_q, int n_heads, int block,
                    const typename F::st* __restrict__ bounds, int first, int last,
                    int top, int32_t* __restrict__ out) {
-  constexpr int REGS = 8;
-  __shared__ uint32_t s_keys[LDS ? kMaxPages : 1];
+  using S = Scorer<F, D>;
+  constexpr int P = S::PAGES;                   // a wavefront's pages at a time
+  __shared__ uint32_t s_keys[CAP];
   __shared__ __attribute__((aligned(16))) uint32_t s_cnt[2][3][kSelWaves];
   int row;
   const Choice c = choice_of(cv, cp, blockIdx.x, block, top, out, &row);
   const int np = c.np, g = n_heads / cv.n_kv;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = ((np + kSelWaves - 1) / kSelWaves + 63) & ~63;
-  const int lo = min(np, wave * per), hi = min(np, lo + per);
   const bool all = np <= top;                   // nothing to choose
 
-  uint32_t kr[REGS] = {};
+  if (all) {
+    for (int p = threadIdx.x; p < ((np + 63) & ~63); p += kSelThreads)
+      s_keys[p] = p < np && (unsigned)c.table[p] < (unsigned)cv.n_pages ? 0xffffffffu : 0u;
+  } else if (wave * P < np) {
+    auto place = [&](int p0) {                  // of page p0 + lane % P
+      const int p = p0 + lane % P;
+      return c.table[min(p, np - 1)];
+    };
+    auto known = [&](int id) { return (unsigned)id < (unsigned)cv.n_pages; };
+    S sc;
+    sc.prepare(bounds, cv.n_kv, c.hk);
+    constexpr int STEP = kSelWaves * P;
+    const int base = lane / S::LP * 8;          // this lane's pages in the step
+    const int mine = base + (lane & 3) + (lane & S::H ? 4 : 0);
+    u32x4 w[8];
+    int id = place(wave * P), next = place(wave * P + STEP);
+    auto load = [&](int ids) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int ph = __shfl(ids, base + i, 64);
+        w[i] = sc.read(known(ph) ? ph : 0);
+      }
+    };
+    load(id);
+    sc.init(q + (int64_t)row * ld_q + (int64_t)c.hk * g * D, g);
+#pragma unroll 1
+    for (int p0 = wave * P; p0 < np; p0 += STEP) {
+      const float x = sc.score8(w);
+      const int now = __shfl(id, mine, 64), p = p0 + mine;
+      id = next;
+      if (p0 + STEP < np) load(id);
+      next = place(p0 + 2 * STEP);
+      // (the other lanes of a page have the same)
+      if ((lane & (S::H - 4)) == 0)
+        s_keys[p] = p >= np || !known(now)             ? 0u
+                    : p < first || p >= np - last ? 0xffffffffu
+                                                  : score_key(x);
+    }
+  }
+  // keys behind the last step's, up to whole 64s
+  {
+    const int from = all ? (np + 63) & ~63 : (np + P - 1) / P * P;
+    if (from + (int)threadIdx.x < ((np + 63) & ~63)) s_keys[from + threadIdx.x] = 0;
+  }
+  __syncthreads();
+
+  constexpr int FEW = 4;                        // 64s that one wavefront ranks alone
+  if (np <= 64 * FEW) {
+    if (wave != 0) return;
+    uint32_t kr[FEW];
+#pragma unroll
+    for (int i = 0; i < FEW; ++i) kr[i] = i * 64 < np ? s_keys[i * 64 + lane] : 0u;
+    choose(kr, (np + 63) / 64, top, all, c.out);
+    return;
+  }
+  // Each wavefront counts and writes a run of whole 64s.
+  const int per = ((np + kSelWaves - 1) / kSelWaves + 63) & ~63;
+  const int lo = min(np, wave * per), hi = min(np, lo + per);
+  constexpr int REGS = CAP / kSelThreads <= 8 ? CAP / kSelThreads : 0;
+  uint32_t kr[REGS ? REGS : 1];
+#pragma unroll
+  for (int i = 0; i < REGS; ++i)
+    kr[i] = lo + i * 64 < hi ? s_keys[lo + i * 64 + lane] : 0u;
   // f(64 pages' first one, their keys) of this wavefront
   auto each = [&](auto f) {
-    if constexpr (LDS) {
-      for (int i = lo; i < hi; i += 64) f(i, s_keys[i + lane]);
-    } else {
+    if constexpr (REGS > 0) {
 #pragma unroll
       for (int i = 0; i < REGS; ++i)
         if (lo + i * 64 < hi) f(lo + i * 64, kr[i]);
+    } else {
+      for (int i = lo; i < hi; i += 64) f(i, s_keys[i + lane]);
     }
   };
-  if (lo < hi) {
-    Scorer<F, D> sc;
-    int next = c.table[min(lo + lane, np - 1)];
-    if (!all)
-      sc.init(q + (int64_t)row * ld_q + (int64_t)c.hk * g * D, g, bounds, cv.n_kv, c.hk);
-#pragma unroll 1
-    for (int i = 0; lo + i * 64 < hi; ++i) {
-      const int p = lo + i * 64 + lane;
-      const bool there = p < np && (unsigned)next < (unsigned)cv.n_pages;
-      const int phys = there ? next : 0;
-      if (p + 64 - lane < hi) next = c.table[min(p + 64, np - 1)];
-      uint32_t key = 0xffffffffu;
-      if (!all) {
-        const float x = sc.score(phys);
-        if (p >= first && p < np - last) key = score_key(x);
-      }
-      if (!there) key = 0;
-      if constexpr (LDS) {
-        s_keys[p] = key;
-      } else {
-#pragma unroll
-        for (int r = 0; r < REGS; ++r) kr[r] = r == i ? key : kr[r];
-      }
-    }
-  }
   // keys of this wavefront that are at least each of x, y, z (above 0)
   auto count = [&](uint32_t x, uint32_t y, uint32_t z, uint32_t (&cnt)[3]) {
     cnt[0] = cnt[1] = cnt[2] = 0;
@@ -325,19 +429,20 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
     });
   };
   int flip = 0;
-  // of all wavefronts; one barrier: the next call writes the other half
+  // Of all wavefronts; one barrier: the next call writes the other half.  (Each lane
+  // reads one count: all of them in every lane, 16 wavefronts of reads, took 10 us of
+  // a selection's 17.)
+  static_assert(kSelWaves == 16, "a row of lanes");
   auto total = [&](uint32_t (&cnt)[3]) {
-    if (lane == 0)
-#pragma unroll
-      for (int i = 0; i < 3; ++i) s_cnt[flip][i][wave] = cnt[i];
+    if (lane < 3) s_cnt[flip][lane][wave] = lane == 0 ? cnt[0] : lane == 1 ? cnt[1] : cnt[2];
     __syncthreads();
+    uint32_t x = s_cnt[flip][min(lane >> 4, 2)][lane & 15];
+    x += lane_xor<1>(x);
+    x += lane_xor<2>(x);
+    x += lane_xor<4>(x);
+    x += lane_xor<8>(x);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      uint32_t x = 0;
-#pragma unroll
-      for (int w = 0; w < kSelWaves; ++w) x += s_cnt[flip][i][w];
-      cnt[i] = x;
-    }
+    for (int i = 0; i < 3; ++i) cnt[i] = (uint32_t)__builtin_amdgcn_readlane((int)x, 16 * i);
     flip ^= 1;
   };
   uint32_t cnt[3];
@@ -361,13 +466,22 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
     s_cnt[flip][1][wave] = eq;
   }
   __syncthreads();
+  // sums over the wavefronts before this one, and over all
   uint32_t gt0 = 0, eq0 = 0, gts = 0;
-#pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) {
-    const uint32_t x = s_cnt[flip][0][w], y = s_cnt[flip][1][w];
-    gt0 += w < wave ? x : 0u;
-    eq0 += w < wave ? y : 0u;
-    gts += x;
+  {
+    const uint32_t x = lane < 2 * kSelWaves ? s_cnt[flip][lane >> 4][lane & 15] : 0u;
+    uint32_t before = (lane & 15) < wave ? x : 0u, sum = x;
+    before += lane_xor<1>(before);
+    before += lane_xor<2>(before);
+    before += lane_xor<4>(before);
+    before += lane_xor<8>(before);
+    sum += lane_xor<1>(sum);
+    sum += lane_xor<2>(sum);
+    sum += lane_xor<4>(sum);
+    sum += lane_xor<8>(sum);
+    gt0 = (uint32_t)__builtin_amdgcn_readlane((int)before, 0);
+    eq0 = (uint32_t)__builtin_amdgcn_readlane((int)before, 16);
+    gts = (uint32_t)__builtin_amdgcn_readlane((int)sum, 0);
   }
   const uint32_t need = keep - gts;     // of those equal to T, the first ones
   if (keep > 0)
@@ -401,11 +515,10 @@ page_select_wave_kernel(CacheView cv, ChunkPack cp, const typename F::st* __rest
   const bool all = np <= top;
   Scorer<F, D> sc;
   int next = c.table[min(lane, np - 1)];
-  if (!all)
-    sc.init(q + (int64_t)row * ld_q + (int64_t)c.hk * g * D, g, bounds, cv.n_kv, c.hk);
+  sc.prepare(bounds, cv.n_kv, c.hk);
+  if (!all) sc.init(q + (int64_t)row * ld_q + (int64_t)c.hk * g * D, g);
   uint32_t kr[kWaveSteps] = {};
   const int steps = (np + 63) / 64;
-  uint32_t there_n = 0;
 #pragma unroll 1
   for (int i = 0; i < steps; ++i) {
     const int p = i * 64 + lane;
@@ -414,45 +527,108 @@ page_select_wave_kernel(CacheView cv, ChunkPack cp, const typename F::st* __rest
     if (i + 1 < steps) next = c.table[min(p + 64, np - 1)];
     uint32_t key = 0xffffffffu;
     if (!all) {
-      const float x = sc.score(phys);
+      const float x = sc.score64(phys);
       if (p >= first && p < np - last) key = score_key(x);
     }
     if (!there) key = 0;
-    there_n += (uint32_t)__popcll(__ballot(key != 0));
 #pragma unroll
     for (int r = 0; r < kWaveSteps; ++r) kr[r] = r == i ? key : kr[r];
   }
-  const uint32_t keep = min((uint32_t)top, there_n);
-  uint32_t T = 1;
-  if (!all && keep > 0) {
-    T = 0;
-    for (int b = 31; b >= 0; --b) {
-      const uint32_t x = T | 1u << b;
-      uint32_t n = 0;
+  choose(kr, steps, top, all, c.out);
+}
+
+// 16 tokens of a sequence against pages of one key head.  Matrix op (c, e) takes element
+// e of chunk c of the lanes' pages, 16 of them by four lanes each, and the same element
+// of Q of 16 tokens, which are in LDS; lane l then holds the scores of token l % 16 and
+// pages 4 i + l / 16.
+struct TilePack {
+  int32_t first[DAVET_MAX_SEQS + 1];    // first tile of each sequence
+};
+constexpr int kTileTokens = 16, kTileThreads = 512, kTileWaves = kTileThreads / 64;
+template <typename F, int D, int CAP>
+__global__ void __launch_bounds__(kTileThreads)
+page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
+                        const typename F::st* __restrict__ q, int64_t ld_q, int n_heads,
+                        int block, const typename F::st* __restrict__ bounds, int first,
+                        int last, int top, int32_t* __restrict__ out) {
+  using st = typename F::st;
+  using S = Scorer<F, D>;
+  typedef double d4 __attribute__((ext_vector_type(4)));
+  constexpr int N = S::N, LP = S::LP, NC = LP / 4;
+  constexpr int KS = CAP + 1;                   // (tokens' keys in different banks)
+  __shared__ double s_q[2 * D][kTileTokens];
+  __shared__ uint32_t s_keys[kTileTokens * KS];
+  const int tile = blockIdx.x / cv.n_kv, hk = blockIdx.x % cv.n_kv;
+  const int s = owner(tp.first, cp.n_seqs, tile);
+  const int tok0 = (tile - tp.first[s]) * kTileTokens;
+  const int n = cp.row0[s + 1] - cp.row0[s], kv = cp.kv[s], lg = cv.lg;
+  const int nt = min(kTileTokens, n - tok0), g = n_heads / cv.n_kv;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t* table = cv.table + (int64_t)s * cv.max_pages;
+  auto pages_of = [&](int tok) {
+    return (visible_end(tok, n, kv, block) + (1 << lg) - 1) >> lg;
+  };
+  // (a later token sees no fewer)
+  const int np = pages_of(tok0 + nt - 1), mine = pages_of(tok0 + min(l16, nt - 1));
+
+  if (np > top) {
+    for (int i = threadIdx.x; i < kTileTokens * LP; i += kTileThreads) {
+      const int tok = i / LP, l = i % LP;
+      double x[N] = {};
+      const st* qp = q + (int64_t)(cp.row0[s] + tok0 + min(tok, nt - 1)) * ld_q +
+                     (int64_t)hk * g * D + l % S::H * N;
+      for (int h = 0; h < g; ++h) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(qp + (int64_t)h * D);
 #pragma unroll
-      for (int i = 0; i < kWaveSteps; ++i)
-        if (i < steps) n += (uint32_t)__popcll(__ballot(kr[i] >= x));
-      if (n >= keep) T = x;
+        for (int e = 0; e < N; ++e) x[e] += S::part(S::elem(w, e), l < S::H);
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) s_q[l * N + e][tok] = x[e];
+    }
+    __syncthreads();
+  }
+  for (int p0 = wave * 16; p0 < np; p0 += kTileWaves * 16) {
+    const int id = table[min(p0 + l16, np - 1)];
+    const bool there = p0 + l16 < np && (unsigned)id < (unsigned)cv.n_pages;
+    const uint32_t known = (uint32_t)__ballot(there);       // (16 bits, four times)
+    d4 acc[2] = {};
+    if (np > top) {
+      const st* b = bounds + ((int64_t)(there ? id : 0) * cv.n_kv + hk) * 2 * D + quad * N;
+      u32x4 w[NC];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) w[c] = *reinterpret_cast<const u32x4*>(b + c * 4 * N);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          acc[e & 1] = __builtin_amdgcn_mfma_f64_16x16x4f64(
+              (double)S::elem(w[c], e), s_q[(c * 4 + quad) * N + e][l16], acc[e & 1], 0, 0,
+              0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = 4 * i + quad, p = p0 + at;
+      uint32_t key = 0;
+      if (p < mine && (known >> at & 1))
+        key = mine <= top || p < first || p >= mine - last
+                  ? 0xffffffffu
+                  : score_key((float)(acc[0][i] + acc[1][i]));
+      s_keys[l16 * KS + p] = key;
     }
   }
-  uint32_t gts = 0;
+  __syncthreads();
+  for (int tok = wave; tok < nt; tok += kTileWaves) {
+    const int mp = pages_of(tok0 + tok), steps = (mp + 63) / 64;
+    uint32_t kr[CAP / 64];
 #pragma unroll
-  for (int i = 0; i < kWaveSteps; ++i)
-    if (i < steps) gts += (uint32_t)__popcll(__ballot(kr[i] > T));
-  const uint32_t need = keep - gts;
-  uint32_t gt0 = 0, eq0 = 0;
-  if (keep > 0)
-#pragma unroll
-    for (int i = 0; i < kWaveSteps; ++i) {
-      if (i >= steps) break;
-      const uint64_t mg = __ballot(kr[i] > T), me = __ballot(kr[i] == T);
-      const uint32_t rg = gt0 + lanes_below(mg), re = eq0 + lanes_below(me);
-      if (kr[i] > T || (kr[i] == T && re < need))
-        c.out[rg + min(re, need)] = i * 64 + lane;
-      gt0 += (uint32_t)__popcll(mg);
-      eq0 += (uint32_t)__popcll(me);
+    for (int i = 0; i < CAP / 64; ++i) {
+      const int p = i * 64 + lane;
+      kr[i] = p < mp ? s_keys[tok * KS + p] : 0u;
     }
-  for (int i = (int)keep + lane; i < top; i += 64) c.out[i] = -1;
+    choose(kr, steps, top, mp <= top,
+           out + ((int64_t)(cp.row0[s] + tok0 + tok) * cv.n_kv + hk) * top);
+  }
 }
 
 }  // namespace
@@ -537,10 +713,22 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
                   "davet_cache_page_select: pages null or not 4-byte aligned");
   ProfScope ps(KC_MISC, stream);
   const int64_t items = total * cv.n_kv;
-  // a wavefront each where they fill the chip
+  int longest = 0;
+  TilePack tp{};
+  for (int s = 0; s < n_seqs; ++s) {
+    const int n = cu_q[s + 1] - cu_q[s];
+    longest = std::max(longest, n);
+    tp.first[s + 1] = tp.first[s] + (n + kTileTokens - 1) / kTileTokens;
+  }
+  const bool tiles = longest >= 8 && most <= 1024;
   const bool waves = items >= kManyItems && most <= 64 * kWaveSteps;
-#define SELECT(F, DIM, LDS)                                                       \
-  hipLaunchKernelGGL((page_select_kernel<F, DIM, LDS>), dim3((unsigned)items),    \
+#define TILES(F, DIM, CAP)                                                        \
+  hipLaunchKernelGGL((page_select_tile_kernel<F, DIM, CAP>),                      \
+                     dim3((unsigned)(tp.first[n_seqs] * cv.n_kv)), dim3(kTileThreads), \
+                     0, stream, cv, cp, tp, (const F::st*)q, ld_q, n_heads, block, \
+                     (const F::st*)bounds, first, last, top, pages)
+#define SELECT(F, DIM, CAP)                                                       \
+  hipLaunchKernelGGL((page_select_kernel<F, DIM, CAP>), dim3((unsigned)items),    \
                      dim3(kSelThreads), 0, stream, cv, cp, (const F::st*)q, ld_q, \
                      n_heads, block, (const F::st*)bounds, first, last, top, pages)
 #define WAVES(F, DIM)                                                             \
@@ -550,9 +738,11 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
                      (const F::st*)bounds, first, last, top, pages, items)
 #define SELECT_N(F, DIM)                                                          \
   do {                                                                            \
-    if (waves) WAVES(F, DIM);                                                     \
-    else if (most <= 64 * 8 * kSelWaves) SELECT(F, DIM, false);                   \
-    else SELECT(F, DIM, true);                                                    \
+    if (tiles && most <= 512) TILES(F, DIM, 512);                                 \
+    else if (tiles) TILES(F, DIM, 1024);                                          \
+    else if (waves) WAVES(F, DIM);                                                \
+    else if (most <= 4096) SELECT(F, DIM, 4096);                                  \
+    else SELECT(F, DIM, kMaxPages);                                               \
   } while (0)
 #define SELECT_D(F) \
   do { if (cache->head_dim == 128) SELECT_N(F, 128); else SELECT_N(F, 64); } while (0)
@@ -563,6 +753,7 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
 #undef SELECT_N
 #undef WAVES
 #undef SELECT
+#undef TILES
   DAVET_HIP(hipGetLastError());
   return DAVET_OK;
 }

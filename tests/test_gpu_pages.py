@@ -94,6 +94,13 @@ SELECT = [  # dtype, new, kv, heads, kv_heads, dim, page, block, top, first, las
     ("f32", [70], [16 * 64], 16, 16, 64, 16, 1, 63, 0, 0),
     ("f32", [34], [530], 32, 32, 128, 16, 0, 5, 2, 0),
     ("f16", [2], [16 * 512], 1024, 1024, 64, 16, 0, 7, 0, 1),
+    ("bf16", [5] * 8, [100, 200, 31, 500, 5, 77, 333, 480], 32, 32, 128, 16, 1, 6, 1, 2),
+    ("f32", [7] * 10, [210] * 10, 16, 16, 64, 16, 4, 5, 0, 1),
+    ("f32", [7] * 5, [210] * 5, 30, 30, 128, 16, 1, 13, 0, 1),
+    # 16 tokens at a time over up to 1024 pages
+    ("f16", [20], [16 * 700], 2, 1, 64, 16, 1, 30, 1, 1),
+    ("f32", [9, 1], [16 * 600, 50], 4, 2, 128, 16, 0, 3, 0, 0),
+    ("bf16", [8, 0, 17], [16 * 1024, 0, 400], 3, 1, 128, 16, 1, 500, 1, 1),
 ]
 
 
