@@ -93,6 +93,31 @@ __device__ __forceinline__ int owner(const int32_t* first, int n, int at) {
   return lo;
 }
 
+// The same, and the entries that go with it, by the lanes of a wavefront: kernel
+// arguments may lie in host memory, where every step of a search would be a trip there
+// and back; so all are read at once.  (first, order and the others have an entry for
+// each lane below DAVET_MAX_SEQS, first one more.)
+struct Lanes {
+  int first, next;
+  __device__ __forceinline__ explicit Lanes(const int32_t* list) {
+    const int lane = threadIdx.x & 63;
+    first = list[lane];
+    next = list[lane + 1];
+  }
+  // the last of the first n entries that is not above `at`
+  __device__ __forceinline__ int owner(int n, int at) const {
+    const uint64_t m = __ballot((int)(threadIdx.x & 63) < n && first <= at);
+    return 63 - __builtin_clzll(m | 1);
+  }
+  __device__ __forceinline__ int start(int i) const {
+    return __builtin_amdgcn_readlane(first, i);
+  }
+  __device__ __forceinline__ int end(int i) const {
+    return __builtin_amdgcn_readlane(next, i);
+  }
+};
+static_assert(DAVET_MAX_SEQS == 64, "one a lane");
+
 // Checks of a cache and, below, of a chunk on it; both fill what kernels take.
 int check_cache(const davet_kv_cache* c, bool need_v, const char* who,
                 CacheView* out);

@@ -114,12 +114,15 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 
   // workgroups of a sequence: [key head][piece][tile, or four of them], tiles fastest
   const int b = ap.xcd ? (int)blockIdx.x >> 3 : (int)blockIdx.x;
-  const int si = owner(ap.blk, cp.n_seqs, b), s = ap.order[si];
-  const int n = cp.row0[s + 1] - cp.row0[s], kv_all = cp.kv[s];
+  const Lanes blks(ap.blk), rows(cp.row0);
+  const int orders = ap.order[lane], kvs = cp.kv[lane];
+  const int si = blks.owner(cp.n_seqs, b), s = __builtin_amdgcn_readlane(orders, si);
+  const int row_s = rows.start(s), n = rows.end(s) - row_s;
+  const int kv_all = __builtin_amdgcn_readlane(kvs, s);
   const int tiles = n * rt, units = W == 4 ? tiles : (tiles + 3) / 4;
   const int kv = listed_keys(kv_all, top, lg);
   const int np = (kv + ap.piece - 1) / ap.piece;
-  int rem = b - ap.blk[si];
+  int rem = b - blks.start(si);
   const int h_ = rem / (units * np);
   rem -= h_ * units * np;
   const int hk = ap.xcd ? ((int)blockIdx.x & 7) + 8 * h_ : h_;
@@ -127,7 +130,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int tile = W == 4 ? rem - piece * units : (rem - piece * units) * 4 + wave;
   if (tile >= tiles) return;                    // (W = 1: no barrier follows)
   const int tok = tile / rt, r0 = (tile - tok * rt) * 16, nr = min(16, g - r0);
-  const int row = cp.row0[s] + tok;
+  const int row = row_s + tok;
   // cache indices below it are visible
   const int lim = visible_end(tok, n, kv_all, block);
   const int begin = piece * ap.piece, end = min(begin + ap.piece, kv);

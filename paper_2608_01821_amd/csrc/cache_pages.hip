@@ -27,6 +27,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
 
@@ -273,9 +274,12 @@ __device__ __forceinline__ Choice choice_of(const CacheView& cv, const ChunkPack
   Choice c;
   *row = (int)(item / cv.n_kv);
   c.hk = (int)(item - (int64_t)*row * cv.n_kv);
-  c.s = owner(cp.row0, cp.n_seqs, *row);
-  const int n = cp.row0[c.s + 1] - cp.row0[c.s];
-  c.np = (visible_end(*row - cp.row0[c.s], n, cp.kv[c.s], block) + (1 << cv.lg) - 1) >> cv.lg;
+  const Lanes rows(cp.row0);
+  const int kvs = cp.kv[threadIdx.x & 63];
+  c.s = rows.owner(cp.n_seqs, *row);
+  const int row0 = rows.start(c.s), n = rows.end(c.s) - row0;
+  const int kv = __builtin_amdgcn_readlane(kvs, c.s);
+  c.np = (visible_end(*row - row0, n, kv, block) + (1 << cv.lg) - 1) >> cv.lg;
   c.table = cv.table + (int64_t)c.s * cv.max_pages;
   c.out = out + item * top;
   return c;
@@ -285,46 +289,65 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t m) {
                                    __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
 }
 
-// The pages of one item by one wavefront: lane l's kr[i] is the key of page 64 i + l, in
-// the first `steps` of R.
+// the largest of the lanes' values
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+  x = max(x, lane_xor<1>(x));
+  x = max(x, lane_xor<2>(x));
+  x = max(x, lane_xor<4>(x));
+  x = max(x, lane_xor<8>(x));
+  x = max(x, lane_xor<16>(x));
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)max(x, lane_xor<32>(x)));
+}
+
+// The pages of one item by one wavefront: lane l's kr[i] is the key of page 64 i + l, 0
+// past the last one.  (No loop over them stops early: 16 branches a round took 7 us of
+// a selection's 12.)
 template <int R>
-__device__ __forceinline__ void choose(const uint32_t (&kr)[R], int steps, int top,
-                                       bool all, int32_t* out) {
-const int lane = threadIdx.x & 63;
-  uint32_t there = 0;
+__device__ __forceinline__ void choose(const uint32_t (&kr)[R], int top, bool all,
+                                       int32_t* out) {
+  const int lane = threadIdx.x & 63;
+  auto at_least = [&](uint32_t x) {
+    uint32_t n = 0;
 #pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (i < steps) there += (uint32_t)__popcll(__ballot(kr[i] != 0));
-  const uint32_t keep = min((uint32_t)top, there);
-  uint32_t T = 1;
+    for (int i = 0; i < R; ++i) n += (uint32_t)__popcll(__ballot(kr[i] >= x));
+    return n;
+  };
+  const uint32_t keep = min((uint32_t)top, at_least(1u));
+  uint32_t T = 1;                       // key of the last page taken
   if (!all && keep > 0) {
-    T = 0;
-    for (int b = 31; b >= 0; --b) {
-      const uint32_t x = T | 1u << b;
-      uint32_t n = 0;
+    T = 0xffffffffu;
+    if (at_least(T) < keep) {           // (that many are sure)
+      // the rest from what their keys begin with
+      uint32_t least = 0xfffffffeu, most = 1;
 #pragma unroll
-      for (int i = 0; i < R; ++i)
-        if (i < steps) n += (uint32_t)__popcll(__ballot(kr[i] >= x));
-      if (n >= keep) T = x;
+      for (int i = 0; i < R; ++i) {
+        const bool ranked = kr[i] - 1u < 0xfffffffeu;
+        least = ranked ? min(least, kr[i]) : least;
+        most = ranked ? max(most, kr[i]) : most;
+      }
+      least = ~lanes_max(~least);
+      most = lanes_max(most);
+      const int bits = 32 - __builtin_clz((least ^ most) | 1);
+      T = most >> (bits - 1) >> 1 << (bits - 1) << 1;
+      for (int b = bits - 1; b >= 0; --b) {
+        const uint32_t x = T | 1u << b;
+        if (at_least(x) >= keep) T = x;
+      }
     }
   }
   uint32_t gts = 0;
 #pragma unroll
-  for (int i = 0; i < R; ++i)
-    if (i < steps) gts += (uint32_t)__popcll(__ballot(kr[i] > T));
-  const uint32_t need = keep - gts;
+  for (int i = 0; i < R; ++i) gts += (uint32_t)__popcll(__ballot(kr[i] > T));
+  const uint32_t need = keep - gts;     // of those equal to T, the first ones
   uint32_t gt0 = 0, eq0 = 0;
-  if (keep > 0)
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      if (i >= steps) break;
-      const uint64_t mg = __ballot(kr[i] > T), me = __ballot(kr[i] == T);
-      const uint32_t rg = gt0 + lanes_below(mg), re = eq0 + lanes_below(me);
-      if (kr[i] > T || (kr[i] == T && re < need))
-        out[rg + min(re, need)] = i * 64 + lane;
-      gt0 += (uint32_t)__popcll(mg);
-      eq0 += (uint32_t)__popcll(me);
-    }
+  for (int i = 0; i < R; ++i) {
+    const uint64_t mg = __ballot(kr[i] > T), me = __ballot(kr[i] == T);
+    const uint32_t rg = gt0 + lanes_below(mg), re = eq0 + lanes_below(me);
+    if (kr[i] > T || (kr[i] == T && re < need)) out[rg + min(re, need)] = i * 64 + lane;
+    gt0 += (uint32_t)__popcll(mg);
+    eq0 += (uint32_t)__popcll(me);
+  }
   for (int i = (int)keep + lane; i < top; i += 64) out[i] = -1;
 }
 
@@ -392,13 +415,22 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
   }
   __syncthreads();
 
-  constexpr int FEW = 4;                        // 64s that one wavefront ranks alone
-  if (np <= 64 * FEW) {
-    if (wave != 0) return;
-    uint32_t kr[FEW];
+  // up to 1024 pages are ranked by one wavefront
+  auto few = [&](auto r) {
+    constexpr int R = decltype(r)::value;
+    uint32_t kr[R];
 #pragma unroll
-    for (int i = 0; i < FEW; ++i) kr[i] = i * 64 < np ? s_keys[i * 64 + lane] : 0u;
-    choose(kr, (np + 63) / 64, top, all, c.out);
+    for (int i = 0; i < R; ++i) {
+      const uint32_t k = s_keys[i * 64 + lane];
+      kr[i] = i * 64 < np ? k : 0u;
+    }
+    choose(kr, top, all, c.out);
+  };
+  if (np <= 1024) {
+    if (wave != 0) return;
+    if (np <= 256) few(std::integral_constant<int, 4>());
+    else if (np <= 512) few(std::integral_constant<int, 8>());
+    else few(std::integral_constant<int, 16>());
     return;
   }
   // Each wavefront counts and writes a run of whole 64s.
@@ -534,7 +566,7 @@ page_select_wave_kernel(CacheView cv, ChunkPack cp, const typename F::st* __rest
 #pragma unroll
     for (int r = 0; r < kWaveSteps; ++r) kr[r] = r == i ? key : kr[r];
   }
-  choose(kr, steps, top, all, c.out);
+  choose(kr, top, all, c.out);
 }
 
 // 16 tokens of a sequence against pages of one key head.  Matrix op (c, e) takes element
@@ -559,9 +591,12 @@ page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
   __shared__ double s_q[2 * D][kTileTokens];
   __shared__ uint32_t s_keys[kTileTokens * KS];
   const int tile = blockIdx.x / cv.n_kv, hk = blockIdx.x % cv.n_kv;
-  const int s = owner(tp.first, cp.n_seqs, tile);
-  const int tok0 = (tile - tp.first[s]) * kTileTokens;
-  const int n = cp.row0[s + 1] - cp.row0[s], kv = cp.kv[s], lg = cv.lg;
+  const Lanes tiles(tp.first), rows(cp.row0);
+  const int kvs = cp.kv[threadIdx.x & 63];
+  const int s = tiles.owner(cp.n_seqs, tile);
+  const int tok0 = (tile - tiles.start(s)) * kTileTokens;
+  const int row0 = rows.start(s), n = rows.end(s) - row0, lg = cv.lg;
+  const int kv = __builtin_amdgcn_readlane(kvs, s);
   const int nt = min(kTileTokens, n - tok0), g = n_heads / cv.n_kv;
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -576,7 +611,7 @@ page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
     for (int i = threadIdx.x; i < kTileTokens * LP; i += kTileThreads) {
       const int tok = i / LP, l = i % LP;
       double x[N] = {};
-      const st* qp = q + (int64_t)(cp.row0[s] + tok0 + min(tok, nt - 1)) * ld_q +
+      const st* qp = q + (int64_t)(row0 + tok0 + min(tok, nt - 1)) * ld_q +
                      (int64_t)hk * g * D + l % S::H * N;
       for (int h = 0; h < g; ++h) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(qp + (int64_t)h * D);
@@ -619,15 +654,15 @@ page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
   }
   __syncthreads();
   for (int tok = wave; tok < nt; tok += kTileWaves) {
-    const int mp = pages_of(tok0 + tok), steps = (mp + 63) / 64;
+    const int mp = pages_of(tok0 + tok);
     uint32_t kr[CAP / 64];
 #pragma unroll
     for (int i = 0; i < CAP / 64; ++i) {
       const int p = i * 64 + lane;
       kr[i] = p < mp ? s_keys[tok * KS + p] : 0u;
     }
-    choose(kr, steps, top, mp <= top,
-           out + ((int64_t)(cp.row0[s] + tok0 + tok) * cv.n_kv + hk) * top);
+    choose(kr, top, mp <= top,
+           out + ((int64_t)(row0 + tok0 + tok) * cv.n_kv + hk) * top);
   }
 }
 
