@@ -35,72 +35,102 @@ __device__ __forceinline__ uint64_t value_key(double x) {
 __device__ __forceinline__ double value_of(uint64_t k) {
   return __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
 }
-// steps O, O / 2, .. 1 of a bitonic join: of each pair of lanes the better one to the
-// lower lane
-template <int O>
-__device__ __forceinline__ void settle(Cand& c) {
+// One step of a bitonic network: of each pair (l, l ^ O) the better one to the lower
+// lane, or, where lane & S, or with `up`, to the upper one (both: the lower again).
+template <int O, int S>
+__device__ __forceinline__ void exchange(Cand& c, bool up) {
   const Cand o = {lane_xor<O>(c.v), lane_xor<O>(c.key), lane_xor<O>(c.row)};
-  const bool lower = (threadIdx.x & O) == 0;
+  const bool lower = ((threadIdx.x & O) == 0) == (((threadIdx.x & S & 63) == 0) != up);
   if (lower != better(c, o)) c = o;
-  if constexpr (O > 1) settle<O / 2>(c);
+}
+// steps O, O / 2, .. 1
+template <int O, int S>
+__device__ __forceinline__ void exchanges(Cand& c, bool up) {
+  exchange<O, S>(c, up);
+  if constexpr (O > 1) exchanges<O / 2, S>(c, up);
 }
 // the 64 best of two lists in order, the second one given in reverse
 __device__ __forceinline__ void join(Cand& c, const Cand& reversed) {
   if (better(reversed, c)) c = reversed;
-  settle<32>(c);
+  exchanges<32, 64>(c, false);
 }
 
-// Every (beam, slice) list is one item; the wavefronts take them in turn, the loads of
-// a few at a time.
-constexpr int kJoinWaves = 16, kItems = 4;
+// First every row's base, score - lse, four rows a wavefront, 16 lanes for the slices
+// of each.  Then the lists, each in order: a wavefront takes 64 / P of them at a time, P
+// the power of two that holds k, every other one in reverse, and merges them pair by
+// pair (k = 4: 18 steps for 16 lists, where a join each is 96).
+constexpr int kJoinWaves = 16;
+static_assert(kMaxSlices <= 16 && DAVET_MAX_BEAMS <= 4 * kJoinWaves, "lanes of a row");
 __global__ void __launch_bounds__(64 * kJoinWaves)
-beam_join_kernel(int rows, int beams, int slices, int k,
+beam_join_kernel(int rows, int beams, int slices, int k, int P,
                  const char* __restrict__ part, const float* scores,
                  const int32_t* __restrict__ done, int pad, float* out_scores,
                  int32_t* __restrict__ out_rows, int32_t* __restrict__ out_tokens) {
   __shared__ uint64_t s_v[kJoinWaves / 2][64], s_key[kJoinWaves / 2][64];
   __shared__ uint32_t s_row[kJoinWaves / 2][64];
+  __shared__ double s_base[DAVET_MAX_BEAMS];    // (NaN: nothing to offer)
+  __shared__ double s_over[DAVET_MAX_BEAMS];    // the score of a row that is over, or NaN
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t* lists = reinterpret_cast<const uint64_t*>(part);
-  const Stat* stats = reinterpret_cast<const Stat*>(lists + (int64_t)rows * slices * k);
-  const int row0 = blockIdx.x * beams, items = beams * slices;
-  Cand best = {0, 0, 0xffffffffu};
-  for (int i0 = wave; i0 < items; i0 += kJoinWaves * kItems) {
-    uint64_t list[kItems];
-    Stat s[kItems];
-    float score[kItems];
-    int over[kItems];
-#pragma unroll
-    for (int u = 0; u < kItems; ++u) {
-      const int it = min(i0 + u * kJoinWaves, items - 1), row = row0 + it / slices;
-      score[u] = scores[row];
-      over[u] = done ? done[row] : 0;
-      // entry j in lane 63 - j: ascending, as the join takes it.  (What a row that is
-      // over left unwritten is not used.)
-      list[u] = 63 - lane < k ? lists[((int64_t)row0 * slices + it) * k + 63 - lane] : 0;
-      s[u] = lane < slices ? stats[(int64_t)row * slices + lane] : stat_none();
-    }
-#pragma unroll
-    for (int u = 0; u < kItems; ++u) {
-      const int it = i0 + u * kJoinWaves;
-      if (it >= items) break;
-      const uint32_t row = row0 + it / slices;
-      Cand c = {0, 0, 0xffffffffu};
-      if (over[u]) {
-        if (it % slices == 0 && lane == 63 && fabsf(score[u]) < INFINITY)
-          c = {value_key((double)score[u]), top_key(0.f, pad), row};
-      } else {
-        const Stat a = stat_wave(s[u]);
-        const double base = (double)score[u] - ((double)a.m + log((double)a.S));
-        if (list[u] && fabs(base) < INFINITY)
-          c = {value_key(base + (double)key_value(list[u])), list[u], row};
-      }
-      join(best, c);
+  const int row0 = blockIdx.x * beams, lists = beams * slices;
+  const uint64_t* keys = reinterpret_cast<const uint64_t*>(part);
+  const Stat* stats = reinterpret_cast<const Stat*>(keys + (int64_t)rows * slices * k);
+  keys += (int64_t)row0 * slices * k;
+
+  const int per = 64 / P, chunks = (lists + per - 1) / per;
+  auto key_of = [&](int chunk, bool up) {       // this lane's entry
+    const int run = lane / P, l = chunk * per + run;
+    const int j = ((run & 1) != 0) != up ? P - 1 - lane % P : lane % P;
+    return l < lists && j < k ? keys[(int64_t)l * k + j] : 0;
+  };
+  // (what a row that is over left unwritten is not used)
+  uint64_t next = wave < chunks ? key_of(wave, false) : 0;
+  {
+    const int b = wave * 4 + lane / 16, sl = lane % 16;
+    const float score = b < beams ? scores[row0 + b] : 0.f;
+    const int over = b < beams && done ? done[row0 + b] : 0;
+    Stat s = stat_none();
+    if (b < beams && sl < slices && !over) s = stats[((int64_t)row0 + b) * slices + sl];
+    s = stat_step<1>(s);
+    s = stat_step<2>(s);
+    s = stat_step<4>(s);
+    s = stat_step<8>(s);
+    const double base = (double)score - ((double)s.m + log((double)s.S));
+    if (b < beams && sl == 0) {
+      s_base[b] = !over && fabs(base) < INFINITY ? base : __builtin_nan("");
+      s_over[b] = over && fabsf(score) < INFINITY ? (double)score : __builtin_nan("");
     }
   }
+  __syncthreads();
+  const Cand none = {0, 0, 0xffffffffu};
+  Cand best = none;
+  for (int chunk = wave; chunk < chunks; chunk += kJoinWaves) {
+    const bool up = chunk != wave;              // (the first one as it is kept)
+    const uint64_t key = next;
+    if (chunk + kJoinWaves < chunks) next = key_of(chunk + kJoinWaves, true);
+    const int run = lane / P, l = chunk * per + run, b = min(l / slices, beams - 1);
+    const bool first = l < lists && l % slices == 0 &&
+                       lane % P == (((run & 1) != 0) != up ? P - 1 : 0);
+    const double base = s_base[b], over = s_over[b];
+    Cand c = none;
+    if (base == base && key)
+      c = {value_key(base + (double)key_value(key)), key, (uint32_t)(row0 + b)};
+    if (over == over && first) c = {value_key(over), top_key(0.f, pad), (uint32_t)(row0 + b)};
+    if (P < 2) exchanges<1, 2>(c, up);
+    if (P < 4) exchanges<2, 4>(c, up);
+    if (P < 8) exchanges<4, 8>(c, up);
+    if (P < 16) exchanges<8, 16>(c, up);
+    if (P < 32) exchanges<16, 32>(c, up);
+    if (P < 64) exchanges<32, 64>(c, up);
+    if (up)
+      join(best, c);
+    else
+      best = c;
+  }
+  const int active = min(kJoinWaves, chunks);
 #pragma unroll
   for (int o = 1; o < kJoinWaves; o <<= 1) {
+    if (o >= active) break;
     const int at = wave / (2 * o);
     if ((wave & (2 * o - 1)) == o) {
       s_v[at][lane] = best.v;
@@ -108,7 +138,7 @@ beam_join_kernel(int rows, int beams, int slices, int k,
       s_row[at][lane] = best.row;
     }
     __syncthreads();
-    if ((wave & (2 * o - 1)) == 0)
+    if ((wave & (2 * o - 1)) == 0 && wave + o < active)
       join(best, {s_v[at][63 - lane], s_key[at][63 - lane], s_row[at][63 - lane]});
     __syncthreads();
   }
@@ -246,9 +276,11 @@ extern "C" int davet_beam_select(int32_t groups, int32_t beams, int32_t vocab,
     DAVET_HIP(hipGetLastError());
   }
 #undef ROWS
+  int P = 1;
+  while (P < top) P *= 2;
   ProfScope ps(KC_MISC, stream);
   hipLaunchKernelGGL(beam_join_kernel, dim3(groups), dim3(64 * kJoinWaves), 0, stream,
-                     rows, beams, slices, top, part, scores, done, pad, out_scores,
+                     rows, beams, slices, top, P, part, scores, done, pad, out_scores,
                      out_rows, out_tokens);
   DAVET_HIP(hipGetLastError());
   return DAVET_OK;
