@@ -313,7 +313,7 @@ __device__ __forceinline__ void choose(const uint32_t (&kr)[R], int top, bool al
     return n;
   };
   const uint32_t keep = min((uint32_t)top, at_least(1u));
-  uint32_t T = 1;                       // key of the last page taken
+  uint32_t T = 1;                       // key of the last page taken, or one below it
   if (!all && keep > 0) {
     T = 0xffffffffu;
     if (at_least(T) < keep) {           // (that many are sure)
@@ -330,8 +330,12 @@ __device__ __forceinline__ void choose(const uint32_t (&kr)[R], int top, bool al
       const int bits = 32 - __builtin_clz((least ^ most) | 1);
       T = most >> (bits - 1) >> 1 << (bits - 1) << 1;
       for (int b = bits - 1; b >= 0; --b) {
-        const uint32_t x = T | 1u << b;
-        if (at_least(x) >= keep) T = x;
+        const uint32_t x = T | 1u << b, n = at_least(x);
+        if (n == keep) {                // (a border between keys: half the rounds)
+          T = x - 1;
+          break;
+        }
+        if (n > keep) T = x;
       }
     }
   }
@@ -487,7 +491,12 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
     for (int b = 30; b >= 0; b -= 2) {
       count(T | 1u << b, T | 2u << b, T | 3u << b, cnt);
       total(cnt);
-      T |= (cnt[2] >= keep ? 3u : cnt[1] >= keep ? 2u : cnt[0] >= keep ? 1u : 0u) << b;
+      const uint32_t d = cnt[2] >= keep ? 3u : cnt[1] >= keep ? 2u : cnt[0] >= keep ? 1u : 0u;
+      T |= d << b;
+      if (d > 0 && cnt[d - 1] == keep) {        // a border between keys
+        --T;
+        break;
+      }
     }
   }
   // above T, and equal to it, in each wavefront
