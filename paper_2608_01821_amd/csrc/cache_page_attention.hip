@@ -37,33 +37,18 @@ __host__ __device__ inline int listed_keys(int kv, int top, int lg) {
   return (top < np ? top : np) << lg;
 }
 
-// 64 consecutive entries of a token's list, one a lane: the pages listed and where they
-// are (-1: not below n); entries asked for must not fall behind `base`.
+// 64 consecutive entries of a token's list, one a lane: where each page starts (a byte of
+// the pools; 0 for none) and how many of its first keys the token sees (0 for none).
+// Worked out for all at once; a tile then only picks its own.
 struct ListIds {
-  const int32_t* list;
-  const int32_t* row;
-  int top, n, base, ids, pages;
-  __device__ __forceinline__ void init(const int32_t* l, int t, const int32_t* r,
-                                       int np) {
-    list = l;
-    top = t;
-    row = r;
-    n = np;
-    base = -64;
-    ids = pages = -1;
+  uint32_t lo, hi;
+  int vis, base;
+  __device__ __forceinline__ int64_t at(int entry) const {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, entry - base) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)lo, entry - base));
   }
-  __device__ __forceinline__ void need(int entry) {
-    if (entry - base < 64) return;
-    base = entry;
-    const int e = entry + (int)(threadIdx.x & 63);
-    pages = e < top ? list[e] : -1;
-    ids = (unsigned)pages < (unsigned)n ? row[pages] : -1;
-  }
-  __device__ __forceinline__ int where(int entry) const {
-    return __builtin_amdgcn_readlane(ids, entry - base);
-  }
-  __device__ __forceinline__ int page(int entry) const {
-    return __builtin_amdgcn_readlane(pages, entry - base);
+  __device__ __forceinline__ int sees(int entry) const {
+    return __builtin_amdgcn_readlane(vis, entry - base);
   }
 };
 
@@ -135,75 +120,72 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int lim = visible_end(tok, n, kv_all, block);
   const int begin = piece * ap.piece, end = min(begin + ap.piece, kv);
 
+  const int32_t* list = lists + ((int64_t)row * cv.n_kv + hk) * top;
+  const int32_t* table = cv.table + (int64_t)s * cv.max_pages;
   ListIds ids;
-  ids.init(lists + ((int64_t)row * cv.n_kv + hk) * top, top,
-           cv.table + (int64_t)s * cv.max_pages, (kv_all + psz - 1) >> lg);
-
-  // Where 16 listed keys are (a byte of the pools), the last row there that is a cached
-  // token, and how many of them nobody sees: the last ones, or all (then anything may
-  // be read: the first page).
-  struct Group { int64_t at; int last, hidden; };
-  auto group = [&](int key) {
-    Group r = {0, 15, 16};
-    if (key >= end) return r;
-    ids.need(key >> lg);
-    const int phys = ids.where(key >> lg), off = key & (psz - 1);
-    const int first = (ids.page(key >> lg) << lg) + off;
-    if ((unsigned)phys >= (unsigned)cv.n_pages || first >= lim) return r;
-    r.at = ((((int64_t)phys * cv.n_kv + hk) << lg) + off) * RB;
-    r.last = min(15, kv_all - 1 - first);
-    r.hidden = max(0, first + 16 - lim);
-    return r;
+  ids.base = -64;
+  auto need = [&](int entry) {
+    if (entry - ids.base < 64) return;
+    ids.base = entry;
+    const int e = entry + lane;
+    const int page = e < kv >> lg ? list[e] : -1;
+    const bool listed = (unsigned)page < (unsigned)((kv_all + psz - 1) >> lg);
+    const int phys = listed ? table[page] : -1;
+    const bool there = (unsigned)phys < (unsigned)cv.n_pages;
+    const uint64_t at =
+        there ? (uint64_t)((((int64_t)phys * cv.n_kv + hk) << lg) * RB) : 0;
+    ids.lo = (uint32_t)at;
+    ids.hi = (uint32_t)(at >> 32);
+    ids.vis = there ? min(psz, max(0, lim - (page << lg))) : 0;
   };
+  // Where 16 listed keys are, and how many of them nobody sees: the last ones.  All 16
+  // are read: what lies behind the cached ones is still their page's, or, for a hole and
+  // behind the list's end, the first page's.
+  struct Group { int64_t at; int hidden; };
   struct Tile16 { Group g[GR]; };
   auto tile_at = [&](int k0) {
+    // (a tile's pages are in one window: windows start at a tile, and hold whole ones)
+    need(k0 >> lg);
     Tile16 t;
 #pragma unroll
-    for (int i = 0; i < GR; ++i) t.g[i] = group(k0 + i * 16);
+    for (int i = 0; i < GR; ++i) {
+      const int key = k0 + i * 16, off = key & (psz - 1);
+      t.g[i].at = ids.at(key >> lg) + off * RB;
+      t.g[i].hidden = 16 - min(16, max(0, ids.sees(key >> lg) - off));
+    }
     return t;
   };
   char* const kbuf = smem + wave * KB;
   typedef uint32_t vreg __attribute__((ext_vector_type(F32 ? 4 : VD / 2)));
   vreg vr[GR][4][VC];
   // Row r = j RPI + lane / C of a group, chunk lane % C of its place in LDS, holds
-  // chunk k_slot(r, lane % C) of memory.  Rows past the last cached one repeat it.
+  // chunk k_slot(r, lane % C) of memory.
   auto load_k = [&](const Tile16& t) {
+    constexpr int N = 16 / T::RPI, RUN = N < 4 ? N : 4;
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
       const char* p = static_cast<const char*>(cv.k) + t.g[i].at;
-      char* to = kbuf + i * 16 * RB;
-      constexpr int N = 16 / T::RPI, RUN = N < 4 ? N : 4;
-      if (t.g[i].last >= 15) {
 #pragma unroll
-        for (int j = 0; j < N; j += RUN) {
-          uint32_t at[RUN];
+      for (int j = 0; j < N; j += RUN) {
+        uint32_t at[RUN];
 #pragma unroll
-          for (int u = 0; u < RUN; ++u)
-            at[u] = (uint32_t)(lane * 16) ^
-                    (T::k_slot((j + u) * T::RPI + lane / T::C, 0) * 16);
-          dma16_run(p + j * 1024, at, to + j * 1024);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const int lr = j * T::RPI + lane / T::C;
-          dma16(p, (uint32_t)min(lr, t.g[i].last) * RB + T::k_slot(lr, lane % T::C) * 16,
-                to + j * 1024);
-        }
+        for (int u = 0; u < RUN; ++u)
+          at[u] = (uint32_t)(lane * 16) ^
+                  (T::k_slot((j + u) * T::RPI + lane / T::C, 0) * 16);
+        dma16_run(p + j * 1024, at, kbuf + i * 16 * RB + j * 1024);
       }
     }
   };
+  const uint32_t v_at = quad * 4 * RB + l16 * (int)sizeof(vreg);
   auto load_v = [&](const Tile16& t) {
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
       const char* p = static_cast<const char*>(cv.v) + t.g[i].at;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t o = min(quad * 4 + e, t.g[i].last) * RB + l16 * (int)sizeof(vreg);
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int c = 0; c < VC; ++c)
-          vr[i][e][c] = *reinterpret_cast<const vreg*>(p + (o + c * 256));
-      }
+          vr[i][e][c] = *reinterpret_cast<const vreg*>(p + (v_at + e * RB + c * 256));
     }
   };
 
