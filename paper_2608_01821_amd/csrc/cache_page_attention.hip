@@ -22,9 +22,9 @@
 // values, and the next values while it multiplies keys.  Rows of Q past the last head
 // repeat it.
 //
-// Four wavefronts share a list's keys and are joined in LDS, or, where there are lists
-// enough to fill the chip, each has its own.  A list may also be cut into pieces, which
-// a second launch joins in order (cache_attn.h).
+// Eight wavefronts share a list's keys and are joined in LDS; four, a piece of a long
+// list, and a second launch joins the pieces in order (cache_attn.h); or, where there
+// are lists enough to fill the chip, each has its own.
 
 #include "cache_attn.h"
 
@@ -68,9 +68,10 @@ __device__ __forceinline__ f32x4 mm16(typename Frag<F>::v8 a, typename Frag<F>::
   return F::mfma16(a, b, c);
 }
 
-// W: wavefronts that share a list (4, 1: each has its own).
+// W: wavefronts that share a list (4, 8; 1: each of four has its own).
 template <typename F, int D, int W>
-__global__ void __launch_bounds__(256, F::dtype == DAVET_F32 && D == 128 ? 2 : 3)
+__global__ void __launch_bounds__(W == 8 ? 512 : 256,
+                                  W == 8 ? 1 : F::dtype == DAVET_F32 && D == 128 ? 2 : 3)
 page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
                  const typename F::st* __restrict__ q, int64_t ld_q,
                  typename F::st* __restrict__ out, int64_t ld_o,
@@ -89,9 +90,10 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   using T = Tile<F, D>;
   constexpr int KB = KT * RB;                   // a tile of keys, 4 or 8 KB
   // each wavefront's keys; then O of its rows, as large
-  __shared__ __attribute__((aligned(1024))) char smem[4 * KB];
+  constexpr int WAVES = W == 8 ? 8 : 4;
+  __shared__ __attribute__((aligned(1024))) char smem[WAVES * KB];
   static_assert(KB == 16 * D * 4, "O takes the keys' place");
-  __shared__ float s_m[4][16], s_l[4][16];
+  __shared__ float s_m[WAVES][16], s_l[WAVES][16];
 
   const int g = n_heads / cv.n_kv, rt = (g + 15) / 16, lg = cv.lg, psz = 1 << lg;
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
@@ -104,7 +106,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int si = blks.owner(cp.n_seqs, b), s = __builtin_amdgcn_readlane(orders, si);
   const int row_s = rows.start(s), n = rows.end(s) - row_s;
   const int kv_all = __builtin_amdgcn_readlane(kvs, s);
-  const int tiles = n * rt, units = W == 4 ? tiles : (tiles + 3) / 4;
+  const int tiles = n * rt, units = W > 1 ? tiles : (tiles + 3) / 4;
   const int kv = listed_keys(kv_all, top, lg);
   const int np = (kv + ap.piece - 1) / ap.piece;
   int rem = b - blks.start(si);
@@ -112,7 +114,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   rem -= h_ * units * np;
   const int hk = ap.xcd ? ((int)blockIdx.x & 7) + 8 * h_ : h_;
   const int piece = rem / units;
-  const int tile = W == 4 ? rem - piece * units : (rem - piece * units) * 4 + wave;
+  const int tile = W > 1 ? rem - piece * units : (rem - piece * units) * 4 + wave;
   if (tile >= tiles) return;                    // (W = 1: no barrier follows)
   const int tok = tile / rt, r0 = (tile - tok * rt) * 16, nr = min(16, g - r0);
   const int row = row_s + tok;
@@ -206,7 +208,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
 
   constexpr int NV = GR * 4 * VC;       // loads of V a tile
   constexpr int STEP = W * KT;
-  int k0 = begin + (W == 4 ? wave * KT : 0);
+  int k0 = begin + (W > 1 ? wave * KT : 0);
   Tile16 cur = {};
   if (k0 < end) {
     cur = tile_at(k0);
@@ -401,15 +403,16 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       s_l[wave][l16] = l_run;
     }
     __syncthreads();
-    constexpr int DP = D / 16;
-    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * DP;
+    // a row's dims over 16 threads, or 32
+    constexpr int DT = W * 4, DP = D / DT;
+    const int r = threadIdx.x / DT, d0 = threadIdx.x % DT * DP;
     if (r >= nr) return;
-    float m = -INFINITY, l = 0.f, wt[4];
+    float m = -INFINITY, l = 0.f, wt[W];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, s_m[w][r]);
-    bool use[4];
+    for (int w = 0; w < W; ++w) m = fmaxf(m, s_m[w][r]);
+    bool use[W];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       use[w] = s_l[w][r] != 0.f;        // (NaN scores: sum NaN, maximum -inf)
       wt[w] = use[w] ? __builtin_amdgcn_exp2f((s_m[w][r] - m) * sc_.c) : 0.f;
       if (use[w]) l += wt[w] * s_l[w][r];
@@ -419,16 +422,14 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
     for (int i = 0; i < DP; ++i) {
       acc[i] = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
+      for (int w = 0; w < W; ++w)
         if (use[w]) acc[i] += wt[w] * o_at(w, r, d0 + i);
     }
     if (ap.pieces > 1) {
       const int64_t at = (int64_t)piece * part_rows + head + r;
       float* po = part + at * D + d0;
 #pragma unroll
-      for (int i = 0; i < DP; i += 4)
-        *reinterpret_cast<f32x4*>(po + i) =
-            f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+      for (int i = 0; i < DP; ++i) po[i] = acc[i];
       if (d0 == 0) {
         float* pm = part + (int64_t)ap.pieces * part_rows * D + at * 2;
         pm[0] = m;
@@ -439,9 +440,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
       st* op = out + (int64_t)row * ld_o + (int64_t)(hk * g + r0 + r) * D + d0;
       if constexpr (F32) {
 #pragma unroll
-        for (int i = 0; i < DP; i += 4)
-          *reinterpret_cast<f32x4*>(op + i) = f32x4{acc[i] * inv, acc[i + 1] * inv,
-                                                    acc[i + 2] * inv, acc[i + 3] * inv};
+        for (int i = 0; i < DP; ++i) op[i] = acc[i] * inv;
       } else {
         typedef uint32_t words __attribute__((ext_vector_type(DP / 2)));
         words x;
@@ -466,24 +465,35 @@ int run_page_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   ChunkPack keys = cp;                  // with the keys of the lists
   for (int s = 0; s < cp.n_seqs; ++s)
     keys.kv[s] = listed_keys(cp.kv[s], top, cv.lg);
-  const bool alone = (int64_t)cp.row0[cp.n_seqs] * rt * cv.n_kv >= 2048;
+  const int64_t items = (int64_t)cp.row0[cp.n_seqs] * rt * cv.n_kv;
+  int longest = 0;
+  for (int s = 0; s < cp.n_seqs; ++s)
+    if (cp.row0[s + 1] > cp.row0[s]) longest = std::max(longest, keys.kv[s]);
+  // 16 bits, 32 heads of 128 over 8: lists of 1024 keys of one, eight and sixteen tokens
+  // 11.5, 14.1 and 19.2 us in pieces, joined by a second launch, 10.2, 12.0 and 15.0 by
+  // eight wavefronts a list; of 512 keys of 32 tokens 19.5 and 15.2; of 2048 keys of one
+  // token 11.6 and 14.5.  512 tokens, 512 keys: 73 us by four, 66 by one.
+  const int W = items >= 2048 ? 1 : longest <= 1024 ? 8 : 4;
   auto units = [&](int s) {
     const int64_t t = (int64_t)(cp.row0[s + 1] - cp.row0[s]) * rt;
-    return alone ? (t + 3) / 4 : t;
+    return W > 1 ? t : (t + 3) / 4;
   };
-  const AttnPlan ap = plan_attn(keys, cv.n_kv, units, alone ? 1 : 256 * 3, 128, 128,
-                                alone ? 1 << 30 : 384, alone ? 1 : max_pieces(rows));
+  const AttnPlan ap =
+      W == 4 ? plan_attn(keys, cv.n_kv, units, 256 * 3, 128, 128, 384, max_pieces(rows))
+             : plan_attn(keys, cv.n_kv, units, 1, 128, 128, 1 << 30, 1);
   const int64_t grid = (int64_t)ap.blk[cp.n_seqs] * (ap.xcd ? 8 : 1);
   DAVET_CHECK_ARG(grid < (1ll << 31), DAVET_ESHAPE,
                   "davet_cache_page_attention: too many tokens");
   {
     ProfScope ps(KC_MISC, stream);
-#define LAUNCH(W)                                                                  \
-  hipLaunchKernelGGL((page_attn_kernel<F, D, W>), dim3((unsigned)grid), dim3(256), 0, \
-                     stream, cv, cp, ap, (const st*)q, ld_q, (st*)out, ld_o, lse,  \
-                     n_heads, block, sc, part, (int)rows, lists, top)
-    if (alone) LAUNCH(1);
-    else LAUNCH(4);
+#define LAUNCH(WW, THREADS)                                                        \
+  hipLaunchKernelGGL((page_attn_kernel<F, D, WW>), dim3((unsigned)grid),           \
+                     dim3(THREADS), 0, stream, cv, cp, ap, (const st*)q, ld_q,     \
+                     (st*)out, ld_o, lse, n_heads, block, sc, part, (int)rows,     \
+                     lists, top)
+    if (W == 1) LAUNCH(1, 256);
+    else if (W == 8) LAUNCH(8, 512);
+    else LAUNCH(4, 256);
 #undef LAUNCH
     DAVET_HIP(hipGetLastError());
   }

@@ -62,11 +62,13 @@ page_bounds_kernel(CacheView cv, BoundsPack bp, typename F::st* __restrict__ bou
   constexpr int U = 4;
   __shared__ float s_lo[4][D], s_hi[4][D];
   const int item = blockIdx.x / cv.n_kv, h = blockIdx.x % cv.n_kv;
-  const int s = owner(bp.item, bp.n_seqs, item);
-  const int page = bp.page[s] + item - bp.item[s], psz = 1 << cv.lg;
+  const Lanes items(bp.item);
+  const int pages = bp.page[threadIdx.x & 63], kvs = bp.kv[threadIdx.x & 63];
+  const int s = items.owner(bp.n_seqs, item), psz = 1 << cv.lg;
+  const int page = __builtin_amdgcn_readlane(pages, s) + item - items.start(s);
   const int phys = cv.table[(int64_t)s * cv.max_pages + page];
   if ((unsigned)phys >= (unsigned)cv.n_pages) return;
-  const int valid = min(psz, bp.kv[s] - page * psz);
+  const int valid = min(psz, __builtin_amdgcn_readlane(kvs, s) - page * psz);
   const int lane = threadIdx.x & 63, c = lane % C;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t at = (int64_t)phys * cv.n_kv + h;

@@ -4,8 +4,9 @@
 // Ancestors by doubling: with A_k(i) the first 2^k tokens on the way up from i (i
 // itself the first) and J_k(i) the one that comes after them,
 //   A_{k+1}(i) = A_k(i) + A_k(J_k(i)),  J_{k+1}(i) = J_k(J_k(i)),
-// so a tree of depth d takes log2 d steps, not d.  One workgroup a sequence, a thread
-// a token, the sets as bits in LDS; a draft of 26 tokens takes a launch's latency.
+// so a tree of depth d takes log2 d steps, not d.  A thread a token: drafts of up to 64
+// tokens by a wavefront a sequence, the sets as two words a lane, larger ones by a
+// workgroup, the sets in LDS.
 //
 // The attention walks the cache once for all tokens of the tree, as for a chunk; only
 // tiles that reach into the chunk read the rows' masks (LDS, a shift a lane and tile).
@@ -62,6 +63,40 @@ tree_plan_kernel(TreePack tp, const int32_t* __restrict__ parent,
   }
 }
 
+// Sequences of at most 64 tokens.
+__global__ void __launch_bounds__(64)
+tree_plan_small_kernel(TreePack tp, const int32_t* __restrict__ parent,
+                       int32_t* __restrict__ pos, uint32_t* __restrict__ mask) {
+  constexpr int W = kTreeWords;
+  const int s = blockIdx.x, i = threadIdx.x;
+  const int row0 = tp.row0[s], n = tp.row0[s + 1] - row0, first = tp.first[s];
+  int j = -1;
+  if (i < n) {
+    j = parent[row0 + i];
+    if (j >= i || j < 0) j = -1;              // no parent comes later
+  }
+  uint32_t lo = i < 32 ? 1u << i : 0u, hi = i < 32 ? 0u : 1u << (i - 32);
+  int d = j >= 0 ? 1 : 0;
+  while (__any(j >= 0)) {
+    const int at = max(j, 0);
+    const uint32_t l = __shfl(lo, at, 64), h = __shfl(hi, at, 64);
+    const int a = __shfl(d, at, 64), k = __shfl(j, at, 64);
+    if (j >= 0) {
+      lo |= l;
+      hi |= h;
+      d += a;
+      j = k;
+    }
+  }
+  if (i >= n) return;
+  if (pos) pos[row0 + i] = first + d;
+  if (mask) {
+    uint32_t* m = mask + (int64_t)(row0 + i) * W;
+#pragma unroll
+    for (int w = 0; w < W; ++w) m[w] = w == 0 ? lo : w == 1 ? hi : 0u;
+  }
+}
+
 }  // namespace
 }  // namespace davet
 
@@ -77,6 +112,7 @@ extern "C" int davet_tree_plan(int32_t n_seqs, const int32_t* cu_q,
   DAVET_CHECK_ARG(cu_q[0] == 0, DAVET_ESHAPE, "davet_tree_plan: cu_q[0] must be 0");
   TreePack tp{};
   tp.n_seqs = n_seqs;
+  int64_t longest = 0;
   for (int s = 0; s < n_seqs; ++s) {
     const int64_t n = (int64_t)cu_q[s + 1] - cu_q[s];
     DAVET_CHECK_ARG(n >= 0 && n <= DAVET_MAX_TREE, DAVET_ESHAPE,
@@ -86,6 +122,7 @@ extern "C" int davet_tree_plan(int32_t n_seqs, const int32_t* cu_q,
                     "below their number");
     DAVET_CHECK_ARG(!first_pos || first_pos[s] <= INT32_MAX - DAVET_MAX_TREE,
                     DAVET_ESHAPE, "davet_tree_plan: first_pos beyond int32");
+    longest = std::max(longest, n);
     tp.row0[s + 1] = cu_q[s + 1];
     tp.first[s] = first_pos ? first_pos[s] : (int32_t)(kv_len[s] - n);
   }
@@ -95,8 +132,12 @@ extern "C" int davet_tree_plan(int32_t n_seqs, const int32_t* cu_q,
   DAVET_CHECK_ARG(aligned4({parent, pos, mask}), DAVET_EINVAL,
                   "davet_tree_plan: parent, pos and mask must be 4-byte aligned");
   ProfScope ps(KC_MISC, stream);
-  hipLaunchKernelGGL(tree_plan_kernel, dim3(n_seqs), dim3(DAVET_MAX_TREE), 0, stream,
-                     tp, parent, pos, mask);
+  if (longest <= 64)
+    hipLaunchKernelGGL(tree_plan_small_kernel, dim3(n_seqs), dim3(64), 0, stream, tp,
+                       parent, pos, mask);
+  else
+    hipLaunchKernelGGL(tree_plan_kernel, dim3(n_seqs), dim3(DAVET_MAX_TREE), 0, stream,
+                       tp, parent, pos, mask);
   DAVET_HIP(hipGetLastError());
   return DAVET_OK;
 }

@@ -186,6 +186,11 @@ ATTEND = [  # dtype, new, kv, heads, kv_heads, dim, page, block, top
     ("f16", [2], [2000], 4, 1, 128, 16, 1, 64),             # pieces
     ("bf16", [1], [3000], 2, 1, 64, 256, 0, 11),
     ("f32", [40], [90], 2, 2, 64, 16, 1, 3),
+    # lists of more than 1024 keys: pieces
+    ("f16", [1], [1500], 8, 2, 128, 64, 1, 20),
+    ("bf16", [2, 1], [1300, 2100], 4, 4, 64, 16, 0, 100),
+    ("f32", [1], [1400], 2, 1, 128, 256, 0, 6),
+    ("f32", [3], [1300], 3, 1, 64, 16, 1, 80),
     # lists enough for a wavefront each
     ("f16", [260, 1], [300, 40], 8, 8, 64, 16, 1, 4),
     ("bf16", [33], [400], 128, 64, 128, 32, 0, 5),
