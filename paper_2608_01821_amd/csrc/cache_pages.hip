@@ -587,7 +587,7 @@ page_select_wave_kernel(CacheView cv, ChunkPack cp, const typename F::st* __rest
 struct TilePack {
   int32_t first[DAVET_MAX_SEQS + 1];    // first tile of each sequence
 };
-constexpr int kTileTokens = 16, kTileThreads = 512, kTileWaves = kTileThreads / 64;
+constexpr int kTileTokens = 16, kTileThreads = 1024, kTileWaves = kTileThreads / 64;
 template <typename F, int D, int CAP>
 __global__ void __launch_bounds__(kTileThreads)
 page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
@@ -620,7 +620,7 @@ page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
 
   if (np > top) {
     for (int i = threadIdx.x; i < kTileTokens * LP; i += kTileThreads) {
-      const int tok = i / LP, l = i % LP;
+      const int tok = i % kTileTokens, l = i / kTileTokens;     // (in LDS side by side)
       double x[N] = {};
       const st* qp = q + (int64_t)(row0 + tok0 + min(tok, nt - 1)) * ld_q +
                      (int64_t)hk * g * D + l % S::H * N;

@@ -67,12 +67,13 @@ __device__ __forceinline__ Stat stat_wave(Stat s) {
   s = stat_step<16>(s);
   return stat_step<32>(s);
 }
-// one logit; ref: s.m, or 0 while that is -inf
+// one logit; ref: s.m, or 0 while that is -inf; without B where no entropy is asked for
+template <bool B = true>
 __device__ __forceinline__ void term(float x, float ref, Stat& s) {
   const float t = (x - ref) * kLog2e;
   const float e = __builtin_amdgcn_exp2f(t);
   s.S += e;
-  s.B = fmaf(e, fmaxf(t, -200.f), s.B);     // -inf: 0 times a finite number
+  if (B) s.B = fmaf(e, fmaxf(t, -200.f), s.B);     // -inf: 0 times a finite number
 }
 
 // 64-bit key of a (value, id): larger value first, then lower id; never 0 for
@@ -346,7 +347,7 @@ logprobs_kernel(const typename F::st* __restrict__ logits, int64_t ld, int vocab
       float v[N];
       unpack<F>(w[u], v);
 #pragma unroll
-      for (int e = 0; e < N; ++e) term(v[e], ref, s);
+      for (int e = 0; e < N; ++e) term<!PART>(v[e], ref, s);
     }
     if (k == 0) continue;
     if (i == 0) {
@@ -387,7 +388,7 @@ logprobs_kernel(const typename F::st* __restrict__ logits, int64_t ld, int vocab
     const float v = lane < ne && id != exclude ? F::load(x[id]) : -INFINITY;
     if (k > 0) insert(__ballot(v > -INFINITY), top_key(v, id));
     if (v > s.m) s = stat_to(s, v);
-    term(v, s.m == -INFINITY ? 0.f : s.m, s);
+    term<!PART>(v, s.m == -INFINITY ? 0.f : s.m, s);
   }
   s = stat_wave(s);
   if (lane == 0) s_stat[wave] = s;
@@ -436,7 +437,7 @@ logprobs_short_kernel(const typename F::st* __restrict__ logits, int64_t ld,
   for (int i = 0; i < kShort; ++i) {
     const int first = (i * kWaves + wave) * 64;
     if (first >= vocab) break;
-    term(v[i], ref, s);
+    term<!PART>(v[i], ref, s);
     if (k == 0) continue;
     const uint64_t run = sort_up(v[i] > -INFINITY ? top_key(v[i], first + lane) : 0);
     list = i == 0 ? lane_reverse(run) : list_join(list, run);
