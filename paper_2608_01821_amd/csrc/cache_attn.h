@@ -277,18 +277,22 @@ struct AttnPlan {
 // With `xcd`, workgroup b runs on XCD b % 8 and takes key heads = b mod 8 only,
 // so the tiles and pieces of a key head share one L2 and every XCD has the same
 // work.
-struct Place { int s, hk, piece, tile; };
+struct Place { int s, hk, piece, tile, row0, n, kv; };
 // The last tile comes first under a causal mask: it sees the most keys.
 __device__ __forceinline__ Place place(const AttnPlan& ap, const ChunkPack& cp,
                                        int n_kv, int g, int rows, bool causal) {
   const int b = ap.xcd ? (int)blockIdx.x >> 3 : (int)blockIdx.x;
-  const int i = owner(ap.blk, cp.n_seqs, b);
+  const Lanes blks(ap.blk), chunk(cp.row0);
+  const int orders = ap.order[threadIdx.x & 63], kvs = cp.kv[threadIdx.x & 63];
+  const int i = blks.owner(cp.n_seqs, b);
   Place p;
-  p.s = ap.order[i];
-  const int n = cp.row0[p.s + 1] - cp.row0[p.s];
-  const int nt = (n * g + rows - 1) / rows;
-  const int np = (cp.kv[p.s] + ap.piece - 1) / ap.piece;
-  int rem = b - ap.blk[i];
+  p.s = __builtin_amdgcn_readlane(orders, i);
+  p.row0 = chunk.start(p.s);
+  p.n = chunk.end(p.s) - p.row0;
+  p.kv = __builtin_amdgcn_readlane(kvs, p.s);
+  const int nt = (p.n * g + rows - 1) / rows;
+  const int np = (p.kv + ap.piece - 1) / ap.piece;
+  int rem = b - blks.start(i);
   const int h = rem / (nt * np);
   rem -= h * nt * np;
   p.hk = ap.xcd ? ((int)blockIdx.x & 7) + 8 * h : h;
@@ -342,7 +346,7 @@ cache_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int lg = cv.lg, psz = 1 << lg;
   const Place pl = place(ap, cp, cv.n_kv, g, 32 * G, block > 0);
   const int s = pl.s, hk = pl.hk;
-  const int row0 = cp.row0[s], n = cp.row0[s + 1] - row0, kv = cp.kv[s];
+  const int row0 = pl.row0, n = pl.n, kv = pl.kv;
   const int past = kv - n;
   const int rows = n * g;
   const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
@@ -1058,8 +1062,10 @@ cache_merge_kernel(ChunkPack cp, const float* __restrict__ part, int part_rows,
   if (row >= part_rows) return;
   const int lane = threadIdx.x & 63, d0 = lane * E;
   const int tok = row / n_heads, h = row % n_heads;
-  const int s = owner(cp.row0, cp.n_seqs, tok);
-  const int np = (cp.kv[s] + piece - 1) / piece;
+  const Lanes chunk(cp.row0);
+  const int kvs = cp.kv[threadIdx.x & 63];
+  const int s = chunk.owner(cp.n_seqs, tok);
+  const int np = (__builtin_amdgcn_readlane(kvs, s) + piece - 1) / piece;
   const float* pm = part + (int64_t)pieces * part_rows * D +
                     ((int64_t)min(lane, np - 1) * part_rows + row) * 2;
   const float mp = pm[0], lp = lane < np ? pm[1] : 0.f;
@@ -1120,8 +1126,10 @@ cache_merge_rows_kernel(ChunkPack cp, const float* __restrict__ part, int part_r
   if (tok >= cp.row0[cp.n_seqs]) return;
   const int lane = threadIdx.x & 63;
   const int h = (w - tok * per) * R + lane / L, d0 = lane % L * 4;
-  const int s = owner(cp.row0, cp.n_seqs, tok);
-  const int np = (cp.kv[s] + piece - 1) / piece;
+  const Lanes chunk(cp.row0);
+  const int kvs = cp.kv[threadIdx.x & 63];
+  const int s = chunk.owner(cp.n_seqs, tok);
+  const int np = (__builtin_amdgcn_readlane(kvs, s) + piece - 1) / piece;
   const int64_t row = (int64_t)tok * n_heads + min(h, n_heads - 1);
   const float* pm = part + (int64_t)pieces * part_rows * D;
   float m = -INFINITY, l = 0.f;
