@@ -703,6 +703,8 @@ class KvCache:
         self.struct = KvCacheT(*addr, page_table.shape[1], k.shape[0], k.shape[2],
                                k.shape[1], k.shape[3], int(dtype))
         self._ref = C.byref(self.struct)
+        devs = {x.get_device() for x in (k, v, page_table) if x is not None}
+        self._dev = devs.pop() if len(devs) == 1 else -1     # its tensors' GPU, or -1
 
     def _chunk(self, cu_q, kv_len):
         n = len(kv_len)
@@ -712,7 +714,13 @@ class KvCache:
         return n, _ints(cu_q), _ints(kv_len), max(0, cu_q[n])
 
     def _gpu(self, *tensors):
-        return _gpu(self.k, self.v, self.page_table, *tensors)
+        dev = self._dev
+        if dev < 0:
+            return _gpu(self.k, self.v, self.page_table, *tensors)
+        for t in tensors:
+            if t is not None and t.get_device() != dev:
+                raise ValueError("davet: tensor arguments must be on one GPU")
+        return dev
 
 
 def davet_cache_append(cache: KvCache, cu_q, kv_len, qkv, n_heads, q_out,
@@ -980,7 +988,7 @@ def davet_rotary(x, n_heads, head_dim, turns, out, dtype, pos=None,
                  layout=DAVET_ROTARY_HALVES, gain=1.0, inverse=False, stream=None):
     """``x`` and ``out`` [rows, n_heads * head_dim] or wider; ``turns`` a dense
     float64 device tensor: twice its length is the part of a head that turns."""
-    kinds, rows = _kinds(dtype), len(x)
+    kinds, rows = _kinds(dtype), x.shape[0]
     n_heads, head_dim = _small(n_heads, "n_heads"), _small(head_dim, "head_dim")
     width = _small(n_heads * head_dim, "n_heads * head_dim")
     a, lda = _rows(x, width, rows, kinds, "x")

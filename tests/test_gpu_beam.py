@@ -119,6 +119,28 @@ def test_ties(vocab):
     assert r.tolist() == [[0] * 3] and t.tolist() == [[9, 0, 1]]
 
 
+@pytest.mark.parametrize("top", [1, 3, 4, 7, 16, 33, 64])
+def test_scores_that_the_logits_vanish_beside(top):
+    """Every value of a row is the same: its tokens in order of their logits all the
+    same, and the lower row first."""
+    rng = np.random.default_rng(top)
+    x = values(rng, (6, 33000), "f32")
+    scores = torch.tensor([-1e30, -1e30, -2.0, -1e30, 1e25, -1e30])
+    o, r, t = select(x.cuda(), "f32", scores, 3, top)
+    big = [np.argsort(-f64(x)[i], kind="stable")[:top].tolist() for i in range(6)]
+    assert r.tolist() == [[2] * top, [4] * top]
+    assert t[0].tolist() == big[2]
+    assert t[1].tolist() == big[4]
+    o, r, t = select(x[[0, 1, 3]].cuda(), "f32", scores[[0, 1, 3]], 3, top)
+    assert r.tolist() == [[0] * top] and t[0].tolist() == big[0]
+    if top > 1:
+        done = torch.tensor([5, 0, 0], dtype=torch.int32).cuda()
+        _, r, t = select(x[[0, 1, 3]].cuda(), "f32", scores[[0, 1, 3]], 3, top, done=done,
+                         pad=-7)
+        assert r.tolist() == [[0] + [1] * (top - 1)]
+        assert t[0].tolist() == [-7] + big[1][:top - 1]
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("vocab", [90, 5000])
 def test_rows_with_nothing_to_offer(dtype, vocab):
