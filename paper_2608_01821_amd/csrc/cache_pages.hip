@@ -13,10 +13,10 @@
 // pages is taken, and equal scores go to the lower page.
 //
 // Three forms:
-//   tiles  chunks of 8 tokens and more: 16 tokens x 16 pages by float64 matrix ops,
-//          which read a page's bounds once for all 16
-//   waves  many (token, key head): a wavefront each, by vector ops, no LDS
-//   group  few of them: a workgroup each
+//   group  a workgroup each (token, key head)
+//   waves  where they are many: a wavefront each, by vector ops, no LDS
+//   tiles  many, and chunks of 8 tokens and more: 16 tokens x 16 pages by float64 matrix
+//          ops, which read a page's bounds once for all 16
 // In the last two a page's bounds are read 16 bytes a lane by 16 to 64 lanes, which keep
 // their elements of Q in registers; the sums of several pages are added over the lanes
 // and dealt out to them at once.
@@ -394,11 +394,9 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
     u32x4 w[8];
     int id = place(wave * P), next = place(wave * P + STEP);
     auto load = [&](int ids) {
+      const int safe = known(ids) ? ids : 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int ph = __shfl(ids, base + i, 64);
-        w[i] = sc.read(known(ph) ? ph : 0);
-      }
+      for (int i = 0; i < 8; ++i) w[i] = sc.read(__shfl(safe, base + i, 64));
     };
     load(id);
     sc.init(q + (int64_t)row * ld_q + (int64_t)c.hk * g * D, g);
@@ -423,7 +421,8 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
   }
   __syncthreads();
 
-  // up to 1024 pages are ranked by one wavefront
+  // up to 1024 pages are ranked by one wavefront (eight lists of 256 pages 9.2 us, by all
+  // 16 wavefronts 19.8; of 1024 pages 21.8 and 31.3)
   auto few = [&](auto r) {
     constexpr int R = decltype(r)::value;
     uint32_t kr[R];
@@ -768,7 +767,14 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
     longest = std::max(longest, n);
     tp.first[s + 1] = tp.first[s] + (n + kTileTokens - 1) / kTileTokens;
   }
-  const bool tiles = longest >= 8 && most <= 1024;
+  // fp16, 8 heads of 128, pages x (sequences x tokens), us of tiles, waves and group:
+  //    64 x (16 x  8)  11.1   9.5  15.2      512 x (16 x  1)  28.8  28.8  14.4
+  //    64 x (16 x 16)  13.5  12.0  26.7      512 x (16 x  6)  29.4  30.3  32.5
+  //   512 x ( 1 x 16)  29.3  26.8  13.1      512 x (16 x  8)  29.3  30.9  40.8
+  //   512 x (64 x  1)  48.4  31.4  30.0      512 x (16 x 16)  31.7  46.1  74.3
+  //   512 x (64 x  2)  47.5  32.2  44.6     1024 x ( 1 x 16)  53.1     -  21.2
+  //   512 x (64 x  4)  48.1  46.4  75.8     1024 x (16 x  8)  52.9     -  63.1
+  const bool tiles = items >= kManyItems && longest >= 8 && most <= 1024;
   const bool waves = items >= kManyItems && most <= 64 * kWaveSteps;
 #define TILES(F, DIM, CAP)                                                        \
   hipLaunchKernelGGL((page_select_tile_kernel<F, DIM, CAP>),                      \
