@@ -469,11 +469,15 @@ int run_page_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   int longest = 0;
   for (int s = 0; s < cp.n_seqs; ++s)
     if (cp.row0[s + 1] > cp.row0[s]) longest = std::max(longest, keys.kv[s]);
-  // 16 bits, 32 heads of 128 over 8: lists of 1024 keys of one, eight and sixteen tokens
-  // 11.5, 14.1 and 19.2 us in pieces, joined by a second launch, 10.2, 12.0 and 15.0 by
-  // eight wavefronts a list; of 512 keys of 32 tokens 19.5 and 15.2; of 2048 keys of one
-  // token 11.6 and 14.5.  512 tokens, 512 keys: 73 us by four, 66 by one.
-  const int W = items >= 2048 ? 1 : longest <= 1024 ? 8 : 4;
+  // fp16, 32 heads of 128 over 8, us of four wavefronts a list (in pieces that a second
+  // launch joins, where there are few), of eight and of one:
+  //     8 lists of  512 keys   8.7   7.8          512 of  512  14.1  16.7  21.1
+  //     8       of 1024        8.6   9.8         1024 of  512  23.6  29.4  23.3
+  //     8       of 2048        9.3  14.5         1024 of 4096   101         127
+  //   128       of 1024       11.5  10.5         2048 of  512  37.4        31.9
+  //   256       of  512       12.5   9.3         2048 of 1024  58.2        54.3
+  //   256       of 1024       18.4  14.1         4096 of  512  65.8        57.0
+  const int W = items >= 2048 ? 1 : longest <= 1024 && items <= 256 ? 8 : 4;
   auto units = [&](int s) {
     const int64_t t = (int64_t)(cp.row0[s + 1] - cp.row0[s]) * rt;
     return W > 1 ? t : (t + 3) / 4;
