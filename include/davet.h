@@ -594,7 +594,8 @@ int davet_cache_append(const davet_kv_cache* cache, int32_t n_seqs,
                        const float* k_gain, float eps, float theta, void* q_out,
                        int64_t ld_q, hipStream_t stream);
 
-/* Workspace (256-byte aligned) that davet_cache_attention and
+/* Workspace (256-byte aligned) that davet_cache_attention,
+ * davet_cache_tree_attention, davet_cache_page_attention and
  * davet_cache_weights need for chunks of at most max_q tokens in all.  Calls
  * that may overlap in time need one each; its contents mean nothing between
  * calls. */
@@ -801,7 +802,7 @@ int davet_token_logprobs(int32_t rows, int32_t vocab, const void* logits,
  *   rows and tokens of the `top` (1 .. 64) best, by (value descending, row ascending,
  *   logit descending, token ascending); values are compared in float64, the sums of
  *   exponentials under them are float32.  Where there are fewer candidates: -inf, -1,
- *   -1.  out_scores may be scores where top is beams.
+ *   -1.  out_scores may be scores where top is beams, and must not overlap it otherwise.
  * beams 1 .. DAVET_MAX_BEAMS, at most 2^22 rows.  workspace:
  * davet_beam_workspace_bytes for these sizes exactly (fewer requests may need more),
  * 256-byte aligned; (rows + 255) * (8 * top + 12) + 255 bytes are enough for any vocab

@@ -9,6 +9,11 @@
 // lists into float64 values (two beams' candidates may be closer than float32
 // roundings) and keep the best 64 in order, one a lane; then their lists are joined.
 //
+// Bound by latency: 64 rows of 126,464 bf16 logits, 4 of 16 requests, take 12.5 us (1.3
+// TB/s), their join 4.6; 4 fp32 rows, 15 slices each, 7.7 and 6.6; 4 requests of 16 beams,
+// 16 best each, 12.5 and 9.9.  The move of 64 sequences' last pages, 8 heads of 55 rows
+// of 128, takes 5.0 us (26 MB, 5.2 TB/s), of one row each 3.
+//
 // Order: value, then row, then (logit, id): within a row values only ever tie where
 // logits do, or where the score is so large that they vanish beside it.
 
@@ -248,6 +253,12 @@ extern "C" int davet_beam_select(int32_t groups, int32_t beams, int32_t vocab,
   DAVET_CHECK_ARG(aligned4({scores, done, out_scores, out_rows, out_tokens}),
                   DAVET_EINVAL,
                   "davet_beam_select: scores, done and outputs must be 4-byte aligned");
+  DAVET_CHECK_ARG((out_scores == scores && top == beams) ||
+                      !overlap(out_scores, (size_t)groups * top * 4, scores,
+                               (size_t)rows * 4),
+                  DAVET_EINVAL,
+                  "davet_beam_select: out_scores overlaps scores (the same address "
+                  "needs top = beams)");
   const size_t need = beam_bytes(rows, vocab, top);
   DAVET_CHECK_ARG(workspace && ((uintptr_t)workspace & 255) == 0 && ws_bytes >= need,
                   DAVET_ENOMEM,

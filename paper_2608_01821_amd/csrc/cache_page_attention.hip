@@ -25,6 +25,12 @@
 // Eight wavefronts share a list's keys and are joined in LDS; four, a piece of a long
 // list, and a second launch joins the pieces in order (cache_attn.h); or, where there
 // are lists enough to fill the chip, each has its own.
+//
+// Measured, 32 heads over 8 of 128: eight tokens with 64 pages of 64 each, fp16, 25.3 us
+// (136 MB, 5.4 TB/s: HBM) and 4.8 to join the pieces; 512 tokens with 32 pages of 16,
+// bf16, 63 us.  Those read 1.07 GB (17 TB/s), the most of it from L2: the load path
+// of a CU is busy for 58 % of the time, vector ALUs for 32, matrix pipes for 16; the rest
+// is waiting with four wavefronts a SIMD (more do not fit the registers).
 
 #include "cache_attn.h"
 

@@ -23,6 +23,12 @@
 //
 // Then the key of the last page taken is found from its highest bit down, by counting,
 // and the pages are written in ascending order.
+//
+// Measured with 8 key heads of 128, 16 bits: bounds of a page 4 to 5 us (a chain of
+// loads); the choice of 64 of up to 1022 pages for eight tokens 22.7 us, of them 16 the scores:
+// vector ops, three of each 16-bit element's five being its way to float64 and its
+// product, 64 CUs at work; of 32 among up to 234 for 512 tokens 20.6 us, bound by the
+// float64 matrix rate (64 cycles for 16 x 16 x 4).
 
 #include <math.h>
 

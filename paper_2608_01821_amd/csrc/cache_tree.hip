@@ -5,11 +5,14 @@
 // itself the first) and J_k(i) the one that comes after them,
 //   A_{k+1}(i) = A_k(i) + A_k(J_k(i)),  J_{k+1}(i) = J_k(J_k(i)),
 // so a tree of depth d takes log2 d steps, not d.  A thread a token: drafts of up to 64
-// tokens by a wavefront a sequence, the sets as two words a lane, larger ones by a
-// workgroup, the sets in LDS.
+// tokens by a wavefront a sequence, the sets as two words a lane (16 of 64 tokens: 2.4
+// us), larger ones by a workgroup, the sets in LDS (those 16: 4.4 us; of 256 tokens 5.5).
 //
 // The attention walks the cache once for all tokens of the tree, as for a chunk; only
 // tiles that reach into the chunk read the rows' masks (LDS, a shift a lane and tile).
+// Bound by HBM: eight trees of 26 tokens on 32,700 cached ones, 32 heads over 8 of 128,
+// fp16, 156 us (779 MB, 5.0 TB/s) and 11 to join the pieces; sixteen of up to 64 on up to
+// 3741, 32 heads, bf16, 126 us (607 MB, 4.8 TB/s).
 
 #include "cache_attn.h"
 

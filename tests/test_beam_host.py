@@ -30,6 +30,7 @@ def _select(groups=2, beams=4, vocab=1000, logits=A, dtype=dv.DAVET_F16, ld=1000
     (dict(logits=A + 1), EINVAL), (dict(scores=A + 2), EINVAL), (dict(done=A + 2), EINVAL),
     (dict(osc=A + 2), EINVAL), (dict(orow=A + 2), EINVAL), (dict(otok=A + 2), EINVAL),
     (dict(ws=None), ENOMEM), (dict(ws=A + 64), ENOMEM), (dict(nb=255), ENOMEM),
+    (dict(top=3), EINVAL), (dict(osc=A + 4), EINVAL), (dict(osc=A - 4), EINVAL),
 ])
 def test_select_refusals(kw, status):
     assert _select(**kw) == status
