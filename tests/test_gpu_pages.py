@@ -101,6 +101,15 @@ SELECT = [  # dtype, new, kv, heads, kv_heads, dim, page, block, top, first, las
     ("f16", [20], [16 * 700], 2, 1, 64, 16, 1, 30, 1, 1),
     ("f32", [9, 1], [16 * 600, 50], 4, 2, 128, 16, 0, 3, 0, 0),
     ("bf16", [8, 0, 17], [16 * 1024, 0, 400], 3, 1, 128, 16, 1, 500, 1, 1),
+    # and many of those
+    ("f16", [70], [16 * 700], 32, 16, 64, 16, 1, 30, 1, 1),
+    ("f32", [35, 1], [16 * 520, 50], 32, 32, 64, 16, 0, 3, 0, 0),
+    ("bf16", [64, 0, 17], [16 * 1024, 0, 400], 16, 16, 64, 16, 1, 500, 1, 1),
+    # every sequence there may be
+    ("f16", [1] * 64, [17 * i + 1 for i in range(64)], 4, 2, 64, 16, 1, 9, 1, 1),
+    ("f32", [i % 3 for i in range(64)], [10 * i + 2 for i in range(64)], 16, 16, 64, 16,
+     1, 4, 0, 2),
+    ("bf16", [8, 0] * 32, [7 * i + 8 for i in range(64)], 4, 4, 64, 16, 0, 5, 1, 0),
 ]
 
 
@@ -197,6 +206,14 @@ ATTEND = [  # dtype, new, kv, heads, kv_heads, dim, page, block, top
     ("f32", [70], [100], 64, 32, 64, 16, 4, 3),
     ("f32", [66], [90], 32, 32, 128, 16, 1, 2),
     ("f16", [130], [140], 320, 16, 64, 16, 0, 3),           # two row tiles each
+    # more than one a CU, of few keys
+    ("f16", [70, 1], [300, 40], 8, 8, 64, 16, 1, 4),
+    ("bf16", [40], [900], 20, 10, 128, 32, 0, 20),
+    ("f32", [33], [1000], 16, 16, 64, 16, 4, 40),
+    # every sequence there may be
+    ("f16", [1] * 64, [17 * i + 1 for i in range(64)], 8, 2, 128, 16, 1, 9),
+    ("bf16", [i % 3 for i in range(64)], [10 * i + 2 for i in range(64)], 4, 4, 64, 16, 1,
+     7),
 ]
 
 
@@ -327,6 +344,34 @@ def test_append_bounds_select_attend(dtype, block):
             check_attention(got, ref, dtype, dim, at)
         whole = oc.attention(host, cu, kv, f64(q), heads, block=block)
         check_attention(got, whole, dtype, dim, at)
+
+
+def test_far_pages_need_64_bit_offsets():
+    """Pages behind the 2^32nd byte of the bounds, all at the pools' end."""
+    hk, d, size = 8, 128, 16
+    s = Setup(3, "f32", [2, 1], [300, 45], 8, hk, d, size)
+    n = (1 << 32) // (hk * 2 * d * 4) + 40
+    far = s.table.copy()
+    far[far >= 0] += n - s.k.shape[0]
+    pool = torch.empty(n, hk, size, d, device="cuda")
+    pool[n - s.k.shape[0]:] = s.k.cuda()        # (keys and values alike)
+    cache = dv.KvCache(pool, pool, torch.from_numpy(far).cuda(), dv.DAVET_F32)
+    bounds = torch.empty(n, hk, 2, d, device="cuda")
+    cu = [0, 300, 345]
+    dv.davet_cache_page_bounds(cache, cu, s.kv, bounds)
+    last = bounds[n - s.k.shape[0]:]
+    db, b = whole_bounds(s)
+    used = sorted({int(p) for p in s.table.reshape(-1) if p >= 0})
+    assert torch.equal(last[used], db[used])
+    q, rows = s.q.cuda(), s.cu[-1]
+    pages = torch.empty(rows, hk, 4, dtype=torch.int32, device="cuda")
+    dv.davet_cache_page_select(cache, s.cu, s.kv, q, 8, bounds, pages, first=1, last=1)
+    want = oc.page_select(s.host, s.cu, s.kv, f64(s.q), 8, b, 4, 1, 1, 0)
+    assert [[h[h >= 0].tolist() for h in r] for r in pages.cpu()] == want
+    got = attend(s, [[h + [-1] * (4 - len(h)) for h in r] for r in want], 0, cache)
+    host = dict(s.host, v=s.host["k"])
+    ref = oc.attention_of(host, s.cu, s.kv, f64(s.q), 8, seen_by(s, want, 0))
+    check_attention(got, ref, "f32", d, 64)
 
 
 def test_two_streams_and_captured():

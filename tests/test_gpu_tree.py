@@ -78,6 +78,9 @@ CASES = [  # dtype, new, kv, heads, kv_heads, dim, page
     ("bf16", [129, 3], [700, 333], 6, 2, 64, 128),
     ("f16", [64] * 5, [300, 65, 64, 191, 257], 4, 2, 128, 16),
     ("f32", [200], [501], 2, 1, 128, 32),
+    # every sequence there may be
+    ("f16", [i % 4 for i in range(64)], [9 * i + 3 for i in range(64)], 4, 2, 64, 16),
+    ("bf16", [i % 40 for i in range(64)], [5 * i + 40 for i in range(64)], 2, 1, 128, 32),
 ]
 
 
