@@ -133,6 +133,7 @@ page_bounds_kernel(CacheView cv, BoundsPack bp, typename F::st* __restrict__ bou
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kMaxPages = 32768;        // of a sequence: their keys fill the LDS
+constexpr int kFewPages = 4096;         // whose keys a wavefront's registers hold
 constexpr int kManyItems = 1024;        // of them a wavefront each
 
 // order of a score: larger first; NaN with -inf, -0 with +0; never 0
@@ -427,42 +428,34 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
   }
   __syncthreads();
 
-  // up to 1024 pages are ranked by one wavefront (eight lists of 256 pages 9.2 us, by all
-  // 16 wavefronts 19.8; of 1024 pages 21.8 and 31.3)
-  auto few = [&](auto r) {
-    constexpr int R = decltype(r)::value;
-    uint32_t kr[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const uint32_t k = s_keys[i * 64 + lane];
-      kr[i] = i * 64 < np ? k : 0u;
-    }
-    choose(kr, top, all, c.out);
-  };
-  if (np <= 1024) {
+  if constexpr (CAP <= kFewPages) {
+    // One wavefront ranks them, and the next workgroup's may begin (eight lists of 1024
+    // pages 21.8 us, by all 16 wavefronts 31.3; of 4096 66.6 and 71.6, 64 of them 113 and
+    // 144).
     if (wave != 0) return;
+    auto few = [&](auto r) {
+      constexpr int R = decltype(r)::value;
+      uint32_t kr[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const uint32_t k = s_keys[i * 64 + lane];
+        kr[i] = i * 64 < np ? k : 0u;
+      }
+      choose(kr, top, all, c.out);
+    };
     if (np <= 256) few(std::integral_constant<int, 4>());
     else if (np <= 512) few(std::integral_constant<int, 8>());
-    else few(std::integral_constant<int, 16>());
+    else if (np <= 1024) few(std::integral_constant<int, 16>());
+    else if (np <= 2048) few(std::integral_constant<int, 32>());
+    else few(std::integral_constant<int, CAP / 64>());
     return;
   }
   // Each wavefront counts and writes a run of whole 64s.
   const int per = ((np + kSelWaves - 1) / kSelWaves + 63) & ~63;
   const int lo = min(np, wave * per), hi = min(np, lo + per);
-  constexpr int REGS = CAP / kSelThreads <= 8 ? CAP / kSelThreads : 0;
-  uint32_t kr[REGS ? REGS : 1];
-#pragma unroll
-  for (int i = 0; i < REGS; ++i)
-    kr[i] = lo + i * 64 < hi ? s_keys[lo + i * 64 + lane] : 0u;
   // f(64 pages' first one, their keys) of this wavefront
   auto each = [&](auto f) {
-    if constexpr (REGS > 0) {
-#pragma unroll
-      for (int i = 0; i < REGS; ++i)
-        if (lo + i * 64 < hi) f(lo + i * 64, kr[i]);
-    } else {
-      for (int i = lo; i < hi; i += 64) f(i, s_keys[i + lane]);
-    }
+    for (int i = lo; i < hi; i += 64) f(i, s_keys[i + lane]);
   };
   // keys of this wavefront that are at least each of x, y, z (above 0)
   auto count = [&](uint32_t x, uint32_t y, uint32_t z, uint32_t (&cnt)[3]) {
@@ -501,8 +494,9 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
       count(T | 1u << b, T | 2u << b, T | 3u << b, cnt);
       total(cnt);
       const uint32_t d = cnt[2] >= keep ? 3u : cnt[1] >= keep ? 2u : cnt[0] >= keep ? 1u : 0u;
+      const uint32_t n = d == 3 ? cnt[2] : d == 2 ? cnt[1] : cnt[0];
       T |= d << b;
-      if (d > 0 && cnt[d - 1] == keep) {        // a border between keys
+      if (d > 0 && n == keep) {                 // a border between keys
         --T;
         break;
       }
@@ -801,7 +795,7 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
     if (tiles && most <= 512) TILES(F, DIM, 512);                                 \
     else if (tiles) TILES(F, DIM, 1024);                                          \
     else if (waves) WAVES(F, DIM);                                                \
-    else if (most <= 4096) SELECT(F, DIM, 4096);                                  \
+    else if (most <= kFewPages) SELECT(F, DIM, kFewPages);                                  \
     else SELECT(F, DIM, kMaxPages);                                               \
   } while (0)
 #define SELECT_D(F) \
