@@ -28,9 +28,10 @@
 //
 // Measured, 32 heads over 8 of 128: eight tokens with 64 pages of 64 each, fp16, 25.3 us
 // (136 MB, 5.4 TB/s: HBM) and 4.8 to join the pieces; 512 tokens with 32 pages of 16,
-// bf16, 63 us.  Those read 1.07 GB (17 TB/s), the most of it from L2: the load path
-// of a CU is busy for 58 % of the time, vector ALUs for 32, matrix pipes for 16; the rest
-// is waiting with four wavefronts a SIMD (more do not fit the registers).
+// bf16, 63 us.  Those read 1.07 GB (17 TB/s), the most of it from L2, and every 512 tokens
+// more cost 52 us (21 TB/s); the load path of a CU is busy for 58 % of the time, vector
+// ALUs for 30, matrix pipes for 16.  Registers hold three wavefronts a SIMD; four, with
+// tiles of 16 keys, gain 4 % at 512 keys a list and nothing at 1024.
 
 #include "cache_attn.h"
 
