@@ -10,8 +10,8 @@
 // roundings) and keep the best 64 in order, one a lane; then their lists are joined.
 //
 // Bound by latency: 64 rows of 126,464 bf16 logits, 4 of 16 requests, take 12.5 us (1.3
-// TB/s), their join 4.6; 4 fp32 rows, 15 slices each, 7.7 and 6.6; 4 requests of 16 beams,
-// 16 best each, 12.5 and 9.9.  The move of 64 sequences' last pages, 8 heads of 55 rows
+// TB/s), their join 4.5; 4 fp32 rows, 15 slices each, 7.7 and 6.4; 4 requests of 16 beams,
+// 16 best each, 12.5 and 8.5 (9.8 with the wavefronts' lists joined two by two).  The move of 64 sequences' last pages, 8 heads of 55 rows
 // of 128, takes 5.0 us (26 MB, 5.2 TB/s), of one row each 3.
 //
 // Order: value, then row, then (logit, id): within a row values only ever tie where
@@ -71,8 +71,8 @@ beam_join_kernel(int rows, int beams, int slices, int k, int P,
                  const char* __restrict__ part, const float* scores,
                  const int32_t* __restrict__ done, int pad, float* out_scores,
                  int32_t* __restrict__ out_rows, int32_t* __restrict__ out_tokens) {
-  __shared__ uint64_t s_v[kJoinWaves / 2][64], s_key[kJoinWaves / 2][64];
-  __shared__ uint32_t s_row[kJoinWaves / 2][64];
+  __shared__ uint64_t s_v[2][kJoinWaves * 64], s_key[2][kJoinWaves * 64];
+  __shared__ uint32_t s_row[2][kJoinWaves * 64];
   __shared__ double s_base[DAVET_MAX_BEAMS];    // (NaN: nothing to offer)
   __shared__ double s_over[DAVET_MAX_BEAMS];    // the score of a row that is over, or NaN
   const int lane = threadIdx.x & 63;
@@ -108,6 +108,17 @@ beam_join_kernel(int rows, int beams, int slices, int k, int P,
   }
   __syncthreads();
   const Cand none = {0, 0, 0xffffffffu};
+  // 64 / P lists of P entries, every other one reversed, to one (with `up` reversed); the
+  // first n of them, if the others are empty and it is not to be reversed
+  auto merge = [&](Cand& c, int n, bool up) {
+    const int end = up ? 64 : n * P;
+    if (P < 2 && end > 1) exchanges<1, 2>(c, up);
+    if (P < 4 && end > 2) exchanges<2, 4>(c, up);
+    if (P < 8 && end > 4) exchanges<4, 8>(c, up);
+    if (P < 16 && end > 8) exchanges<8, 16>(c, up);
+    if (P < 32 && end > 16) exchanges<16, 32>(c, up);
+    if (P < 64 && end > 32) exchanges<32, 64>(c, up);
+  };
   Cand best = none;
   for (int chunk = wave; chunk < chunks; chunk += kJoinWaves) {
     const bool up = chunk != wave;              // (the first one as it is kept)
@@ -121,31 +132,33 @@ beam_join_kernel(int rows, int beams, int slices, int k, int P,
     if (base == base && key)
       c = {value_key(base + (double)key_value(key)), key, (uint32_t)(row0 + b)};
     if (over == over && first) c = {value_key(over), top_key(0.f, pad), (uint32_t)(row0 + b)};
-    if (P < 2) exchanges<1, 2>(c, up);
-    if (P < 4) exchanges<2, 4>(c, up);
-    if (P < 8) exchanges<4, 8>(c, up);
-    if (P < 16) exchanges<8, 16>(c, up);
-    if (P < 32) exchanges<16, 32>(c, up);
-    if (P < 64) exchanges<32, 64>(c, up);
+    merge(c, lists - chunk * per, up);
     if (up)
       join(best, c);
     else
       best = c;
   }
-  const int active = min(kJoinWaves, chunks);
-#pragma unroll
-  for (int o = 1; o < kJoinWaves; o <<= 1) {
-    if (o >= active) break;
-    const int at = wave / (2 * o);
-    if ((wave & (2 * o - 1)) == o) {
-      s_v[at][lane] = best.v;
-      s_key[at][lane] = best.key;
-      s_row[at][lane] = best.row;
+  // the wavefronts' lists, P entries of each, in the same way (of 64: two at a time)
+  int active = min(kJoinWaves, chunks);
+  for (int half = 0; active > 1; half ^= 1) {
+    if (wave < active && lane < P) {
+      s_v[half][wave * P + lane] = best.v;
+      s_key[half][wave * P + lane] = best.key;
+      s_row[half][wave * P + lane] = best.row;
     }
     __syncthreads();
-    if ((wave & (2 * o - 1)) == 0 && wave + o < active)
-      join(best, {s_v[at][63 - lane], s_key[at][63 - lane], s_row[at][63 - lane]});
-    __syncthreads();
+    auto entry = [&](int l, int j) {
+      const int i = min(l, active - 1) * P + j;
+      const Cand c = {s_v[half][i], s_key[half][i], s_row[half][i]};
+      return l < active ? c : none;
+    };
+    const int take = max(2, per), run = lane / P, l = wave * take + run;
+    if (wave * take < active) {
+      best = entry(l, run & 1 ? P - 1 - lane % P : lane % P);
+      merge(best, active - wave * take, false);
+      if (P == 64) join(best, entry(l + 1, 63 - lane));
+    }
+    active = (active + take - 1) / take;
   }
   if (wave != 0 || lane >= k) return;
   const int64_t at = (int64_t)blockIdx.x * k + lane;
