@@ -9,8 +9,8 @@
 // lists into float64 values (two beams' candidates may be closer than float32
 // roundings) and keep the best 64 in order, one a lane; then their lists are joined.
 //
-// Bound by latency: 64 rows of 126,464 bf16 logits, 4 of 16 requests, take 12.5 us (1.3
-// TB/s), their join 4.5; 4 fp32 rows, 15 slices each, 7.7 and 6.4; 4 requests of 16 beams,
+// Bound by latency: 64 rows of 126,464 bf16 logits, 4 of 16 requests, take 12.2 us (1.4
+// TB/s), their join 4.5; 4 fp32 rows, 15 slices each, 7.3 and 6.4; 4 requests of 16 beams,
 // 16 best each, 12.5 and 8.5 (9.8 with the wavefronts' lists joined two by two).  The move of 64 sequences' last pages, 8 heads of 55 rows
 // of 128, takes 5.0 us (26 MB, 5.2 TB/s), of one row each 3.
 //

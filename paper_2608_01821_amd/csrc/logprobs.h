@@ -23,7 +23,7 @@
 // of the list's 9 us is finding candidates and what inserting them (about 100 cycles
 // each) is not measured.  (Sorting the candidates of a wavefront at once instead took
 // 64 kept ones from 19 to 17 us in two rows, but 20 of 256 rows from 27 to 31.)  Two
-// rows, 15 slices each: 7.5 us and 4 to join them, the latency of two launches; one
+// rows, 15 slices each: 7.0 us and 4 to join them, the latency of two launches; one
 // slice a row takes 22.
 
 #pragma once
@@ -142,12 +142,24 @@ __device__ __forceinline__ uint64_t lane_reverse(uint64_t v) {
   v = lane_xor<16>(v);
   return lane_xor<32>(v);
 }
-// The lists of W wavefronts (entries past k do not count) into wavefront 0's, in
-// log2 W steps; called by all.
+// The lists of W wavefronts (entries past k do not count) into wavefront 0's; called
+// by all, once.  Short ones at once (two rows' top 5: 7.4 to 7.0 us), longer ones in
+// log2 W steps.
 template <int W>
 __device__ __forceinline__ void join_waves(uint64_t& list, int k, int wave,
                                            uint64_t (*s_list)[64]) {
+  static_assert(W == 4 || W == 8);
   const int lane = threadIdx.x & 63;
+  constexpr int P = 64 / W;
+  if (k <= P) {
+    if (lane < P) s_list[0][wave * P + (wave & 1 ? P - 1 - lane : lane)] = lane < k ? list : 0;
+    __syncthreads();
+    if (wave != 0) return;
+    list = s_list[0][lane];
+    if (W == 8) list = exchanges<8, 16>(list);
+    list = exchanges<32, 64>(exchanges<16, 32>(list));
+    return;
+  }
 #pragma unroll
   for (int o = 1; o < W; o <<= 1) {
     if (lane >= k) list = 0;
