@@ -484,6 +484,7 @@ int run_page_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   //   128       of 1024       11.5  10.5         2048 of  512  37.4        31.9
   //   256       of  512       12.5   9.3         2048 of 1024  58.2        54.3
   //   256       of 1024       18.4  14.1         4096 of  512  65.8        57.0
+  // (8 of 1024: called one by one, not from a graph, the second launch costs 3 more.)
   const int W = items >= 2048 ? 1 : longest <= 1024 && items <= 256 ? 8 : 4;
   auto units = [&](int s) {
     const int64_t t = (int64_t)(cp.row0[s + 1] - cp.row0[s]) * rt;
