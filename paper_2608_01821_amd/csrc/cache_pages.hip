@@ -8,6 +8,11 @@
 // together, by the sum of their bounds; that is one product with Q+ = sum q+ and
 // Q- = sum q-, whatever their number.
 //
+// That product is NaN where an infinite bound meets a half of Q that is 0 because of the
+// signs (q = 1, lo = -inf: max(q lo, q hi) is q hi, but Q- lo is 0 times an infinity).  An
+// infinity or NaN among bounds or queries always leaves a sum that is not finite, so
+// such pages, and no others, are scored again term by term.
+//
 // Scores are float64 sums rounded to float32: the products of 16-bit values are exact
 // and their sum almost, so the order of summation does not decide which of two close
 // pages is taken, and equal scores go to the lower page.
@@ -142,6 +147,7 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t kAgain = 1;  // no score's: one still to be worked out term by term
 
 // a where this lane's bit O is clear, b where it is set, each plus that of lane ^ O
 template <int O>
@@ -211,6 +217,25 @@ struct Scorer {
         q[e] += part(elem(w, e), l < H);
       }
     }
+  }
+  // The score by its definition, term by term: of the g query heads' rows at `heads` for
+  // the page whose bounds start at b.
+  __device__ __forceinline__ static float defined(const st* heads, int g, const st* b) {
+    double x = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < g * H; ++i) {
+      const int at = i % H * N;
+      const u32x4 w = *reinterpret_cast<const u32x4*>(heads + (int64_t)(i / H) * D + at);
+      const u32x4 lo = *reinterpret_cast<const u32x4*>(b + at);
+      const u32x4 hi = *reinterpret_cast<const u32x4*>(b + D + at);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const double u = (double)elem(w, e) * (double)elem(lo, e);
+        const double v = (double)elem(w, e) * (double)elem(hi, e);
+        x += u != u || u > v ? u : v;           // (a NaN stays)
+      }
+    }
+    return (float)x;
   }
   // of the 64 pages whose places the lanes hold (0 for none): lane l's score is its own
   // page's
@@ -406,16 +431,20 @@ page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict_
       for (int i = 0; i < 8; ++i) w[i] = sc.read(__shfl(safe, base + i, 64));
     };
     load(id);
-    sc.init(q + (int64_t)row * ld_q + (int64_t)c.hk * g * D, g);
+    const typename F::st* heads = q + (int64_t)row * ld_q + (int64_t)c.hk * g * D;
+    sc.init(heads, g);
 #pragma unroll 1
     for (int p0 = wave * P; p0 < np; p0 += STEP) {
-      const float x = sc.score8(w);
+      float x = sc.score8(w);
       const int now = __shfl(id, mine, 64), p = p0 + mine;
+      // (the other lanes of a page have the same)
+      const bool own = (lane & (S::H - 4)) == 0;
+      if (own && !(fabsf(x) < INFINITY) && known(now) && p >= first && p < np - last)
+        x = S::defined(heads, g, bounds + ((int64_t)now * cv.n_kv + c.hk) * 2 * D);
       id = next;
       if (p0 + STEP < np) load(id);
       next = place(p0 + 2 * STEP);
-      // (the other lanes of a page have the same)
-      if ((lane & (S::H - 4)) == 0)
+      if (own)
         s_keys[p] = p >= np || !known(now)             ? 0u
                     : p < first || p >= np - last ? 0xffffffffu
                                                   : score_key(x);
@@ -560,7 +589,8 @@ page_select_wave_kernel(CacheView cv, ChunkPack cp, const typename F::st* __rest
   Scorer<F, D> sc;
   int next = c.table[min(lane, np - 1)];
   sc.prepare(bounds, cv.n_kv, c.hk);
-  if (!all) sc.init(q + (int64_t)row * ld_q + (int64_t)c.hk * g * D, g);
+  const typename F::st* heads = q + (int64_t)row * ld_q + (int64_t)c.hk * g * D;
+  if (!all) sc.init(heads, g);
   uint32_t kr[kWaveSteps] = {};
   const int steps = (np + 63) / 64;
 #pragma unroll 1
@@ -571,8 +601,12 @@ page_select_wave_kernel(CacheView cv, ChunkPack cp, const typename F::st* __rest
     if (i + 1 < steps) next = c.table[min(p + 64, np - 1)];
     uint32_t key = 0xffffffffu;
     if (!all) {
-      const float x = sc.score64(phys);
-      if (p >= first && p < np - last) key = score_key(x);
+      float x = sc.score64(phys);
+      if (there && p >= first && p < np - last) {
+        if (!(fabsf(x) < INFINITY))
+          x = sc.defined(heads, g, bounds + ((int64_t)phys * cv.n_kv + c.hk) * 2 * D);
+        key = score_key(x);
+      }
     }
     if (!there) key = 0;
 #pragma unroll
@@ -589,8 +623,9 @@ struct TilePack {
   int32_t first[DAVET_MAX_SEQS + 1];    // first tile of each sequence
 };
 constexpr int kTileTokens = 16, kTileThreads = 1024, kTileWaves = kTileThreads / 64;
+// (16 bits: two workgroups a CU where their LDS allows it)
 template <typename F, int D, int CAP>
-__global__ void __launch_bounds__(kTileThreads)
+__global__ void __launch_bounds__(kTileThreads, CAP <= 512 && F::dtype != DAVET_F32 ? 8 : 4)
 page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
                         const typename F::st* __restrict__ q, int64_t ld_q, int n_heads,
                         int block, const typename F::st* __restrict__ bounds, int first,
@@ -657,10 +692,13 @@ page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
     for (int i = 0; i < 4; ++i) {
       const int at = 4 * i + quad, p = p0 + at;
       uint32_t key = 0;
-      if (p < mine && (known >> at & 1))
-        key = mine <= top || p < first || p >= mine - last
-                  ? 0xffffffffu
-                  : score_key((float)(acc[0][i] + acc[1][i]));
+      if (p < mine && (known >> at & 1)) {
+        key = 0xffffffffu;
+        if (mine > top && p >= first && p < mine - last) {
+          const float x = (float)(acc[0][i] + acc[1][i]);
+          key = fabsf(x) < INFINITY ? score_key(x) : kAgain;
+        }
+      }
       s_keys[l16 * KS + p] = key;
     }
   }
@@ -668,10 +706,24 @@ page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
   for (int tok = wave; tok < nt; tok += kTileWaves) {
     const int mp = pages_of(tok0 + tok);
     uint32_t kr[CAP / 64];
+    bool again = false;
+    auto read = [&]() {
 #pragma unroll
-    for (int i = 0; i < CAP / 64; ++i) {
-      const int p = i * 64 + lane;
-      kr[i] = p < mp ? s_keys[tok * KS + p] : 0u;
+      for (int i = 0; i < CAP / 64; ++i) {
+        const int p = i * 64 + lane;
+        kr[i] = p < mp ? s_keys[tok * KS + p] : 0u;
+        again |= kr[i] == kAgain;
+      }
+    };
+    read();
+    if (__any(again)) {
+      const st* heads = q + (int64_t)(row0 + tok0 + tok) * ld_q + (int64_t)hk * g * D;
+#pragma unroll 1
+      for (int p = lane; p < mp; p += 64)
+        if (s_keys[tok * KS + p] == kAgain)
+          s_keys[tok * KS + p] = score_key(
+              S::defined(heads, g, bounds + ((int64_t)table[p] * cv.n_kv + hk) * 2 * D));
+      read();
     }
     choose(kr, top, mp <= top,
            out + ((int64_t)(row0 + tok0 + tok) * cv.n_kv + hk) * top);

@@ -166,6 +166,44 @@ def test_equal_and_odd_scores(dtype, dim):
     assert got[0, 0].tolist() == [0, 1, 2, 89, 90]
 
 
+@pytest.mark.parametrize("dtype,dim", [("f16", 128), ("bf16", 64), ("f32", 64),
+                                       ("f32", 128)])
+@pytest.mark.parametrize("new,hk", [(2, 2), (5, 256), (16, 64)],
+                         ids=["group", "waves", "tiles"])
+def test_scores_of_infinite_bounds(dtype, dim, new, hk):
+    """The score is the sum of max(q lo, q hi) also where a bound is infinite: a -inf
+    among the keys is nothing to a positive element of the query, +inf nothing to a
+    negative one; an element of 0 makes it NaN, which comes last."""
+    s = Setup(5 + dim, dtype, [new], [16 * 40 + 3], 2 * hk, hk, dim, 16)
+    rng, heads = s.rng, s.q.view(new, hk, 2, dim)
+    heads[:, ::2, 1] = heads[:, ::2, 0].abs() * heads[:, ::2, 1].sign()
+    heads[:, :, 0, 3] = heads[:, :, 1, 3] = 0.0
+    same = torch.from_numpy(rng.random((hk, dim)) < 0.7)    # both heads of one sign
+    heads[:, :, 1] = torch.where(same, heads[:, :, 1].abs() * heads[:, :, 0].sign(),
+                                 heads[:, :, 1])
+    inf = float("inf")
+    for h in range(hk):
+        for j in rng.permutation(41)[:24]:
+            page, e = s.table[0, j], int(rng.integers(0, dim))
+            kind = rng.random()
+            if kind < 0.9:                      # (most under a sign that ignores it)
+                up = rng.random() < (0.8 if heads[0, h, 0, e] < 0 else 0.2)
+                s.k[page, h, int(rng.integers(0, 3)), e] = inf if up else -inf
+            elif kind < 0.95:                   # either bound
+                s.k[page, h, 0, e], s.k[page, h, 1, e] = inf, -inf
+            else:                               # no other value
+                s.k[page, h, :, e] = inf if rng.random() < 0.5 else -inf
+    db, b = whole_bounds(s)
+    with np.errstate(invalid="ignore"):
+        for top, first, last in ((9, 0, 0), (30, 1, 2)):
+            got = select(s, db, top, first, last, 0).cpu().numpy()
+            want = oc.page_select(s.host, s.cu, s.kv, f64(s.q), 2 * hk, b, top, first,
+                                  last)
+            for r, row in enumerate(want):
+                for h, ps in enumerate(row):
+                    assert got[r, h].tolist() == ps, (r, h, top)
+
+
 def test_close_scores_do_not_depend_on_order():
     """Pages whose scores differ by less than float32 sums of their terms would be off
     by: chosen as in float64."""
