@@ -2,6 +2,7 @@
 // kernels see it, the packed chunk of new tokens, and the host's checks.
 #pragma once
 
+#include <algorithm>
 #include <initializer_list>
 
 #include "common.h"
@@ -127,6 +128,14 @@ int check_rows(const void* p, int64_t ld, int64_t width, int dtype,
                const char* who, const char* what);
 // n_heads a multiple of the cache's heads, at most 1024
 int check_heads(const davet_kv_cache* c, int32_t n_heads, const char* who);
+// A launch has fewer than 2^32 threads; of a grid with more only what is past a multiple
+// of that would run.  f(first workgroup, workgroups), in runs that each fit, of whole
+// eights.
+template <typename F>
+inline void in_runs(int64_t groups, int threads, F f) {
+  const int64_t most = (((1ll << 32) - 1) / threads) & ~7ll;
+  for (int64_t at = 0; at < groups; at += most) f((int)at, std::min(most, groups - at));
+}
 // whether all start at 4-byte boundaries (NULL does)
 inline bool aligned4(std::initializer_list<const void*> ps) {
   uintptr_t x = 0;

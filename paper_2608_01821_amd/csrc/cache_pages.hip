@@ -397,13 +397,13 @@ __global__ void __launch_bounds__(kSelThreads)
 page_select_kernel(CacheView cv, ChunkPack cp, const typename F::st* __restrict__ q,
                    int64_t ld_q, int n_heads, int block,
                    const typename F::st* __restrict__ bounds, int first, int last,
-                   int top, int32_t* __restrict__ out) {
+                   int top, int32_t* __restrict__ out, int wg0) {
   using S = Scorer<F, D>;
   constexpr int P = S::PAGES;                   // a wavefront's pages at a time
   __shared__ uint32_t s_keys[CAP];
   __shared__ __attribute__((aligned(16))) uint32_t s_cnt[2][3][kSelWaves];
   int row;
-  const Choice c = choice_of(cv, cp, blockIdx.x, block, top, out, &row);
+  const Choice c = choice_of(cv, cp, wg0 + (int)blockIdx.x, block, top, out, &row);
   const int np = c.np, g = n_heads / cv.n_kv;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kTileThreads, CAP <= 512 && F::dtype != DAVET_
 page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
                         const typename F::st* __restrict__ q, int64_t ld_q, int n_heads,
                         int block, const typename F::st* __restrict__ bounds, int first,
-                        int last, int top, int32_t* __restrict__ out) {
+                        int last, int top, int32_t* __restrict__ out, int wg0) {
   using st = typename F::st;
   using S = Scorer<F, D>;
   typedef double d4 __attribute__((ext_vector_type(4)));
@@ -637,7 +637,7 @@ page_select_tile_kernel(CacheView cv, ChunkPack cp, TilePack tp,
   constexpr int KS = CAP + 1;                   // (tokens' keys in different banks)
   __shared__ double s_q[2 * D][kTileTokens];
   __shared__ uint32_t s_keys[kTileTokens * KS];
-  const int tile = blockIdx.x / cv.n_kv, hk = blockIdx.x % cv.n_kv;
+  const int wg = wg0 + (int)blockIdx.x, tile = wg / cv.n_kv, hk = wg % cv.n_kv;
   const Lanes tiles(tp.first), rows(cp.row0);
   const int kvs = cp.kv[threadIdx.x & 63];
   const int s = tiles.owner(cp.n_seqs, tile);
@@ -828,15 +828,22 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
   //   512 x (64 x  4)  48.1  46.4  75.8     1024 x (16 x  8)  52.9     -  63.1
   const bool tiles = items >= kManyItems && longest >= 8 && most <= 1024;
   const bool waves = items >= kManyItems && most <= 64 * kWaveSteps;
+  const int64_t tile_wgs = (int64_t)tp.first[n_seqs] * cv.n_kv;
 #define TILES(F, DIM, CAP)                                                        \
-  hipLaunchKernelGGL((page_select_tile_kernel<F, DIM, CAP>),                      \
-                     dim3((unsigned)(tp.first[n_seqs] * cv.n_kv)), dim3(kTileThreads), \
-                     0, stream, cv, cp, tp, (const F::st*)q, ld_q, n_heads, block, \
-                     (const F::st*)bounds, first, last, top, pages)
+  in_runs(tile_wgs, kTileThreads, [&](int at, int64_t n) {                        \
+    hipLaunchKernelGGL((page_select_tile_kernel<F, DIM, CAP>), dim3((unsigned)n), \
+                       dim3(kTileThreads), 0, stream, cv, cp, tp,                 \
+                       (const F::st*)q, ld_q, n_heads, block,                     \
+                       (const F::st*)bounds, first, last, top, pages, at);        \
+  })
 #define SELECT(F, DIM, CAP)                                                       \
-  hipLaunchKernelGGL((page_select_kernel<F, DIM, CAP>), dim3((unsigned)items),    \
-                     dim3(kSelThreads), 0, stream, cv, cp, (const F::st*)q, ld_q, \
-                     n_heads, block, (const F::st*)bounds, first, last, top, pages)
+  in_runs(items, kSelThreads, [&](int at, int64_t n) {                            \
+    hipLaunchKernelGGL((page_select_kernel<F, DIM, CAP>), dim3((unsigned)n),      \
+                       dim3(kSelThreads), 0, stream, cv, cp, (const F::st*)q,     \
+                       ld_q, n_heads, block, (const F::st*)bounds, first, last,   \
+                       top, pages, at);                                           \
+  })
+// (at most 64 sequences of 7 tokens, or they would be tiles)
 #define WAVES(F, DIM)                                                             \
   hipLaunchKernelGGL((page_select_wave_kernel<F, DIM>),                           \
                      dim3((unsigned)((items + 3) / 4)), dim3(256), 0, stream, cv, \

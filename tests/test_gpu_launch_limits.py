@@ -1,0 +1,71 @@
+"""Calls of documented sizes whose grid has 2^32 threads and more, which is more than one
+launch takes: every row of them is answered."""
+
+import pytest
+import torch
+
+import paper_2608_01821_amd as dv
+
+pytestmark = pytest.mark.gpu
+HALF = torch.float16
+
+
+def rand(shape, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(HALF)
+
+
+def cache_of(tables, hk, dim, page, seed):
+    """A pool of three pages and these table rows."""
+    k = rand((3, hk, page, dim), seed)
+    v = rand((3, hk, page, dim), seed + 1)
+    return dv.KvCache(k, v, tables, dv.DAVET_F16)
+
+
+def table_of(seqs, pages):
+    t = torch.arange(pages, device="cuda") % 3
+    return t.to(torch.int32).expand(seqs, pages).contiguous()
+
+
+def test_selected_pages_a_workgroup_each():
+    """2^22 and more choices, one history of more than 1024 pages among them: 1024
+    threads each.  Sequences 1 .. 63 are alike."""
+    hk, dim, n = 1024, 64, 66
+    seqs = 64
+    table = table_of(seqs, 1025)
+    table[0, 3] = 1                             # (a history of its own)
+    cache = cache_of(table, hk, dim, 16, 3)
+    bounds = torch.stack([cache.k.amin(2), cache.k.amax(2)], 2)
+    cu = [0, 1] + [1 + n * (i + 1) for i in range(seqs - 1)]
+    kv = [16400] + [n] * (seqs - 1)
+    q = torch.cat([rand((1, hk * dim), 5), rand((n, hk * dim), 6).repeat(seqs - 1, 1)])
+    pages = torch.full((cu[-1], hk, 2), 7, dtype=torch.int32, device="cuda")
+    assert cu[-1] * hk * 1024 > 1 << 32
+    dv.davet_cache_page_select(cache, cu, kv, q, hk, bounds, pages)
+    one = dv.KvCache(cache.k, cache.v, table[1:2].contiguous(), dv.DAVET_F16)
+    want = torch.empty(n, hk, 2, dtype=torch.int32, device="cuda")
+    dv.davet_cache_page_select(one, [0, n], [n], q[1:1 + n], hk, bounds, want)
+    assert torch.equal(pages[1:].view(seqs - 1, n, hk, 2),
+                       want.expand(seqs - 1, n, hk, 2))
+    assert (want[..., 0] < want[..., 1]).all() and (want[..., 0] >= 0).all()
+
+
+def test_selected_pages_in_tiles():
+    """Chunks of 1041 tokens and 1024 key heads: 2^22 tiles of 16 choices, 1024 threads
+    each.  The sequences are alike."""
+    hk, dim, n, seqs = 1024, 64, 1041, 64
+    table = table_of(seqs, 66)
+    cache = cache_of(table, hk, dim, 16, 7)
+    bounds = torch.stack([cache.k.amin(2), cache.k.amax(2)], 2)
+    one = dv.KvCache(cache.k, cache.v, table[:1].contiguous(), dv.DAVET_F16)
+    first = rand((n, hk * dim), 8)
+    want = torch.empty(n, hk, 1, dtype=torch.int32, device="cuda")
+    dv.davet_cache_page_select(one, [0, n], [n], first, hk, bounds, want)
+    assert ((want >= 0) & (want < 3)).all()
+    cu, kv = [n * i for i in range(seqs + 1)], [n] * seqs
+    assert (n + 15) // 16 * seqs * hk * 1024 > 1 << 32
+    pages = torch.full((cu[-1], hk, 1), 7, dtype=torch.int32, device="cuda")
+    dv.davet_cache_page_select(cache, cu, kv, first.repeat(seqs, 1), hk, bounds, pages)
+    for i in range(seqs):
+        assert torch.equal(pages[cu[i]:cu[i + 1]], want), i
