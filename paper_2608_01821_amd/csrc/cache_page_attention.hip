@@ -84,7 +84,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
                  typename F::st* __restrict__ out, int64_t ld_o,
                  float* __restrict__ lse, int n_heads, int block, Scale sc_,
                  float* __restrict__ part, int part_rows,
-                 const int32_t* __restrict__ lists, int top) {
+                 const int32_t* __restrict__ lists, int top, int wg0) {
   using st = typename F::st;
   constexpr bool F32 = F::dtype == DAVET_F32;
   constexpr int RB = D * (int)sizeof(st);       // bytes of a row
@@ -107,7 +107,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // workgroups of a sequence: [key head][piece][tile, or four of them], tiles fastest
-  const int b = ap.xcd ? (int)blockIdx.x >> 3 : (int)blockIdx.x;
+  const int wg = wg0 + (int)blockIdx.x, b = ap.xcd ? wg >> 3 : wg;
   const Lanes blks(ap.blk), rows(cp.row0);
   const int orders = ap.order[lane], kvs = cp.kv[lane];
   const int si = blks.owner(cp.n_seqs, b), s = __builtin_amdgcn_readlane(orders, si);
@@ -119,7 +119,7 @@ page_attn_kernel(CacheView cv, ChunkPack cp, AttnPlan ap,
   int rem = b - blks.start(si);
   const int h_ = rem / (units * np);
   rem -= h_ * units * np;
-  const int hk = ap.xcd ? ((int)blockIdx.x & 7) + 8 * h_ : h_;
+  const int hk = ap.xcd ? (wg & 7) + 8 * h_ : h_;
   const int piece = rem / units;
   const int tile = W > 1 ? rem - piece * units : (rem - piece * units) * 4 + wave;
   if (tile >= tiles) return;                    // (W = 1: no barrier follows)
@@ -499,10 +499,12 @@ int run_page_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   {
     ProfScope ps(KC_MISC, stream);
 #define LAUNCH(WW, THREADS)                                                        \
-  hipLaunchKernelGGL((page_attn_kernel<F, D, WW>), dim3((unsigned)grid),           \
-                     dim3(THREADS), 0, stream, cv, cp, ap, (const st*)q, ld_q,     \
-                     (st*)out, ld_o, lse, n_heads, block, sc, part, (int)rows,     \
-                     lists, top)
+  in_runs(grid, THREADS, [&](int at, int64_t wgs) {                                \
+    hipLaunchKernelGGL((page_attn_kernel<F, D, WW>), dim3((unsigned)wgs),          \
+                       dim3(THREADS), 0, stream, cv, cp, ap, (const st*)q, ld_q,   \
+                       (st*)out, ld_o, lse, n_heads, block, sc, part, (int)rows,   \
+                       lists, top, at);                                            \
+  })
     if (W == 1) LAUNCH(1, 256);
     else if (W == 8) LAUNCH(8, 512);
     else LAUNCH(4, 256);

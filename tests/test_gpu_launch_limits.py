@@ -69,3 +69,30 @@ def test_selected_pages_in_tiles():
     dv.davet_cache_page_select(cache, cu, kv, first.repeat(seqs, 1), hk, bounds, pages)
     for i in range(seqs):
         assert torch.equal(pages[cu[i]:cu[i + 1]], want), i
+
+
+def test_attention_over_many_lists():
+    """Chunks of 1041 tokens and 1024 key heads: 2^24 workgroups of four lists, 256
+    threads each.  The sequences are alike."""
+    hk, dim, n, seqs = 1024, 64, 1041, 64
+    table = table_of(seqs, 66)
+    cache = cache_of(table, hk, dim, 16, 7)
+    one = dv.KvCache(cache.k, cache.v, table[:1].contiguous(), dv.DAVET_F16)
+    first = rand((n, hk * dim), 8)
+    pages = (torch.arange(n * hk, device="cuda") * 7 % 66).int().view(n, hk, 1)
+    ws = torch.empty(dv.davet_cache_workspace_bytes(hk, dim, n * seqs),
+                     dtype=torch.uint8, device="cuda")
+    o, e = torch.empty_like(first), torch.empty(n, hk, device="cuda")
+    dv.davet_cache_page_attention(one, [0, n], [n], first, hk, pages, o, lse=e,
+                                  workspace=ws)
+    assert torch.isfinite(o).all() and torch.isfinite(e).all()
+    cu, kv = [n * i for i in range(seqs + 1)], [n] * seqs
+    assert cu[-1] * hk // 4 * 256 > 1 << 32
+    q = first.repeat(seqs, 1)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((cu[-1], hk), 7.0, device="cuda")
+    dv.davet_cache_page_attention(cache, cu, kv, q, hk, pages.repeat(seqs, 1, 1), out,
+                                  lse=lse, workspace=ws)
+    for i in range(seqs):
+        rows = slice(cu[i], cu[i + 1])
+        assert torch.equal(out[rows], o) and torch.equal(lse[rows], e), i
