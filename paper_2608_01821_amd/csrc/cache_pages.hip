@@ -66,13 +66,14 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 // values are the keys' own, so storing them rounds nothing.
 template <typename F, int D>
 __global__ void __launch_bounds__(256)
-page_bounds_kernel(CacheView cv, BoundsPack bp, typename F::st* __restrict__ bounds) {
+page_bounds_kernel(CacheView cv, BoundsPack bp, typename F::st* __restrict__ bounds,
+                   int wg0) {
   using st = typename F::st;
   constexpr int N = 16 / (int)sizeof(st);       // elements a lane
   constexpr int C = D / N, R = 64 / C;          // lanes a row, rows a load
   constexpr int U = 4;
   __shared__ float s_lo[4][D], s_hi[4][D];
-  const int item = blockIdx.x / cv.n_kv, h = blockIdx.x % cv.n_kv;
+  const int wg = wg0 + (int)blockIdx.x, item = wg / cv.n_kv, h = wg % cv.n_kv;
   const Lanes items(bp.item);
   const int pages = bp.page[threadIdx.x & 63], kvs = bp.kv[threadIdx.x & 63];
   const int s = items.owner(bp.n_seqs, item), psz = 1 << cv.lg;
@@ -759,10 +760,11 @@ extern "C" int davet_cache_page_bounds(const davet_kv_cache* cache, int32_t n_se
   }
   if (at == 0) return DAVET_OK;
   ProfScope ps(KC_MISC, stream);
-  const dim3 grid((unsigned)(at * cv.n_kv));
 #define BOUNDS(F, DIM)                                                            \
-  hipLaunchKernelGGL((page_bounds_kernel<F, DIM>), grid, dim3(256), 0, stream, cv, \
-                     bp, (F::st*)bounds)
+  in_runs(at * cv.n_kv, 256, [&](int wg, int64_t n) {                             \
+    hipLaunchKernelGGL((page_bounds_kernel<F, DIM>), dim3((unsigned)n), dim3(256), \
+                       0, stream, cv, bp, (F::st*)bounds, wg);                    \
+  })
 #define BOUNDS_D(F) \
   do { if (cache->head_dim == 128) BOUNDS(F, 128); else BOUNDS(F, 64); } while (0)
   if (cache->dtype == DAVET_F16) BOUNDS_D(F16S);

@@ -96,3 +96,21 @@ def test_attention_over_many_lists():
     for i in range(seqs):
         rows = slice(cu[i], cu[i + 1])
         assert torch.equal(out[rows], o) and torch.equal(lse[rows], e), i
+
+
+def test_bounds_of_many_pages():
+    """2^24 and more pages and key heads, 256 threads each; most of the pages are
+    holes."""
+    hk, dim, seqs, count = 1024, 64, 64, 257
+    table = torch.full((seqs, count), -1, dtype=torch.int32, device="cuda")
+    where = [(0, 0), (31, 5), (seqs - 1, count - 1)]
+    for i, (s, p) in enumerate(where):
+        table[s, p] = i
+    k = rand((4, hk, 16, dim), 9)
+    cache = dv.KvCache(k, None, table, dv.DAVET_F16)
+    bounds = torch.full((4, hk, 2, dim), 7.0, dtype=HALF, device="cuda")
+    kv = [16 * count] * seqs
+    assert seqs * count * hk * 256 > 1 << 32
+    dv.davet_cache_page_bounds(cache, [16 * count * i for i in range(seqs + 1)], kv, bounds)
+    assert torch.equal(bounds[:3], torch.stack([k.amin(2), k.amax(2)], 2)[:3])
+    assert (bounds[3:] == 7).all()
