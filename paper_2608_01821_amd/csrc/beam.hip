@@ -70,14 +70,16 @@ __global__ void __launch_bounds__(64 * kJoinWaves)
 beam_join_kernel(int rows, int beams, int slices, int k, int P,
                  const char* __restrict__ part, const float* scores,
                  const int32_t* __restrict__ done, int pad, float* out_scores,
-                 int32_t* __restrict__ out_rows, int32_t* __restrict__ out_tokens) {
+                 int32_t* __restrict__ out_rows, int32_t* __restrict__ out_tokens,
+                 int wg0) {
   __shared__ uint64_t s_v[2][kJoinWaves * 64], s_key[2][kJoinWaves * 64];
   __shared__ uint32_t s_row[2][kJoinWaves * 64];
   __shared__ double s_base[DAVET_MAX_BEAMS];    // (NaN: nothing to offer)
   __shared__ double s_over[DAVET_MAX_BEAMS];    // the score of a row that is over, or NaN
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = blockIdx.x * beams, lists = beams * slices;
+  const int group = wg0 + (int)blockIdx.x;
+  const int row0 = group * beams, lists = beams * slices;
   const uint64_t* keys = reinterpret_cast<const uint64_t*>(part);
   const Stat* stats = reinterpret_cast<const Stat*>(keys + (int64_t)rows * slices * k);
   keys += (int64_t)row0 * slices * k;
@@ -161,7 +163,7 @@ beam_join_kernel(int rows, int beams, int slices, int k, int P,
     active = (active + take - 1) / take;
   }
   if (wave != 0 || lane >= k) return;
-  const int64_t at = (int64_t)blockIdx.x * k + lane;
+  const int64_t at = (int64_t)group * k + lane;
   out_scores[at] = best.v ? (float)value_of(best.v) : -INFINITY;
   out_rows[at] = best.v ? (int)best.row : -1;
   out_tokens[at] = best.v ? key_id(best.key) : -1;
@@ -303,9 +305,11 @@ extern "C" int davet_beam_select(int32_t groups, int32_t beams, int32_t vocab,
   int P = 1;
   while (P < top) P *= 2;
   ProfScope ps(KC_MISC, stream);
-  hipLaunchKernelGGL(beam_join_kernel, dim3(groups), dim3(64 * kJoinWaves), 0, stream,
-                     rows, beams, slices, top, P, part, scores, done, pad, out_scores,
-                     out_rows, out_tokens);
+  in_runs(groups, 64 * kJoinWaves, [&](int at, int64_t n) {
+    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)n), dim3(64 * kJoinWaves), 0,
+                       stream, rows, beams, slices, top, P, part, scores, done, pad,
+                       out_scores, out_rows, out_tokens, at);
+  });
   DAVET_HIP(hipGetLastError());
   return DAVET_OK;
 }

@@ -114,3 +114,22 @@ def test_bounds_of_many_pages():
     dv.davet_cache_page_bounds(cache, [16 * count * i for i in range(seqs + 1)], kv, bounds)
     assert torch.equal(bounds[:3], torch.stack([k.amin(2), k.amax(2)], 2)[:3])
     assert (bounds[3:] == 7).all()
+
+
+def test_beams_of_as_many_requests_as_there_may_be():
+    """2^22 requests of one beam: a workgroup of 1024 threads each."""
+    n, vocab, top = 1 << 22, 3, 2
+    x = rand((n, vocab), 1)
+    scores = torch.arange(n, device="cuda").float() / -64
+    s = torch.full((n, top), 7.0, device="cuda")
+    r, t = (torch.full((n, top), 7, dtype=torch.int32, device="cuda") for _ in range(2))
+    ws = torch.empty(dv.davet_beam_workspace_bytes(n, 1, vocab, top), dtype=torch.uint8,
+                     device="cuda")
+    dv.davet_beam_select(x, dv.DAVET_F16, scores, 1, s, r, t, workspace=ws)
+    want, at = x.double().sort(dim=1, descending=True, stable=True)
+    assert torch.equal(t, at[:, :top].int())
+    assert torch.equal(r, torch.arange(n, device="cuda").int()[:, None].expand(n, top))
+    want = scores.double()[:, None] + want[:, :top] - x.double().logsumexp(1)[:, None]
+    # the float32 sum of three exponentials (3 roundings of a number up to 3, and those
+    # of the exponentials, 2 each), then the value's own
+    assert ((s - want).abs() <= 12 * 2.0 ** -24 + 2.0 ** -24 * want.abs()).all()
