@@ -263,12 +263,12 @@ template <int RB>     // bytes of a row
 __global__ void __launch_bounds__(256)
 cache_gather_kernel(CacheView cv, GatherPack gp, const int32_t* __restrict__ kept,
                     int64_t ld_kept, const int32_t* __restrict__ dst_table,
-                    int32_t dst_max_pages) {
+                    int32_t dst_max_pages, int wg0) {
   constexpr int kRows = gather_rows(RB);
   constexpr int C = RB / 16, PER = kRows * C / 256;   // loads a thread, of K or V
   __shared__ int64_t src[kRows], dst[kRows];
   const int nblk = gp.blk[gp.n_seqs];
-  const int blk = blockIdx.x % nblk, h = blockIdx.x / nblk;
+  const int wg = wg0 + (int)blockIdx.x, blk = wg % nblk, h = wg / nblk;
   const int s = owner(gp.blk, gp.n_seqs, blk);
   const int j0 = (blk - gp.blk[s]) * kRows, lg = cv.lg, psz = 1 << lg;
   if (threadIdx.x < kRows) {
@@ -402,10 +402,12 @@ extern "C" int davet_cache_gather(const davet_kv_cache* cache, int32_t n_seqs,
   }
   if (at == 0) return DAVET_OK;
   ProfScope ps(KC_MISC, stream);
-  const dim3 grid((unsigned)(at * cv.n_kv));
 #define GATHER(RB)                                                             \
-  hipLaunchKernelGGL((cache_gather_kernel<RB>), grid, dim3(256), 0, stream, cv, \
-                     gp, kept, ld_kept, dst_table, dst_max_pages)
+  in_runs(at * cv.n_kv, 256, [&](int wg, int64_t n) {                          \
+    hipLaunchKernelGGL((cache_gather_kernel<RB>), dim3((unsigned)n), dim3(256), \
+                       0, stream, cv, gp, kept, ld_kept, dst_table,            \
+                       dst_max_pages, wg);                                     \
+  })
   if (rb == 128) GATHER(128);
   else if (rb == 256) GATHER(256);
   else GATHER(512);

@@ -133,3 +133,24 @@ def test_beams_of_as_many_requests_as_there_may_be():
     # the float32 sum of three exponentials (3 roundings of a number up to 3, and those
     # of the exponentials, 2 each), then the value's own
     assert ((s - want).abs() <= 12 * 2.0 ** -24 + 2.0 ** -24 * want.abs()).all()
+
+
+def test_gather_of_many_entries():
+    """2^24 and more blocks of 128 entries and a key head, 256 threads each; most
+    destinations are holes."""
+    hk, dim, page, seqs, keep = 1024, 64, 16, 64, 128 * 257
+    pages = keep // page
+    k, v = rand((5, hk, page, dim), 11), rand((5, hk, page, dim), 12)
+    table = torch.zeros((seqs, 1), dtype=torch.int32, device="cuda")
+    kept = (torch.arange(keep, device="cuda") * 5 % page).int().expand(seqs, keep)
+    dst = torch.full((seqs, pages), -1, dtype=torch.int32, device="cuda")
+    where = [(0, 0), (31, 5), (seqs - 1, pages - 1)]
+    for i, (s, p) in enumerate(where):
+        dst[s, p] = i + 1
+    want_k, want_v, order = k.clone(), v.clone(), torch.arange(page) * 5 % page
+    for i in range(len(where)):
+        want_k[i + 1], want_v[i + 1] = k[0][:, order], v[0][:, order]
+    assert seqs * keep // 128 * hk * 256 > 1 << 32
+    cache = dv.KvCache(k, v, table, dv.DAVET_F16)
+    dv.davet_cache_gather(cache, kept.contiguous(), [keep] * seqs, dst)
+    assert torch.equal(k, want_k) and torch.equal(v, want_v)
