@@ -35,7 +35,7 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
                      const typename F::st* __restrict__ q, int64_t ld_q,
                      const float* __restrict__ lse, int n_heads, int block,
                      Scale sc_, const float* prev, float* weights, int64_t ld_w,
-                     float* __restrict__ part) {
+                     float* __restrict__ part, int wg0) {
   using st = typename F::st;
   using T = Tile<F, D>;
   using v8 = typename Frag<F>::v8;
@@ -47,7 +47,7 @@ cache_weights_kernel(CacheView cv, ChunkPack cp, WeightPlan wp,
   __shared__ __attribute__((aligned(16))) float ls[NBUF][4][64];
   __shared__ __attribute__((aligned(16))) int lim[NBUF][4][32];
   const int nblk = wp.blk[cp.n_seqs];
-  const int blk = blockIdx.x % nblk, chunk = blockIdx.x / nblk;
+  const int wg = wg0 + (int)blockIdx.x, blk = wg % nblk, chunk = wg / nblk;
   const int s = owner(wp.blk, cp.n_seqs, blk);
   const int g = n_heads / cv.n_kv;
   const int row0 = cp.row0[s], n = cp.row0[s + 1] - row0, kv = cp.kv[s];
@@ -312,9 +312,11 @@ int launch_weights(const CacheView& cv, const ChunkPack& cp, const void* q,
                   "davet_cache_weights: too many key blocks");
   {
     ProfScope ps(KC_MISC, stream);
-    hipLaunchKernelGGL((cache_weights_kernel<F, D, KW>), dim3((unsigned)grid), dim3(256),
-                       0, stream, cv, cp, wp, (const typename F::st*)q, ld_q, lse,
-                       n_heads, block, scale, prev, weights, ld_w, part);
+    in_runs(grid, 256, [&](int at, int64_t wgs) {
+      hipLaunchKernelGGL((cache_weights_kernel<F, D, KW>), dim3((unsigned)wgs),
+                         dim3(256), 0, stream, cv, cp, wp, (const typename F::st*)q,
+                         ld_q, lse, n_heads, block, scale, prev, weights, ld_w, part, at);
+    });
     DAVET_HIP(hipGetLastError());
   }
   if (wp.chunks > 1) {

@@ -154,3 +154,32 @@ def test_gather_of_many_entries():
     cache = dv.KvCache(k, v, table, dv.DAVET_F16)
     dv.davet_cache_gather(cache, kept.contiguous(), [keep] * seqs, dst)
     assert torch.equal(k, want_k) and torch.equal(v, want_v)
+
+
+def test_weights_of_many_keys():
+    """2^24 and more blocks of 128 keys, 256 threads each: two histories of 2^30 tokens
+    that share three pages."""
+    page, n = 256, 1 << 30
+    table = table_of(3, n // page)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(13)
+    k = torch.randn((3, 1, page, 64), generator=g, device="cuda")
+    q = torch.randn((1, 64), generator=g, device="cuda").repeat(3, 1)
+    cache = dv.KvCache(k, None, table, dv.DAVET_F32)
+    w = torch.full((3, n), 7.0, device="cuda")
+    lse = torch.full((3, 1), 2.0, device="cuda")
+    ws = torch.empty(dv.davet_cache_workspace_bytes(1, 64, 3), dtype=torch.uint8,
+                     device="cuda")
+    kv = [n, n, 1]
+    assert sum(-(-x // 128) for x in kv) * 256 > 1 << 32
+    dv.davet_cache_weights(cache, [0, 1, 2, 3], kv, q, 1, lse, w, workspace=ws)
+    one = w[0, :3 * page]
+    want = torch.exp(k.view(-1, 64).double() @ q[0].double() / 8 - 2)
+    # a score is off by at most 67 roundings of the sum of its terms' magnitudes
+    off = 67 * 2.0 ** -24 * (k.view(-1, 64).double().abs() @ q[0].double().abs() / 8 + 4)
+    assert ((one - want).abs() <= want * (2 * off + 16 * 2.0 ** -24)).all()
+    whole = n // (3 * page) * 3 * page
+    for s in range(2):
+        assert (w[s, :whole].view(-1, 3 * page) == one).all()
+        assert torch.equal(w[s, whole:], one[:n - whole])
+    assert w[2, 0] == one[0] and (w[2, 1:] == 7).all()
