@@ -102,7 +102,6 @@ _P_i32 = C.POINTER(C.c_int32)
 _P_f64 = C.POINTER(C.c_double)
 _P_i64 = C.POINTER(C.c_int64)
 _P_vp = C.POINTER(C.c_void_p)
-_list = C.c_void_p      # a host list: arrays and, with less ado, _words
 
 _SIGS = {
     "davet_last_error": (C.c_char_p, []),
@@ -154,31 +153,31 @@ _SIGS = {
     "davet_mailbox_create": (C.c_int, [_P_vp]),
     "davet_mailbox_destroy": (C.c_int, [_vp]),
     "davet_set_wait_limit": (C.c_int, [C.c_double]),
-    "davet_cache_append": (C.c_int, [C.POINTER(KvCacheT), _i32, _list, _list,
+    "davet_cache_append": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _P_i32,
                                      _vp, _i64, _i32, _vp, _i32, _vp, _vp,
                                      C.c_float, C.c_float, _vp, _i64, _vp]),
     "davet_cache_workspace_bytes": (C.c_int, [_i32, _i32, _i32,
                                               C.POINTER(C.c_size_t)]),
-    "davet_cache_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _list,
-                                        _list, _vp, _i64, _i32, C.c_float,
+    "davet_cache_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                        _P_i32, _vp, _i64, _i32, C.c_float,
                                         _i32, _vp, _i64, _vp, _vp, C.c_size_t,
                                         _vp]),
-    "davet_cache_weights": (C.c_int, [C.POINTER(KvCacheT), _i32, _list, _list,
+    "davet_cache_weights": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _P_i32,
                                       _vp, _i64, _i32, C.c_float, _i32, _vp,
                                       _vp, _vp, _i64, _vp, C.c_size_t, _vp]),
-    "davet_tree_plan": (C.c_int, [_i32, _list, _list, _list, _vp, _vp, _vp,
+    "davet_tree_plan": (C.c_int, [_i32, _P_i32, _P_i32, _P_i32, _vp, _vp, _vp,
                                   _vp]),
-    "davet_cache_tree_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _list,
-                                             _list, _vp, _i64, _i32, C.c_float,
+    "davet_cache_tree_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                             _P_i32, _vp, _i64, _i32, C.c_float,
                                              _vp, _vp, _i64, _vp, _vp,
                                              C.c_size_t, _vp]),
-    "davet_cache_page_bounds": (C.c_int, [C.POINTER(KvCacheT), _i32, _list,
-                                          _list, _vp, _vp]),
-    "davet_cache_page_select": (C.c_int, [C.POINTER(KvCacheT), _i32, _list,
-                                          _list, _vp, _i64, _i32, _i32, _vp,
+    "davet_cache_page_bounds": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                          _P_i32, _vp, _vp]),
+    "davet_cache_page_select": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                          _P_i32, _vp, _i64, _i32, _i32, _vp,
                                           _i32, _i32, _i32, _vp, _vp]),
-    "davet_cache_page_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _list,
-                                             _list, _vp, _i64, _i32, C.c_float,
+    "davet_cache_page_attention": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32,
+                                             _P_i32, _vp, _i64, _i32, C.c_float,
                                              _i32, _vp, _i32, _vp, _i64, _vp,
                                              _vp, C.c_size_t, _vp]),
     "davet_beam_workspace_bytes": (C.c_int, [_i32, _i32, _i32, _i32,
@@ -186,7 +185,7 @@ _SIGS = {
     "davet_beam_select": (C.c_int, [_i32, _i32, _i32, _vp, _i32, _i64, _i32, _vp,
                                     _vp, _i32, _i32, _vp, _vp, _vp, _vp,
                                     C.c_size_t, _vp]),
-    "davet_cache_reorder": (C.c_int, [C.POINTER(KvCacheT), _i32, _list, _vp, _vp,
+    "davet_cache_reorder": (C.c_int, [C.POINTER(KvCacheT), _i32, _P_i32, _vp, _vp,
                                       _vp, _i32, _vp]),
     "davet_rotary_turns": (C.c_int, [_i32, C.c_double, _i32, C.c_double,
                                      C.c_double, C.c_double, C.c_double,
@@ -215,6 +214,21 @@ for _name, (_res, _args) in _SIGS.items():
     _f.argtypes = _args
 
 EXPORTED = tuple(_SIGS)
+
+
+class _ByBytes:
+    """The calls that take host lists as _words gives them: functions of their own, so
+    that raw()'s take int32 arrays and nothing else."""
+
+
+for _name in ("davet_cache_append", "davet_cache_attention", "davet_cache_weights",
+              "davet_tree_plan", "davet_cache_tree_attention",
+              "davet_cache_page_bounds", "davet_cache_page_select",
+              "davet_cache_page_attention", "davet_cache_reorder"):
+    _f = _L[_name]
+    _f.restype, _args = _SIGS[_name]
+    _f.argtypes = [C.c_char_p if _a is _P_i32 else _a for _a in _args]
+    setattr(_ByBytes, _name, _f)
 
 
 def raw():
@@ -747,7 +761,7 @@ def davet_cache_append(cache: KvCache, cu_q, kv_len, qkv, n_heads, q_out,
     p = _dense(pos, rows, _INT, "pos")
     gq, gk = _dense(q_gain, D, _FLOAT, "q_gain"), _dense(k_gain, D, _FLOAT, "k_gain")
     _launch(cache._gpu(qkv, q_out, pos, q_gain, k_gain), stream,
-            _L.davet_cache_append, cache._ref, n, cu, kv, x, ldx, n_heads, p,
+            _ByBytes.davet_cache_append, cache._ref, n, cu, kv, x, ldx, n_heads, p,
             1 if norm else 0, gq, gk, eps, theta, q, ldq)
 
 
@@ -768,7 +782,7 @@ def davet_cache_attention(cache: KvCache, cu_q, kv_len, q, n_heads, out,
     x, ldx = _rows(q, width, rows, cache.kinds, "q")
     o, ldo = _rows(out, width, rows, cache.kinds, "out")
     e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
-    _launch(cache._gpu(q, out, lse, workspace), stream, _L.davet_cache_attention,
+    _launch(cache._gpu(q, out, lse, workspace), stream, _ByBytes.davet_cache_attention,
             cache._ref, n, cu, kv, x, ldx, n_heads, scale, block, o, ldo, e, ws, nb)
 
 
@@ -787,7 +801,7 @@ def davet_cache_weights(cache: KvCache, cu_q, kv_len, q, n_heads, lse, weights,
             raise ValueError("davet: prev and weights need one row stride")
     e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
     _launch(cache._gpu(q, lse, weights, prev, workspace), stream,
-            _L.davet_cache_weights, cache._ref, n, cu, kv, x, ldx, n_heads, scale,
+            _ByBytes.davet_cache_weights, cache._ref, n, cu, kv, x, ldx, n_heads, scale,
             block, e, p, w, ldw, ws, nb)
 
 
@@ -869,8 +883,8 @@ def davet_tree_plan(cu_q, kv_len, parent, pos=None, mask=None, first_pos=None,
     m = _dense(mask, rows * TREE_WORDS, _BITS, "mask")
     cu, kv = _words(cu_q), None if kv_len is None else _words(kv_len)
     first = None if first_pos is None else _words(first_pos)
-    _launch(_gpu(parent, pos, mask), stream, _L.davet_tree_plan, n, cu, kv, first, up,
-            p, m)
+    _launch(_gpu(parent, pos, mask), stream, _ByBytes.davet_tree_plan, n, cu, kv,
+            first, up, p, m)
 
 
 def davet_cache_tree_attention(cache: KvCache, cu_q, kv_len, q, n_heads, mask, out,
@@ -882,7 +896,7 @@ def davet_cache_tree_attention(cache: KvCache, cu_q, kv_len, q, n_heads, mask, o
     m = _dense(mask, rows * TREE_WORDS, _BITS, "mask")
     e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
     _launch(cache._gpu(q, mask, out, lse, workspace), stream,
-            _L.davet_cache_tree_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
+            _ByBytes.davet_cache_tree_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
             scale, m, o, ldo, e, ws, nb)
 
 
@@ -907,8 +921,8 @@ def davet_cache_page_bounds(cache: KvCache, cu_q, kv_len, bounds, stream=None):
     """``bounds``: dense [n_pages, n_kv_heads, 2, head_dim] of the cache's type."""
     n, cu, kv, _ = cache._chunk(cu_q, kv_len)
     b = _page_bounds(cache, bounds)
-    _launch(cache._gpu(bounds), stream, _L.davet_cache_page_bounds, cache._ref, n, cu,
-            kv, b)
+    _launch(cache._gpu(bounds), stream, _ByBytes.davet_cache_page_bounds, cache._ref,
+            n, cu, kv, b)
 
 
 def davet_cache_page_select(cache: KvCache, cu_q, kv_len, q, n_heads, bounds, pages,
@@ -919,7 +933,7 @@ def davet_cache_page_select(cache: KvCache, cu_q, kv_len, q, n_heads, bounds, pa
     first, last = _small(first, "first"), _small(last, "last")
     x, ldx = _rows(q, n_heads * cache.head_dim, rows, cache.kinds, "q")
     b, (p, top) = _page_bounds(cache, bounds), _page_list(cache, pages, rows)
-    _launch(cache._gpu(q, bounds, pages), stream, _L.davet_cache_page_select,
+    _launch(cache._gpu(q, bounds, pages), stream, _ByBytes.davet_cache_page_select,
             cache._ref, n, cu, kv, x, ldx, n_heads, block, b, first, last, top, p)
 
 
@@ -934,7 +948,7 @@ def davet_cache_page_attention(cache: KvCache, cu_q, kv_len, q, n_heads, pages, 
     p, top = _page_list(cache, pages, rows)
     e, (ws, nb) = _dense(lse, rows * n_heads, _FLOAT, "lse"), _space(workspace)
     _launch(cache._gpu(q, pages, out, lse, workspace), stream,
-            _L.davet_cache_page_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
+            _ByBytes.davet_cache_page_attention, cache._ref, n, cu, kv, x, ldx, n_heads,
             scale, block, p, top, o, ldo, e, ws, nb)
 
 
@@ -984,7 +998,7 @@ def davet_cache_reorder(cache: KvCache, kv_len, parent, fresh, dst_table,
                          "of page_table's")
     p, f = _dense(parent, n, _INT, "parent"), _dense(fresh, n, _INT, "fresh")
     dst = _dense(dst_table, 0, _INT, "dst_table")
-    _launch(cache._gpu(parent, fresh, dst_table), stream, _L.davet_cache_reorder,
+    _launch(cache._gpu(parent, fresh, dst_table), stream, _ByBytes.davet_cache_reorder,
             cache._ref, n, _words(kv_len), p, f, dst, dst_table.shape[1])
 
 

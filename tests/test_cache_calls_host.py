@@ -129,6 +129,28 @@ def test_lists_reach_the_library_whole():
         assert dv._lib._ints(got) is got
 
 
+@pytest.mark.parametrize("name", [
+    "davet_cache_append", "davet_cache_attention", "davet_cache_weights",
+    "davet_tree_plan", "davet_cache_tree_attention", "davet_cache_page_bounds",
+    "davet_cache_page_select", "davet_cache_page_attention", "davet_cache_reorder",
+    "davet_evict_select", "davet_cache_gather"])
+def test_raw_calls_take_lists_of_int32_alone(name):
+    """An array of other integers would be read as int32, a number as an address."""
+    f = getattr(dv.raw(), name)
+    lists = [i for i, t in enumerate(f.argtypes) if t is C.POINTER(C.c_int32)]
+    assert len(lists) == {"davet_tree_plan": 3, "davet_cache_reorder": 1,
+                          "davet_cache_gather": 1}.get(name, 2)
+    i32 = (C.c_int32 * 3)(0, 0, 0)
+    for at in lists:
+        for bad in ((C.c_int64 * 3)(0, 0, 0), (C.c_float * 3)(), A, b"\0" * 12):
+            args = [i32 if i in lists else None if t is C.POINTER(dv.KvCacheT) else
+                    t(0) for i, t in enumerate(f.argtypes)]
+            assert f(*args) < 0                 # no cache, or no sequence
+            args[at] = bad
+            with pytest.raises(C.ArgumentError):
+                f(*args)
+
+
 def test_streams_by_public_names(monkeypatch):
     """A torch without the short cuts that the binding takes."""
     class Stream:
