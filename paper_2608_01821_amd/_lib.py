@@ -685,6 +685,10 @@ def _small(v, name):
     return v
 
 
+def _too_large():
+    raise ValueError("davet: a tensor's sizes must be 32-bit integers")
+
+
 def _gpu(first, *tensors):
     """Index of the GPU that holds all tensors (None entries aside)."""
     dev = first.get_device()
@@ -723,6 +727,8 @@ class KvCache:
             raise ValueError("davet: k and v must be [n_pages, n_kv_heads, "
                              "page_size, head_dim] alike, page_table [n_seqs, "
                              "max_pages]")
+        if max(*k.shape, page_table.shape[1]) >> 31:
+            _too_large()
         addr = (_dense(k, 0, kinds, "k"), _dense(v, 0, kinds, "v"),
                 _dense(page_table, 0, _INT, "page_table"))
         self.k, self.v, self.page_table = k, v, page_table
@@ -828,6 +834,8 @@ def davet_cache_gather(cache: KvCache, kept, keep, dst_table, stream=None):
     n = len(keep)
     if n == 0 or n > cache.n_seqs or dst_table.dim() != 2 or len(dst_table) < n:
         raise ValueError("davet: the page tables need a row a sequence")
+    if dst_table.shape[1] >> 31:
+        _too_large()
     k, ldk = _rows(kept, max(keep), n, _INT, "kept")
     dst = _dense(dst_table, 0, _INT, "dst_table")
     _launch(cache._gpu(kept, dst_table), stream, _L.davet_cache_gather, cache._ref,
@@ -848,6 +856,8 @@ def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
     """``logits`` [rows, vocab]; ``top_logp`` and ``top_ids`` [rows, top], dense
     (both or neither)."""
     rows, vocab = logits.shape
+    if (rows | vocab) >> 31:
+        _too_large()
     x, ld = _rows(logits, vocab, rows, _kinds(dtype), "logits")
     g, lp = _dense(targets, rows, _INT, "targets"), _dense(logp, rows, _FLOAT, "logp")
     en = _dense(entropy, rows, _FLOAT, "entropy")
@@ -857,6 +867,8 @@ def davet_token_logprobs(logits, dtype, targets=None, logp=None, entropy=None,
                 top_ids.shape != top_logp.shape:
             raise ValueError("davet: top_logp and top_ids must be [rows, top]")
         top = top_ids.shape[1]
+        if top >> 31:
+            _too_large()
         tl = _dense(top_logp, rows * top, _FLOAT, "top_logp")
         ti = _dense(top_ids, rows * top, _INT, "top_ids")
     exclude, (ws, nb) = _small(exclude, "exclude"), _space(workspace)
@@ -914,6 +926,8 @@ def _page_list(cache, pages, rows):
     shape = pages.shape
     if len(shape) != 3 or shape[0] < rows or shape[1] != cache.n_kv_heads:
         raise ValueError("davet: pages must be [rows, n_kv_heads, top]")
+    if shape[2] >> 31:
+        _too_large()
     return _dense(pages, 0, _INT, "pages"), shape[2]
 
 
@@ -978,6 +992,8 @@ def davet_beam_select(logits, dtype, scores, beams, out_scores, out_rows, out_to
             out_tokens.shape != shape:
         raise ValueError("davet: out_scores, out_rows and out_tokens must be "
                          "[groups, top]")
+    if (rows | vocab | shape[1]) >> 31:
+        _too_large()
     o = _dense(out_scores, 0, _FLOAT, "out_scores")
     r, t = _dense(out_rows, 0, _INT, "out_rows"), _dense(out_tokens, 0, _INT,
                                                          "out_tokens")
@@ -996,6 +1012,8 @@ def davet_cache_reorder(cache: KvCache, kv_len, parent, fresh, dst_table,
     if n == 0 or n != cache.n_seqs or dst_table.dim() != 2 or len(dst_table) < n:
         raise ValueError("davet: kv_len needs an entry, and dst_table a row, for each "
                          "of page_table's")
+    if dst_table.shape[1] >> 31:
+        _too_large()
     p, f = _dense(parent, n, _INT, "parent"), _dense(fresh, n, _INT, "fresh")
     dst = _dense(dst_table, 0, _INT, "dst_table")
     _launch(cache._gpu(parent, fresh, dst_table), stream, _ByBytes.davet_cache_reorder,
@@ -1018,7 +1036,9 @@ def davet_rotary(x, n_heads, head_dim, turns, out, dtype, pos=None,
                  layout=DAVET_ROTARY_HALVES, gain=1.0, inverse=False, stream=None):
     """``x`` and ``out`` [rows, n_heads * head_dim] or wider; ``turns`` a dense
     float64 device tensor: twice its length is the part of a head that turns."""
-    kinds, rows = _kinds(dtype), x.shape[0]
+    kinds, rows, dim = _kinds(dtype), x.shape[0], 2 * turns.numel()
+    if (rows | dim) >> 31:
+        _too_large()
     n_heads, head_dim = _small(n_heads, "n_heads"), _small(head_dim, "head_dim")
     width = _small(n_heads * head_dim, "n_heads * head_dim")
     a, lda = _rows(x, width, rows, kinds, "x")
@@ -1026,7 +1046,7 @@ def davet_rotary(x, n_heads, head_dim, turns, out, dtype, pos=None,
     t, p = _dense(turns, 1, _DOUBLE, "turns"), _dense(pos, rows, _INT, "pos")
     layout = _small(layout, "layout")
     _launch(_gpu(x, out, turns, pos), stream, _L.davet_rotary, rows, n_heads,
-            head_dim, 2 * turns.numel(), layout, a, lda, o, ldo, int(dtype), p, t,
+            head_dim, dim, layout, a, lda, o, ldo, int(dtype), p, t,
             gain, 1 if inverse else 0)
 
 

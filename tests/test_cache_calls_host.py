@@ -129,6 +129,45 @@ def test_lists_reach_the_library_whole():
         assert dv._lib._ints(got) is got
 
 
+def test_sizes_of_tensors_beyond_32_bits_are_refused():
+    """Not taken modulo 2^32: a vocabulary of 2^32 + 3 is not one of 3."""
+    big, f16, i = 2 ** 32 + 3, torch.float16, torch.int32
+
+    def of(*shape, dtype=f16):
+        return torch.empty(shape, dtype=dtype, device="meta")
+    c = dv.KvCache(K16, K16, TABLE, dv.DAVET_F16)
+    k, one = of(4, 2, 16, 64), torch.zeros(2, dtype=i)
+    s, turns = of(3, 2, dtype=torch.float32), of(1, dtype=torch.float64)
+    ids, h = of(3, 2, dtype=i), dv.DAVET_F16
+    for call in (
+            lambda: dv.KvCache(k, k, of(1, big, dtype=i), h),
+            lambda: dv.KvCache(of(big, 2, 16, 64), None, of(1, 4, dtype=i), h),
+            lambda: dv.davet_token_logprobs(of(1, big), h),
+            lambda: dv.davet_token_logprobs(of(big, 1), h),
+            lambda: dv.davet_token_logprobs(of(1, 9), h, top_ids=of(1, big, dtype=i),
+                                            top_logp=of(1, big, dtype=torch.float32)),
+            lambda: dv.davet_cache_gather(c, I, [2], of(1, big, dtype=i)),
+            lambda: dv.davet_cache_reorder(c, [1, 1], one, one, of(2, big, dtype=i)),
+            lambda: dv.davet_cache_page_select(c, *CHUNK, Q16, 4,
+                                               torch.zeros(4, 2, 2, 64, dtype=f16),
+                                               of(3, 2, big, dtype=i)),
+            lambda: dv.davet_cache_page_attention(c, *CHUNK, Q16, 4,
+                                                  of(3, 2, big, dtype=i), Q16),
+            lambda: dv.davet_beam_select(of(3, big), h, s, 1, s, ids, ids),
+            lambda: dv.davet_beam_select(of(big, 1), h, of(big, dtype=torch.float32), 1,
+                                         of(big, 2, dtype=torch.float32),
+                                         of(big, 2, dtype=i), of(big, 2, dtype=i)),
+            lambda: dv.davet_beam_select(of(3, 9), h, s, 1,
+                                         of(3, big, dtype=torch.float32),
+                                         of(3, big, dtype=i), of(3, big, dtype=i)),
+            lambda: dv.davet_rotary(of(big, 64), 1, 64, turns, of(big, 64), h),
+            lambda: dv.davet_rotary(of(3, 64), 1, 64, of(2 ** 31 + 1,
+                                                         dtype=torch.float64),
+                                    of(3, 64), h)):
+        with pytest.raises(ValueError, match="32-bit"):
+            call()
+
+
 @pytest.mark.parametrize("name", [
     "davet_cache_append", "davet_cache_attention", "davet_cache_weights",
     "davet_tree_plan", "davet_cache_tree_attention", "davet_cache_page_bounds",
