@@ -870,8 +870,9 @@ int davet_rotary_turns(int32_t dim, double theta, int32_t scaling, double factor
  * and copies the others.  inverse 1: by -t, which makes it the gradient of the call
  * with inverse 0 (dx from dout, the same gain).
  *   pos: device int32 [rows], any values, or NULL for the row numbers; turns: device
- *   double [dim / 2].  Whole turns are taken off in float64, so that every int32
- *   position is turned as exactly as a small one.
+ *   double [dim / 2].  Whole turns are taken off in float64 without a rounding, so a
+ *   far position adds only what its rate is off by, up to |pos| turns[i] 2^-53 turns
+ *   (4e-8 for the fastest pair at 2^31).
  *   gain: finite (1; a scaled model's attention factor, once on queries and keys).
  *   out may be x (same address and, of several rows, stride) and must not overlap
  *   it otherwise.  Strides and addresses need no more than the elements' alignment;

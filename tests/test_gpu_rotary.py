@@ -2,6 +2,8 @@
 sizes, strides and alignments, far positions, in place, backwards; its gradient; and
 a cache whose keys it turned."""
 
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -85,6 +87,28 @@ def test_rotary(case, in_place):
     assert torch.equal(out[:, heads * width:], before[:, heads * width:])
     if not in_place:
         assert np.array_equal(f64(store), f64(flat))
+
+
+@pytest.mark.parametrize("far", [10, 1 << 16, 1 << 24, 1 << 31])
+def test_far_positions_add_no_error(far):
+    """cos and sin themselves (a pair of 1 and 0, fp32) against the stored rates' angles
+    in exact arithmetic: the functions' unit in the last place and the correction's
+    half, of numbers up to 1, whatever the position."""
+    rng = np.random.default_rng(far)
+    pos = rng.integers(-far, far, 2048)
+    per = dv.davet_rotary_turns(128, 1e4)
+    x = torch.zeros(2048, 128)
+    x[:, :64] = 1.0
+    out = torch.empty(2048, 128, device="cuda")
+    dv.davet_rotary(x.cuda(), 1, 128, torch.tensor(per, dtype=torch.float64).cuda(), out,
+                    dv.DAVET_F32, pos=torch.from_numpy(pos.astype(np.int32)).cuda())
+    got = f64(out)
+    for i in (0, 1, 7, 20, 63):
+        rate = Fraction(per[i])
+        turns = [int(p) * rate for p in pos]
+        angle = 2 * np.pi * np.array([float(t - round(t)) for t in turns])
+        assert np.abs(got[:, i] - np.cos(angle)).max() <= 1.5 * 2.0 ** -24
+        assert np.abs(got[:, 64 + i] - np.sin(angle)).max() <= 1.5 * 2.0 ** -24
 
 
 @pytest.mark.parametrize("pairs", [False, True])
