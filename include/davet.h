@@ -733,8 +733,11 @@ int davet_cache_page_bounds(const davet_kv_cache* cache, int32_t n_seqs,
  * ranked first by (score descending, page ascending), NaN with -inf,
  *   score = sum_{heads of the key head} sum_e max(q_e lo_e, q_e hi_e),
  * no less than the sum of their scores (without the scale) with any key of the page.
- * The sum is taken in float64 and rounded to float32, so what is selected depends on no
- * order of summation.
+ * The sum is taken in float64, in an order that goes by the sizes of the call, and
+ * rounded to float32.  Where products and sums are exact in float64 (16-bit values whose
+ * products lie within some 2^20 of each other) the order does not matter; elsewhere it
+ * may seldom round a score to the neighbouring float32, and so decide between two pages
+ * that close.
  *   pages: device int32 [rows, n_kv_heads, top]: indices in the sequence's page table,
  *   ascending, then -1.
  * top in [1, 32768], first + last <= top; sequences with new tokens have at most 32768

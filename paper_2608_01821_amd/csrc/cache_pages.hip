@@ -13,9 +13,10 @@
 // infinity or NaN among bounds or queries always leaves a sum that is not finite, so
 // such pages, and no others, are scored again term by term.
 //
-// Scores are float64 sums rounded to float32: the products of 16-bit values are exact
-// and their sum almost, so the order of summation does not decide which of two close
-// pages is taken, and equal scores go to the lower page.
+// Scores are float64 sums rounded to float32, and equal ones go to the lower page.  The
+// forms below add in different orders: of 16-bit values products are exact, and sums too
+// unless they span more than 2^20 or so; then, and in fp32, a score may seldom come out
+// as the neighbouring float32.
 //
 // Three forms:
 //   group  a workgroup each (token, key head)

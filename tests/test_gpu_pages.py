@@ -220,6 +220,49 @@ def test_close_scores_do_not_depend_on_order():
     assert got[0, 0].tolist() == want[0][0]
 
 
+@pytest.mark.parametrize("dtype,dim", [("f16", 128), ("bf16", 64), ("f32", 64),
+                                       ("f32", 128)])
+def test_the_batch_around_it_does_not_change_a_choice(dtype, dim):
+    """The same five rows by a workgroup each, by a wavefront each (seven such sequences)
+    and in tiles (a longer chunk beside them).  16-bit values of a coarse grid: every sum
+    is exact, the lists are equal.  fp32: every form's pages are the best ones up to the
+    roundings of a score (to float32, and of at most 4 dim products and sums in
+    float64)."""
+    hk, heads, np_, top = 32, 64, 300, 40
+    s = Setup(dim, dtype, [5, 40], [16 * np_, 60], heads, hk, dim, 16)
+    if dtype != "f32":
+        s.q[:], s.k[:] = (s.q * 8).round() / 8, (s.k * 8).round() / 8
+    db, b = whole_bounds(s)
+    q, table = s.q.cuda(), torch.from_numpy(s.table).cuda()
+    got = []
+    for rows, kv, tables in (
+            ([5], [16 * np_], table[:1]),
+            ([5] * 7, [16 * np_] * 7, table[:1].repeat(7, 1)),
+            ([5, 40], [16 * np_, 60], table)):
+        cu = [0] + [int(x) for x in np.cumsum(rows)]
+        cache = dv.KvCache(s.dk, s.dv, tables.contiguous(), CODE[dtype])
+        x = q[:5].repeat(7, 1) if len(rows) == 7 else q[:cu[-1]]
+        pages = torch.full((cu[-1], hk, top), 7, dtype=torch.int32, device="cuda")
+        dv.davet_cache_page_select(cache, cu, kv, x, heads, db, pages)
+        got += [p.cpu().numpy() for p in pages[:35 if len(rows) == 7 else 5].split(5)]
+    if dtype != "f32":
+        for p in got[1:]:
+            assert np.array_equal(p, got[0])
+        return
+    lo, hi = np.moveaxis(b[s.table[0]].astype(np.longdouble), 2, 0)     # [pages, hk, D]
+    qs = f64(s.q)[:5].astype(np.longdouble).reshape(5, hk, 2, 1, dim)
+    lo, hi = (np.moveaxis(x, 1, 0)[:, None] for x in (lo, hi))          # [hk, 1, pages, D]
+    score = np.maximum(qs * lo, qs * hi).sum((2, 4))                    # [5, hk, pages]
+    mass = (np.abs(qs) * np.maximum(np.abs(lo), np.abs(hi))).sum((2, 4))
+    off = 2.0 ** -24 * np.abs(score) + 4 * dim * 2.0 ** -53 * mass
+    for p in got:
+        took = np.zeros(score.shape, bool)
+        np.put_along_axis(took, p, True, 2)
+        assert (took.sum(2) == top).all()
+        least = np.where(took, score + off, np.inf).min(2)
+        assert (least >= np.where(took, -np.inf, score - off).max(2)).all()
+
+
 ATTEND = [  # dtype, new, kv, heads, kv_heads, dim, page, block, top
     ("f16", [1], [1], 1, 1, 64, 16, 0, 1),
     ("f16", [1], [700], 8, 2, 128, 16, 1, 8),
