@@ -1,6 +1,6 @@
 // The attention kernels over a paged key/value cache, for a chunk of new tokens
 // (cache_attention.hip) and a tree of them (cache_tree.hip); what they share with the
-// attention over listed pages (cache_pages.hip).
+// attention over listed pages (cache_page_attention.hip).
 //
 //   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),
 //   lse_i = ln sum_j exp(scale q_i.k_j)
