@@ -831,7 +831,11 @@ int davet_beam_select(int32_t groups, int32_t beams, int32_t vocab,
  * they are.  Fresh pages must be distinct and hold no key that the call reads (fresh[s]
  * may be the parent's own last page: then it stays there, uncopied).  A parent outside
  * [0, n_seqs), a hole for a last page and a fresh page outside the pool make the
- * entries concerned -1. */
+ * entries concerned -1.
+ * n_seqs is at most DAVET_MAX_SEQS and parents count from this call's first row, while
+ * davet_beam_select counts rows over its whole batch: a batch of more rows is moved in
+ * several calls of whole requests, each on its rows of the page tables, with the first
+ * of them taken off out_rows (on the device). */
 int davet_cache_reorder(const davet_kv_cache* cache, int32_t n_seqs,
                         const int32_t* kv_len, const int32_t* parent,
                         const int32_t* fresh, int32_t* dst_table,

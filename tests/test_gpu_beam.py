@@ -202,6 +202,32 @@ def test_reorder(case, odd):
     assert np.array_equal(cache.page_table.cpu().numpy(), table)
 
 
+def test_more_rows_than_one_reordering_takes():
+    """Twenty requests of four beams: one selection, the cache moved in two calls of
+    whole requests, with the first row of each taken off the parents."""
+    rng = np.random.default_rng(5)
+    groups, beams, kv, page = 20, 4, 37, 16
+    rows = groups * beams
+    total, table = page_table(rng, [kv] * rows, page, extra=rows)
+    free = np.array([p for p in range(total) if p not in table], np.int32)
+    k, v = (values(rng, (total, 2, page, 64), "f16") for _ in range(2))
+    dk, dvv, dtable = k.cuda(), v.cuda(), torch.from_numpy(table).cuda()
+    x, scores = values(rng, (rows, 50), "f32", 3.0), values(rng, (rows,), "f32")
+    o, r, _ = select(x.cuda(), "f32", scores, beams, beams)
+    parents, fresh = torch.from_numpy(r).cuda().view(-1), torch.from_numpy(free).cuda()
+    dst = torch.full((rows, table.shape[1]), 77, dtype=torch.int32, device="cuda")
+    for n in range(0, rows, 64):
+        m = slice(n, min(n + 64, rows))
+        cache = dv.KvCache(dk, dvv, dtable[m], dv.DAVET_F16)
+        dv.davet_cache_reorder(cache, [kv] * (m.stop - n), parents[m] - n, fresh[m],
+                               dst[m])
+    want = np.full(dst.shape, 77, np.int32)
+    rk, rv, rd = oc.reorder(dict(k=f64(k), v=f64(v), table=table), [kv] * rows,
+                            r.reshape(-1), free, want)
+    assert np.array_equal(dst.cpu().numpy(), rd)
+    assert np.array_equal(f64(dk), rk) and np.array_equal(f64(dvv), rv)
+
+
 def test_steps_of_a_search():
     """Two requests, three beams, five tokens over two layers: selection, reordering,
     append, attention.  The cache a beam ends with is that of its own tokens alone."""
