@@ -845,7 +845,8 @@ int davet_cache_reorder(const davet_kv_cache* cache, int32_t n_seqs,
 
 /* davet_cache_append turns whole heads in halves by unscaled frequencies.  For
  * models with another layout these calls turn queries and keys first; the append
- * then gets pos all zero, which turns nothing (cos 0 = 1, sin 0 = 0, exactly). */
+ * then gets pos all zero, which turns no finite value (cos 0 = 1 and sin 0 = 0 exactly;
+ * an infinity, 0 times which is NaN, makes its partner NaN there as in any turn). */
 typedef enum davet_rotary_layout {
   DAVET_ROTARY_HALVES = 0,   /* pair i: elements i and i + dim / 2 */
   DAVET_ROTARY_PAIRS = 1     /* pair i: elements 2 i and 2 i + 1   */

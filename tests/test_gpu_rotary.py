@@ -144,6 +144,25 @@ def test_infinities_stay_in_their_pairs(pairs):
     assert out[1, 2 * 64 + 60].item() == float("inf")
 
 
+def test_an_infinity_at_position_0():
+    """A turn by nothing is one of 0 times its partner too: NaN beside an infinity, in
+    the rotary call and in the append alike; finite values stay as they are."""
+    x = values(np.random.default_rng(4), (1, 3 * 64), "f16").cuda()
+    x[0, 5] = float("inf")
+    turns = torch.tensor(dv.davet_rotary_turns(64, 1e4), dtype=torch.float64).cuda()
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, q = torch.empty_like(x), torch.empty(1, 64, dtype=x.dtype, device="cuda")
+    dv.davet_rotary(x, 3, 64, turns, out, dv.DAVET_F16, pos=zero)
+    k = torch.zeros(1, 1, 16, 64, dtype=x.dtype, device="cuda")
+    cache = dv.KvCache(k, k.clone(), zero.view(1, 1), dv.DAVET_F16)
+    dv.davet_cache_append(cache, [0, 1], [1], x, 1, q, pos=zero)
+    for got in (out[0, :64], q[0]):
+        assert got[5] == float("inf") and torch.isnan(got[5 + 32])
+        rest = [i for i in range(64) if i not in (5, 5 + 32)]
+        assert torch.equal(got[rest], x[0, rest])
+    assert torch.equal(out[0, 64:], x[0, 64:]) and torch.equal(k[0, 0, 0], x[0, 64:128])
+
+
 @pytest.mark.parametrize("pairs", [False, True])
 @pytest.mark.parametrize("dim", [128, 40])
 def test_gradient(pairs, dim):
