@@ -1281,7 +1281,11 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   // Rows from which the wide form is taken, by the longest chunk of the batch (one
   // launch): a short one beside it has its probabilities rounded once too.  Error of
   // the output against 64 bits, its own rounding included: 2.1e-4 narrow, 2.8e-4 wide
-  // in fp16; 1.7e-3 and 2.2e-3 in bf16.  16 bits: sixteen sequences over up to
+  // in fp16; 1.7e-3 and 2.3e-3 in bf16.  The rest carried in the wide form too (half the
+  // fragments read ahead, or its registers spill) gives narrow's error and costs 14 % of
+  // eight trees of 26 tokens on 32,700, 4 % of sixteen of 64 on 3741, and 10 to 24 % of 48
+  // to 256 tokens on 3000; prompts, bound by the matrix ops, more.  A tree that is a chain
+  // gives the causal chunk's bits, so both are rounded alike.  16 bits: sixteen sequences over up to
   // 3000 keys, 32 heads of 128, take 109 us with 48 rows where narrow takes 161, and
   // 100 both with 32, where narrow keeps more of the probabilities.  fp32 (one
   // buffer): four sequences, 8 heads, 58 us with 64 rows where narrow takes 43, and

@@ -29,9 +29,13 @@
 // Measured, 32 heads over 8 of 128: eight tokens with 64 pages of 64 each, fp16, 25.3 us
 // (136 MB, 5.4 TB/s: HBM) and 4.8 to join the pieces; 512 tokens with 32 pages of 16,
 // bf16, 63 us.  Those read 1.07 GB (17 TB/s), the most of it from L2, and every 512 tokens
-// more cost 52 us (21 TB/s); the load path of a CU is busy for 58 % of the time, vector
-// ALUs for 30, matrix pipes for 16.  Registers hold three wavefronts a SIMD; four, with
-// tiles of 16 keys, gain 4 % at 512 keys a list and nothing at 1024.
+// more cost 52 us (21 TB/s).  The difference is the last round: 768 of the 1024 workgroups
+// run at once, three a CU, and 256 after them.  No unit is busy throughout: the load path
+// of a CU for 58 % of the time, vector ALUs for 30, matrix pipes for 16, and a wavefront
+// waits for data for 37 % and for its turn for 39.  Registers hold three wavefronts a SIMD;
+// four, with tiles of 16 keys, gain 4 % at 512 keys a list and nothing at 1024.  fp32, over
+// and over: 155 us for the 512 tokens where fp16 takes 50, 35 for the eight where it
+// takes 20.
 
 #include "cache_attn.h"
 

@@ -30,11 +30,17 @@
 // Then the key of the last page taken is found from its highest bit down, by counting,
 // and the pages are written in ascending order.
 //
-// Measured with 8 key heads of 128, 16 bits: bounds of a page 4 to 5 us (a chain of
-// loads); the choice of 64 of up to 1022 pages for eight tokens 22.7 us, of them 16 the scores:
+// Measured with 8 key heads of 128, 16 bits.  Bounds of a page 4 to 5 us (a chain of
+// loads); of 49,408 tokens' pages, over and over, 72 us in pages of 16 (1.6 TB/s: 4 KB of
+// work a workgroup, and of each lane's four loads three repeat the last row), 40 of 32,
+// 22 of 64 (4.8 TB/s; fp32 40 and 32, 5.7 and 6.6 TB/s, part of it from the last-level
+// cache).
+// The choice of 64 of up to 1022 pages for eight tokens 21.4 us, of them 16 the scores:
 // vector ops, three of each 16-bit element's five being its way to float64 and its
-// product, 64 CUs at work; of 32 among up to 234 for 512 tokens 20.6 us, bound by the
-// float64 matrix rate (64 cycles for 16 x 16 x 4).
+// product, 64 CUs at work (fp32 2 us more).  Of 32 among up to 234 for 512 tokens 20.4 us
+// (fp32 the same): about 7 of launch, loads and Q's sums, 9 of products (6.8 at the
+// float64 matrix rate, 64 cycles for 16 x 16 x 4) and 6 of ranking, each timed by leaving
+// the others out; of 64 pages 13.7, of them 4, 4 and 6.
 
 #include <math.h>
 
@@ -829,6 +835,8 @@ extern "C" int davet_cache_page_select(const davet_kv_cache* cache, int32_t n_se
   //   512 x (64 x  1)  48.4  31.4  30.0      512 x (16 x 16)  31.7  46.1  74.3
   //   512 x (64 x  2)  47.5  32.2  44.6     1024 x ( 1 x 16)  53.1     -  21.2
   //   512 x (64 x  4)  48.1  46.4  75.8     1024 x (16 x  8)  52.9     -  63.1
+  // (Of few pages waves are faster by 1.5 us than the tiles that the rule takes; and one
+  // chunk of 8 tokens takes shorter ones beside it into tiles that are mostly empty.)
   const bool tiles = items >= kManyItems && longest >= 8 && most <= 1024;
   const bool waves = items >= kManyItems && most <= 64 * kWaveSteps;
   const int64_t tile_wgs = (int64_t)tp.first[n_seqs] * cv.n_kv;

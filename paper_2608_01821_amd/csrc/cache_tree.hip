@@ -11,8 +11,9 @@
 // The attention walks the cache once for all tokens of the tree, as for a chunk; only
 // tiles that reach into the chunk read the rows' masks (LDS, a shift a lane and tile).
 // Bound by HBM: eight trees of 26 tokens on 32,700 cached ones, 32 heads over 8 of 128,
-// fp16, 156 us (779 MB, 5.0 TB/s) and 11 to join the pieces; sixteen of up to 64 on up to
-// 3741, 32 heads, bf16, 126 us (607 MB, 4.8 TB/s).
+// fp16, 151 us (779 MB, 5.1 TB/s) and 10 to join the pieces; sixteen of up to 64 on up to
+// 3741, 32 heads, bf16, 127 us (607 MB, 4.8 TB/s).  fp32, eight of 64 to 256 on up to
+// 3000, 32 heads over 8: 88 to 104 TFLOP/s of 154, with one buffer as the chunk's.
 
 #include "cache_attn.h"
 
