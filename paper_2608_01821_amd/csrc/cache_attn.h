@@ -1285,11 +1285,11 @@ int run_attention(const CacheView& cv, const ChunkPack& cp, const void* q,
   // fragments read ahead, or its registers spill) gives narrow's error and costs 14 % of
   // eight trees of 26 tokens on 32,700, 4 % of sixteen of 64 on 3741, and 10 to 24 % of 48
   // to 256 tokens on 3000; prompts, bound by the matrix ops, more.  A tree that is a chain
-  // gives the causal chunk's bits, so both are rounded alike.  16 bits: sixteen sequences over up to
-  // 3000 keys, 32 heads of 128, take 109 us with 48 rows where narrow takes 161, and
-  // 100 both with 32, where narrow keeps more of the probabilities.  fp32 (one
-  // buffer): four sequences, 8 heads, 58 us with 64 rows where narrow takes 43, and
-  // 62 with 96 where it takes 63.
+  // gives the causal chunk's bits, so both are rounded alike.
+  // 16 bits: sixteen sequences over up to 3000 keys, 32 heads of 128, take 109 us with
+  // 48 rows where narrow takes 161, and 100 both with 32, where narrow keeps more of the
+  // probabilities.  fp32 (one buffer): four sequences, 8 heads, 58 us with 64 rows where
+  // narrow takes 43, and 62 with 96 where it takes 63.
   constexpr bool f32 = F::dtype == DAVET_F32;
   const bool wide = (int64_t)most * g > (f32 ? 64 : 32);
   constexpr int WB = f32 ? 1 : 2;                       // wide: buffers

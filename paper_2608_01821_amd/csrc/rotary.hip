@@ -10,9 +10,11 @@
 // nearest whole number, so a far position adds only what the rate itself is off by, up
 // to |p| turns[i] 2^-53 turns.  What is left, at most half a turn, goes through the fp32
 // sine and cosine, and what its rounding to float took off is added to first order
-// (fp32: error 2.5e-8 in the 2-norm, 3.2e-8 without it, in the same time).  A workgroup takes a run of rows: one
-// wavefront computes the dim/2 angles of the next row into LDS while the others work
-// on this one's heads, and the next pieces of x are on their way meanwhile.
+// (fp32: error 2.5e-8 in the 2-norm, 3.2e-8 without it, in the same time).
+//
+// A workgroup takes a run of rows: one wavefront computes the dim/2 angles of the next
+// row into LDS while the others work on this one's heads, and the next pieces of x are
+// on their way meanwhile.
 //
 // A thread moves vectors of V elements: V is the largest of 8, 4, 2, 1 that divides
 // every offset (half the turned part, the rest of the head, the head, the strides,
