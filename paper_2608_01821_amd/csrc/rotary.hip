@@ -23,9 +23,8 @@
 // Bound by HBM: read once, written once.  Measured: those 3092 rows 13.5 us (4.7 TB/s),
 // 4099 fp32 rows of 32 x 80, 32 of each head turned, 16.0 (5.2 TB/s; a large copy
 // reaches 5.1); one row 2.4, a launch's latency.  An odd half, stride or address leaves
-// one element an access and is bound by the accesses: those 3092 rows, over and over, 24
-// to 26 us in halves and 19 in pairs where 16 bytes each take 11.3 (fp32 24 to 26 and 22,
-// and 20.8).
+// one element an access: those 3092 rows in fp16, over and over, take 24 to 26 us in halves
+// and 19 in pairs where 16 bytes an access take 11.3 (fp32 24 to 26, 22 and 20.8).
 
 #include <math.h>
 
